@@ -12,15 +12,20 @@
 #include <vector>
 
 #include "common.h"
+#include "host.h"
 #include "specverify.h"
-
-#define SPEC_API extern "C" __attribute__((visibility("default")))
 
 using namespace spec;
 
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+namespace spec {
+
+Profiler g_prof;
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -36,20 +41,7 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(SPEC_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-#define HIP_TRY(expr, what)               \
-  do {                                    \
-    hipError_t e_ = (expr);               \
-    if (e_ != hipSuccess) return hip_fail(e_, what); \
-  } while (0)
-
-constexpr size_t kAlign = 256;
-constexpr int kPartCap = 8192;          // split-KV partial tiles per call
-constexpr int kTargetSlots = 512;       // attention CU slots aimed for (two rounds of 256 CUs)
-constexpr int kMinChunk = 64;           // keys per split, lower bound
-constexpr int kSmallChunk = 256;        // small calls: chunks of 64-key multiples up to this
-constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+void clear_error() { g_err.clear(); }
 
 bool config_ok(const spec_model_config* c, std::string* why) {
   char buf[256];
@@ -78,6 +70,16 @@ bool same_config(const spec_model_config* a, const spec_model_config* b) {
          a->n_kv_heads == b->n_kv_heads && a->head_dim == b->head_dim && a->ffn == b->ffn &&
          a->vocab == b->vocab;
 }
+
+}  // namespace spec
+
+namespace {
+
+constexpr int kPartCap = 8192;          // split-KV partial tiles per call
+constexpr int kTargetSlots = 512;       // attention CU slots aimed for (two rounds of 256 CUs)
+constexpr int kMinChunk = 64;           // keys per split, lower bound
+constexpr int kSmallChunk = 256;        // small calls: chunks of 64-key multiples up to this
+constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
 
 size_t sample_bytes(const spec_model_config* c, int32_t cap) {
   return align_up((size_t)c->n_layers * 2 * c->n_kv_heads * (size_t)cap * c->head_dim * 2);
@@ -146,29 +148,6 @@ GemmPlan product_plan(const spec_model_config* c, int kind, int n) {
   }
 }
 
-// Process-wide kernel timing state (measurement only).
-struct Profiler {
-  bool on = false;
-  int kind = -1, max = 0, count = 0;
-  std::vector<hipEvent_t> ev;
-} g_prof;
-
-template <class F>
-hipError_t timed(int kind, hipStream_t s, F&& fn) {
-  const bool rec = g_prof.on && g_prof.kind == kind && g_prof.count < g_prof.max;
-  if (rec) {
-    const hipError_t e = hipEventRecord(g_prof.ev[2 * g_prof.count], s);
-    if (e != hipSuccess) return e;
-  }
-  const hipError_t e = fn();
-  if (rec) {
-    const hipError_t e2 = hipEventRecord(g_prof.ev[2 * g_prof.count + 1], s);
-    ++g_prof.count;
-    if (e2 != hipSuccess) return e2;
-  }
-  return e;
-}
-
 }  // namespace
 
 // Library-owned part of a KV pool: capacities, block offsets and a two-slot
@@ -181,53 +160,62 @@ struct spec_kv {
   bf16* pool = nullptr;
   size_t bytes = 0;
   size_t ctl_off = 0;            // byte offset of the control area (commit descriptors)
-  struct Slot {
-    void* host = nullptr;
-    size_t size = 0;
-    hipEvent_t ev = nullptr;
-    bool pending = false;
-  } slots[2];
-  int next = 0;
+  StagingRing<2> ring;
 };
 
 namespace {
 
-// Copy `bytes` of `src` to device `dst` through the next pinned staging slot.
-int stage_upload(spec_kv* kv, const void* src, size_t bytes, void* dst, hipStream_t s) {
-  spec_kv::Slot& sl = kv->slots[kv->next];
-  kv->next ^= 1;
-  if (sl.pending) {
-    HIP_TRY(hipEventSynchronize(sl.ev), "staging wait");
-    sl.pending = false;
-  }
-  if (sl.ev == nullptr) HIP_TRY(hipEventCreateWithFlags(&sl.ev, hipEventDisableTiming), "event");
-  if (sl.size < bytes) {
-    if (sl.host) HIP_TRY(hipHostFree(sl.host), "free staging");
-    sl.host = nullptr;
-    sl.size = 0;
-    const size_t want = std::max(bytes, (size_t)1 << 20);
-    HIP_TRY(hipHostMalloc(&sl.host, want, hipHostMallocDefault), "pinned staging");
-    sl.size = want;
-  }
-  memcpy(sl.host, src, bytes);
-  HIP_TRY(hipMemcpyAsync(dst, sl.host, bytes, hipMemcpyHostToDevice, s), "upload");
-  HIP_TRY(hipEventRecord(sl.ev, s), "staging event");
-  sl.pending = true;
-  return SPEC_OK;
+int check_samples(const spec_kv* kv, int32_t batch, const int32_t* ids) {
+  return check_sample_ids(kv->n, batch, ids);
 }
 
-int check_samples(const spec_kv* kv, int32_t batch, const int32_t* ids) {
-  std::vector<char> seen(kv->n, 0);
+}  // namespace
+
+namespace spec {
+
+int check_sample_ids(int n, int32_t batch, const int32_t* ids) {
+  std::vector<char> seen(n, 0);
   for (int b = 0; b < batch; ++b) {
     const int id = ids[b];
-    if (id < 0 || id >= kv->n) return fail(SPEC_ERR_INVALID, "sample_ids[%d] = %d out of range", b, id);
+    if (id < 0 || id >= n) return fail(SPEC_ERR_INVALID, "sample_ids[%d] = %d out of range", b, id);
     if (seen[id]) return fail(SPEC_ERR_INVALID, "sample id %d appears twice", id);
     seen[id] = 1;
   }
   return SPEC_OK;
 }
 
-}  // namespace
+void deal_items(std::vector<AttnItem>& list) {
+  struct Group { size_t first, count; int64_t work; };
+  std::vector<Group> groups;
+  for (size_t i = 0; i < list.size();) {
+    size_t j = i;
+    while (j < list.size() && list[j].sample == list[i].sample && list[j].kvh == list[i].kvh &&
+           list[j].key0 == list[i].key0)
+      ++j;
+    groups.push_back(Group{i, j - i, (int64_t)(list[i].key1 - list[i].key0) * (int64_t)(j - i)});
+    i = j;
+  }
+  std::stable_sort(groups.begin(), groups.end(),
+                   [](const Group& x, const Group& y) { return x.work > y.work; });
+  std::vector<AttnItem> xcd[8];
+  int64_t load[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (const Group& gp : groups) {
+    const int x = (int)(std::min_element(load, load + 8) - load);
+    load[x] += gp.work;
+    xcd[x].insert(xcd[x].end(), list.begin() + gp.first, list.begin() + gp.first + gp.count);
+  }
+  size_t per = 0;
+  for (auto& v : xcd) per = std::max(per, v.size());
+  std::vector<AttnItem> dealt;
+  dealt.reserve(per * 8);
+  for (auto& v : xcd) {
+    dealt.insert(dealt.end(), v.begin(), v.end());
+    dealt.resize(dealt.size() + (per - v.size()), AttnItem{-1, 0, 0, 0, 0, 1, 0, 0});
+  }
+  list.swap(dealt);
+}
+
+}  // namespace spec
 
 SPEC_API const char* spec_last_error(void) { return g_err.c_str(); }
 
@@ -283,12 +271,7 @@ SPEC_API int spec_kv_alloc(const spec_model_config* cfg, int32_t n_samples,
 
 SPEC_API int spec_kv_free(spec_kv* kv) {
   if (!kv) return fail(SPEC_ERR_INVALID, "null handle");
-  int rc = SPEC_OK;
-  for (auto& sl : kv->slots) {
-    if (sl.pending && hipEventSynchronize(sl.ev) != hipSuccess) rc = SPEC_ERR_HIP;
-    if (sl.ev) (void)hipEventDestroy(sl.ev);
-    if (sl.host) (void)hipHostFree(sl.host);
-  }
+  const int rc = kv->ring.release();
   delete kv;
   return rc;
 }
@@ -463,43 +446,9 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
       if (ns > 1) part += ns * tiles;
     }
   }
-  // Longest-first per XCD: a kernel hands XCD x the items [x*per, (x+1)*per)
-  // in order.  Deal the groups of items that share a key range (adjacent, so
-  // they meet in one XCD's L2), longest first, to the XCD with the least work
-  // so far; pad every XCD's list to `per` with empty items (sample -1).
-  auto deal = [](std::vector<AttnItem>& list) {
-    struct Group { size_t first, count; int64_t work; };
-    std::vector<Group> groups;
-    for (size_t i = 0; i < list.size();) {
-      size_t j = i;
-      while (j < list.size() && list[j].sample == list[i].sample && list[j].kvh == list[i].kvh &&
-             list[j].key0 == list[i].key0)
-        ++j;
-      groups.push_back(Group{i, j - i, (int64_t)(list[i].key1 - list[i].key0) * (int64_t)(j - i)});
-      i = j;
-    }
-    std::stable_sort(groups.begin(), groups.end(),
-                     [](const Group& x, const Group& y) { return x.work > y.work; });
-    std::vector<AttnItem> xcd[8];
-    int64_t load[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (const Group& gp : groups) {
-      const int x = (int)(std::min_element(load, load + 8) - load);
-      load[x] += gp.work;
-      xcd[x].insert(xcd[x].end(), list.begin() + gp.first, list.begin() + gp.first + gp.count);
-    }
-    size_t per = 0;
-    for (auto& v : xcd) per = std::max(per, v.size());
-    std::vector<AttnItem> dealt;
-    dealt.reserve(per * 8);
-    for (auto& v : xcd) {
-      dealt.insert(dealt.end(), v.begin(), v.end());
-      dealt.resize(dealt.size() + (per - v.size()), AttnItem{-1, 0, 0, 0, 0, 1, 0, 0});
-    }
-    list.swap(dealt);
-  };
-  deal(items);
-  deal(wide4);
-  deal(wide8);
+  deal_items(items);
+  deal_items(wide4);
+  deal_items(wide8);
 
   // ---- one upload of the per-call descriptors ----
   const size_t o_si = 0;
@@ -521,7 +470,7 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   if (noalloc)   // no pinned staging: a copy from pageable memory, done before the call returns
     HIP_TRY(hipMemcpyAsync(ws + ly.blob, blob.data(), blob_bytes, hipMemcpyHostToDevice, s),
             "upload");
-  else if (int rc = stage_upload(kv, blob.data(), blob_bytes, ws + ly.blob, s))
+  else if (int rc = kv->ring.upload(blob.data(), blob_bytes, ws + ly.blob, s))
     return rc;
 
   const SampleInfo* d_si = (const SampleInfo*)(ws + ly.blob + o_si);
@@ -740,7 +689,7 @@ SPEC_API int spec_kv_commit(spec_kv* kv, int32_t batch, const int32_t* sample_id
   }
   hipStream_t s = (hipStream_t)stream;
   void* ctl = (char*)kv->pool + kv->ctl_off;
-  if (int rc = stage_upload(kv, si.data(), batch * sizeof(SampleInfo), ctl, s)) return rc;
+  if (int rc = kv->ring.upload(si.data(), batch * sizeof(SampleInfo), ctl, s)) return rc;
   const spec_model_config& c = kv->cfg;
   HIP_TRY(timed(SPEC_K_COMMIT, s, [&] {
             return launch_compact((const SampleInfo*)ctl, batch, kv->pool, c.n_layers,
@@ -797,7 +746,7 @@ int transfer(bool to_buffer, spec_kv* kv, int32_t n, const int32_t* sample_ids,
   if (wg == 0) return SPEC_OK;
   hipStream_t s = (hipStream_t)stream;
   void* ctl = (char*)kv->pool + kv->ctl_off;
-  if (int rc = stage_upload(kv, info.data(), n * sizeof(MigrateInfo), ctl, s)) return rc;
+  if (int rc = kv->ring.upload(info.data(), n * sizeof(MigrateInfo), ctl, s)) return rc;
   HIP_TRY(timed(SPEC_K_TRANSFER, s, [&] {
             return launch_kv_transfer(to_buffer, (const MigrateInfo*)ctl, n, wg, (int)tok, kv->pool,
                                       (bf16*)buf, c.n_layers, c.n_kv_heads, c.head_dim, s);
