@@ -286,6 +286,135 @@ int spec_kv_pack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int32_
 int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int32_t* tok_begin,
                    const int32_t* tok_end, const void* buf, size_t buf_bytes, void* stream);
 
+/* ---- A KV cache in 4 bits, in pages ------------------------------------
+ *
+ * The bf16 pool above gives every sample one block of fixed capacity.  This
+ * one holds K and V in about 4.2 bits per number, in pages of
+ * SPEC_KV4_PAGE positions that the caller hands out: a sample grows page by
+ * page, and samples of one prompt can share the pages of their common prefix.
+ *
+ * Numbers.  A number is an E2M1 code (sign, 2 exponent bits, 1 mantissa bit:
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and negatives) times a power of two 2^e.  32
+ * consecutive numbers of a K row share their e, so do all head_dim numbers of
+ * a V row.  e is the smallest exponent in [-126, 125] with which no
+ * magnitude of the group exceeds 6 * 2^e (125 if none is: 6 * 2^125 is the
+ * largest number here, and larger ones take it); a number takes the code
+ * nearest to x / 2^e, the even one (0, 1, 2, 4) of two equally near; zero, also
+ * a negative one, takes code 0.  A group with an infinity or NaN has no e: it
+ * reads as NaN, and rows that see it attend to NaN or infinities.
+ * Every reader sees the same numbers, whether a key is a tree node of this
+ * step or was committed long ago, so a verified tree gives what one-token
+ * steps over the same cache give.
+ *
+ * Pages.  Page p lies at byte p * spec_kv4_page_bytes(cfg); in it, layer l
+ * and KV head g take 64 * (head_dim + head_dim / 32 + 2) bytes at
+ * (l * n_kv_heads + g) times that:
+ *   K codes   [2 blocks of 32 keys][head_dim / 32][32 keys][16 bytes]: numbers
+ *             2n and 2n + 1 of the 32 in the low and high half of byte n
+ *   V codes   [8 octets of keys][32][head_dim / 32][4 bytes]: word (m, i) holds
+ *             number 32 i + m of the octet's 8 keys, keys 2n and 2n + 1 in the
+ *             low and high half of byte n
+ *   K scales  [64 keys][head_dim / 32] bytes e + 127 (255: none)
+ *   V scales  [64 keys] bf16 2^e (NaN: none)
+ *
+ * Use, per model step:
+ *   spec_kv4_step_begin    plans the step's rows: once
+ *   spec_kv4_append        every layer: the rows' K/V into the cache
+ *   spec_kv4_attend        every layer: their attention
+ *   spec_kv4_commit        after acceptance, for trees
+ * or spec_verify_kv4, which does all but the commit.  spec_kv4_append,
+ * _read and _attend only launch kernels: they can be captured into a graph and
+ * replayed while the step, its workspace and its pages stay as they are.
+ * _step_begin and _commit upload descriptors and refuse a capturing stream. */
+#define SPEC_KV4_PAGE 64
+
+typedef struct spec_kv4 spec_kv4;             /* opaque pool handle (host, owned by the library) */
+typedef struct spec_kv4_step spec_kv4_step;   /* opaque plan of one step */
+
+/* Bytes of one page (all layers and KV heads); 0 if cfg is invalid. */
+size_t spec_kv4_page_bytes(const spec_model_config* cfg);
+
+/* Bytes of a pool of n_pages pages for n_samples samples: the pages, padded to
+ * 256 bytes, then a control area of 32 bytes per sample, padded alike; 0 if an
+ * argument is invalid. */
+size_t spec_kv4_bytes(const spec_model_config* cfg, int32_t n_samples, int32_t n_pages);
+
+/* Create a handle over caller memory device_buf (device, >= spec_kv4_bytes,
+ * 256-byte aligned).  No sample has pages at first.  One handle must not be used
+ * from two threads or two streams at once. */
+int spec_kv4_alloc(const spec_model_config* cfg, int32_t n_samples, int32_t n_pages,
+                   void* device_buf, size_t buf_bytes, spec_kv4** out);
+
+/* Release the handle (not device_buf, and after its steps).  Waits for the
+ * handle's pending uploads. */
+int spec_kv4_free(spec_kv4* kv);
+
+/* Set the pages of one sample: positions [64 i, 64 i + 64) lie in page pages[i].
+ *   pages  host [n_pages]  distinct ids in [0, pool pages); n_pages may be 0
+ * A page may belong to several samples (a shared prefix): it is then read only,
+ * and a step or commit that would write to it is refused with
+ * SPEC_ERR_INVALID.  Host bookkeeping only: contents stay as they are, and steps
+ * begun before keep the pages they were begun with. */
+int spec_kv4_map(spec_kv4* kv, int32_t sample, int32_t n_pages, const int32_t* pages);
+
+/* Workspace bytes of a step of up to max_batch samples and max_rows rows, whose
+ * keys (committed and new) lie in up to max_pages pages, summed over the
+ * samples; 0 if an argument is invalid. */
+size_t spec_kv4_step_bytes(const spec_model_config* cfg, int32_t max_batch, int32_t max_rows,
+                           int32_t max_pages);
+
+/* Plan a step: sample sample_ids[b] has S_b = seq_lens[b] committed positions and
+ * gets T_b = row_offsets[b + 1] - row_offsets[b] >= 1 new rows, in slots S_b + i.
+ *   sample_ids   host [batch]    distinct
+ *   row_offsets  host [batch+1]  row_offsets[0] = 0
+ *   parents      host [N]        trees as in spec_verify (T_b <= SPEC_MAX_TREE):
+ *                                row i sits at position S_b + depth(i) and sees the
+ *                                committed keys and its ancestors, itself included.
+ *                                NULL: runs, of any length: row i sits at position
+ *                                S_b + i and sees the keys [0, S_b + i]
+ *   seq_lens     host [batch]    S_b >= 0, S_b + T_b <= 64 * (pages of the sample)
+ *   workspace    device, 256-byte aligned; the step's until its last launch is done
+ * *out receives the plan; spec_kv4_step_free releases it (host memory only: call it
+ * once no more launches are to be made). */
+int spec_kv4_step_begin(spec_kv4* kv, int32_t batch, const int32_t* sample_ids,
+                        const int32_t* row_offsets, const int32_t* parents, const int32_t* seq_lens,
+                        void* workspace, size_t ws_bytes, void* stream, spec_kv4_step** out);
+int spec_kv4_step_free(spec_kv4_step* step);
+
+/* Write the K/V of the step's N rows into their slots of one layer.
+ *   k, v       device bf16; row r, KV head g, number j at r * stride + g * head_dim + j
+ *              (strides in values, multiples of 8; 16-byte aligned), so that a slice
+ *              of a fused projection's output can be passed as it is
+ *   rotate     nonzero: k is rotated by its position first (rope_theta of the pool's
+ *              config; angles, products and sums in double precision, rounded once,
+ *              to the code); zero: k has been rotated already
+ * Bytes of positions outside the rows' slots are not changed. */
+int spec_kv4_append(const spec_kv4_step* step, int32_t layer, const void* k, int64_t k_stride,
+                    const void* v, int64_t v_stride, int32_t rotate, void* stream);
+
+/* What the cache holds for the step's rows, exactly, as bf16 (same layout of k and
+ * v, which are written). */
+int spec_kv4_read(const spec_kv4_step* step, int32_t layer, void* k, int64_t k_stride, void* v,
+                  int64_t v_stride, void* stream);
+
+/* Attention of the step's rows over one layer of the cache, their own K/V included
+ * (append them first): softmax(q . K / sqrt(head_dim)) V over the keys that each
+ * row sees.
+ *   q    device bf16, rotated; row r, query head i at r * q_stride + i * head_dim
+ *        (q_stride a multiple of 8, 16-byte aligned)
+ *   out  device bf16 [N][n_heads * head_dim], 16-byte aligned
+ * K and V enter as the numbers they stand for; probabilities are rounded to bf16,
+ * sums and softmax statistics are fp32.  Bitwise the same for the same step. */
+int spec_kv4_attend(const spec_kv4_step* step, int32_t layer, const void* q, int64_t q_stride,
+                    void* out, void* stream);
+
+/* spec_kv_commit for this pool: the codes and scales of node accepted_nodes[b][d]
+ * move to position S_b + d for d = 1 .. accepted_len[b], all layers, and
+ * new_seq_lens[b] = S_b + accepted_len[b] + 1. */
+int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* seq_lens,
+                    const int32_t* accepted_len, const int32_t* accepted_nodes,
+                    int32_t* new_seq_lens, void* stream);
+
 /* ---- Drafting-strategy selection (Section 5) ----------------------------
  *
  * Verification-cost predictor (Section 5.2, "the execution time"): a
@@ -355,7 +484,8 @@ enum {
   SPEC_K_COMMIT = 6,
   SPEC_K_TRANSFER = 7,   /* spec_kv_pack / spec_kv_unpack */
   SPEC_K_ACCEPT = 8,     /* tree acceptance: greedy, greedy with EOS, or sampled */
-  SPEC_K_COUNT = 9
+  SPEC_K_KV4_APPEND = 9, /* spec_kv4_append (SPEC_K_ATTENTION: spec_kv4_attend too) */
+  SPEC_K_COUNT = 10
 };
 int spec_profile_begin(int32_t kernel_class, int32_t max_launches);
 int spec_profile_end(float* total_ms, int32_t* launches);

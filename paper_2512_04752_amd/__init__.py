@@ -8,12 +8,22 @@ loaded on first use and its absence is an error.
 from .binding import (  # noqa: F401
     EXPORTS,
     CostModel,
+    KV4Pool,
+    KV4Step,
     KVPool,
+    SPEC_KV4_PAGE,
     SPEC_MAX_TREE,
     SpecError,
     Weights,
     lib,
     spec_gemm_plan,
+    spec_kv4_append,
+    spec_kv4_attend,
+    spec_kv4_bytes,
+    spec_kv4_commit,
+    spec_kv4_page_bytes,
+    spec_kv4_read,
+    spec_kv4_step_bytes,
     spec_kv_alloc,
     spec_kv_bytes,
     spec_kv_commit,

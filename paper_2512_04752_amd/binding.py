@@ -22,6 +22,7 @@ STATUS = {0: "SPEC_OK", -1: "SPEC_ERR_INVALID", -2: "SPEC_ERR_TREE", -3: "SPEC_E
 KERNEL_CLASS = {"gemm_qkv": 0, "attention": 1, "gemm_o": 2, "gemm_gate_up": 3, "gemm_down": 4,
                 "lm_head": 5, "commit": 6, "accept": 8}   # the kernel classes of one verify step
 TRANSFER_CLASS = 7                                    # spec_kv_pack / spec_kv_unpack
+KV4_APPEND_CLASS = 9                                  # spec_kv4_append
 
 # Every symbol the public header declares.
 EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout",
@@ -29,7 +30,11 @@ EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_lay
            "spec_profile_begin", "spec_profile_end", "spec_kv_transfer_bytes", "spec_kv_pack",
            "spec_kv_unpack", "spec_cost_model_create", "spec_cost_model_free", "spec_cost_predict",
            "spec_cost_model_stats", "spec_select_draft_count", "spec_workspace_bytes_sampled",
-           "spec_verify_sampled", "spec_verify_noalloc", "spec_gemm_plan")
+           "spec_verify_sampled", "spec_verify_noalloc", "spec_gemm_plan", "spec_kv4_page_bytes",
+           "spec_kv4_bytes", "spec_kv4_alloc", "spec_kv4_free", "spec_kv4_map",
+           "spec_kv4_step_bytes", "spec_kv4_step_begin", "spec_kv4_step_free", "spec_kv4_append",
+           "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit")
+SPEC_KV4_PAGE = 64                # positions per page of the 4-bit pool
 SPEC_NOALLOC_SCRATCH_BYTES = 320 << 20
 
 
@@ -119,11 +124,32 @@ def lib():
     L.spec_profile_begin.argtypes = [c_int32, c_int32]
     L.spec_profile_end.argtypes = [POINTER(c_float), i32p]
     L.spec_gemm_plan.argtypes = [POINTER(spec_model_config), c_int32, c_int32, i32p, i32p, i32p]
+    L.spec_kv4_page_bytes.argtypes = [POINTER(spec_model_config)]
+    L.spec_kv4_page_bytes.restype = c_size_t
+    L.spec_kv4_bytes.argtypes = [POINTER(spec_model_config), c_int32, c_int32]
+    L.spec_kv4_bytes.restype = c_size_t
+    L.spec_kv4_alloc.argtypes = [POINTER(spec_model_config), c_int32, c_int32, c_void_p, c_size_t,
+                                 POINTER(c_void_p)]
+    L.spec_kv4_free.argtypes = [c_void_p]
+    L.spec_kv4_map.argtypes = [c_void_p, c_int32, c_int32, i32p]
+    L.spec_kv4_step_bytes.argtypes = [POINTER(spec_model_config), c_int32, c_int32, c_int32]
+    L.spec_kv4_step_bytes.restype = c_size_t
+    L.spec_kv4_step_begin.argtypes = [c_void_p, c_int32, i32p, i32p, i32p, i32p, c_void_p, c_size_t,
+                                      c_void_p, POINTER(c_void_p)]
+    L.spec_kv4_step_free.argtypes = [c_void_p]
+    L.spec_kv4_append.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_int32,
+                                  c_void_p]
+    L.spec_kv4_read.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
+    L.spec_kv4_attend.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p]
+    L.spec_kv4_commit.argtypes = [c_void_p, c_int32, i32p, i32p, c_void_p, c_void_p, c_void_p,
+                                  c_void_p]
     for name in ("spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
                  "spec_kv_commit", "spec_profile_begin", "spec_profile_end", "spec_kv_pack",
                  "spec_kv_unpack", "spec_cost_model_create", "spec_cost_model_free",
                  "spec_cost_model_stats", "spec_select_draft_count", "spec_verify_sampled",
-                 "spec_verify_noalloc", "spec_gemm_plan"):
+                 "spec_verify_noalloc", "spec_gemm_plan", "spec_kv4_alloc", "spec_kv4_free",
+                 "spec_kv4_map", "spec_kv4_step_begin", "spec_kv4_step_free", "spec_kv4_append",
+                 "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit"):
         getattr(L, name).restype = c_int32
     _lib = L
     return L
@@ -353,6 +379,165 @@ def spec_kv_unpack(kv: KVPool, sample_ids, tok_begin, tok_end, buf, stream=None)
                                 buf.numel() * buf.element_size(), _stream(stream)))
 
 
+def spec_kv4_page_bytes(cfg) -> int:
+    c = make_config(cfg)
+    return int(lib().spec_kv4_page_bytes(ctypes.byref(c)))
+
+
+def spec_kv4_bytes(cfg, n_samples, n_pages) -> int:
+    c = make_config(cfg)
+    return int(lib().spec_kv4_bytes(ctypes.byref(c), n_samples, n_pages))
+
+
+def spec_kv4_step_bytes(cfg, max_batch, max_rows, max_pages) -> int:
+    c = make_config(cfg)
+    return int(lib().spec_kv4_step_bytes(ctypes.byref(c), max_batch, max_rows, max_pages))
+
+
+class KV4Pool:
+    """A 4-bit paged KV pool over a torch-owned device buffer (spec_kv4_alloc)."""
+
+    def __init__(self, cfg, n_samples, n_pages, buf=None, device="cuda"):
+        """buf: a contiguous uint8 device tensor of at least spec_kv4_bytes bytes (allocated
+        on ``device`` when None)."""
+        self.handle = None
+        self.cfg = cfg
+        self.n_samples, self.n_pages = int(n_samples), int(n_pages)
+        self.pages = {}
+        nbytes = spec_kv4_bytes(cfg, self.n_samples, self.n_pages)
+        if nbytes == 0:
+            raise SpecError(-1, "invalid KV pool request")
+        if buf is None:
+            buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        elif buf.dtype != torch.uint8 or not buf.is_cuda or not buf.is_contiguous():
+            raise ValueError("buf must be a contiguous uint8 device tensor")
+        self.buf = buf
+        c = make_config(cfg)
+        h = c_void_p()
+        with torch.cuda.device(buf.device):
+            _check(lib().spec_kv4_alloc(ctypes.byref(c), self.n_samples, self.n_pages,
+                                        c_void_p(buf.data_ptr()), buf.numel(), ctypes.byref(h)))
+        self.handle = h
+
+    def map(self, sample, pages):
+        """Set the pages of one sample (spec_kv4_map)."""
+        arr, p = _i32(pages)
+        _check(lib().spec_kv4_map(self.handle, int(sample), len(arr), p))
+        self.pages[int(sample)] = arr.tolist()
+
+    def close(self):
+        if self.handle is not None:
+            h, self.handle = self.handle, None
+            _check(lib().spec_kv4_free(h))
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KV4Step:
+    """The plan of one step over a KV4Pool (spec_kv4_step_begin).
+
+    parents: the trees' parents, or None for runs.  workspace: a uint8 tensor on the pool's
+    device of at least spec_kv4_step_bytes bytes (allocated when None).  The step's launches
+    go to streams of the pool's device."""
+
+    def __init__(self, pool: KV4Pool, sample_ids, row_offsets, parents, seq_lens, workspace=None,
+                 stream=None):
+        self.handle = None
+        self.pool = pool
+        ids, p_ids = _i32(sample_ids)
+        offs, p_offs = _i32(row_offsets)
+        lens, p_lens = _i32(seq_lens)
+        pars, p_pars = (None, None) if parents is None else _i32(parents)
+        if len(offs) != len(ids) + 1 or len(lens) != len(ids):
+            raise ValueError("row_offsets must have one entry more than sample_ids, seq_lens as many")
+        if len(ids) and pars is not None and len(pars) != int(offs[-1]):
+            raise ValueError("parents must have one entry per row")
+        self.n_rows = int(offs[-1])
+        if workspace is None:
+            pages = int(((lens.astype(np.int64) + np.diff(offs) + SPEC_KV4_PAGE - 1)
+                         // SPEC_KV4_PAGE).sum())
+            nbytes = spec_kv4_step_bytes(pool.cfg, len(ids), self.n_rows, max(pages, 1))
+            workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
+        self.workspace = workspace
+        h = c_void_p()
+        with torch.cuda.device(pool.buf.device):
+            _check(lib().spec_kv4_step_begin(pool.handle, len(ids), p_ids, p_offs, p_pars, p_lens,
+                                             _ptr(workspace),
+                                             workspace.numel() * workspace.element_size(),
+                                             _stream(stream), ctypes.byref(h)))
+        self.handle = h
+
+    def close(self):
+        if self.handle is not None:
+            h, self.handle = self.handle, None
+            _check(lib().spec_kv4_step_free(h))
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _kv4_rows(step, t, heads, what):
+    """Row stride of a bf16 device tensor [rows, heads, head_dim] or [rows, heads * head_dim] whose
+    rows are contiguous."""
+    d = step.pool.cfg.head_dim
+    flat = t.dim() == 2 and t.shape[1] == heads * d and t.stride(1) == 1
+    split = (t.dim() == 3 and tuple(t.shape[1:]) == (heads, d) and t.stride(2) == 1
+             and (heads == 1 or t.stride(1) == d))
+    if (t.dtype != torch.bfloat16 or t.device != step.pool.buf.device or t.shape[0] != step.n_rows
+            or not (flat or split)):
+        raise ValueError(f"{what} must be a bfloat16 [{step.n_rows}, {heads}, {d}] tensor on the "
+                         "pool's device with contiguous rows")
+    return t.stride(0) if step.n_rows > 1 else heads * d
+
+
+def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
+    """Write the rows' K and V ([rows, kv heads, head_dim], rows may be strided) into the cache,
+    rotating k by position unless it has been."""
+    n = step.pool.cfg.n_kv_heads
+    ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
+    with torch.cuda.device(step.pool.buf.device):
+        _check(lib().spec_kv4_append(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs, int(rotate),
+                                     _stream(stream)))
+
+
+def spec_kv4_read(step: KV4Step, layer, k, v, stream=None):
+    """Write what the cache holds for the step's rows into k and v (as in spec_kv4_append)."""
+    n = step.pool.cfg.n_kv_heads
+    ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
+    with torch.cuda.device(step.pool.buf.device):
+        _check(lib().spec_kv4_read(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs,
+                                   _stream(stream)))
+
+
+def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
+    """Attention of the step's rows: q [rows, heads, head_dim] (rows may be strided), rotated;
+    out [rows, heads * head_dim], contiguous."""
+    n = step.pool.cfg.n_heads
+    qs = _kv4_rows(step, q, n, "q")
+    _kv4_rows(step, out, n, "out")
+    if not out.is_contiguous():
+        raise ValueError("out must be contiguous")
+    with torch.cuda.device(step.pool.buf.device):
+        _check(lib().spec_kv4_attend(step.handle, int(layer), _ptr(q), qs, _ptr(out),
+                                     _stream(stream)))
+
+
+def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_nodes, new_seq_lens,
+                    stream=None):
+    ids, p_ids = _i32(sample_ids)
+    lens, p_lens = _i32(seq_lens)
+    with torch.cuda.device(pool.buf.device):
+        _check(lib().spec_kv4_commit(pool.handle, len(ids), p_ids, p_lens, _ptr(accepted_len),
+                                     _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))
+
+
 class CostModel:
     """The library's verification-cost predictor (spec_cost_model_*)."""
 
@@ -410,6 +595,8 @@ def spec_select_draft_count(model: CostModel, seq_lens, tree_offsets, parents, w
 def spec_profile_begin(kernel_class, max_launches):
     if kernel_class == "transfer":
         k = TRANSFER_CLASS
+    elif kernel_class == "kv4_append":
+        k = KV4_APPEND_CLASS
     else:
         k = KERNEL_CLASS[kernel_class] if isinstance(kernel_class, str) else int(kernel_class)
     _check(lib().spec_profile_begin(k, max_launches))

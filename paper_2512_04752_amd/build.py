@@ -14,7 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libspecverify.so")
 BUILD = os.path.join(PKG, "_build")
 SOURCES = ["api.cpp", "gemm.hip", "attention.hip", "elementwise.hip", "migrate.hip",
-           "strategy.cpp", "sampling.hip", "noalloc.hip"]
+           "strategy.cpp", "sampling.hip", "noalloc.hip", "kv4.cpp", "kv4_cache.hip",
+           "kv4_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-x", "hip", "-std=c++17", "-O3", "--offload-arch=gfx950", "-fPIC",
@@ -23,8 +24,10 @@ FLAGS = ["-x", "hip", "-std=c++17", "-O3", "--offload-arch=gfx950", "-fPIC",
 
 
 # Per-source extra flags.  The attention kernels never see NaN (masked scores
-# are -inf), so fmax needs no NaN canonicalisation of the MFMA outputs.
-EXTRA = {"attention.hip": ["-fno-honor-nans"]}
+# are -inf), so fmax needs no NaN canonicalisation of the MFMA outputs.  (Over the
+# 4-bit cache a score may be NaN, where a key was not finite: any result will do
+# for the maximum then, the row's sums still carry the NaN.)
+EXTRA = {"attention.hip": ["-fno-honor-nans"], "kv4_attention.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src):

@@ -1,0 +1,503 @@
+// Host side of the 4-bit paged KV cache: page tables, a step's plan (row octets,
+// attention work items) and its one upload, and the launches of append, read,
+// attend and commit.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "kv4_host.h"
+
+using namespace spec;
+
+namespace {
+
+constexpr int kPartCap = 8192;          // partial row tiles per step
+constexpr int kTargetGroups = 1024;     // attention work-groups aimed for: two rounds of two per CU
+constexpr int kMinChunk = 256;          // keys per split, lower bound
+constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
+
+// Run the body of an entry point; no exception leaves it.
+template <class F>
+int guarded(F&& body) {
+  clear_error();
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return fail(SPEC_ERR_CAPACITY, "out of host memory");
+  } catch (const std::exception& e) {
+    return fail(SPEC_ERR_INVALID, "%s", e.what());
+  }
+}
+
+// Uploads go through staging memory that the next calls reuse, so a captured one
+// would replay another call's descriptors.
+int refuse_capture(void* stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  HIP_TRY(hipStreamIsCapturing((hipStream_t)stream, &st), "stream capture status");
+  if (st != hipStreamCaptureStatusNone)
+    return fail(SPEC_ERR_INVALID, "the call uploads its plan and cannot be captured into a graph");
+  return SPEC_OK;
+}
+
+int64_t page_bytes_of(const spec_model_config* c) {
+  return (int64_t)c->n_layers * c->n_kv_heads * kv4_head_bytes(c->head_dim);
+}
+
+// Positions that the sample's mapped pages hold.
+int64_t mapped(const spec_kv4* kv, int sample) { return (int64_t)kv->pages[sample].size() * kKv4Page; }
+
+// No page of positions [begin, end) of a sample may be another sample's too.
+int check_unshared(const spec_kv4* kv, int sample, int64_t begin, int64_t end) {
+  for (int64_t p = begin / kKv4Page; p * kKv4Page < end; ++p) {
+    const int page = kv->pages[sample][p];
+    if (kv->uses[page] > 1)
+      return fail(SPEC_ERR_INVALID, "sample %d: page %d of positions to be written is mapped to %d samples", sample,
+                  page, kv->uses[page]);
+  }
+  return SPEC_OK;
+}
+
+struct StepLayout {
+  size_t blob, toks, anc, part_o, part_ml, total;
+};
+
+StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, int64_t pages) {
+  const int64_t G = c->n_heads / c->n_kv_heads;
+  const int64_t groups = (int64_t)c->n_kv_heads * ((rows * G + 31) / 32 + batch);   // row groups, at most
+  const int64_t items = 8 * (groups + kPartCap);                                    // padded per XCD
+  const int64_t octets = rows / 8 + 2 * batch;
+  const size_t blob = align_up(batch * sizeof(SampleInfo)) + align_up(rows * 4) + align_up(pages * 4) +
+                      align_up(c->head_dim / 2 * sizeof(double)) + align_up(octets * sizeof(Kv4Octet)) +
+                      align_up(items * sizeof(AttnItem)) + 3 * kAlign +
+                      align_up(kPartCap * sizeof(CombineItem));
+  StepLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align_up(bytes);
+    return at;
+  };
+  L.blob = take(blob);
+  L.toks = take(rows * sizeof(TokInfo));
+  L.anc = take(rows * 8 * kAncWords);
+  L.part_o = take((size_t)kPartCap * 32 * c->head_dim * 4);
+  L.part_ml = take((size_t)kPartCap * 32 * 2 * 4);
+  L.total = off;
+  return L;
+}
+
+// The attention work of a step: items by row tiles per work-group (1, 2, 4) and
+// the combine jobs of split key ranges.
+struct AttnPlan {
+  std::vector<AttnItem> items[3];
+  std::vector<CombineItem> comb;
+};
+
+// A (sample, kv head) has ceil(T G / 32) row tiles; they go in groups of up to
+// four, one work-group each: four waves share a tile's keys when it is alone, two
+// when there are two, and each has its own from three on.  A group's key range is
+// cut into chunks of about the same work (keys x tiles), so that the step has
+// about kTargetGroups work-groups.
+void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, AttnPlan* plan) {
+  const int G = c->n_heads / c->n_kv_heads, nkv = c->n_kv_heads;
+  struct Group {
+    int b, tile0, tiles, keys;
+  };
+  std::vector<Group> groups;
+  double work = 0.0;
+  auto weight = [](int tiles) { return tiles == 1 ? 1 : tiles == 2 ? 2 : 4; };
+  for (int b = 0; b < (int)si.size(); ++b) {
+    const int64_t rows = (int64_t)si[b].ntok * G;
+    const int tiles = (int)((rows + 31) / 32);
+    for (int t = 0; t < tiles; t += 4) {
+      const int n = std::min(4, tiles - t);
+      const int64_t last = std::min<int64_t>(rows, 32ll * (t + n)) - 1;      // last row of the group
+      const int keys = si[b].seq_len + (runs ? (int)(last / G) + 1 : si[b].ntok);
+      groups.push_back(Group{b, t, n, keys});
+      work += (double)nkv * keys * weight(n);
+    }
+  }
+  auto chunk_of = [&](const Group& g, double unit) {
+    const int64_t least = ((int64_t)g.keys + kMaxSplits - 1) / kMaxSplits;
+    const int64_t want = std::max<int64_t>({kMinChunk, least, (int64_t)(unit / weight(g.tiles))});
+    return (want + 127) / 128 * 128;
+  };
+  auto splits_of = [&](const Group& g, double unit) {
+    const int64_t ch = chunk_of(g, unit);
+    return (int)((g.keys + ch - 1) / ch);
+  };
+  double unit = work / kTargetGroups;
+  for (;;) {      // ends: with units beyond the longest range times four nothing is split
+    int64_t slots = 0;
+    for (const Group& g : groups) {
+      const int ns = splits_of(g, unit);
+      if (ns > 1) slots += (int64_t)ns * nkv * g.tiles;
+    }
+    if (slots <= kPartCap) break;
+    unit = unit * 1.25 + 128;
+  }
+  int slot = 0;
+  for (const Group& g : groups) {
+    const int64_t ch = chunk_of(g, unit);
+    const int ns = splits_of(g, unit);
+    const int list = g.tiles == 1 ? 0 : g.tiles == 2 ? 1 : 2;
+    for (int kvh = 0; kvh < nkv; ++kvh) {
+      for (int k = 0; k < ns; ++k)
+        plan->items[list].push_back(AttnItem{g.b, kvh, g.tile0 * 32, (int)(k * ch),
+                                             (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns,
+                                             ns > 1 ? slot + k : 0, 0});
+      if (ns > 1) {
+        for (int t = 0; t < g.tiles; ++t)
+          plan->comb.push_back(CombineItem{g.b, kvh, (g.tile0 + t) * 32, ns, slot + t * ns, 0, 0, 0});
+        slot += ns * g.tiles;
+      }
+    }
+  }
+  for (auto& list : plan->items) deal_items(list);
+}
+
+}  // namespace
+
+namespace spec {
+
+int kv4_check_rows(const spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* offsets,
+                   const int32_t* parents, const int32_t* seq_lens) {
+  if (batch < 1) return fail(SPEC_ERR_INVALID, "batch must be >= 1");
+  if (int rc = check_sample_ids(kv->n, batch, sample_ids)) return rc;
+  if (offsets[0] != 0) return fail(SPEC_ERR_TREE, "row_offsets[0] must be 0");
+  for (int b = 0; b < batch; ++b) {
+    const int64_t T = (int64_t)offsets[b + 1] - offsets[b];
+    if (T < 1) return fail(SPEC_ERR_TREE, "sample %d has %lld rows", b, (long long)T);
+    if (parents && T > SPEC_MAX_TREE) return fail(SPEC_ERR_UNSUPPORTED, "sample %d has %lld tree nodes", b, (long long)T);
+    const int S = seq_lens[b];
+    if (S < 0) return fail(SPEC_ERR_INVALID, "seq_lens[%d] = %d", b, S);
+    if (S + T > mapped(kv, sample_ids[b]))
+      return fail(SPEC_ERR_CAPACITY, "sample %d: %d committed + %lld rows exceed the %lld positions of its pages", b, S,
+                  (long long)T, (long long)mapped(kv, sample_ids[b]));
+    if (int rc = check_unshared(kv, sample_ids[b], S, S + T)) return rc;
+    if (!parents) continue;
+    const int32_t* p = parents + offsets[b];
+    if (p[0] != -1) return fail(SPEC_ERR_TREE, "sample %d: root parent must be -1", b);
+    for (int i = 1; i < T; ++i)
+      if (p[i] < 0 || p[i] >= i)
+        return fail(SPEC_ERR_TREE, "sample %d node %d: parent %d not before the node", b, i, p[i]);
+  }
+  return SPEC_OK;
+}
+
+size_t kv4_step_bytes(const spec_model_config* cfg, int64_t batch, int64_t rows, int64_t pages) {
+  return step_layout(cfg, batch, rows, pages).total;
+}
+
+int64_t kv4_step_pages(const spec_kv4*, int32_t batch, const int32_t* offsets, const int32_t* seq_lens) {
+  int64_t pages = 0;
+  for (int b = 0; b < batch; ++b)
+    pages += ((int64_t)seq_lens[b] + offsets[b + 1] - offsets[b] + kKv4Page - 1) / kKv4Page;
+  return pages;
+}
+
+int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* offsets,
+                  const int32_t* parents, const int32_t* seq_lens, void* workspace, hipStream_t s,
+                  const spec_debug& dbg, spec_kv4_step* st) {
+  const spec_model_config& c = kv->cfg;
+  const int64_t N = offsets[batch];
+  const int64_t pages = kv4_step_pages(kv, batch, offsets, seq_lens);
+  const bool runs = parents == nullptr;
+  std::vector<SampleInfo> si(batch);
+  std::vector<int32_t> table;
+  table.reserve(pages);
+  std::vector<Kv4Octet> octets;
+  octets.reserve(N / 8 + 2 * batch);
+  for (int b = 0; b < batch; ++b) {
+    const int id = sample_ids[b], S = seq_lens[b], T = offsets[b + 1] - offsets[b];
+    const int np = (int)(((int64_t)S + T + kKv4Page - 1) / kKv4Page);
+    si[b] = SampleInfo{(int64_t)table.size(), np * kKv4Page, S, offsets[b], T, 0, 0};
+    table.insert(table.end(), kv->pages[id].begin(), kv->pages[id].begin() + np);
+    for (int o = S / 8 * 8; o < S + T; o += 8)
+      octets.push_back(Kv4Octet{b, o, std::max(0, S - o), std::min(8, S + T - o)});
+  }
+  AttnPlan plan;
+  plan_attention(&c, si, runs, &plan);
+  std::vector<double> freq(c.head_dim / 2);
+  for (int j = 0; j < c.head_dim / 2; ++j)
+    freq[j] = std::pow((double)c.rope_theta, -2.0 * j / c.head_dim);
+
+  // ---- one upload ----
+  const StepLayout L = step_layout(&c, batch, N, pages);
+  std::vector<char> blob;
+  auto put = [&](const void* src, size_t bytes) {
+    const size_t at = align_up(blob.size());
+    blob.resize(at + bytes);
+    if (bytes) memcpy(blob.data() + at, src, bytes);
+    return at;
+  };
+  const size_t o_si = put(si.data(), si.size() * sizeof(SampleInfo));
+  const size_t o_par = put(parents, runs ? 0 : N * 4);
+  const size_t o_table = put(table.data(), table.size() * 4);
+  const size_t o_freq = put(freq.data(), freq.size() * sizeof(double));
+  const size_t o_oct = put(octets.data(), octets.size() * sizeof(Kv4Octet));
+  size_t o_items[3];
+  for (int i = 0; i < 3; ++i) o_items[i] = put(plan.items[i].data(), plan.items[i].size() * sizeof(AttnItem));
+  const size_t o_comb = put(plan.comb.data(), plan.comb.size() * sizeof(CombineItem));
+  char* ws = (char*)workspace;
+  char* d = ws + L.blob;
+  if (int rc = kv->ring.upload(blob.data(), blob.size(), d, s)) return rc;
+  const SampleInfo* d_si = (const SampleInfo*)(d + o_si);
+  TokInfo* toks = (TokInfo*)(ws + L.toks);
+  uint64_t* anc = (uint64_t*)(ws + L.anc);
+  if (!runs)
+    HIP_TRY(launch_tree_meta(d_si, batch, (const int32_t*)(d + o_par), toks, anc, dbg.depth, dbg.pos, dbg.anc, s),
+            "tree meta");
+
+  st->kv = kv;
+  st->n_rows = (int)N;
+  Kv4View view{kv->pool, page_bytes_of(&c), (const int32_t*)(d + o_table), d_si, 0, c.n_kv_heads, c.head_dim};
+  st->rows = Kv4RowArgs{view, (const Kv4Octet*)(d + o_oct), (int)octets.size(), runs ? nullptr : toks,
+                        (const double*)(d + o_freq), nullptr, nullptr, 0, 0, 0};
+  Kv4AttnArgs& a = st->attn;
+  a = Kv4AttnArgs{};
+  a.v = view;
+  a.anc = runs ? nullptr : anc;
+  for (int i = 0; i < 3; ++i) {
+    a.items[i] = (const AttnItem*)(d + o_items[i]);
+    a.n_items[i] = (int)plan.items[i].size();
+  }
+  a.part_o = (float*)(ws + L.part_o);
+  a.part_ml = (float*)(ws + L.part_ml);
+  a.n_heads = c.n_heads;
+  a.comb = (const CombineItem*)(d + o_comb);
+  a.n_comb = (int)plan.comb.size();
+  return SPEC_OK;
+}
+
+int kv4_append(const spec_kv4_step* st, int layer, const bf16* k, int64_t k_stride, const bf16* v, int64_t v_stride,
+               int rotate, hipStream_t s) {
+  Kv4RowArgs a = st->rows;
+  a.v.layer = layer;
+  a.k = const_cast<bf16*>(k);
+  a.val = const_cast<bf16*>(v);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.rotate = rotate;
+  HIP_TRY(timed(SPEC_K_KV4_APPEND, s, [&] { return launch_kv4_append(a, s); }), "kv4 append");
+  return SPEC_OK;
+}
+
+int kv4_attend(const spec_kv4_step* st, int layer, const bf16* q, int64_t q_stride, bf16* out, hipStream_t s) {
+  Kv4AttnArgs a = st->attn;
+  a.v.layer = layer;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.out = out;
+  HIP_TRY(timed(SPEC_K_ATTENTION, s, [&] { return launch_kv4_attention(a, s); }), "kv4 attention");
+  return SPEC_OK;
+}
+
+}  // namespace spec
+
+SPEC_API size_t spec_kv4_page_bytes(const spec_model_config* cfg) {
+  std::string why;
+  if (!cfg || !config_ok(cfg, &why)) return 0;
+  return (size_t)page_bytes_of(cfg);
+}
+
+SPEC_API size_t spec_kv4_bytes(const spec_model_config* cfg, int32_t n_samples, int32_t n_pages) {
+  const size_t page = spec_kv4_page_bytes(cfg);
+  if (page == 0 || n_samples < 1 || n_pages < 1) return 0;
+  return align_up(page * n_pages) + align_up((size_t)n_samples * sizeof(Kv4CommitInfo));
+}
+
+SPEC_API int spec_kv4_alloc(const spec_model_config* cfg, int32_t n_samples, int32_t n_pages, void* device_buf,
+                            size_t buf_bytes, spec_kv4** out) {
+  return guarded([&]() -> int {
+    if (!cfg || !device_buf || !out) return fail(SPEC_ERR_INVALID, "null argument");
+    if (n_samples < 1 || n_pages < 1) return fail(SPEC_ERR_INVALID, "n_samples and n_pages must be >= 1");
+    std::string why;
+    if (!config_ok(cfg, &why)) return fail(SPEC_ERR_UNSUPPORTED, "%s", why.c_str());
+    if ((uintptr_t)device_buf % kAlign) return fail(SPEC_ERR_INVALID, "device_buf not 256-byte aligned");
+    const size_t need = spec_kv4_bytes(cfg, n_samples, n_pages);
+    if (buf_bytes < need)
+      return fail(SPEC_ERR_CAPACITY, "KV buffer holds %zu bytes, needs %zu", buf_bytes, need);
+    spec_kv4* kv = new spec_kv4;
+    kv->cfg = *cfg;
+    kv->n = n_samples;
+    kv->pages.resize(n_samples);
+    kv->uses.assign(n_pages, 0);
+    kv->pool = (char*)device_buf;
+    kv->ctl_off = align_up((size_t)page_bytes_of(cfg) * n_pages);
+    *out = kv;
+    return SPEC_OK;
+  });
+}
+
+SPEC_API int spec_kv4_free(spec_kv4* kv) {
+  if (!kv) return fail(SPEC_ERR_INVALID, "null handle");
+  const int rc = kv->ring.release();
+  delete kv;
+  return rc;
+}
+
+SPEC_API int spec_kv4_map(spec_kv4* kv, int32_t sample, int32_t n_pages, const int32_t* pages) {
+  return guarded([&]() -> int {
+    if (!kv || (n_pages > 0 && !pages)) return fail(SPEC_ERR_INVALID, "null argument");
+    if (sample < 0 || sample >= kv->n) return fail(SPEC_ERR_INVALID, "sample %d out of range", sample);
+    const int total = (int)kv->uses.size();
+    if (n_pages < 0 || n_pages > total || n_pages > 0x7fffffff / kKv4Page)
+      return fail(SPEC_ERR_INVALID, "%d pages of %d", n_pages, total);
+    std::vector<char> seen(total, 0);
+    for (int i = 0; i < n_pages; ++i) {
+      if (pages[i] < 0 || pages[i] >= total)
+        return fail(SPEC_ERR_INVALID, "pages[%d] = %d outside the pool's %d", i, pages[i], total);
+      if (seen[pages[i]]) return fail(SPEC_ERR_INVALID, "page %d appears twice", pages[i]);
+      seen[pages[i]] = 1;
+    }
+    std::vector<int32_t> next(pages, pages + n_pages);
+    for (const int32_t p : kv->pages[sample]) --kv->uses[p];
+    for (const int32_t p : next) ++kv->uses[p];
+    kv->pages[sample].swap(next);
+    return SPEC_OK;
+  });
+}
+
+SPEC_API size_t spec_kv4_step_bytes(const spec_model_config* cfg, int32_t max_batch, int32_t max_rows,
+                                    int32_t max_pages) {
+  std::string why;
+  if (!cfg || max_batch < 1 || max_rows < max_batch || max_pages < 1 || !config_ok(cfg, &why)) return 0;
+  return step_layout(cfg, max_batch, max_rows, max_pages).total;
+}
+
+SPEC_API int spec_kv4_step_begin(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* row_offsets,
+                                 const int32_t* parents, const int32_t* seq_lens, void* workspace, size_t ws_bytes,
+                                 void* stream, spec_kv4_step** out) {
+  return guarded([&]() -> int {
+    if (!kv || !sample_ids || !row_offsets || !seq_lens || !workspace || !out)
+      return fail(SPEC_ERR_INVALID, "null argument");
+    if (int rc = kv4_check_rows(kv, batch, sample_ids, row_offsets, parents, seq_lens)) return rc;
+    if ((uintptr_t)workspace % kAlign) return fail(SPEC_ERR_INVALID, "workspace not 256-byte aligned");
+    const size_t need = kv4_step_bytes(&kv->cfg, batch, row_offsets[batch],
+                                       kv4_step_pages(kv, batch, row_offsets, seq_lens));
+    if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
+    if (int rc = refuse_capture(stream)) return rc;
+    spec_kv4_step* st = new spec_kv4_step;
+    int rc;
+    try {
+      rc = kv4_plan_step(kv, batch, sample_ids, row_offsets, parents, seq_lens, workspace, (hipStream_t)stream,
+                         spec_debug{}, st);
+    } catch (...) {
+      delete st;
+      throw;
+    }
+    if (rc != SPEC_OK) {
+      delete st;
+      return rc;
+    }
+    *out = st;
+    return SPEC_OK;
+  });
+}
+
+SPEC_API int spec_kv4_step_free(spec_kv4_step* step) {
+  if (!step) return fail(SPEC_ERR_INVALID, "null handle");
+  delete step;
+  return SPEC_OK;
+}
+
+namespace {
+
+int check_layer(const spec_kv4_step* step, int32_t layer) {
+  if (layer < 0 || layer >= step->kv->cfg.n_layers) return fail(SPEC_ERR_INVALID, "layer %d out of range", layer);
+  return SPEC_OK;
+}
+
+// Rows of `width` values `stride` apart, accessed 16 bytes at a time.
+int check_strided(const char* what, const void* p, int64_t stride, int64_t width) {
+  if (!p) return fail(SPEC_ERR_INVALID, "null argument");
+  if ((uintptr_t)p % 16) return fail(SPEC_ERR_INVALID, "%s not 16-byte aligned", what);
+  if (stride < width || stride % 8)
+    return fail(SPEC_ERR_INVALID, "%s: row stride %lld must be a multiple of 8 and at least %lld", what,
+                (long long)stride, (long long)width);
+  return SPEC_OK;
+}
+
+int check_kv_rows(const spec_kv4_step* step, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                  int64_t v_stride) {
+  if (!step) return fail(SPEC_ERR_INVALID, "null argument");
+  if (int rc = check_layer(step, layer)) return rc;
+  const spec_model_config& c = step->kv->cfg;
+  if (int rc = check_strided("k", k, k_stride, (int64_t)c.n_kv_heads * c.head_dim)) return rc;
+  return check_strided("v", v, v_stride, (int64_t)c.n_kv_heads * c.head_dim);
+}
+
+}  // namespace
+
+SPEC_API int spec_kv4_append(const spec_kv4_step* step, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, int32_t rotate, void* stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_kv_rows(step, layer, k, k_stride, v, v_stride)) return rc;
+    return kv4_append(step, layer, (const bf16*)k, k_stride, (const bf16*)v, v_stride, rotate != 0,
+                      (hipStream_t)stream);
+  });
+}
+
+SPEC_API int spec_kv4_read(const spec_kv4_step* step, int32_t layer, void* k, int64_t k_stride, void* v,
+                           int64_t v_stride, void* stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_kv_rows(step, layer, k, k_stride, v, v_stride)) return rc;
+    Kv4RowArgs a = step->rows;
+    a.v.layer = layer;
+    a.k = (bf16*)k;
+    a.val = (bf16*)v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    HIP_TRY(launch_kv4_read(a, (hipStream_t)stream), "kv4 read");
+    return SPEC_OK;
+  });
+}
+
+SPEC_API int spec_kv4_attend(const spec_kv4_step* step, int32_t layer, const void* q, int64_t q_stride, void* out,
+                             void* stream) {
+  return guarded([&]() -> int {
+    if (!step || !out) return fail(SPEC_ERR_INVALID, "null argument");
+    if (int rc = check_layer(step, layer)) return rc;
+    const spec_model_config& c = step->kv->cfg;
+    if (int rc = check_strided("q", q, q_stride, (int64_t)c.n_heads * c.head_dim)) return rc;
+    if ((uintptr_t)out % 16) return fail(SPEC_ERR_INVALID, "out not 16-byte aligned");
+    return kv4_attend(step, layer, (const bf16*)q, q_stride, (bf16*)out, (hipStream_t)stream);
+  });
+}
+
+SPEC_API int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* seq_lens,
+                             const int32_t* accepted_len, const int32_t* accepted_nodes, int32_t* new_seq_lens,
+                             void* stream) {
+  return guarded([&]() -> int {
+    if (!kv || !sample_ids || !seq_lens || !accepted_len || !accepted_nodes || !new_seq_lens)
+      return fail(SPEC_ERR_INVALID, "null argument");
+    if (batch < 1 || batch > kv->n) return fail(SPEC_ERR_INVALID, "batch %d out of range", batch);
+    if (int rc = check_sample_ids(kv->n, batch, sample_ids)) return rc;
+    std::vector<Kv4CommitInfo> info(batch);
+    for (int b = 0; b < batch; ++b) {
+      const int id = sample_ids[b], S = seq_lens[b];
+      const int64_t cap = mapped(kv, id);
+      if (S < 0 || S >= cap)
+        return fail(SPEC_ERR_CAPACITY, "seq_lens[%d] = %d outside the %lld positions of its pages", b, S,
+                    (long long)cap);
+      if (int rc = check_unshared(kv, id, S, std::min<int64_t>(cap, (int64_t)S + SPEC_MAX_TREE))) return rc;
+      info[b] = Kv4CommitInfo{S, (int32_t)cap, {-1, -1, -1, -1, -1, -1}};
+      for (int i = 0; i < 6 && S / kKv4Page + i < (int)kv->pages[id].size(); ++i)
+        info[b].pages[i] = kv->pages[id][S / kKv4Page + i];
+    }
+    if (int rc = refuse_capture(stream)) return rc;
+    hipStream_t s = (hipStream_t)stream;
+    void* ctl = kv->pool + kv->ctl_off;
+    if (int rc = kv->ring.upload(info.data(), batch * sizeof(Kv4CommitInfo), ctl, s)) return rc;
+    const spec_model_config& c = kv->cfg;
+    HIP_TRY(timed(SPEC_K_COMMIT, s, [&] {
+              return launch_kv4_compact((const Kv4CommitInfo*)ctl, batch, kv->pool, page_bytes_of(&c), c.n_layers,
+                                        c.n_kv_heads, c.head_dim, accepted_len, accepted_nodes, new_seq_lens, s);
+            }),
+            "kv4 compact");
+    return SPEC_OK;
+  });
+}

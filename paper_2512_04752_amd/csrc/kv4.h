@@ -1,0 +1,78 @@
+// The 4-bit paged KV cache: layout, device descriptors and launcher prototypes.
+#pragma once
+
+#include "common.h"
+
+namespace spec {
+
+constexpr int kKv4Page = SPEC_KV4_PAGE;   // positions per page
+static_assert(kKv4Page == 64, "two blocks of 32 keys, eight octets");
+
+// One head of one layer in a page, see specverify.h: key codes, value codes, key
+// scales, value scales.
+constexpr __host__ __device__ int kv4_head_bytes(int hd) { return kKv4Page * (hd + hd / 32 + 2); }
+constexpr __host__ __device__ int kv4_block_bytes(int hd) { return 16 * hd; }      // codes of 32 keys
+constexpr __host__ __device__ int kv4_octet_bytes(int hd) { return 4 * hd; }       // value codes of 8 keys
+constexpr __host__ __device__ int kv4_value_at(int hd) { return kKv4Page * hd / 2; }
+constexpr __host__ __device__ int kv4_kscale_at(int hd) { return kKv4Page * hd; }
+constexpr __host__ __device__ int kv4_vscale_at(int hd) { return kKv4Page * (hd + hd / 32); }
+
+// Where a step's cache lies.  SampleInfo::kv_base is the sample's first entry in `table`.
+struct Kv4View {
+  char* pool;
+  int64_t page_bytes;
+  const int32_t* table;          // page ids, each sample's in position order
+  const SampleInfo* samples;
+  int layer, n_kv_heads, head_dim;
+};
+
+// The rows of one sample that fall into one aligned group of eight positions
+// [slot0, slot0 + 8): positions slot0 + lo .. slot0 + hi - 1.
+struct Kv4Octet {
+  int32_t sample, slot0, lo, hi;
+};
+static_assert(sizeof(Kv4Octet) == 16, "Kv4Octet layout");
+
+struct Kv4RowArgs {
+  Kv4View v;
+  const Kv4Octet* octets;
+  int n_octets;
+  const TokInfo* toks;           // rows' positions (trees); NULL: a row's position is its slot
+  const double* freq;            // [head_dim / 2] rotary frequencies
+  bf16* k;                       // row r, head g at k + r * k_stride + g * head_dim
+  bf16* val;
+  int64_t k_stride, v_stride;
+  int rotate;
+};
+
+// Quantise rows into the cache (k, val are read), or read them back (written).
+hipError_t launch_kv4_append(const Kv4RowArgs& a, hipStream_t s);
+hipError_t launch_kv4_read(const Kv4RowArgs& a, hipStream_t s);
+
+struct Kv4AttnArgs {
+  Kv4View v;
+  const bf16* q;                 // row r, query head i at q + r * q_stride + i * head_dim
+  int64_t q_stride;
+  const uint64_t* anc;           // [N][kAncWords] (trees); NULL: row i sees rows 0 .. i (runs)
+  const AttnItem* items[3];      // work-groups of 1, 2 and 4 row tiles (four waves each)
+  int n_items[3];
+  float* part_o;                 // [slots][32][head_dim], divided by its l
+  float* part_ml;                // [slots][32][2]
+  bf16* out;                     // [N][n_heads*head_dim]
+  int n_heads;
+  const CombineItem* comb;
+  int n_comb;
+};
+hipError_t launch_kv4_attention(const Kv4AttnArgs& a, hipStream_t s);
+
+// One sample of a commit: the pages of positions from seq_len / 64 * 64 on.
+struct Kv4CommitInfo {
+  int32_t seq_len, cap;          // cap: positions the mapped pages hold
+  int32_t pages[6];              // -1 past the mapped pages
+};
+static_assert(sizeof(Kv4CommitInfo) == 32, "Kv4CommitInfo layout");
+hipError_t launch_kv4_compact(const Kv4CommitInfo* info, int batch, char* pool, int64_t page_bytes,
+                              int n_layers, int n_kv_heads, int head_dim, const int32_t* accepted_len,
+                              const int32_t* accepted_nodes, int32_t* new_seq_lens, hipStream_t s);
+
+}  // namespace spec

@@ -1,0 +1,381 @@
+// The 4-bit paged KV cache: rows quantised into it, read back, and moved when a
+// branch is committed.
+//
+// A number is an E2M1 code times its group's power of two s = 2^e: 32
+// consecutive dims of a key make a group, so do all dims of a value.  e is the
+// smallest exponent in [-126, 125] with max |x| <= 6 s, or 125; the code is the one
+// nearest to x / s, the even one of two equally near.
+#include <algorithm>
+#include <math.h>
+
+#include "kv4.h"
+
+namespace spec {
+
+namespace {
+
+constexpr int kWaves = 4;                        // waves per work-group
+constexpr int64_t kMaxGrid = 0xffffffffll / 256;
+
+// x rounded to fp32 so that a second rounding to at most 22 bits gives what one
+// rounding of x would: toward zero, with the last bit set when something was cut.
+__device__ __forceinline__ float round_to_odd(double x) {
+  const float f = (float)x;
+  const double d = (double)f;
+  uint32_t b = __float_as_uint(f);
+  if (d != x) b = (b - (fabs(d) > fabs(x) ? 1u : 0u)) | 1u;
+  return __uint_as_float(b);
+}
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// e + 127 for a group whose largest magnitude has the fp32 bits `top`; 255 when
+// the group holds an infinity or NaN.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  if (top >= 0x7f800000u) return 255u;
+  // top = 1.m 2^(E - 127) <= 6 2^e = 1.5 2^(e + 2)
+  const int b = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x400000u ? 1 : 0);
+  return (uint32_t)min(max(b, 1), 252);
+}
+
+// Eight E2M1 codes of f / 2^(byte - 127), dim n in bits 4n .. 4n + 3; 0 for a
+// group without a scale, and 0 rather than -0.
+__device__ __forceinline__ uint32_t pack_codes(const float (&f)[8], uint32_t byte) {
+  const float s = __uint_as_float(byte << 23);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], s, 3);
+  const uint32_t some = ((w & 0x77777777u) + 0x77777777u) & 0x88888888u;   // magnitude bits set
+  w &= some | 0x77777777u;
+  return byte == 255u ? 0u : w;
+}
+
+// The number of a code: its exponent and mantissa bits read as fp32's are 2^-126
+// times the E2M1 number, subnormals included.
+__device__ __forceinline__ float code_value(uint32_t code, float s) {
+  const float m = __uint_as_float((code & 7u) << 22) * 0x1p126f;
+  return (code & 8u ? -m : m) * s;
+}
+
+// A row's lanes: HD / 8 lanes of 8 consecutive dims, so a wave holds 64 / (HD / 8)
+// rows at a time and takes an octet's 8 keys in KPL steps.
+template <int HD>
+struct Rows {
+  static constexpr int LPR = HD / 8;
+  static constexpr int RPW = 64 / LPR;
+  static constexpr int KPL = 8 / RPW;
+  static constexpr int WORDS = HD / 64;       // value-code words of an octet per lane
+};
+
+// Quantise one octet's rows of a sample, a wave per head at a time.
+//
+// The rotation is computed in doubles and rounded once, to the code: every
+// angle's sine and cosine is taken once per work-group (position and pair) and
+// shared by its heads through LDS.
+// A value's codes are held with the octet's 8 keys in one word per dim, so the
+// wave transposes them through LDS; positions of the octet that are not written
+// keep their codes.
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4RowArgs a, int heads_per_wg) {
+  using R = Rows<HD>;
+  constexpr int HALF = HD / 2;
+  __shared__ double2 turn[8][HALF + HALF / 8];        // one pad every 8: lanes of a row 144 bytes apart
+  __shared__ uint32_t vcode[kWaves][8][HD / 8];
+  const Kv4Octet oc = a.octets[blockIdx.x];
+  const SampleInfo si = a.v.samples[oc.sample];
+  const int row0 = si.tok0 + (oc.slot0 - si.seq_len);  // row of position slot0, below tok0 when lo > 0
+  if (a.rotate) {
+    for (int x = threadIdx.x; x < 8 * HALF; x += 256) {
+      const int t = x / HALF, j = x % HALF;
+      if (t >= oc.lo && t < oc.hi) {
+        const int pos = a.toks ? a.toks[row0 + t].pos : oc.slot0 + t;
+        double sn, cn;
+        sincos((double)pos * a.freq[j], &sn, &cn);
+        turn[t][j + j / 8] = make_double2(cn, sn);
+      }
+    }
+    __syncthreads();
+  }
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int q = lane / R::LPR, l = lane % R::LPR;
+  const int at = oc.slot0 % kKv4Page;                 // in the page
+  char* page = a.v.pool + (int64_t)a.v.table[si.kv_base + oc.slot0 / kKv4Page] * a.v.page_bytes;
+  const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, a.v.n_kv_heads);
+  for (int head = h0 + w; head < h1; head += kWaves) {
+    char* base = page + ((int64_t)a.v.layer * a.v.n_kv_heads + head) * kv4_head_bytes(HD);
+    i32x4 kx[R::KPL], vx[R::KPL];
+#pragma unroll
+    for (int kk = 0; kk < R::KPL; ++kk) {
+      const int t = q + R::RPW * kk;
+      kx[kk] = vx[kk] = i32x4{0, 0, 0, 0};
+      if (t >= oc.lo && t < oc.hi) {
+        kx[kk] = *(const i32x4*)(a.k + (row0 + t) * a.k_stride + head * HD + 8 * l);
+        vx[kk] = *(const i32x4*)(a.val + (row0 + t) * a.v_stride + head * HD + 8 * l);
+      }
+    }
+#pragma unroll
+    for (int kk = 0; kk < R::KPL; ++kk) {
+      const int t = q + R::RPW * kk;
+      const bool live = t >= oc.lo && t < oc.hi;
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (uint32_t)kx[kk][i];
+        f[2 * i] = bf16_lo(x);
+        f[2 * i + 1] = bf16_hi(x);
+      }
+      if (a.rotate) {
+        const double sign = l < R::LPR / 2 ? -1.0 : 1.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t y = (uint32_t)__shfl_xor(kx[kk][i], R::LPR / 2);
+          const int j = 8 * (l % (R::LPR / 2)) + 2 * i;
+          const double2 c0 = turn[t][j + j / 8], c1 = turn[t][j + j / 8 + 1];
+          f[2 * i] = round_to_odd((double)f[2 * i] * c0.x + sign * (double)bf16_lo(y) * c0.y);
+          f[2 * i + 1] = round_to_odd((double)f[2 * i + 1] * c1.x + sign * (double)bf16_hi(y) * c1.y);
+        }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+      const uint32_t sb = scale_byte(top);
+      if (live) {
+        const int s = at + t;
+        *(uint32_t*)(base + (s / 32) * kv4_block_bytes(HD) + (l / 4) * 512 + (s % 32) * 16 + (l % 4) * 4) =
+            pack_codes(f, sb);
+        if (l % 4 == 0) *(uint8_t*)(base + kv4_kscale_at(HD) + s * (HD / 32) + l / 4) = (uint8_t)sb;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (uint32_t)vx[kk][i];
+        f[2 * i] = bf16_lo(x);
+        f[2 * i + 1] = bf16_hi(x);
+      }
+      top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+#pragma unroll
+      for (int m = 1; m < R::LPR; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+      const uint32_t vb = scale_byte(top);
+      vcode[w][t][l] = pack_codes(f, vb);
+      if (live && l == 0)
+        *(uint16_t*)(base + kv4_vscale_at(HD) + 2 * (at + t)) = vb == 255u ? 0x7fc0 : (uint16_t)(vb << 7);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    // Word (m, i) of the octet: dim 32 i + m of keys 0 .. 7.
+    uint32_t* vw = (uint32_t*)(base + kv4_value_at(HD) + (at / 8) * kv4_octet_bytes(HD)) + lane * R::WORDS;
+    const uint32_t hi_mask = oc.hi == 8 ? 0xffffffffu : (1u << (4 * oc.hi)) - 1;
+    const uint32_t mask = hi_mask & ~((1u << (4 * oc.lo)) - 1);
+#pragma unroll
+    for (int x = 0; x < R::WORDS; ++x) {
+      const int wi = lane * R::WORDS + x, m = wi / (HD / 32), d = 32 * (wi % (HD / 32)) + m;
+      uint32_t word = 0;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) word |= (vcode[w][t][d / 8] >> (4 * (d % 8)) & 15u) << (4 * t);
+      if (mask != 0xffffffffu) word = (vw[x] & ~mask) | (word & mask);
+      vw[x] = word;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// What the cache holds for one octet's rows, as bf16 (exact: two significant bits).
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowArgs a, int heads_per_wg) {
+  using R = Rows<HD>;
+  __shared__ uint32_t vword[kWaves][HD];
+  const Kv4Octet oc = a.octets[blockIdx.x];
+  const SampleInfo si = a.v.samples[oc.sample];
+  const int row0 = si.tok0 + (oc.slot0 - si.seq_len);
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int q = lane / R::LPR, l = lane % R::LPR;
+  const int at = oc.slot0 % kKv4Page;
+  const char* page = a.v.pool + (int64_t)a.v.table[si.kv_base + oc.slot0 / kKv4Page] * a.v.page_bytes;
+  const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, a.v.n_kv_heads);
+  for (int head = h0 + w; head < h1; head += kWaves) {
+    const char* base = page + ((int64_t)a.v.layer * a.v.n_kv_heads + head) * kv4_head_bytes(HD);
+    const uint32_t* vw = (const uint32_t*)(base + kv4_value_at(HD) + (at / 8) * kv4_octet_bytes(HD));
+#pragma unroll
+    for (int x = 0; x < R::WORDS; ++x) vword[w][lane * R::WORDS + x] = vw[lane * R::WORDS + x];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int kk = 0; kk < R::KPL; ++kk) {
+      const int t = q + R::RPW * kk;
+      if (t < oc.lo || t >= oc.hi) continue;
+      const int s = at + t;
+      const uint32_t kw = *(const uint32_t*)(base + (s / 32) * kv4_block_bytes(HD) + (l / 4) * 512 +
+                                             (s % 32) * 16 + (l % 4) * 4);
+      const uint32_t sb = *(const uint8_t*)(base + kv4_kscale_at(HD) + s * (HD / 32) + l / 4);
+      const uint32_t vs = *(const uint16_t*)(base + kv4_vscale_at(HD) + 2 * s);
+      const float ks = sb == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(sb << 23);
+      const float fs = __uint_as_float(vs << 16);
+      i32x4 ko, vo;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t kb[2], vb[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int n = 2 * i + j, d = 8 * l + n;
+          kb[j] = __float_as_uint(code_value(kw >> (4 * n) & 15u, ks)) >> 16;
+          vb[j] = __float_as_uint(code_value(vword[w][(d % 32) * (HD / 32) + d / 32] >> (4 * t) & 15u, fs)) >> 16;
+        }
+        ko[i] = (int)(kb[0] | kb[1] << 16);
+        vo[i] = (int)(vb[0] | vb[1] << 16);
+      }
+      *(i32x4*)(a.k + (row0 + t) * a.k_stride + head * HD + 8 * l) = ko;
+      *(i32x4*)(a.val + (row0 + t) * a.v_stride + head * HD + 8 * l) = vo;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Move the accepted branch of one sample, one layer and head: position seq_len + d
+// takes the codes and scales of node path[d] > d, d = 1 .. accepted_len.  A thread
+// owns one word column of the keys and one dim of the values, and within those it
+// goes up in d.  What it overwrites lies at d, what it still has to read at
+// path[d'] > d' > d, so nothing is lost and no thread waits for another.
+template <int HD>
+__global__ __launch_bounds__(128) void kv4_compact_kernel(const Kv4CommitInfo* info, char* pool,
+                                                          int64_t page_bytes, int n_kv_heads,
+                                                          const int32_t* accepted_len,
+                                                          const int32_t* accepted_nodes,
+                                                          int32_t* new_seq_lens) {
+  constexpr int PER = 8;
+  const int b = blockIdx.x, layer = blockIdx.y, head = blockIdx.z, x = threadIdx.x;
+  const Kv4CommitInfo& c = info[b];
+  const int S = c.seq_len;
+  int acc = accepted_len[b];
+  acc = min(max(acc, 0), min(kMaxTree - 1, c.cap - 1 - S));
+  if (layer == 0 && head == 0 && x == 0) new_seq_lens[b] = S + acc + 1;
+  if (acc == 0) return;
+  const int32_t* path = accepted_nodes + (size_t)b * kMaxTree;
+  const int first = S / kKv4Page * kKv4Page;
+  const int64_t in_page = ((int64_t)layer * n_kv_heads + head) * kv4_head_bytes(HD);
+  auto base = [&](int slot) { return pool + (int64_t)c.pages[(slot - first) / kKv4Page] * page_bytes + in_page; };
+  // The node that position S + d takes, or -1 when it keeps what it has.
+  auto source = [&](int d) {
+    const int nd = path[d];
+    return nd > d && nd < kMaxTree && S + nd < c.cap ? nd : -1;
+  };
+  // One column of the keys: codes (a word of every row), then scales.
+  constexpr int KW = HD / 8;
+  if (x < KW) {
+    auto word = [&](int slot) {
+      const int s = slot % kKv4Page;
+      return (uint32_t*)(base(slot) + (s / 32) * kv4_block_bytes(HD) + (x / 4) * 512 + (s % 32) * 16 + (x % 4) * 4);
+    };
+    for (int d0 = 1; d0 <= acc; d0 += PER) {
+      uint32_t v[PER];
+      int nd[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        nd[i] = d0 + i <= acc ? source(d0 + i) : -1;
+        if (nd[i] >= 0) v[i] = *word(S + nd[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (nd[i] >= 0) *word(S + d0 + i) = v[i];
+    }
+  } else if (x >= 64 && x < 64 + HD / 32 + 2) {       // a byte column of the key or value scales
+    const int y = x - 64;
+    auto byte = [&](int slot) {
+      const int s = slot % kKv4Page;
+      return (uint8_t*)(base(slot) + (y < HD / 32 ? kv4_kscale_at(HD) + s * (HD / 32) + y
+                                                  : kv4_vscale_at(HD) + 2 * s + y - HD / 32));
+    };
+    for (int d0 = 1; d0 <= acc; d0 += PER) {
+      uint8_t v[PER];
+      int nd[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        nd[i] = d0 + i <= acc ? source(d0 + i) : -1;
+        if (nd[i] >= 0) v[i] = *byte(S + nd[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (nd[i] >= 0) *byte(S + d0 + i) = v[i];
+    }
+  }
+  // One dim of the values: a word of every octet.
+  if (x < HD) {
+    const int m = x % 32, i = x / 32;
+    auto word = [&](int slot) {
+      return (uint32_t*)(base(slot) + kv4_value_at(HD) + (slot % kKv4Page) / 8 * kv4_octet_bytes(HD)) +
+             m * (HD / 32) + i;
+    };
+    for (int o = (S + 1) / 8 * 8; o <= S + acc; o += 8) {
+      uint32_t got[8];
+      uint32_t mask = 0;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int d = o + t - S;
+        const int nd = d >= 1 && d <= acc ? source(d) : -1;
+        got[t] = 0;
+        if (nd >= 0) {
+          got[t] = (*word(S + nd) >> (4 * ((S + nd) % 8)) & 15u) << (4 * t);
+          mask |= 15u << (4 * t);
+        }
+      }
+      if (mask == 0) continue;
+      uint32_t v = *word(o) & ~mask;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v |= got[t];
+      *word(o) = v;
+    }
+  }
+}
+
+// Heads per work-group of the row kernels: all of them when there are octets
+// enough to fill the chip (an angle is then taken once), else one per wave.
+int heads_per_wg(int n_octets, int n_kv_heads) {
+  return n_octets >= 1024 ? n_kv_heads : std::min(n_kv_heads, kWaves);
+}
+
+template <class K64, class K128>
+hipError_t launch_rows(const Kv4RowArgs& a, hipStream_t s, K64 k64, K128 k128) {
+  if (a.n_octets == 0) return hipSuccess;
+  if (a.n_octets > kMaxGrid) return hipErrorInvalidValue;
+  const int hpw = heads_per_wg(a.n_octets, a.v.n_kv_heads);
+  const dim3 grid(a.n_octets, (a.v.n_kv_heads + hpw - 1) / hpw);
+  if ((int64_t)grid.x * grid.y > kMaxGrid) return hipErrorInvalidValue;
+  if (a.v.head_dim == 128) k128<<<grid, 256, 0, s>>>(a, hpw);
+  else if (a.v.head_dim == 64) k64<<<grid, 256, 0, s>>>(a, hpw);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_append(const Kv4RowArgs& a, hipStream_t s) {
+  return launch_rows(a, s, kv4_append_kernel<64>, kv4_append_kernel<128>);
+}
+
+hipError_t launch_kv4_read(const Kv4RowArgs& a, hipStream_t s) {
+  return launch_rows(a, s, kv4_read_kernel<64>, kv4_read_kernel<128>);
+}
+
+hipError_t launch_kv4_compact(const Kv4CommitInfo* info, int batch, char* pool, int64_t page_bytes,
+                              int n_layers, int n_kv_heads, int head_dim, const int32_t* accepted_len,
+                              const int32_t* accepted_nodes, int32_t* new_seq_lens, hipStream_t s) {
+  const dim3 grid(batch, n_layers, n_kv_heads);
+  if (head_dim == 128)
+    kv4_compact_kernel<128><<<grid, 128, 0, s>>>(info, pool, page_bytes, n_kv_heads, accepted_len,
+                                                 accepted_nodes, new_seq_lens);
+  else if (head_dim == 64)
+    kv4_compact_kernel<64><<<grid, 128, 0, s>>>(info, pool, page_bytes, n_kv_heads, accepted_len,
+                                                accepted_nodes, new_seq_lens);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace spec
