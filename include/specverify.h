@@ -325,7 +325,8 @@ int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int3
  * or spec_verify_kv4, which does all but the commit.  spec_kv4_append,
  * _read and _attend only launch kernels: they can be captured into a graph and
  * replayed while the step, its workspace and its pages stay as they are.
- * _step_begin and _commit upload descriptors and refuse a capturing stream. */
+ * _step_begin, _commit and spec_verify_kv4 upload descriptors and refuse a
+ * capturing stream. */
 #define SPEC_KV4_PAGE 64
 
 typedef struct spec_kv4 spec_kv4;             /* opaque pool handle (host, owned by the library) */
@@ -407,6 +408,21 @@ int spec_kv4_read(const spec_kv4_step* step, int32_t layer, void* k, int64_t k_s
  * sums and softmax statistics are fp32.  Bitwise the same for the same step. */
 int spec_kv4_attend(const spec_kv4_step* step, int32_t layer, const void* q, int64_t q_stride,
                     void* out, void* stream);
+
+/* Workspace bytes spec_verify_kv4 needs; max_pages as in spec_kv4_step_bytes, sampled
+ * nonzero for a temperature > 0; 0 if an argument is invalid. */
+size_t spec_workspace_bytes_kv4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
+                                int32_t max_pages, int32_t sampled);
+
+/* spec_verify (samp NULL) or spec_verify_sampled over this pool: the same arguments
+ * and outputs, committed positions in kv's pages (S_b + T_b <= 64 * pages, the pages
+ * of positions from S_b on not shared), workspace 256-byte aligned.  K and V leave the
+ * projection as bf16 (rotated) and enter the cache, and the attention, in 4 bits. */
+int spec_verify_kv4(const spec_model_config* cfg, const spec_weights* w, spec_kv4* kv, int32_t batch,
+                    const int32_t* sample_ids, const int32_t* tree_offsets, const int32_t* tree_tokens,
+                    const int32_t* tree_parents, const int32_t* seq_lens, void* workspace,
+                    size_t ws_bytes, void* stream, const spec_sampling* samp, int32_t* accepted_len,
+                    int32_t* next_token, int32_t* accepted_nodes, const spec_debug* dbg);
 
 /* spec_kv_commit for this pool: the codes and scales of node accepted_nodes[b][d]
  * move to position S_b + d for d = 1 .. accepted_len[b], all layers, and

@@ -33,7 +33,8 @@ EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_lay
            "spec_verify_sampled", "spec_verify_noalloc", "spec_gemm_plan", "spec_kv4_page_bytes",
            "spec_kv4_bytes", "spec_kv4_alloc", "spec_kv4_free", "spec_kv4_map",
            "spec_kv4_step_bytes", "spec_kv4_step_begin", "spec_kv4_step_free", "spec_kv4_append",
-           "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit")
+           "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit",
+           "spec_workspace_bytes_kv4", "spec_verify_kv4")
 SPEC_KV4_PAGE = 64                # positions per page of the 4-bit pool
 SPEC_NOALLOC_SCRATCH_BYTES = 320 << 20
 
@@ -143,7 +144,11 @@ def lib():
     L.spec_kv4_attend.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p]
     L.spec_kv4_commit.argtypes = [c_void_p, c_int32, i32p, i32p, c_void_p, c_void_p, c_void_p,
                                   c_void_p]
-    for name in ("spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
+    L.spec_workspace_bytes_kv4.argtypes = [POINTER(spec_model_config), c_int32, c_int32, c_int32,
+                                           c_int32]
+    L.spec_workspace_bytes_kv4.restype = c_size_t
+    L.spec_verify_kv4.argtypes = L.spec_verify_sampled.argtypes
+    for name in ("spec_verify_kv4", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
                  "spec_kv_commit", "spec_profile_begin", "spec_profile_end", "spec_kv_pack",
                  "spec_kv_unpack", "spec_cost_model_create", "spec_cost_model_free",
                  "spec_cost_model_stats", "spec_select_draft_count", "spec_verify_sampled",
@@ -314,6 +319,15 @@ def spec_workspace_bytes_sampled(cfg, max_batch, max_tokens) -> int:
     return int(lib().spec_workspace_bytes_sampled(ctypes.byref(c), max_batch, max_tokens))
 
 
+def _sampling(cfg, n, temperature, eos_token, draft_probs, uniforms) -> spec_sampling:
+    if temperature > 0:
+        for t, cols, what in ((draft_probs, cfg.vocab, "draft_probs"), (uniforms, 2, "uniforms")):
+            if (t is None or t.dtype != torch.float32 or not t.is_contiguous()
+                    or tuple(t.shape) != (n, cols)):
+                raise ValueError(f"{what} must be a contiguous float32 [{n}, {cols}] tensor")
+    return spec_sampling(float(temperature), int(eos_token), _ptr(draft_probs), _ptr(uniforms))
+
+
 def spec_verify_sampled(cfg, weights: Weights, kv: KVPool, sample_ids, tree_offsets, tree_tokens,
                         tree_parents, seq_lens, workspace, accepted_len, next_token,
                         accepted_nodes, temperature, eos_token=-1, draft_probs=None,
@@ -327,13 +341,7 @@ def spec_verify_sampled(cfg, weights: Weights, kv: KVPool, sample_ids, tree_offs
     toks, p_toks = _i32(tree_tokens)
     pars, p_pars = _i32(tree_parents)
     lens, p_lens = _i32(seq_lens)
-    n = int(offs[-1])
-    if temperature > 0:
-        for t, cols, what in ((draft_probs, cfg.vocab, "draft_probs"), (uniforms, 2, "uniforms")):
-            if (t is None or t.dtype != torch.float32 or not t.is_contiguous()
-                    or tuple(t.shape) != (n, cols)):
-                raise ValueError(f"{what} must be a contiguous float32 [{n}, {cols}] tensor")
-    samp = spec_sampling(float(temperature), int(eos_token), _ptr(draft_probs), _ptr(uniforms))
+    samp = _sampling(cfg, int(offs[-1]), temperature, eos_token, draft_probs, uniforms)
     dbg = None
     if debug:
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
@@ -527,6 +535,37 @@ def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
     with torch.cuda.device(step.pool.buf.device):
         _check(lib().spec_kv4_attend(step.handle, int(layer), _ptr(q), qs, _ptr(out),
                                      _stream(stream)))
+
+
+def spec_workspace_bytes_kv4(cfg, max_batch, max_tokens, max_pages, sampled=False) -> int:
+    c = make_config(cfg)
+    return int(lib().spec_workspace_bytes_kv4(ctypes.byref(c), max_batch, max_tokens, max_pages,
+                                              int(sampled)))
+
+
+def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offsets, tree_tokens,
+                    tree_parents, seq_lens, workspace, accepted_len, next_token, accepted_nodes,
+                    temperature=0.0, eos_token=-1, draft_probs=None, uniforms=None, debug=None,
+                    stream=None):
+    """spec_verify (or, with a temperature or an EOS token, spec_verify_sampled) over a 4-bit
+    pool."""
+    c = make_config(cfg)
+    ids, p_ids = _i32(sample_ids)
+    offs, p_offs = _i32(tree_offsets)
+    toks, p_toks = _i32(tree_tokens)
+    pars, p_pars = _i32(tree_parents)
+    lens, p_lens = _i32(seq_lens)
+    samp = _sampling(cfg, int(offs[-1]), temperature, eos_token, draft_probs, uniforms)
+    dbg = None
+    if debug:
+        dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
+                           for k in ("logits", "argmax", "depth", "pos", "anc")])
+    with torch.cuda.device(pool.buf.device):
+        _check(lib().spec_verify_kv4(ctypes.byref(c), ctypes.byref(weights.struct), pool.handle,
+                                     len(ids), p_ids, p_offs, p_toks, p_pars, p_lens, _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream(stream),
+                                     ctypes.byref(samp), _ptr(accepted_len), _ptr(next_token),
+                                     _ptr(accepted_nodes), ctypes.byref(dbg) if dbg else None))
 
 
 def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_nodes, new_seq_lens,

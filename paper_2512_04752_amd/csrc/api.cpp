@@ -12,7 +12,7 @@
 #include <vector>
 
 #include "common.h"
-#include "host.h"
+#include "kv4_host.h"
 #include "specverify.h"
 
 using namespace spec;
@@ -88,7 +88,7 @@ size_t sample_bytes(const spec_model_config* c, int32_t cap) {
 // Workspace carving; every region 256-byte aligned.
 struct WsLayout {
   size_t blob, toks, anc, rope, x, h, q, o, act, part_o, part_ml, lm_val, lm_idx, argmax, splitk,
-      logits, resid, total;
+      logits, resid, kv4_step, kv4_rows, total;
   size_t blob_bytes;
 };
 
@@ -97,14 +97,17 @@ int64_t max_row_tiles(const spec_model_config* c, int64_t max_batch, int64_t max
   return (int64_t)c->n_kv_heads * ((max_tokens * G + 31) / 32 + max_batch);
 }
 
+// kv4_pages > 0: over the 4-bit pool, the attention's plan and partials are the step's.
 WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_tokens,
-                   bool sampling = false) {
+                   bool sampling = false, int64_t kv4_pages = 0) {
   WsLayout L{};
+  const bool kv4 = kv4_pages > 0;
+  const int64_t part_cap = kv4 ? 0 : kPartCap;
   // attention items: one per row tile and split, then padded per XCD (at most 8x)
-  const int64_t items = 8 * (max_row_tiles(c, max_batch, max_tokens) + kPartCap);
+  const int64_t items = kv4 ? 0 : 8 * (max_row_tiles(c, max_batch, max_tokens) + kPartCap);
   L.blob_bytes = align_up(max_batch * sizeof(SampleInfo)) + 2 * align_up(max_tokens * 4) +
                  align_up(items * sizeof(AttnItem)) + 2 * kAlign +  // narrow + two wide lists
-                 align_up(kPartCap * sizeof(CombineItem));
+                 align_up(part_cap * sizeof(CombineItem));
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -113,16 +116,16 @@ WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_to
   };
   const size_t nq_hd = (size_t)c->n_heads * c->head_dim;
   L.blob = take(L.blob_bytes);
-  L.toks = take(max_tokens * sizeof(TokInfo));
-  L.anc = take(max_tokens * 8 * kAncWords);
+  L.toks = take(kv4 ? 0 : max_tokens * sizeof(TokInfo));
+  L.anc = take(kv4 ? 0 : max_tokens * 8 * kAncWords);
   L.rope = take(max_tokens * (size_t)(c->head_dim / 2) * 8);
   L.x = take(max_tokens * (size_t)c->hidden * 4);
   L.h = take(max_tokens * (size_t)c->hidden * 2);
   L.q = take(max_tokens * nq_hd * 2);
   L.o = take(max_tokens * nq_hd * 2);
   L.act = take(max_tokens * (size_t)c->ffn * 2);
-  L.part_o = take((size_t)kPartCap * 32 * c->head_dim * 2);
-  L.part_ml = take((size_t)kPartCap * 32 * 2 * 4);
+  L.part_o = take((size_t)part_cap * 32 * c->head_dim * 2);
+  L.part_ml = take((size_t)part_cap * 32 * 2 * 4);
   L.lm_val = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.lm_idx = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.argmax = take(max_tokens * 4);
@@ -130,6 +133,10 @@ WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_to
   if (sampling) {   // speculative sampling: fp32 logits, node decisions, fp64 residual rows
     L.logits = take(max_tokens * (size_t)c->vocab * 4);
     L.resid = take(sample_accept_scratch((int)max_batch, (int)max_tokens, c->vocab));
+  }
+  if (kv4) {   // the step's plan, and one layer's rotated K/V on their way into the cache
+    L.kv4_step = take(kv4_step_bytes(c, max_batch, max_tokens, kv4_pages));
+    L.kv4_rows = take(max_tokens * 2 * (size_t)c->n_kv_heads * c->head_dim * 2);
   }
   L.total = off;
   return L;
@@ -294,86 +301,14 @@ SPEC_API size_t spec_workspace_bytes(const spec_model_config* cfg, int32_t max_b
 
 namespace {
 
-int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv, int32_t batch,
-                const int32_t* sample_ids, const int32_t* tree_offsets, const int32_t* tree_tokens,
-                const int32_t* tree_parents, const int32_t* seq_lens, void* workspace,
-                size_t ws_bytes, void* stream, const spec_sampling* samp, int32_t* accepted_len,
-                int32_t* next_token, int32_t* accepted_nodes, const spec_debug* dbg,
-                bool noalloc = false) {
-  // ---- validation (no side effects) ----
-  if (!cfg || !w || !kv || !sample_ids || !tree_offsets || !tree_tokens || !tree_parents ||
-      !seq_lens || (!workspace && !noalloc) || !accepted_len || !next_token || !accepted_nodes)
-    return fail(SPEC_ERR_INVALID, "null argument");
-  std::string why;
-  if (!config_ok(cfg, &why)) return fail(SPEC_ERR_UNSUPPORTED, "%s", why.c_str());
-  if (!same_config(cfg, &kv->cfg)) return fail(SPEC_ERR_INVALID, "config differs from the KV pool's");
-  if (batch < 1) return fail(SPEC_ERR_INVALID, "batch must be >= 1");
-  if (!w->tok_embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wq || !w->wk ||
-      !w->wv || !w->wo || !w->ffn_norm || !w->w_gate || !w->w_up || !w->w_down)
-    return fail(SPEC_ERR_INVALID, "null weight pointer");
-  for (int l = 0; l < cfg->n_layers; ++l)
-    if (!w->attn_norm[l] || !w->wq[l] || !w->wk[l] || !w->wv[l] || !w->wo[l] || !w->ffn_norm[l] ||
-        !w->w_gate[l] || !w->w_up[l] || !w->w_down[l])
-      return fail(SPEC_ERR_INVALID, "null weight pointer in layer %d", l);
-  if (int rc = check_samples(kv, batch, sample_ids)) return rc;
-  if (tree_offsets[0] != 0) return fail(SPEC_ERR_TREE, "tree_offsets[0] must be 0");
-  for (int b = 0; b < batch; ++b) {
-    const int T = tree_offsets[b + 1] - tree_offsets[b];
-    if (T < 1 || T > SPEC_MAX_TREE)
-      return fail(T < 1 ? SPEC_ERR_TREE : SPEC_ERR_UNSUPPORTED, "sample %d has %d tree nodes", b, T);
-    const int S = seq_lens[b];
-    if (S < 0) return fail(SPEC_ERR_INVALID, "seq_lens[%d] = %d", b, S);
-    if ((int64_t)S + T > kv->cap[sample_ids[b]])
-      return fail(SPEC_ERR_CAPACITY, "sample %d: %d committed + %d nodes exceed capacity %d", b, S,
-                  T, kv->cap[sample_ids[b]]);
-    const int t0 = tree_offsets[b];
-    if (tree_parents[t0] != -1) return fail(SPEC_ERR_TREE, "sample %d: root parent must be -1", b);
-    for (int i = 0; i < T; ++i) {
-      const int tok = tree_tokens[t0 + i];
-      if (tok < 0 || tok >= cfg->vocab)
-        return fail(SPEC_ERR_TREE, "sample %d node %d: token %d out of range", b, i, tok);
-      if (i > 0) {
-        const int p = tree_parents[t0 + i];
-        if (p < 0 || p >= i)
-          return fail(SPEC_ERR_TREE, "sample %d node %d: parent %d not before the node", b, i, p);
-      }
-    }
-  }
-  const bool sampled = samp && samp->temperature > 0.f;
-  if (samp) {
-    if (!(samp->temperature >= 0.f) || !std::isfinite(samp->temperature))
-      return fail(SPEC_ERR_INVALID, "temperature must be finite and >= 0");
-    if (samp->eos_token < -1 || samp->eos_token >= cfg->vocab)
-      return fail(SPEC_ERR_INVALID, "eos_token %d out of range", samp->eos_token);
-    if (sampled && (!samp->draft_probs || !samp->uniforms))
-      return fail(SPEC_ERR_INVALID, "sampling needs draft_probs and uniforms");
-  }
-  const int N = tree_offsets[batch];
-  const size_t need = ws_layout(cfg, batch, N, sampled).total;
-  if (noalloc && need > SPEC_NOALLOC_SCRATCH_BYTES)
-    return fail(SPEC_ERR_WORKSPACE,
-                "%d samples with %d tree nodes need %zu bytes of workspace, more than the %zu "
-                "bytes of spec_verify_noalloc's static scratch",
-                batch, N, need, (size_t)SPEC_NOALLOC_SCRATCH_BYTES);
-  if (noalloc) {
-    HIP_TRY(noalloc_scratch(&workspace), "static scratch lookup");
-    ws_bytes = SPEC_NOALLOC_SCRATCH_BYTES;
-  }
-  if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
+// Attention work items of a step over the bf16 pool, by kernel, and the combine jobs.
+struct AttnWork {
+  std::vector<AttnItem> items, wide4, wide8;
+  std::vector<CombineItem> comb;
+};
 
-  // ---- planning ----
-  const int L = cfg->n_layers, H = cfg->hidden, nq = cfg->n_heads, nkv = cfg->n_kv_heads;
-  const int hd = cfg->head_dim, G = nq / nkv, F = cfg->ffn, V = cfg->vocab;
-  const WsLayout ly = ws_layout(cfg, batch, N, sampled);
-  char* ws = (char*)workspace;
-  hipStream_t s = (hipStream_t)stream;
-
-  std::vector<SampleInfo> si(batch);
-  for (int b = 0; b < batch; ++b) {
-    const int id = sample_ids[b];
-    si[b] = SampleInfo{kv->base[id], kv->cap[id], seq_lens[b], tree_offsets[b],
-                       tree_offsets[b + 1] - tree_offsets[b], 0, 0};
-  }
+void plan_split_kv(const spec_model_config* cfg, const std::vector<SampleInfo>& si, AttnWork* out) {
+  const int batch = (int)si.size(), nkv = cfg->n_kv_heads, G = cfg->n_heads / nkv;
   // Split-KV plan.  A row tile is 32 query rows of one (sample, kv head).  A
   // (sample, kv head) with one tile gets narrow items (2 waves dealing the
   // keys among themselves, two work-groups per CU); 2-4 tiles get one 4-wave
@@ -422,8 +357,8 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   while (part_slots(chunk) > kPartCap) chunk += 128;    // terminates: one chunk per range has none
   // Work items.  Split key ranges write their partial states to per-tile
   // slots part + tile * ns + split.
-  std::vector<AttnItem> items, wide4, wide8;
-  std::vector<CombineItem> comb;
+  std::vector<AttnItem>&items = out->items, &wide4 = out->wide4, &wide8 = out->wide8;
+  std::vector<CombineItem>& comb = out->comb;
   int part = 0;
   for (int b = 0; b < batch; ++b) {
     const int keys = (int)keys_of(b);
@@ -449,6 +384,107 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   deal_items(items);
   deal_items(wide4);
   deal_items(wide8);
+}
+
+// Over the bf16 pool `kv`, or over the 4-bit one `kv4`.
+int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv, spec_kv4* kv4,
+                int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets, const int32_t* tree_tokens,
+                const int32_t* tree_parents, const int32_t* seq_lens, void* workspace,
+                size_t ws_bytes, void* stream, const spec_sampling* samp, int32_t* accepted_len,
+                int32_t* next_token, int32_t* accepted_nodes, const spec_debug* dbg,
+                bool noalloc = false) {
+  // ---- validation (no side effects) ----
+  if (!cfg || !w || (!kv && !kv4) || !sample_ids || !tree_offsets || !tree_tokens || !tree_parents ||
+      !seq_lens || (!workspace && !noalloc) || !accepted_len || !next_token || !accepted_nodes)
+    return fail(SPEC_ERR_INVALID, "null argument");
+  std::string why;
+  if (!config_ok(cfg, &why)) return fail(SPEC_ERR_UNSUPPORTED, "%s", why.c_str());
+  if (!same_config(cfg, kv4 ? &kv4->cfg : &kv->cfg)) return fail(SPEC_ERR_INVALID, "config differs from the KV pool's");
+  if (batch < 1) return fail(SPEC_ERR_INVALID, "batch must be >= 1");
+  if (!w->tok_embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wq || !w->wk ||
+      !w->wv || !w->wo || !w->ffn_norm || !w->w_gate || !w->w_up || !w->w_down)
+    return fail(SPEC_ERR_INVALID, "null weight pointer");
+  for (int l = 0; l < cfg->n_layers; ++l)
+    if (!w->attn_norm[l] || !w->wq[l] || !w->wk[l] || !w->wv[l] || !w->wo[l] || !w->ffn_norm[l] ||
+        !w->w_gate[l] || !w->w_up[l] || !w->w_down[l])
+      return fail(SPEC_ERR_INVALID, "null weight pointer in layer %d", l);
+  if (kv4) {
+    if (int rc = kv4_check_rows(kv4, batch, sample_ids, tree_offsets, tree_parents, seq_lens)) return rc;
+    for (int i = 0; i < tree_offsets[batch]; ++i)
+      if (tree_tokens[i] < 0 || tree_tokens[i] >= cfg->vocab)
+        return fail(SPEC_ERR_TREE, "row %d: token %d out of range", i, tree_tokens[i]);
+  } else {
+    if (int rc = check_samples(kv, batch, sample_ids)) return rc;
+    if (tree_offsets[0] != 0) return fail(SPEC_ERR_TREE, "tree_offsets[0] must be 0");
+    for (int b = 0; b < batch; ++b) {
+      const int T = tree_offsets[b + 1] - tree_offsets[b];
+      if (T < 1 || T > SPEC_MAX_TREE)
+        return fail(T < 1 ? SPEC_ERR_TREE : SPEC_ERR_UNSUPPORTED, "sample %d has %d tree nodes", b, T);
+      const int S = seq_lens[b];
+      if (S < 0) return fail(SPEC_ERR_INVALID, "seq_lens[%d] = %d", b, S);
+      if ((int64_t)S + T > kv->cap[sample_ids[b]])
+        return fail(SPEC_ERR_CAPACITY, "sample %d: %d committed + %d nodes exceed capacity %d", b, S,
+                    T, kv->cap[sample_ids[b]]);
+      const int t0 = tree_offsets[b];
+      if (tree_parents[t0] != -1) return fail(SPEC_ERR_TREE, "sample %d: root parent must be -1", b);
+      for (int i = 0; i < T; ++i) {
+        const int tok = tree_tokens[t0 + i];
+        if (tok < 0 || tok >= cfg->vocab)
+          return fail(SPEC_ERR_TREE, "sample %d node %d: token %d out of range", b, i, tok);
+        if (i > 0) {
+          const int p = tree_parents[t0 + i];
+          if (p < 0 || p >= i)
+            return fail(SPEC_ERR_TREE, "sample %d node %d: parent %d not before the node", b, i, p);
+        }
+      }
+    }
+  }
+  const bool sampled = samp && samp->temperature > 0.f;
+  if (samp) {
+    if (!(samp->temperature >= 0.f) || !std::isfinite(samp->temperature))
+      return fail(SPEC_ERR_INVALID, "temperature must be finite and >= 0");
+    if (samp->eos_token < -1 || samp->eos_token >= cfg->vocab)
+      return fail(SPEC_ERR_INVALID, "eos_token %d out of range", samp->eos_token);
+    if (sampled && (!samp->draft_probs || !samp->uniforms))
+      return fail(SPEC_ERR_INVALID, "sampling needs draft_probs and uniforms");
+  }
+  const int N = tree_offsets[batch];
+  const int64_t pages = kv4 ? kv4_step_pages(kv4, batch, tree_offsets, seq_lens) : 0;
+  const size_t need = ws_layout(cfg, batch, N, sampled, pages).total;
+  if (noalloc && need > SPEC_NOALLOC_SCRATCH_BYTES)
+    return fail(SPEC_ERR_WORKSPACE,
+                "%d samples with %d tree nodes need %zu bytes of workspace, more than the %zu "
+                "bytes of spec_verify_noalloc's static scratch",
+                batch, N, need, (size_t)SPEC_NOALLOC_SCRATCH_BYTES);
+  if (noalloc) {
+    HIP_TRY(noalloc_scratch(&workspace), "static scratch lookup");
+    ws_bytes = SPEC_NOALLOC_SCRATCH_BYTES;
+  }
+  if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
+  if (kv4) {
+    if ((uintptr_t)workspace % kAlign) return fail(SPEC_ERR_INVALID, "workspace not 256-byte aligned");
+    if (int rc = refuse_capture(stream)) return rc;
+  }
+
+  // ---- planning ----
+  const int L = cfg->n_layers, H = cfg->hidden, nq = cfg->n_heads, nkv = cfg->n_kv_heads;
+  const int hd = cfg->head_dim, F = cfg->ffn, V = cfg->vocab;
+  const WsLayout ly = ws_layout(cfg, batch, N, sampled, pages);
+  char* ws = (char*)workspace;
+  hipStream_t s = (hipStream_t)stream;
+
+  std::vector<SampleInfo> si(batch);
+  for (int b = 0; b < batch; ++b) {
+    const int id = sample_ids[b], T = tree_offsets[b + 1] - tree_offsets[b];
+    // The q/k/v product writes K/V to the bf16 pool, or, on their way to the 4-bit one, to
+    // this layer's rows: a block [K, V][kv head][node][head_dim] per sample.
+    si[b] = kv4 ? SampleInfo{(int64_t)tree_offsets[b] * 2 * nkv * hd, T, 0, tree_offsets[b], T, 0, 0}
+                : SampleInfo{kv->base[id], kv->cap[id], seq_lens[b], tree_offsets[b], T, 0, 0};
+  }
+  AttnWork aw;
+  if (!kv4) plan_split_kv(cfg, si, &aw);
+  const std::vector<AttnItem>&items = aw.items, &wide4 = aw.wide4, &wide8 = aw.wide8;
+  const std::vector<CombineItem>& comb = aw.comb;
 
   // ---- one upload of the per-call descriptors ----
   const size_t o_si = 0;
@@ -470,7 +506,8 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   if (noalloc)   // no pinned staging: a copy from pageable memory, done before the call returns
     HIP_TRY(hipMemcpyAsync(ws + ly.blob, blob.data(), blob_bytes, hipMemcpyHostToDevice, s),
             "upload");
-  else if (int rc = kv->ring.upload(blob.data(), blob_bytes, ws + ly.blob, s))
+  else if (int rc = kv4 ? kv4->ring.upload(blob.data(), blob_bytes, ws + ly.blob, s)
+                        : kv->ring.upload(blob.data(), blob_bytes, ws + ly.blob, s))
     return rc;
 
   const SampleInfo* d_si = (const SampleInfo*)(ws + ly.blob + o_si);
@@ -480,8 +517,8 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   const AttnItem* d_wide4 = (const AttnItem*)(ws + ly.blob + o_wide4);
   const AttnItem* d_wide8 = (const AttnItem*)(ws + ly.blob + o_wide8);
   const CombineItem* d_comb = (const CombineItem*)(ws + ly.blob + o_comb);
-  TokInfo* d_toks = (TokInfo*)(ws + ly.toks);
-  uint64_t* d_anc = (uint64_t*)(ws + ly.anc);
+  const TokInfo* d_toks = (const TokInfo*)(ws + ly.toks);
+  const uint64_t* d_anc = (const uint64_t*)(ws + ly.anc);
   float2* d_rope = (float2*)(ws + ly.rope);
   float* d_x = (float*)(ws + ly.x);
   bf16* d_h = (bf16*)(ws + ly.h);
@@ -496,7 +533,19 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   const spec_debug& D = dbg ? *dbg : nodbg;
 
   // ---- the step ----
-  HIP_TRY(launch_tree_meta(d_si, batch, d_par, d_toks, d_anc, D.depth, D.pos, D.anc, s), "tree meta");
+  spec_kv4_step step;
+  bf16* d_kv4 = (bf16*)(ws + ly.kv4_rows);
+  if (kv4) {
+    if (int rc = kv4_plan_step(kv4, batch, sample_ids, tree_offsets, tree_parents, seq_lens, ws + ly.kv4_step, s, D,
+                               &step))
+      return rc;
+    d_toks = step.rows.toks;
+    d_anc = step.attn.anc;
+  } else {
+    HIP_TRY(launch_tree_meta(d_si, batch, d_par, (TokInfo*)(ws + ly.toks), (uint64_t*)(ws + ly.anc), D.depth, D.pos,
+                             D.anc, s),
+            "tree meta");
+  }
   HIP_TRY(launch_row_front(d_toks, d_tok, (const bf16*)w->tok_embed, (const bf16*)w->attn_norm[0], d_x, d_h,
                            N, H, cfg->rms_eps, hd, cfg->rope_theta, d_rope, s),
           "row front");
@@ -505,14 +554,14 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   ga.M = N;
   ga.samples = d_si;
   ga.toks = d_toks;
-  ga.kv_pool = kv->pool;
+  ga.kv_pool = kv4 ? d_kv4 : kv->pool;
   ga.n_kv_heads = nkv;
   ga.head_dim = hd;
   ga.rope_cs = d_rope;
   ga.partial = (float*)(ws + ly.splitk);
   AttnArgs aa{};
   aa.q = d_q;
-  aa.kv_pool = kv->pool;
+  aa.kv_pool = ga.kv_pool;
   aa.samples = d_si;
   aa.toks = d_toks;
   aa.anc = d_anc;
@@ -559,10 +608,15 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
     g.n1 = g.n2 = nkv * hd;
     g.N = g.n0 + g.n1 + g.n2;
     g.q_out = d_q;
-    g.layer = l;
+    g.layer = kv4 ? 0 : l;
     HIP_TRY(timed(SPEC_K_GEMM_QKV, s, [&] { return launch_gemm(EPI_QKV, g, s); }), "qkv gemm");
-    aa.layer = l;
-    HIP_TRY(timed(SPEC_K_ATTENTION, s, [&] { return launch_attention(aa, s); }), "attention");
+    if (kv4) {
+      if (int rc = kv4_append_blocks(&step, l, d_kv4, s)) return rc;
+      if (int rc = kv4_attend(&step, l, d_q, (int64_t)nq * hd, d_o, s)) return rc;
+    } else {
+      aa.layer = l;
+      HIP_TRY(timed(SPEC_K_ATTENTION, s, [&] { return launch_attention(aa, s); }), "attention");
+    }
     g = ga;
     g.plan = p_o;
     g.A = d_o;
@@ -633,7 +687,7 @@ SPEC_API int spec_verify(const spec_model_config* cfg, const spec_weights* w, sp
                          int32_t* accepted_len, int32_t* next_token, int32_t* accepted_nodes,
                          const spec_debug* dbg) {
   g_err.clear();
-  return verify_impl(cfg, w, kv, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
+  return verify_impl(cfg, w, kv, nullptr, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
                      seq_lens, workspace, ws_bytes, stream, nullptr, accepted_len, next_token,
                      accepted_nodes, dbg);
 }
@@ -655,7 +709,7 @@ SPEC_API int spec_verify_sampled(const spec_model_config* cfg, const spec_weight
                                  const spec_debug* dbg) {
   g_err.clear();
   if (!samp) return fail(SPEC_ERR_INVALID, "null sampling parameters");
-  return verify_impl(cfg, w, kv, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
+  return verify_impl(cfg, w, kv, nullptr, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
                      seq_lens, workspace, ws_bytes, stream, samp, accepted_len, next_token,
                      accepted_nodes, dbg);
 }
@@ -667,9 +721,29 @@ SPEC_API int spec_verify_noalloc(const spec_model_config* cfg, const spec_weight
                                  void* stream, int32_t* accepted_len, int32_t* next_token,
                                  int32_t* accepted_nodes, const spec_debug* dbg) {
   g_err.clear();
-  return verify_impl(cfg, w, kv, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
+  return verify_impl(cfg, w, kv, nullptr, batch, sample_ids, tree_offsets, tree_tokens, tree_parents,
                      seq_lens, nullptr, 0, stream, nullptr, accepted_len, next_token,
                      accepted_nodes, dbg, true);
+}
+
+SPEC_API size_t spec_workspace_bytes_kv4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
+                                         int32_t max_pages, int32_t sampled) {
+  std::string why;
+  if (!cfg || max_batch < 1 || max_tokens < max_batch || max_pages < 1 || !config_ok(cfg, &why)) return 0;
+  return ws_layout(cfg, max_batch, max_tokens, sampled != 0, max_pages).total;
+}
+
+SPEC_API int spec_verify_kv4(const spec_model_config* cfg, const spec_weights* w, spec_kv4* kv,
+                             int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets,
+                             const int32_t* tree_tokens, const int32_t* tree_parents,
+                             const int32_t* seq_lens, void* workspace, size_t ws_bytes, void* stream,
+                             const spec_sampling* samp, int32_t* accepted_len, int32_t* next_token,
+                             int32_t* accepted_nodes, const spec_debug* dbg) {
+  return guarded([&]() -> int {
+    if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
+    return verify_impl(cfg, w, nullptr, kv, batch, sample_ids, tree_offsets, tree_tokens, tree_parents, seq_lens,
+                       workspace, ws_bytes, stream, samp, accepted_len, next_token, accepted_nodes, dbg);
+  });
 }
 
 SPEC_API int spec_kv_commit(spec_kv* kv, int32_t batch, const int32_t* sample_ids,

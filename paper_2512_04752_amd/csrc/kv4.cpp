@@ -18,29 +18,6 @@ constexpr int kTargetGroups = 1024;     // attention work-groups aimed for: two 
 constexpr int kMinChunk = 256;          // keys per split, lower bound
 constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
 
-// Run the body of an entry point; no exception leaves it.
-template <class F>
-int guarded(F&& body) {
-  clear_error();
-  try {
-    return body();
-  } catch (const std::bad_alloc&) {
-    return fail(SPEC_ERR_CAPACITY, "out of host memory");
-  } catch (const std::exception& e) {
-    return fail(SPEC_ERR_INVALID, "%s", e.what());
-  }
-}
-
-// Uploads go through staging memory that the next calls reuse, so a captured one
-// would replay another call's descriptors.
-int refuse_capture(void* stream) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  HIP_TRY(hipStreamIsCapturing((hipStream_t)stream, &st), "stream capture status");
-  if (st != hipStreamCaptureStatusNone)
-    return fail(SPEC_ERR_INVALID, "the call uploads its plan and cannot be captured into a graph");
-  return SPEC_OK;
-}
-
 int64_t page_bytes_of(const spec_model_config* c) {
   return (int64_t)c->n_layers * c->n_kv_heads * kv4_head_bytes(c->head_dim);
 }
@@ -162,6 +139,14 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
 
 namespace spec {
 
+int refuse_capture(void* stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  HIP_TRY(hipStreamIsCapturing((hipStream_t)stream, &st), "stream capture status");
+  if (st != hipStreamCaptureStatusNone)
+    return fail(SPEC_ERR_INVALID, "the call uploads its plan and cannot be captured into a graph");
+  return SPEC_OK;
+}
+
 int kv4_check_rows(const spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const int32_t* offsets,
                    const int32_t* parents, const int32_t* seq_lens) {
   if (batch < 1) return fail(SPEC_ERR_INVALID, "batch must be >= 1");
@@ -255,7 +240,7 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   st->n_rows = (int)N;
   Kv4View view{kv->pool, page_bytes_of(&c), (const int32_t*)(d + o_table), d_si, 0, c.n_kv_heads, c.head_dim};
   st->rows = Kv4RowArgs{view, (const Kv4Octet*)(d + o_oct), (int)octets.size(), runs ? nullptr : toks,
-                        (const double*)(d + o_freq), nullptr, nullptr, 0, 0, 0};
+                        (const double*)(d + o_freq), nullptr, nullptr, 0, 0, 0, 0};
   Kv4AttnArgs& a = st->attn;
   a = Kv4AttnArgs{};
   a.v = view;
@@ -281,6 +266,15 @@ int kv4_append(const spec_kv4_step* st, int layer, const bf16* k, int64_t k_stri
   a.k_stride = k_stride;
   a.v_stride = v_stride;
   a.rotate = rotate;
+  HIP_TRY(timed(SPEC_K_KV4_APPEND, s, [&] { return launch_kv4_append(a, s); }), "kv4 append");
+  return SPEC_OK;
+}
+
+int kv4_append_blocks(const spec_kv4_step* st, int layer, const bf16* kv, hipStream_t s) {
+  Kv4RowArgs a = st->rows;
+  a.v.layer = layer;
+  a.k = a.val = const_cast<bf16*>(kv);
+  a.blocks = 1;
   HIP_TRY(timed(SPEC_K_KV4_APPEND, s, [&] { return launch_kv4_append(a, s); }), "kv4 append");
   return SPEC_OK;
 }

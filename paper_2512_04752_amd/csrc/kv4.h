@@ -43,6 +43,7 @@ struct Kv4RowArgs {
   bf16* val;
   int64_t k_stride, v_stride;
   int rotate;
+  int blocks;                    // append: k holds [K, V][kv head][row][head_dim] per sample instead
 };
 
 // Quantise rows into the cache (k, val are read), or read them back (written).

@@ -104,6 +104,14 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4RowArgs a, int heads
   const int at = oc.slot0 % kKv4Page;                 // in the page
   char* page = a.v.pool + (int64_t)a.v.table[si.kv_base + oc.slot0 / kKv4Page] * a.v.page_bytes;
   const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, a.v.n_kv_heads);
+  const int64_t ks = a.blocks ? HD : a.k_stride, vs = a.blocks ? HD : a.v_stride;
+  const int64_t hs = a.blocks ? (int64_t)si.ntok * HD : HD;             // between heads
+  const bf16* k0 = a.k + row0 * ks;
+  const bf16* v0 = a.val + row0 * vs;
+  if (a.blocks) {
+    k0 = a.k + (int64_t)si.tok0 * 2 * a.v.n_kv_heads * HD + (int64_t)(row0 - si.tok0) * HD;
+    v0 = k0 + a.v.n_kv_heads * hs;
+  }
   for (int head = h0 + w; head < h1; head += kWaves) {
     char* base = page + ((int64_t)a.v.layer * a.v.n_kv_heads + head) * kv4_head_bytes(HD);
     i32x4 kx[R::KPL], vx[R::KPL];
@@ -112,8 +120,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4RowArgs a, int heads
       const int t = q + R::RPW * kk;
       kx[kk] = vx[kk] = i32x4{0, 0, 0, 0};
       if (t >= oc.lo && t < oc.hi) {
-        kx[kk] = *(const i32x4*)(a.k + (row0 + t) * a.k_stride + head * HD + 8 * l);
-        vx[kk] = *(const i32x4*)(a.val + (row0 + t) * a.v_stride + head * HD + 8 * l);
+        kx[kk] = *(const i32x4*)(k0 + t * ks + head * hs + 8 * l);
+        vx[kk] = *(const i32x4*)(v0 + t * vs + head * hs + 8 * l);
       }
     }
 #pragma unroll

@@ -21,13 +21,30 @@ def flatten_trees(trees):
 
 
 class Verifier:
-    def __init__(self, cfg, W, capacity, max_batch, max_tokens, device="cuda", sampling=False):
-        """sampling=True sizes the workspace for verify_sampled at temperature > 0."""
+    def __init__(self, cfg, W, capacity, max_batch, max_tokens, device="cuda", sampling=False,
+                 cache="bf16"):
+        """sampling=True sizes the workspace for verify_sampled at temperature > 0.  cache="kv4"
+        holds K and V in the 4-bit paged pool, every sample with pages of its own for its
+        capacity (remap them with self.kv.map)."""
         self.cfg = cfg
+        self.cache = cache
         self.weights = B.Weights(W)
-        self.kv = B.KVPool(cfg, capacity, device=device)
-        nbytes = (B.spec_workspace_bytes_sampled if sampling else B.spec_workspace_bytes)(
-            cfg, max_batch, max_tokens)
+        if cache == "kv4":
+            need = [-(-int(c) // B.SPEC_KV4_PAGE) for c in capacity]
+            self.kv = B.KV4Pool(cfg, len(need), sum(need), device=device)
+            first = 0
+            for s, n in enumerate(need):
+                self.kv.map(s, range(first, first + n))
+                first += n
+            # pages of the longest samples that a step can hold at once
+            most = sum(sorted(need)[-max_batch:])
+            nbytes = B.spec_workspace_bytes_kv4(cfg, max_batch, max_tokens, most, sampling)
+        elif cache == "bf16":
+            self.kv = B.KVPool(cfg, capacity, device=device)
+            nbytes = (B.spec_workspace_bytes_sampled if sampling else B.spec_workspace_bytes)(
+                cfg, max_batch, max_tokens)
+        else:
+            raise ValueError(f"cache must be 'bf16' or 'kv4', not {cache!r}")
         if nbytes == 0:
             raise B.SpecError(-1, "invalid workspace request")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -52,6 +69,11 @@ class Verifier:
         """Enqueue one verify step; returns views of the device outputs."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
+        if self.cache == "kv4":
+            B.spec_verify_kv4(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
+                              seq_lens, self.workspace, self.accepted_len, self.next_token,
+                              self.accepted_nodes, debug=debug, stream=stream)
+            return self.accepted_len[:b], self.next_token[:b], self.accepted_nodes[:b]
         B.spec_verify(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
                       seq_lens, self.workspace, self.accepted_len, self.next_token,
                       self.accepted_nodes, debug=debug, stream=stream)
@@ -62,6 +84,8 @@ class Verifier:
         session's workspace (spec_verify_noalloc)."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
+        if self.cache != "bf16":
+            raise ValueError("verify_noalloc runs over the bf16 cache")
         B.spec_verify_noalloc(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens,
                               parents, seq_lens, self.accepted_len, self.next_token,
                               self.accepted_nodes, debug=debug, stream=stream)
@@ -72,6 +96,12 @@ class Verifier:
         """Enqueue one verify step with speculative-sampling acceptance."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
+        if self.cache == "kv4":
+            B.spec_verify_kv4(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
+                              seq_lens, self.workspace, self.accepted_len, self.next_token,
+                              self.accepted_nodes, temperature, eos_token, draft_probs, uniforms,
+                              debug=debug, stream=stream)
+            return self.accepted_len[:b], self.next_token[:b], self.accepted_nodes[:b]
         B.spec_verify_sampled(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
                               seq_lens, self.workspace, self.accepted_len, self.next_token,
                               self.accepted_nodes, temperature, eos_token, draft_probs, uniforms,
@@ -80,6 +110,7 @@ class Verifier:
 
     def commit(self, sample_ids, seq_lens, stream=None):
         b = len(sample_ids)
-        B.spec_kv_commit(self.kv, sample_ids, seq_lens, self.accepted_len, self.accepted_nodes,
-                         self.new_seq_lens, stream=stream)
+        commit = B.spec_kv4_commit if self.cache == "kv4" else B.spec_kv_commit
+        commit(self.kv, sample_ids, seq_lens, self.accepted_len, self.accepted_nodes,
+               self.new_seq_lens, stream=stream)
         return self.new_seq_lens[:b]
