@@ -24,10 +24,8 @@ FLAGS = ["-x", "hip", "-std=c++17", "-O3", "--offload-arch=gfx950", "-fPIC",
 
 
 # Per-source extra flags.  The attention kernels never see NaN (masked scores
-# are -inf), so fmax needs no NaN canonicalisation of the MFMA outputs.  (Over the
-# 4-bit cache a score may be NaN, where a key was not finite: any result will do
-# for the maximum then, the row's sums still carry the NaN.)
-EXTRA = {"attention.hip": ["-fno-honor-nans"], "kv4_attention.hip": ["-fno-honor-nans"]}
+# are -inf), so fmax needs no NaN canonicalisation of the MFMA outputs.
+EXTRA = {"attention.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src):

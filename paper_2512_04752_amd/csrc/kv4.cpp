@@ -13,9 +13,11 @@ using namespace spec;
 
 namespace {
 
-constexpr int kPartCap = 8192;          // partial row tiles per step
-constexpr int kTargetGroups = 1024;     // attention work-groups aimed for: two rounds of two per CU
-constexpr int kMinChunk = 256;          // keys per split, lower bound
+constexpr int kPartCap = 16384;         // partial tiles of 16 rows per step
+constexpr int kTargetGroups1 = 512;     // attention work-groups aimed for, a wave on one row tile
+constexpr int kTargetGroups2 = 768;     // and on two
+constexpr int kPairRows = 128;          // rows per KV head from which on a wave takes two tiles
+constexpr int kMinWork = 2048;          // keys x (row tile share) of a work-group, lower bound
 constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
 
 int64_t page_bytes_of(const spec_model_config* c) {
@@ -42,12 +44,12 @@ struct StepLayout {
 
 StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, int64_t pages) {
   const int64_t G = c->n_heads / c->n_kv_heads;
-  const int64_t groups = (int64_t)c->n_kv_heads * ((rows * G + 31) / 32 + batch);   // row groups, at most
+  const int64_t groups = (int64_t)c->n_kv_heads * ((rows * G + 15) / 16 + batch);   // row groups, at most
   const int64_t items = 8 * (groups + kPartCap);                                    // padded per XCD
   const int64_t octets = rows / 8 + 2 * batch;
   const size_t blob = align_up(batch * sizeof(SampleInfo)) + align_up(rows * 4) + align_up(pages * 4) +
                       align_up(c->head_dim / 2 * sizeof(double)) + align_up(octets * sizeof(Kv4Octet)) +
-                      align_up(items * sizeof(AttnItem)) + 3 * kAlign +
+                      align_up(items * sizeof(AttnItem)) +
                       align_up(kPartCap * sizeof(CombineItem));
   StepLayout L{};
   size_t off = 0;
@@ -59,38 +61,54 @@ StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, 
   L.blob = take(blob);
   L.toks = take(rows * sizeof(TokInfo));
   L.anc = take(rows * 8 * kAncWords);
-  L.part_o = take((size_t)kPartCap * 32 * c->head_dim * 4);
-  L.part_ml = take((size_t)kPartCap * 32 * 2 * 4);
+  L.part_o = take((size_t)kPartCap * 16 * c->head_dim * 4);
+  L.part_ml = take((size_t)kPartCap * 16 * 2 * 4);
   L.total = off;
   return L;
 }
 
-// The attention work of a step: items by row tiles per work-group (1, 2, 4) and
-// the combine jobs of split key ranges.
+// The attention work of a step: items (AttnItem::pad is Kv4Item::waves) and the
+// combine jobs of split key ranges.
 struct AttnPlan {
-  std::vector<AttnItem> items[3];
+  std::vector<AttnItem> items;
   std::vector<CombineItem> comb;
+  int wave_tiles = 1;
 };
 
-// A (sample, kv head) has ceil(T G / 32) row tiles; they go in groups of up to
-// four, one work-group each: four waves share a tile's keys when it is alone, two
-// when there are two, and each has its own from three on.  A group's key range is
-// cut into chunks of about the same work (keys x tiles), so that the step has
-// about kTargetGroups work-groups.
+// A (sample, kv head) has ceil(T G / 16) row tiles.  A wave takes one (three waves per
+// SIMD) or, when some sample has more than kPairRows rows, two (two per SIMD, and V is
+// decoded once for both).  A work-group's four waves share the keys of the first tile
+// (pair) by four, of two by two, or have one each; more tiles go to more work-groups.
+// A group's key range is cut into chunks of about the same work (keys x waves' share),
+// so that the step has about kTargetGroups work-groups, but of at least kMinWork: below
+// that a split's merge launch costs more than it saves.  Measured, us, 8B heads:
+//                                   one tile per wave   two tiles
+//   128 samples, 175K keys, 32 rows        59.6            65.0
+//   4 samples, 15K keys, 64 rows           17.4            21.9
+//   4 samples, 101K keys, 256 rows         139             127
+//   prompt pieces of 500 - 1170 rows       173             158
+// and work-groups aimed for 384 / 512 / 768 / 1024, one tile: 256 samples, 227K keys,
+// 4 rows 51.9 / 51.7 / 55.8 / 55.6; two tiles: the third row 144 / 133 / 127 / 132, the
+// fourth 154 / 161 / 158 / 161.  One sample of 580 keys: 10.5 unsplit, 14.5 in chunks of 256.
 void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, AttnPlan* plan) {
   const int G = c->n_heads / c->n_kv_heads, nkv = c->n_kv_heads;
   struct Group {
     int b, tile0, tiles, keys;
   };
   std::vector<Group> groups;
+  int64_t most_rows = 0;
+  for (const SampleInfo& x : si) most_rows = std::max(most_rows, (int64_t)x.ntok * G);
+  plan->wave_tiles = most_rows <= kPairRows ? 1 : 2;
+  const int wt = plan->wave_tiles;
+  auto waves_of = [&](int tiles) { return tiles <= wt ? 4 : tiles <= 2 * wt ? 2 : 1; };
+  auto weight = [&](int tiles) { return 4 / waves_of(tiles); };
   double work = 0.0;
-  auto weight = [](int tiles) { return tiles == 1 ? 1 : tiles == 2 ? 2 : 4; };
   for (int b = 0; b < (int)si.size(); ++b) {
     const int64_t rows = (int64_t)si[b].ntok * G;
-    const int tiles = (int)((rows + 31) / 32);
-    for (int t = 0; t < tiles; t += 4) {
-      const int n = std::min(4, tiles - t);
-      const int64_t last = std::min<int64_t>(rows, 32ll * (t + n)) - 1;      // last row of the group
+    const int tiles = (int)((rows + 15) / 16);
+    for (int t = 0; t < tiles; t += 4 * wt) {
+      const int n = std::min(4 * wt, tiles - t);
+      const int64_t last = std::min<int64_t>(rows, 16ll * (t + n)) - 1;      // last row of the group
       const int keys = si[b].seq_len + (runs ? (int)(last / G) + 1 : si[b].ntok);
       groups.push_back(Group{b, t, n, keys});
       work += (double)nkv * keys * weight(n);
@@ -98,14 +116,14 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
   }
   auto chunk_of = [&](const Group& g, double unit) {
     const int64_t least = ((int64_t)g.keys + kMaxSplits - 1) / kMaxSplits;
-    const int64_t want = std::max<int64_t>({kMinChunk, least, (int64_t)(unit / weight(g.tiles))});
+    const int64_t want = std::max<int64_t>(least, (int64_t)(unit / weight(g.tiles)));
     return (want + 127) / 128 * 128;
   };
   auto splits_of = [&](const Group& g, double unit) {
     const int64_t ch = chunk_of(g, unit);
     return (int)((g.keys + ch - 1) / ch);
   };
-  double unit = work / kTargetGroups;
+  double unit = std::max<double>(kMinWork, work / (wt == 1 ? kTargetGroups1 : kTargetGroups2));
   for (;;) {      // ends: with units beyond the longest range times four nothing is split
     int64_t slots = 0;
     for (const Group& g : groups) {
@@ -119,20 +137,19 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
   for (const Group& g : groups) {
     const int64_t ch = chunk_of(g, unit);
     const int ns = splits_of(g, unit);
-    const int list = g.tiles == 1 ? 0 : g.tiles == 2 ? 1 : 2;
     for (int kvh = 0; kvh < nkv; ++kvh) {
       for (int k = 0; k < ns; ++k)
-        plan->items[list].push_back(AttnItem{g.b, kvh, g.tile0 * 32, (int)(k * ch),
-                                             (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns,
-                                             ns > 1 ? slot + k : 0, 0});
+        plan->items.push_back(AttnItem{g.b, kvh, g.tile0 * 16, (int)(k * ch),
+                                       (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns, ns > 1 ? slot + k : 0,
+                                       waves_of(g.tiles)});
       if (ns > 1) {
         for (int t = 0; t < g.tiles; ++t)
-          plan->comb.push_back(CombineItem{g.b, kvh, (g.tile0 + t) * 32, ns, slot + t * ns, 0, 0, 0});
+          plan->comb.push_back(CombineItem{g.b, kvh, (g.tile0 + t) * 16, ns, slot + t * ns, 0, 0, 0});
         slot += ns * g.tiles;
       }
     }
   }
-  for (auto& list : plan->items) deal_items(list);
+  deal_items(plan->items);
 }
 
 }  // namespace
@@ -155,6 +172,10 @@ int kv4_check_rows(const spec_kv4* kv, int32_t batch, const int32_t* sample_ids,
   for (int b = 0; b < batch; ++b) {
     const int64_t T = (int64_t)offsets[b + 1] - offsets[b];
     if (T < 1) return fail(SPEC_ERR_TREE, "sample %d has %lld rows", b, (long long)T);
+    const int64_t G = kv->cfg.n_heads / kv->cfg.n_kv_heads;
+    if (T * G * G > 0xffffffffll)
+      return fail(SPEC_ERR_UNSUPPORTED, "sample %d: %lld rows of %lld query heads each are more than one step takes", b,
+                  (long long)T, (long long)G);
     if (parents && T > SPEC_MAX_TREE) return fail(SPEC_ERR_UNSUPPORTED, "sample %d has %lld tree nodes", b, (long long)T);
     const int S = seq_lens[b];
     if (S < 0) return fail(SPEC_ERR_INVALID, "seq_lens[%d] = %d", b, S);
@@ -191,15 +212,16 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   const int64_t pages = kv4_step_pages(kv, batch, offsets, seq_lens);
   const bool runs = parents == nullptr;
   std::vector<SampleInfo> si(batch);
-  std::vector<int32_t> table;
+  std::vector<uint32_t> table;
   table.reserve(pages);
+  const uint32_t page_units = (uint32_t)(page_bytes_of(&c) / kKv4Unit);
   std::vector<Kv4Octet> octets;
   octets.reserve(N / 8 + 2 * batch);
   for (int b = 0; b < batch; ++b) {
     const int id = sample_ids[b], S = seq_lens[b], T = offsets[b + 1] - offsets[b];
     const int np = (int)(((int64_t)S + T + kKv4Page - 1) / kKv4Page);
     si[b] = SampleInfo{(int64_t)table.size(), np * kKv4Page, S, offsets[b], T, 0, 0};
-    table.insert(table.end(), kv->pages[id].begin(), kv->pages[id].begin() + np);
+    for (int p = 0; p < np; ++p) table.push_back((uint32_t)kv->pages[id][p] * page_units);
     for (int o = S / 8 * 8; o < S + T; o += 8)
       octets.push_back(Kv4Octet{b, o, std::max(0, S - o), std::min(8, S + T - o)});
   }
@@ -223,8 +245,7 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   const size_t o_table = put(table.data(), table.size() * 4);
   const size_t o_freq = put(freq.data(), freq.size() * sizeof(double));
   const size_t o_oct = put(octets.data(), octets.size() * sizeof(Kv4Octet));
-  size_t o_items[3];
-  for (int i = 0; i < 3; ++i) o_items[i] = put(plan.items[i].data(), plan.items[i].size() * sizeof(AttnItem));
+  const size_t o_items = put(plan.items.data(), plan.items.size() * sizeof(AttnItem));
   const size_t o_comb = put(plan.comb.data(), plan.comb.size() * sizeof(CombineItem));
   char* ws = (char*)workspace;
   char* d = ws + L.blob;
@@ -238,20 +259,21 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
 
   st->kv = kv;
   st->n_rows = (int)N;
-  Kv4View view{kv->pool, page_bytes_of(&c), (const int32_t*)(d + o_table), d_si, 0, c.n_kv_heads, c.head_dim};
+  Kv4View view{kv->pool, (const uint32_t*)(d + o_table), d_si, 0, c.n_kv_heads, c.head_dim};
   st->rows = Kv4RowArgs{view, (const Kv4Octet*)(d + o_oct), (int)octets.size(), runs ? nullptr : toks,
                         (const double*)(d + o_freq), nullptr, nullptr, 0, 0, 0, 0};
   Kv4AttnArgs& a = st->attn;
   a = Kv4AttnArgs{};
   a.v = view;
   a.anc = runs ? nullptr : anc;
-  for (int i = 0; i < 3; ++i) {
-    a.items[i] = (const AttnItem*)(d + o_items[i]);
-    a.n_items[i] = (int)plan.items[i].size();
-  }
+  a.items = (const Kv4Item*)(d + o_items);
+  a.n_items = (int)plan.items.size();
+  a.wave_tiles = plan.wave_tiles;
   a.part_o = (float*)(ws + L.part_o);
   a.part_ml = (float*)(ws + L.part_ml);
   a.n_heads = c.n_heads;
+  a.group = c.n_heads / c.n_kv_heads;
+  a.group_inv = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   a.comb = (const CombineItem*)(d + o_comb);
   a.n_comb = (int)plan.comb.size();
   return SPEC_OK;
@@ -311,6 +333,8 @@ SPEC_API int spec_kv4_alloc(const spec_model_config* cfg, int32_t n_samples, int
     std::string why;
     if (!config_ok(cfg, &why)) return fail(SPEC_ERR_UNSUPPORTED, "%s", why.c_str());
     if ((uintptr_t)device_buf % kAlign) return fail(SPEC_ERR_INVALID, "device_buf not 256-byte aligned");
+    if ((int64_t)n_pages > (int64_t)0xffffffff / (page_bytes_of(cfg) / kKv4Unit))
+      return fail(SPEC_ERR_UNSUPPORTED, "%d pages are more than the 512 GB a pool can have", n_pages);
     const size_t need = spec_kv4_bytes(cfg, n_samples, n_pages);
     if (buf_bytes < need)
       return fail(SPEC_ERR_CAPACITY, "KV buffer holds %zu bytes, needs %zu", buf_bytes, need);

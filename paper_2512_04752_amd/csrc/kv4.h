@@ -17,11 +17,16 @@ constexpr __host__ __device__ int kv4_value_at(int hd) { return kKv4Page * hd / 
 constexpr __host__ __device__ int kv4_kscale_at(int hd) { return kKv4Page * hd; }
 constexpr __host__ __device__ int kv4_vscale_at(int hd) { return kKv4Page * (hd + hd / 32); }
 
+// Tables hold a page's place in units of 128 bytes, which every page and head is a
+// multiple of (a shift instead of a 64-bit product where the attention looks it up).
+constexpr int kKv4Unit = 128;
+static_assert(kv4_head_bytes(64) % kKv4Unit == 0 && kv4_head_bytes(128) % kKv4Unit == 0, "page unit");
+constexpr __host__ __device__ uint64_t kv4_page_offset(uint32_t page) { return (uint64_t)page * kKv4Unit; }
+
 // Where a step's cache lies.  SampleInfo::kv_base is the sample's first entry in `table`.
 struct Kv4View {
   char* pool;
-  int64_t page_bytes;
-  const int32_t* table;          // page ids, each sample's in position order
+  const uint32_t* table;         // each sample's pages in position order, kv4_page_offset()
   const SampleInfo* samples;
   int layer, n_kv_heads, head_dim;
 };
@@ -50,17 +55,29 @@ struct Kv4RowArgs {
 hipError_t launch_kv4_append(const Kv4RowArgs& a, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4RowArgs& a, hipStream_t s);
 
+// One attention work-group: four waves on up to 4 * wave_tiles tiles of 16 query rows
+// of one (sample, kv head), from row row0 on, against keys [key0, key1).  It takes
+// AttnItem's place in the dealing, whose last field is free.
+struct Kv4Item {
+  int32_t sample, kvh, row0, key0, key1, nsplit, part;
+  int32_t waves;                 // waves that share wave_tiles row tiles: 4, 2 or 1
+};
+static_assert(sizeof(Kv4Item) == sizeof(AttnItem), "dealt as AttnItem");
+
 struct Kv4AttnArgs {
   Kv4View v;
   const bf16* q;                 // row r, query head i at q + r * q_stride + i * head_dim
   int64_t q_stride;
   const uint64_t* anc;           // [N][kAncWords] (trees); NULL: row i sees rows 0 .. i (runs)
-  const AttnItem* items[3];      // work-groups of 1, 2 and 4 row tiles (four waves each)
-  int n_items[3];
-  float* part_o;                 // [slots][32][head_dim], divided by its l
-  float* part_ml;                // [slots][32][2]
+  const Kv4Item* items;
+  int n_items;
+  int wave_tiles;                // row tiles of a wave: 1 or 2
+  float* part_o;                 // [slots][16][head_dim], divided by its l
+  float* part_ml;                // [slots][16][2]
   bf16* out;                     // [N][n_heads*head_dim]
   int n_heads;
+  int group;                     // query heads per KV head
+  uint32_t group_inv;            // ceil(2^32 / group): row / group = high word of row * group_inv
   const CombineItem* comb;
   int n_comb;
 };

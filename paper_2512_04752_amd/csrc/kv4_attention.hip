@@ -4,32 +4,51 @@
 // (G query heads share a KV head).  It sees every committed key and, of the
 // step's own keys, its ancestors (trees) or the ones up to itself (runs).
 //
-// A wave takes a tile of 32 rows through 32 keys at a time, with the products
-// transposed so that a lane owns one query row (its softmax state and output
-// column never leave the lane and its partner, lane ^ 32):
+// A wave takes one or two tiles of 16 rows through 32 keys at a time, with the
+// products transposed so that a row's scores and output stay in four lanes
+// (l, l + 16, l + 32, l + 48, "groups" g = 0 .. 3):
 //
-//   S^T (32 keys x 32 rows)  = K . Q^T     v_mfma_f32_32x32x16_bf16
-//   O^T (dims x 32 rows)    += V^T . P^T   the same, P straight from S^T's registers
+//   S^T (keys x 16 rows)   = K . Q^T     v_mfma_scale_f32_16x16x128_f8f6f4
+//   O^T (dims x 16 rows)  += V^T . P^T   v_mfma_f32_16x16x32_bf16
 //
-// The cache is stored in the order of those operands.  Four bits are little
-// enough to need no staging: a lane loads its own 16 bytes of codes (K: 32 dims
-// of one key; V: its dims of 8 keys, one word each), 1 KB contiguous per wave
-// and load, and turns a byte into two bf16 numbers with one conversion.  K's
-// power of two goes into that conversion (a lane's 32 dims share one); V's is
-// the same for all dims of a key, so it scales the key's probability instead.
-// So K and V enter the products exactly; probabilities are rounded to bf16, as
-// in the bf16 cache's kernels.  There is no LDS traffic and no barrier until a
-// wave's last key; loads run a few blocks ahead in registers.
+// Four bits are little enough to need no staging: the cache is stored in the
+// order of the operands, a lane loads its own 16 bytes of codes, and there is no
+// LDS traffic and no barrier until a wave's last key; loads run a block ahead in
+// registers.
 //
-// Row r of K's operand takes key kappa(r) of the block, bits 2 and 3 of r
-// swapped: S^T's accumulators of lane half h are then 8 consecutive keys each
-// (16 k + 8 h ..), which is an octet of V's layout.
+// K's codes and powers of two are the scaled MFMA's own format (E2M1 with a power
+// of two per 32 numbers), so they are multiplied as they lie: no instruction
+// decodes them.  Its other operand has 8 bits at most, so a query number is held
+// as the sum of two e4m3 numbers of four significant bits each, which carries
+// bf16's eight; both share a power of two per row that puts the row's largest
+// magnitude in [128, 256).  What that loses is below 2^-18 of the row's largest
+// magnitude (numbers more than 2^10 below it run into e4m3's smallest step).
 //
-// A work-group has four waves: RT row tiles, and 4 / RT waves per tile that deal
-// its keys in blocks and merge through LDS at the end.
+// V's codes are turned into bf16 (one conversion per byte), without their power of
+// two: it is the same for all dims of a key and scales the key's probability
+// instead.  So K and V enter the products exactly.  Probabilities are rounded to
+// bf16, as over the bf16 cache: an eight-bit significand, 2^-8 relative.
+//
+// Tile T of S^T takes keys 16 T + 0 .. 15 of the block, so that a load of K covers
+// whole cache lines (64-byte pieces of twice as many lines stalled on the pieces
+// still under way); group g then holds keys 16 T + 4 g + i.  P^T wants an octet of
+// keys per group, as V's words hold them: two lane swaps per register pair.
+//
+// A work-group has four waves: one, two or four share a row tile (pair)'s keys, block
+// by block, and merge through LDS at the end.
+//
+// What bounds it: up to about 16 rows per KV head the cache's bytes (256 samples, 227K
+// keys of 8 heads, 243 MB: 51 us, 4.8 TB/s, what a copy reaches); above that the vector
+// instructions of a block (the softmax and V's conversions), which do not overlap the
+// MFMAs of their own wave.  A first form, 32 rows by v_mfma_f32_32x32x16_bf16 with K
+// decoded to bf16 as well and the blocks' scores in 32 keys x 32 rows, took (this form in
+// brackets, us): one sample of 1100 keys 12.5 (9.4); 4 x 16 nodes, 15K keys 21.6 (16.5);
+// 1B heads, 32 x 15 nodes 25.4 (20.7); 128 x 8 nodes, 175K keys 62.8 (58.8); 256 x 1
+// 67 (51.2); 4 x 64 nodes, 101K keys 151 (123); prompt pieces of 500 - 1170 rows 181 (158).
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "kv4.h"
 
@@ -41,6 +60,8 @@ constexpr int KBLK = 32;
 constexpr int kWaves = 4;
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -48,256 +69,409 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // row's maximum outgrows it by this many binary orders (a wave-uniform test).
 constexpr float kRescaleSlack = 8.f;
 
-// max / sum of a value and its copy in lane ^ 32.
-__device__ __forceinline__ float max_xor32(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+// IEEE maximum: one instruction, and a NaN (the score of a key that was not finite)
+// stays one; fmaxf would first have to quiet the MFMA outputs.
+__device__ __forceinline__ float maximum(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// A value and its copy in the next group (lane ^ 16), or in lane ^ 32.
+__device__ __forceinline__ uint2 with16(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return make_uint2(r[0], r[1]);
 }
-__device__ __forceinline__ float sum_xor32(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+__device__ __forceinline__ uint2 with32(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return make_uint2(r[0], r[1]);
 }
 
-// Eight codes (a word) as bf16, times the power of two s.
-__device__ __forceinline__ bf16x8 decode(uint32_t w, float s) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+// Over the four lanes of a row.
+__device__ __forceinline__ float max_groups(float x) {
+  uint2 r = with16(__float_as_uint(x));
+  r = with32(__float_as_uint(maximum(__uint_as_float(r.x), __uint_as_float(r.y))));
+  return maximum(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float sum_groups(float x) {
+  uint2 r = with16(__float_as_uint(x));
+  r = with32(__float_as_uint(__uint_as_float(r.x) + __uint_as_float(r.y)));
+  return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// Eight codes (a word) as bf16.
+__device__ __forceinline__ bf16x8 decode(uint32_t w) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.f, 3);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// One lane's share of a 32-key block.
+// Two floats as a pair of bf16, in one conversion.
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
+}
+
+// A row's query as the scaled MFMA's operand.  Lane group g holds k = 16 g .. 16 g + 15
+// in registers 0 .. 3 and k = 64 + 16 g .. in 4 .. 7.  HD 128: k is the dim, q[0] the
+// high parts and q[1] the low ones.  HD 64: one operand, k = dim the high parts and
+// k = 64 + dim the low ones (K's codes are then given twice).
 template <int HD>
-struct Block;
-template <>
-struct Block<128> {
-  i32x4 k[2], v[2];        // k[j]: dims 32 (2j + h) .. of key kappa(r); v[k][i]: dim 32 i + r of octet 2k + h
-  uint32_t ks;             // the key's four scale bytes
-  i32x4 vs[2];             // value scales of the two octets
-};
-template <>
-struct Block<64> {
-  i32x4 k[1];
-  i32x2 v[2];
-  uint32_t ks;
-  i32x4 vs[2];
+struct Query {
+  i32x8 q[HD / 64];
+  int scale;               // exponent + 127; 255 for a row with an infinity or NaN
+
+  __device__ __forceinline__ void load(const bf16* row, int g, bool live) {
+    constexpr int N = HD / 4;                 // numbers of this lane
+    uint32_t x[N / 2];
+#pragma unroll
+    for (int c = 0; c < N / 8; ++c) {
+      const i32x4 v = *(const i32x4*)(row + 16 * g + (c & 1) * 8 + (c >> 1) * 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * c + i] = live ? (uint32_t)v[i] : 0u;
+    }
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    u16x2 most = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i)
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+    uint32_t top = max((uint32_t)most[0], (uint32_t)most[1]);
+    uint2 other = with16(top);
+    other = with32(max(other.x, other.y));
+    top = max(other.x, other.y);
+    const int e = (int)(top >> 7);            // a NaN or infinity has 255
+    scale = e == 255 ? 255 : max(e - 7, 1);
+    const float f = __uint_as_float((uint32_t)min(scale, 247) << 23);
+    i32x4 hi[HD / 64], lo[HD / 64];
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        typedef __attribute__((ext_vector_type(2))) short i16x2;
+        i16x2 h = {0, 0}, l = {0, 0};
+        const uint32_t w0 = x[8 * c + 2 * i], w1 = x[8 * c + 2 * i + 1];
+        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, w0), f, false);
+        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, w1), f, true);
+        hi[c][i] = __builtin_bit_cast(int, h);
+        const f32x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[c][i], f, false);
+        const f32x2 b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[c][i], f, true);
+        l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, __uint_as_float(w0 << 16) - b0[0],
+                                                     __uint_as_float(w0 & 0xffff0000u) - b0[1], f, false);
+        l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, __uint_as_float(w1 << 16) - b1[0],
+                                                     __uint_as_float(w1 & 0xffff0000u) - b1[1], f, true);
+        lo[c][i] = __builtin_bit_cast(int, l);
+      }
+    if constexpr (HD == 128) {
+      q[0] = __builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      q[1] = __builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      q[0] = __builtin_shufflevector(hi[0], lo[0], 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+
+  // Scores of 16 keys (codes k, scale byte ks) in the lane's row.
+  __device__ __forceinline__ f32x4 scores(i32x4 k, int ks) const {
+    const i32x8 a = __builtin_shufflevector(k, k, 0, 1, 2, 3, -1, -1, -1, -1);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i)
+      s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[i], s, 4, 0, 0, ks, 0, scale);   // E2M1 . E4M3
+    return s;
+  }
 };
 
-template <int HD, int RT>
-__global__ __launch_bounds__(256, 2) void kv4_attention_kernel(Kv4AttnArgs a, const AttnItem* items,
-                                                               int n_items) {
-  constexpr int KS = kWaves / RT;             // waves per row tile
-  constexpr int NB = HD / 32;                 // 32-dim output blocks
-  constexpr int NJ = HD / 64;                 // 16-byte key loads per lane
-  constexpr int AHEAD = 2;                    // blocks in registers
-  constexpr int PITCH = HD + 4;               // floats per merged row
+// One lane's share of a 32-key block.
+template <int HD>
+struct Block {
+  typedef __attribute__((ext_vector_type(HD / 32))) int words;
+  i32x4 k[2];              // 32 dims of key 16 T + r, r = lane % 16
+  int ks[2];               // and their scale
+  words v[2];              // octet g: dims 32 i + r + 16 j in v[j][i]
+  i32x2 vs[2];             // value scales of keys 16 T + 4 g + 0 .. 3
+};
+
+template <int HD, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4AttnArgs a) {
+  constexpr int NB = HD / 16;                 // 16-dim output tiles
   extern __shared__ __attribute__((aligned(16))) float smem[];
 
   const int per_xcd = gridDim.x >> 3;
   const int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (item >= n_items) return;
-  const AttnItem it = items[item];
+  if (item >= a.n_items) return;
+  const Kv4Item it = a.items[item];
   if (it.sample < 0) return;                  // padding of a shorter per-XCD list
   const SampleInfo si = a.v.samples[it.sample];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 31, h = lane >> 5;
-  const int tile = w / KS, part = w % KS;
-  const int G = a.n_heads / a.v.n_kv_heads;
-  const int row0 = it.row0 + 32 * tile;
+  const int r = lane & 15, g = lane >> 4;
+  const int KS = it.waves, part = w & (KS - 1);                     // waves per row tile (pair)
+  const int pair = KS == 4 ? 0 : KS == 2 ? w >> 1 : w;
+  const int G = a.group;
+  auto node_of = [&](int row) { return G == 1 ? row : (int)__umulhi((uint32_t)row, a.group_inv); };
+  const int row0 = it.row0 + 16 * NT * pair;
 
-  const int grow = row0 + r;
-  const int node = grow / G, head = it.kvh * G + grow % G;
-  const bool row_ok = node < si.ntok;
-  bf16x8 qf[HD / 16];
-  {
-    const bf16* qrow = a.q + (size_t)(si.tok0 + (row_ok ? node : 0)) * a.q_stride + (row_ok ? head : 0) * HD;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        qf[4 * j + u] = *(const bf16x8*)(qrow + 32 * (2 * j + h) + 8 * u);
-        if (!row_ok) qf[4 * j + u] = bf16x8{};
-      }
-  }
-  // What the row sees: of a tree its ancestors, of a run the keys before `limit`.
+  // What the rows are and see: of a tree their ancestors, of a run the keys before `limit`.
   const bool runs = a.anc == nullptr;
-  NodeSet anc;
-  anc.clear();
-  anc.w0 = 1ull;
-  if (!runs && row_ok) anc.load(a.anc + (size_t)(si.tok0 + node) * kAncWords);
-  const int limit = si.seq_len + min(node, si.ntok - 1) + 1;
+  int node[NT], head[NT], limit[NT];
+  NodeSet anc[NT];
+  Query<HD> qf[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int grow = row0 + 16 * n + r;
+    node[n] = node_of(grow);
+    head[n] = it.kvh * G + grow - node[n] * G;
+    const bool ok = node[n] < si.ntok;
+    qf[n].load(a.q + (size_t)(si.tok0 + (ok ? node[n] : 0)) * a.q_stride + (ok ? head[n] : 0) * HD, g, ok);
+    anc[n].clear();
+    anc[n].w0 = 1ull;
+    if (!runs && ok) anc[n].load(a.anc + (size_t)(si.tok0 + node[n]) * kAncWords);
+    limit[n] = si.seq_len + min(node[n], si.ntok - 1) + 1;
+  }
 
-  // The tile's keys end with its last row's, and blocks past `mask_from` are masked.
+  // The wave's keys end with its last row's, and blocks past `mask_from` are masked.
   int key1 = it.key1, mask_from = si.seq_len;
   if (runs) {
-    const int last = min((row0 + 31) / G, si.ntok - 1);
+    const int last = min(node_of(row0 + 16 * NT - 1), si.ntok - 1);
     key1 = min(key1, si.seq_len + last + 1);
-    mask_from = si.seq_len + min(row0 / G, si.ntok - 1) + 1;
+    mask_from = si.seq_len + min(node_of(row0), si.ntok - 1) + 1;
   }
   mask_from = min(mask_from, key1);
   const int nblk = key1 > it.key0 ? (key1 - it.key0 + KBLK - 1) / KBLK : 0;
   const int mine = nblk > part ? (nblk - part + KS - 1) / KS : 0;
 
   const char* in_page = a.v.pool + ((int64_t)a.v.layer * a.v.n_kv_heads + it.kvh) * kv4_head_bytes(HD);
-  const int32_t* table = a.v.table + si.kv_base;
-  const int kappa = (r & 0x13) | ((r & 4) << 1) | ((r & 8) >> 1);
-  const int k_off = h * 512 + kappa * 16, ks_off = kv4_kscale_at(HD) + kappa * (HD / 32);
-  const int v_off = kv4_value_at(HD) + h * kv4_octet_bytes(HD) + r * (HD / 8);
-  const int vs_off = kv4_vscale_at(HD) + 16 * h;
+  const uint32_t* table = a.v.table + si.kv_base;
+  const int chunk = HD == 128 ? g : g & 1;
+  const uint32_t k_off = chunk * 512 + r * 16, ks_off = kv4_kscale_at(HD) + r * (HD / 32) + chunk;
+  const uint32_t v_off = kv4_value_at(HD) + g * kv4_octet_bytes(HD) + r * (HD / 8);
+  const uint32_t vs_off = kv4_vscale_at(HD) + 8 * g;
 
-  auto first_key = [&](int t) { return it.key0 + (part + KS * t) * KBLK; };
-  auto load = [&](Block<HD>& b, int t) {
-    const int kb = first_key(t);
-    const char* base = in_page + (int64_t)table[kb / kKv4Page] * a.v.page_bytes;
-    const int half = kb / KBLK % 2;
-    const char* codes = base + half * kv4_block_bytes(HD);
+  auto first_key = [&](int t) { return (uint32_t)(it.key0 + (part + KS * t) * KBLK); };
+  // The blocks go from the last one down, through two sets of registers.  A block's K is
+  // loaded when the one two above it has been multiplied, its V likewise: a whole
+  // block's work passes before it is needed.  Its page is read a block before that.
+  uint32_t page = mine > 0 ? table[first_key(mine - 1) / kKv4Page] : 0;
+  const char *codes, *vscales;                 // of the block whose V comes next
+  auto load_k = [&](Block<HD>& b, int t) __attribute__((always_inline)) {
+    const uint32_t half = first_key(t) / KBLK % 2;
+    const char* base = in_page + kv4_page_offset(page);
+    page = table[first_key(max(t - 1, 0)) / kKv4Page];
+    codes = base + half * kv4_block_bytes(HD);
+    vscales = base + half * 64;
+    const char* scales = base + half * HD;     // 32 keys' scales: HD bytes of K's, 64 of V's
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) b.k[j] = *(const i32x4*)(codes + k_off + j * 1024);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      b.v[k] = *(const decltype(b.v[0] + b.v[0])*)(codes + v_off + 2 * k * kv4_octet_bytes(HD));
-      b.vs[k] = *(const i32x4*)(base + half * 64 + vs_off + 32 * k);
+    for (int j = 0; j < 2; ++j) {
+      b.k[j] = *(const i32x4*)(codes + k_off + 256 * j);
+      b.ks[j] = *(const uint8_t*)(scales + ks_off + 16 * j * (HD / 32));
     }
-    if constexpr (HD == 128) b.ks = *(const uint32_t*)(base + half * 128 + ks_off);
-    else b.ks = *(const uint16_t*)(base + half * 64 + ks_off);
+  };
+  auto load_vs = [&](Block<HD>& b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b.vs[j] = *(const i32x2*)(vscales + vs_off + 32 * j);
+  };
+  auto load_v = [&](Block<HD>& b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) b.v[j] = *(const typename Block<HD>::words*)(codes + v_off + j * 2 * HD);
   };
 
   const float sl2 = 1.4426950408889634f / sqrtf((float)HD);   // log2(e) / sqrt(d)
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x16 o[NB];
+  float m_run[NT], l_run[NT];                 // the row's reference maximum; this lane's share of its sum
+  f32x4 o[NT][NB];
 #pragma unroll
-  for (int i = 0; i < NB; ++i) o[i] = f32x16{};
+  for (int n = 0; n < NT; ++n) {
+    m_run[n] = -INFINITY;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
-  auto compute = [&](const Block<HD>& b, int kb) {
-    f32x16 s0 = f32x16{}, s1 = f32x16{};
+  // Block `t`, whose loads are in b; then b takes the loads of block t - 2 (of block 0
+  // again when there is none: the waits below count on them).
+  auto step = [&](Block<HD>& b, int t) __attribute__((always_inline)) {
+    const int kb = (int)first_key(t);
+    float s[NT][8];                            // s[n][e]: key kb + 16 (e / 4) + 4 g + e % 4
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const float ks = __uint_as_float((b.ks >> (16 * j + 8 * h) & 255u) << 23);
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int u = 0; u < 4; u += 2) {
-        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode((uint32_t)b.k[j][u], ks), qf[4 * j + u], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode((uint32_t)b.k[j][u + 1], ks), qf[4 * j + u + 1], s1, 0,
-                                                     0, 0);
+      for (int n = 0; n < NT; ++n) {
+        const f32x4 x = qf[n].scores(b.k[j], b.ks[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][4 * j + i] = x[i];
+      }
+    load_k(b, max(t - 2, 0));
+    float vscale[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t pair = (uint32_t)b.vs[e >> 2][(e >> 1) & 1];
+      vscale[e] = __uint_as_float(e & 1 ? pair & 0xffff0000u : pair << 16);
+    }
+    // Keys that a row does not see score -inf and weigh 0.  Blocks that reach past
+    // `mask_from` only; there a value scale that is not a number (or was never written) is
+    // taken as 0, and the rows that see the key score NaN instead.
+    if (kb + KBLK > mask_from) {
+      const int x0 = kb - si.seq_len;          // the block's nodes lie in at most two words
+      uint32_t seen[NT];                       // bit e
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint64_t lo = anc[n].word(x0), hi = anc[n].word(x0 + 31);
+        seen[n] = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3), x = key - si.seq_len;
+          const uint64_t word = (x >> 6) == (x0 >> 6) ? lo : hi;
+          const uint32_t in_tree = (uint32_t)(word >> (x & 63)) | (uint32_t)x >> 31;
+          const uint32_t in_run = (uint32_t)(key - limit[n]) >> 31;
+          seen[n] |= ((runs ? in_run : in_tree) & (uint32_t)(key - key1) >> 31 & 1u) << e;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool bad = (__float_as_uint(vscale[e]) & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          s[n][e] = !(seen[n] >> e & 1u) ? -INFINITY : bad ? __uint_as_float(0x7fc00000u) : s[n][e];
+        vscale[e] = bad ? 0.f : vscale[e];
       }
     }
-    f32x16 s = s0 + s1;                        // s[e]: key kb + 16 (e / 8) + 8 h + e % 8
-    const bool mask = kb + KBLK > mask_from;
-    if (mask) {
-      const int t0 = kb - si.seq_len;
-      const uint64_t lo = anc.word(t0), hi = anc.word(t0 + 31);
+    float smax[NT];
+    bool grows = false;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = kb + 16 * (e >> 3) + 8 * h + (e & 7);
-        const int tt = key - si.seq_len;
-        const uint64_t word = (tt >> 6) == (t0 >> 6) ? lo : hi;
-        const bool in_tree = (tt < 0) | (bool)((word >> (tt & 63)) & 1ull);
-        const bool seen = (key < key1) & (runs ? key < limit : in_tree);
-        s[e] = seen ? s[e] : -INFINITY;
+    for (int n = 0; n < NT; ++n) {
+      smax[n] = maximum(maximum(maximum(s[n][0], s[n][1]), s[n][2]), maximum(maximum(s[n][3], s[n][4]), s[n][5]));
+      smax[n] = maximum(maximum(smax[n], s[n][6]), s[n][7]);
+      grows |= smax[n] * sl2 > m_run[n] + kRescaleSlack;
+    }
+    if (__ballot(grows)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float m_new = maximum(m_run[n], max_groups(smax[n]) * sl2);
+        const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_run[n] - m_new);
+        l_run[n] *= alpha;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) o[n][i] *= alpha;
+        m_run[n] = m_new;
       }
     }
-    float smax = s[0];
+    i32x4 pb[NT];
 #pragma unroll
-    for (int e = 1; e < 16; ++e) smax = fmaxf(smax, s[e]);
-    smax = max_xor32(smax);
-    const float m_new = fmaxf(m_run, smax * sl2);
-    if (__ballot(m_new > m_run + kRescaleSlack)) {
-      const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_run - m_new);
-      l_run *= alpha;
+    for (int n = 0; n < NT; ++n) {
+      const float mb = m_run[n] == -INFINITY ? 0.f : m_run[n];
+      float psum = 0.f;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) o[i] *= alpha;
-      m_run = m_new;
+      for (int e = 0; e < 8; e += 2) {
+        const float p0 = fast_exp2(fmaf(s[n][e], sl2, -mb)), p1 = fast_exp2(fmaf(s[n][e + 1], sl2, -mb));
+        psum += p0 + p1;
+        pb[n][e >> 1] = (int)pack_bf16(p0 * vscale[e], p1 * vscale[e + 1]);
+      }
+      l_run[n] += psum;
+      // [tile 0: groups' keys 0-3, 4-7, 8-11, 12-15; tile 1: 16-19, ..] -> group g: keys 8 g .. 8 g + 7
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const auto x = __builtin_amdgcn_permlane32_swap(pb[n][i], pb[n][2 + i], false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+        pb[n][i] = (int)y[0];
+        pb[n][2 + i] = (int)y[1];
+      }
     }
-    const float mb = m_run == -INFINITY ? 0.f : m_run;
-    float psum = 0.f;
-    bf16x8 pb[2];
+    load_vs(b);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float pe = fast_exp2(fmaf(s[e], sl2, -mb));
-      psum += pe;
-      const uint32_t sw = (uint32_t)b.vs[e >> 3][(e & 7) >> 1];
-      float ps = pe * __uint_as_float(e & 1 ? sw & 0xffff0000u : sw << 16);
-      if (mask) ps = s[e] == -INFINITY ? 0.f : ps;     // an unseen key's scale may be anything
-      pb[e >> 3][e & 7] = (bf16)ps;
-    }
-    l_run += psum;
+    for (int i = 0; i < HD / 32; ++i)
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+      for (int j = 0; j < 2; ++j) {
+        const bf16x8 vt = decode((uint32_t)b.v[j][i]);
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode((uint32_t)b.v[k][i], 1.f), pb[k], o[i], 0, 0, 0);
+        for (int n = 0; n < NT; ++n)
+          o[n][2 * i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, pb[n]),
+                                                                   o[n][2 * i + j], 0, 0, 0);
+      }
+    load_v(b);
   };
 
-  Block<HD> blk[AHEAD];
-#pragma unroll
-  for (int u = 0; u < AHEAD; ++u)
-    if (u < mine) load(blk[u], u);
-  for (int t0 = 0; t0 < mine; t0 += AHEAD) {
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int t = t0 + u;
-      if (t >= mine) break;
-      compute(blk[u], first_key(t));
-      if (t + AHEAD < mine) load(blk[u], t + AHEAD);
+  if (mine > 0) {
+    Block<HD> b0, b1;
+    int t = mine - 1;
+    // In the order in which step() issues them, which is what its waits count on.
+    auto fill = [&](Block<HD>& b, int at) __attribute__((always_inline)) {
+      load_k(b, at);
+      __builtin_amdgcn_sched_barrier(0);
+      load_vs(b);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(b);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    fill(b0, t);
+    fill(b1, max(t - 1, 0));
+    for (; t > 0; t -= 2) {
+      step(b0, t);
+      __builtin_amdgcn_sched_barrier(0);       // the registers of two blocks' steps at once are too many
+      step(b1, t - 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (t == 0) step(b0, 0);
   }
-  l_run = sum_xor32(l_run);
 
-  // Every wave leaves its 32 rows in LDS; a tile's waves then share its rows.
-  float* own = smem + w * 32 * PITCH;
-  float* ml = smem + kWaves * 32 * PITCH;      // [wave][32][2]
+  // o[n][i][j]: dim 16 i + 4 g + j of row row0 + 16 n + r.  Row r of tile n, normalised by
+  // its sum l: to the output, or to its key range's partial state.
+  const bool split = it.nsplit > 1;
+  auto put = [&](int n, int i, f32x4 x) __attribute__((always_inline)) {
+    if (split) {
+      const size_t row = (size_t)(it.part + (NT * pair + n) * it.nsplit) * 16 + r;
+      *(f32x4*)(a.part_o + row * HD + 16 * i + 4 * g) = x;
+    } else {
+      bf16* dst = a.out + ((size_t)(si.tok0 + node[n]) * a.n_heads + head[n]) * HD + 16 * i + 4 * g;
+      *(i32x2*)dst = i32x2{(int)pack_bf16(x[0], x[1]), (int)pack_bf16(x[2], x[3])};
+    }
+  };
+  auto put_ml = [&](int n, float m, float l) __attribute__((always_inline)) {
+    const size_t row = (size_t)(it.part + (NT * pair + n) * it.nsplit) * 16 + r;
+    if (split && g == 0) *(float2*)(a.part_ml + row * 2) = make_float2(m, l);
+  };
+  if (KS == 1) {
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
+    for (int n = 0; n < NT; ++n) {
+      const float l = sum_groups(l_run[n]), inv = l == 0.f ? 0.f : 1.f / l;
+      if (node[n] >= si.ntok) continue;
+      put_ml(n, m_run[n], l);
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      *(f32x4*)(own + r * PITCH + 32 * i + 8 * c + 4 * h) =
-          f32x4{o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]};
-  if (h == 0) {
-    ml[(w * 32 + r) * 2] = m_run;
-    ml[(w * 32 + r) * 2 + 1] = l_run;
+      for (int i = 0; i < NB; ++i) put(n, i, o[n][i] * inv);
+    }
+    return;
+  }
+  // Waves that share a row tile leave their states in LDS, lane by lane; each then merges
+  // its share of the dims.
+  constexpr int STATE = (NB * 4 + 2) * 64;     // floats of a wave and tile
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float* p = smem + (w * NT + n) * STATE;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) *(f32x4*)(p + i * 256 + lane * 4) = o[n][i];
+    *(float2*)(p + NB * 256 + lane * 2) = make_float2(m_run[n], l_run[n]);
   }
   __syncthreads();
-  constexpr int LPR = HD / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
-  const bool split = it.nsplit > 1;
-  const int slot = it.part + tile * it.nsplit;
 #pragma unroll
-  for (int p = 0; p < 32 / KS; p += RPP) {
-    const int rr = part * (32 / KS) + p + lane / LPR, d = lane % LPR * 8;
-    const int gr = row0 + rr, nd = gr / G;
-    if (nd >= si.ntok) continue;
-    float m = -INFINITY;
+  for (int n = 0; n < NT; ++n) {
+    if (row0 + 16 * n >= si.ntok * G) break;   // wave-uniform: no row in the tile
+    const float* p = smem + (w - part) * NT * STATE + n * STATE;
+    float2 ml[kWaves];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) m = fmaxf(m, ml[((tile * KS + k) * 32 + rr) * 2]);
-    float l = 0.f;
-    f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = x0;
+    for (int k = 0; k < kWaves; ++k)
+      if (k < KS) {
+        ml[k] = *(const float2*)(p + k * NT * STATE + NB * 256 + lane * 2);
+        m = maximum(m, ml[k].x);
+      }
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const float mk = ml[((tile * KS + k) * 32 + rr) * 2];
-      const float f = mk == -INFINITY ? 0.f : fast_exp2(mk - m);
-      const float* src = smem + ((tile * KS + k) * 32 + rr) * PITCH + d;
-      l += f * ml[((tile * KS + k) * 32 + rr) * 2 + 1];
-      x0 += f * *(const f32x4*)src;
-      x1 += f * *(const f32x4*)(src + 4);
-    }
+    for (int k = 0; k < kWaves; ++k)
+      if (k < KS) {
+        ml[k].x = ml[k].x == -INFINITY ? 0.f : fast_exp2(ml[k].x - m);
+        l += ml[k].x * ml[k].y;
+      }
+    l = sum_groups(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    x0 *= inv;
-    x1 *= inv;
-    if (split) {
-      float* dst = a.part_o + ((size_t)slot * 32 + rr) * HD + d;
-      *(f32x4*)dst = x0;
-      *(f32x4*)(dst + 4) = x1;
-      if (d == 0) {
-        a.part_ml[((size_t)slot * 32 + rr) * 2] = m;
-        a.part_ml[((size_t)slot * 32 + rr) * 2 + 1] = l;
-      }
-    } else {
-      bf16x8 y;
+    if (node[n] >= si.ntok) continue;
+    if (part == 0) put_ml(n, m, l);
+    for (int i = part * NB / KS; i < (part + 1) * NB / KS; ++i) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        y[j] = (bf16)x0[j];
-        y[4 + j] = (bf16)x1[j];
-      }
-      *(bf16x8*)(a.out + ((size_t)(si.tok0 + nd) * a.n_heads + it.kvh * G + gr % G) * HD + d) = y;
+      for (int k = 0; k < kWaves; ++k)
+        if (k < KS) x += ml[k].x * *(const f32x4*)(p + k * NT * STATE + i * 256 + lane * 4);
+      put(n, i, x * inv);
     }
   }
 }
@@ -309,7 +483,7 @@ template <int HD>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   constexpr int LPR = HD / 4, RPB = 256 / LPR, MAXS = 64;
   __shared__ float wgt[RPB][MAXS];
-  const CombineItem ci = a.comb[blockIdx.x];
+  const CombineItem ci = a.comb[blockIdx.x];        // a tile of 16 rows
   const int lane = threadIdx.x % LPR, rr = threadIdx.x / LPR;
   const int row = blockIdx.y * RPB + rr;
   const SampleInfo si = a.v.samples[ci.sample];
@@ -318,12 +492,12 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   if (nd >= si.ntok) return;                   // a row's lanes lie in one wave: nobody waits for them
   const int ns = ci.nsplit;
   float M = -INFINITY;
-  for (int sp = lane; sp < ns; sp += LPR) M = fmaxf(M, a.part_ml[((size_t)(ci.part0 + sp) * 32 + row) * 2]);
+  for (int sp = lane; sp < ns; sp += LPR) M = maximum(M, a.part_ml[((size_t)(ci.part0 + sp) * 16 + row) * 2]);
 #pragma unroll
-  for (int m = LPR / 2; m >= 1; m >>= 1) M = fmaxf(M, __shfl_xor(M, m));
+  for (int m = LPR / 2; m >= 1; m >>= 1) M = maximum(M, __shfl_xor(M, m));
   float L = 0.f;
   for (int sp = lane; sp < ns; sp += LPR) {
-    const size_t slot = (size_t)(ci.part0 + sp) * 32 + row;
+    const size_t slot = (size_t)(ci.part0 + sp) * 16 + row;
     const float ms = a.part_ml[slot * 2];
     const float f = ms == -INFINITY ? 0.f : fast_exp2(ms - M) * a.part_ml[slot * 2 + 1];
     wgt[rr][sp] = f;
@@ -333,8 +507,8 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   for (int m = LPR / 2; m >= 1; m >>= 1) L += __shfl_xor(L, m);
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const float* src = a.part_o + ((size_t)ci.part0 * 32 + row) * HD + 4 * lane;
-  constexpr size_t STRIDE = (size_t)32 * HD;   // elements between consecutive ranges
+  const float* src = a.part_o + ((size_t)ci.part0 * 16 + row) * HD + 4 * lane;
+  constexpr size_t STRIDE = (size_t)16 * HD;   // elements between consecutive ranges
   f32x4 O = {0.f, 0.f, 0.f, 0.f};
   int sp = 0;
   for (; sp + 4 <= ns; sp += 4) {
@@ -352,35 +526,32 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   *(bf16x4*)(a.out + ((size_t)(si.tok0 + nd) * a.n_heads + ci.kvh * G + gr % G) * HD + 4 * lane) = v;
 }
 
-template <int HD, int RT>
-hipError_t launch_tiles(const Kv4AttnArgs& a, const AttnItem* items, int n, hipStream_t s) {
-  if (n == 0) return hipSuccess;
-  constexpr int SMEM = kWaves * 32 * (HD + 4 + 2) * 4;
-  const auto kernel = kv4_attention_kernel<HD, RT>;
-  static std::atomic<uint64_t> configured{0};  // a bit per device
-  int dev = 0;
-  if (const hipError_t e = hipGetDevice(&dev)) return e;
-  const uint64_t bit = 1ull << (dev & 63);
-  if (!(configured.load() & bit)) {
-    if (const hipError_t e = hipFuncSetAttribute((const void*)kernel,
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, SMEM))
-      return e;
-    configured.fetch_or(bit);
+template <int HD, int NT>
+hipError_t launch_tiles(const Kv4AttnArgs& a, hipStream_t s) {
+  constexpr int SMEM = kWaves * NT * (HD / 4 + 2) * 64 * 4;
+  const auto kernel = kv4_attention_kernel<HD, NT>;
+  if constexpr (SMEM > 64 * 1024) {
+    static std::atomic<uint64_t> configured{0};               // a bit per device
+    int dev = 0;
+    if (const hipError_t e = hipGetDevice(&dev)) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(configured.load() & bit)) {
+      if (const hipError_t e = hipFuncSetAttribute((const void*)kernel,
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, SMEM))
+        return e;
+      configured.fetch_or(bit);
+    }
   }
-  kernel<<<(n + 7) / 8 * 8, 64 * kWaves, SMEM, s>>>(a, items, n);
+  kernel<<<(a.n_items + 7) / 8 * 8, 64 * kWaves, SMEM, s>>>(a);
   return hipGetLastError();
 }
 
 template <int HD>
 hipError_t launch_hd(const Kv4AttnArgs& a, hipStream_t s) {
-  hipError_t e = launch_tiles<HD, 1>(a, a.items[0], a.n_items[0], s);
-  if (e == hipSuccess) e = launch_tiles<HD, 2>(a, a.items[1], a.n_items[1], s);
-  if (e == hipSuccess) e = launch_tiles<HD, 4>(a, a.items[2], a.n_items[2], s);
-  if (e == hipSuccess && a.n_comb) {
-    kv4_combine_kernel<HD><<<dim3(a.n_comb, 32 / (256 / (HD / 4))), 256, 0, s>>>(a);
-    e = hipGetLastError();
-  }
-  return e;
+  const hipError_t e = a.wave_tiles == 1 ? launch_tiles<HD, 1>(a, s) : launch_tiles<HD, 2>(a, s);
+  if (e != hipSuccess) return e;
+  if (a.n_comb) kv4_combine_kernel<HD><<<dim3(a.n_comb, 16 / (256 / (HD / 4))), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4RowArgs a, int heads
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int q = lane / R::LPR, l = lane % R::LPR;
   const int at = oc.slot0 % kKv4Page;                 // in the page
-  char* page = a.v.pool + (int64_t)a.v.table[si.kv_base + oc.slot0 / kKv4Page] * a.v.page_bytes;
+  char* page = a.v.pool + kv4_page_offset(a.v.table[si.kv_base + oc.slot0 / kKv4Page]);
   const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, a.v.n_kv_heads);
   const int64_t ks = a.blocks ? HD : a.k_stride, vs = a.blocks ? HD : a.v_stride;
   const int64_t hs = a.blocks ? (int64_t)si.ntok * HD : HD;             // between heads
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowArgs a, int heads_p
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int q = lane / R::LPR, l = lane % R::LPR;
   const int at = oc.slot0 % kKv4Page;
-  const char* page = a.v.pool + (int64_t)a.v.table[si.kv_base + oc.slot0 / kKv4Page] * a.v.page_bytes;
+  const char* page = a.v.pool + kv4_page_offset(a.v.table[si.kv_base + oc.slot0 / kKv4Page]);
   const int h0 = blockIdx.y * heads_per_wg, h1 = min(h0 + heads_per_wg, a.v.n_kv_heads);
   for (int head = h0 + w; head < h1; head += kWaves) {
     const char* base = page + ((int64_t)a.v.layer * a.v.n_kv_heads + head) * kv4_head_bytes(HD);
