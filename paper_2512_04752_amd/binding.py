@@ -6,6 +6,7 @@ kernels; PyTorch only provides device memory and the stream.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
@@ -175,8 +176,8 @@ def _ptr(t):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # the raw handle: a Stream object takes 3 us to make
+        return c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return c_void_p(stream.cuda_stream)
 
 
@@ -402,6 +403,14 @@ def spec_kv4_step_bytes(cfg, max_batch, max_rows, max_pages) -> int:
     return int(lib().spec_kv4_step_bytes(ctypes.byref(c), max_batch, max_rows, max_pages))
 
 
+_NOTHING = contextlib.nullcontext()
+
+
+def _on(device):
+    """torch.cuda.device(device), which costs nothing when that is the current one."""
+    return _NOTHING if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 class KV4Pool:
     """A 4-bit paged KV pool over a torch-owned device buffer (spec_kv4_alloc)."""
 
@@ -422,7 +431,7 @@ class KV4Pool:
         self.buf = buf
         c = make_config(cfg)
         h = c_void_p()
-        with torch.cuda.device(buf.device):
+        with _on(buf.device):
             _check(lib().spec_kv4_alloc(ctypes.byref(c), self.n_samples, self.n_pages,
                                         c_void_p(buf.data_ptr()), buf.numel(), ctypes.byref(h)))
         self.handle = h
@@ -465,19 +474,35 @@ class KV4Step:
         if len(ids) and pars is not None and len(pars) != int(offs[-1]):
             raise ValueError("parents must have one entry per row")
         self.n_rows = int(offs[-1])
+        self._made_on = False                # or the stream of a workspace of the step's own
         if workspace is None:
             pages = int(((lens.astype(np.int64) + np.diff(offs) + SPEC_KV4_PAGE - 1)
                          // SPEC_KV4_PAGE).sum())
             nbytes = spec_kv4_step_bytes(pool.cfg, len(ids), self.n_rows, max(pages, 1))
             workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
+            with _on(pool.buf.device):
+                self._made_on = _stream(None).value
+        elif (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
+              or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous uint8 tensor on the pool's device")
         self.workspace = workspace
         h = c_void_p()
-        with torch.cuda.device(pool.buf.device):
+        with _on(pool.buf.device):
             _check(lib().spec_kv4_step_begin(pool.handle, len(ids), p_ids, p_offs, p_pars, p_lens,
                                              _ptr(workspace),
                                              workspace.numel() * workspace.element_size(),
-                                             _stream(stream), ctypes.byref(h)))
+                                             self._on_stream(stream), ctypes.byref(h)))
         self.handle = h
+
+    def _on_stream(self, stream):
+        """The stream's handle.  A workspace of the step's own is not given away before that
+        stream has passed its use."""
+        if self.pool.handle is None:
+            raise ValueError("the step's pool is closed")
+        s = _stream(stream)
+        if self._made_on is not False and s.value != self._made_on:
+            self.workspace.record_stream(torch.cuda.current_stream() if stream is None else stream)
+        return s
 
     def close(self):
         if self.handle is not None:
@@ -495,6 +520,9 @@ def _kv4_rows(step, t, heads, what):
     """Row stride of a bf16 device tensor [rows, heads, head_dim] or [rows, heads * head_dim] whose
     rows are contiguous."""
     d = step.pool.cfg.head_dim
+    if t.shape == (step.n_rows, heads, d) and t.is_contiguous() and t.dtype == torch.bfloat16 \
+            and t.device == step.pool.buf.device:
+        return heads * d
     flat = t.dim() == 2 and t.shape[1] == heads * d and t.stride(1) == 1
     split = (t.dim() == 3 and tuple(t.shape[1:]) == (heads, d) and t.stride(2) == 1
              and (heads == 1 or t.stride(1) == d))
@@ -510,18 +538,18 @@ def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
     rotating k by position unless it has been."""
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with torch.cuda.device(step.pool.buf.device):
+    with _on(step.pool.buf.device):
         _check(lib().spec_kv4_append(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs, int(rotate),
-                                     _stream(stream)))
+                                     step._on_stream(stream)))
 
 
 def spec_kv4_read(step: KV4Step, layer, k, v, stream=None):
     """Write what the cache holds for the step's rows into k and v (as in spec_kv4_append)."""
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with torch.cuda.device(step.pool.buf.device):
+    with _on(step.pool.buf.device):
         _check(lib().spec_kv4_read(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs,
-                                   _stream(stream)))
+                                   step._on_stream(stream)))
 
 
 def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
@@ -532,9 +560,9 @@ def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
     _kv4_rows(step, out, n, "out")
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    with torch.cuda.device(step.pool.buf.device):
+    with _on(step.pool.buf.device):
         _check(lib().spec_kv4_attend(step.handle, int(layer), _ptr(q), qs, _ptr(out),
-                                     _stream(stream)))
+                                     step._on_stream(stream)))
 
 
 def spec_workspace_bytes_kv4(cfg, max_batch, max_tokens, max_pages, sampled=False) -> int:
@@ -560,7 +588,7 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
     if debug:
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
                            for k in ("logits", "argmax", "depth", "pos", "anc")])
-    with torch.cuda.device(pool.buf.device):
+    with _on(pool.buf.device):
         _check(lib().spec_verify_kv4(ctypes.byref(c), ctypes.byref(weights.struct), pool.handle,
                                      len(ids), p_ids, p_offs, p_toks, p_pars, p_lens, _ptr(workspace),
                                      workspace.numel() * workspace.element_size(), _stream(stream),
@@ -572,7 +600,7 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
                     stream=None):
     ids, p_ids = _i32(sample_ids)
     lens, p_lens = _i32(seq_lens)
-    with torch.cuda.device(pool.buf.device):
+    with _on(pool.buf.device):
         _check(lib().spec_kv4_commit(pool.handle, len(ids), p_ids, p_lens, _ptr(accepted_len),
                                      _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))
 
