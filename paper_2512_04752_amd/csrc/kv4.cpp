@@ -223,7 +223,8 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
     si[b] = SampleInfo{(int64_t)table.size(), np * kKv4Page, S, offsets[b], T, 0, 0};
     for (int p = 0; p < np; ++p) table.push_back((uint32_t)kv->pages[id][p] * page_units);
     for (int o = S / 8 * 8; o < S + T; o += 8)
-      octets.push_back(Kv4Octet{b, o, std::max(0, S - o), std::min(8, S + T - o)});
+      octets.push_back(Kv4Octet{table[si[b].kv_base + o / kKv4Page], o, std::max(0, S - o), std::min(8, S + T - o),
+                                offsets[b] + (o - S), offsets[b], T, 0});
   }
   AttnPlan plan;
   plan_attention(&c, si, runs, &plan);

@@ -34,9 +34,13 @@ struct Kv4View {
 // The rows of one sample that fall into one aligned group of eight positions
 // [slot0, slot0 + 8): positions slot0 + lo .. slot0 + hi - 1.
 struct Kv4Octet {
-  int32_t sample, slot0, lo, hi;
+  uint32_t page;                 // of slot0, kv4_page_offset()
+  int32_t slot0, lo, hi;
+  int32_t row0;                  // row of slot0, which may lie before the sample's first
+  int32_t tok0, ntok;            // the sample's rows
+  int32_t pad;
 };
-static_assert(sizeof(Kv4Octet) == 16, "Kv4Octet layout");
+static_assert(sizeof(Kv4Octet) == 32, "Kv4Octet layout");
 
 struct Kv4RowArgs {
   Kv4View v;
