@@ -65,9 +65,12 @@ typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The running output is relative to a reference maximum that moves only when a
-// row's maximum outgrows it by this many binary orders (a wave-uniform test).
-constexpr float kRescaleSlack = 8.f;
+// The running output is relative to a reference maximum that moves only when a lane's
+// probabilities of a block, which are summed anyway, come to more than this: no maximum
+// is taken otherwise.  The first reference is so low that any key's probability is
+// infinite under it.
+constexpr float kMostSum = 256.f;
+constexpr float kNoKeys = -3e38f;
 
 // IEEE maximum: one instruction, and a NaN (the score of a key that was not finite)
 // stays one; fmaxf would first have to quiet the MFMA outputs.
@@ -199,29 +202,23 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   if (it.sample < 0) return;                  // padding of a shorter per-XCD list
   const SampleInfo si = a.v.samples[it.sample];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, g = lane >> 4;
+  int r = lane & 15;
+  const int g = lane >> 4;
   const int KS = it.waves, part = w & (KS - 1);                     // waves per row tile (pair)
   const int pair = KS == 4 ? 0 : KS == 2 ? w >> 1 : w;
   const int G = a.group;
   auto node_of = [&](int row) { return G == 1 ? row : (int)__umulhi((uint32_t)row, a.group_inv); };
   const int row0 = it.row0 + 16 * NT * pair;
 
-  // What the rows are and see: of a tree their ancestors, of a run the keys before `limit`.
   const bool runs = a.anc == nullptr;
-  int node[NT], head[NT], limit[NT];
-  NodeSet anc[NT];
+  // The node and query head of the lane's row in tile n.
+  auto node_at = [&](int n) { return node_of(row0 + 16 * n + r); };
+  auto head_at = [&](int n) { return it.kvh * G + row0 + 16 * n + r - node_at(n) * G; };
   Query<HD> qf[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int grow = row0 + 16 * n + r;
-    node[n] = node_of(grow);
-    head[n] = it.kvh * G + grow - node[n] * G;
-    const bool ok = node[n] < si.ntok;
-    qf[n].load(a.q + (size_t)(si.tok0 + (ok ? node[n] : 0)) * a.q_stride + (ok ? head[n] : 0) * HD, g, ok);
-    anc[n].clear();
-    anc[n].w0 = 1ull;
-    if (!runs && ok) anc[n].load(a.anc + (size_t)(si.tok0 + node[n]) * kAncWords);
-    limit[n] = si.seq_len + min(node[n], si.ntok - 1) + 1;
+    const bool ok = node_at(n) < si.ntok;
+    qf[n].load(a.q + (size_t)(si.tok0 + (ok ? node_at(n) : 0)) * a.q_stride + (ok ? head_at(n) : 0) * HD, g, ok);
   }
 
   // The wave's keys end with its last row's, and blocks past `mask_from` are masked.
@@ -275,7 +272,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   f32x4 o[NT][NB];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    m_run[n] = -INFINITY;
+    m_run[n] = kNoKeys;
     l_run[n] = 0.f;
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -305,18 +302,27 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
     // `mask_from` only; there a value scale that is not a number (or was never written) is
     // taken as 0, and the rows that see the key score NaN instead.
     if (kb + KBLK > mask_from) {
+      int at_lane = lane;                      // nothing of this is worth a register between blocks
+      asm("" : "+v"(at_lane) : "s"(kb));
+      const int r = at_lane & 15, g = at_lane >> 4;
       const int x0 = kb - si.seq_len;          // the block's nodes lie in at most two words
       uint32_t seen[NT];                       // bit e
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const uint64_t lo = anc[n].word(x0), hi = anc[n].word(x0 + 31);
+        const int node = min(node_of(row0 + 16 * n + r), si.ntok - 1), limit = si.seq_len + node + 1;
+        uint64_t lo = 0, hi = 0;               // of a tree its ancestors; a run sees the keys before `limit`
+        if (!runs) {
+          const uint64_t* anc = a.anc + (size_t)(si.tok0 + node) * kAncWords;
+          lo = anc[min(max(x0 >> 6, 0), kAncWords - 1)];
+          hi = anc[min(max((x0 + 31) >> 6, 0), kAncWords - 1)];
+        }
         seen[n] = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3), x = key - si.seq_len;
           const uint64_t word = (x >> 6) == (x0 >> 6) ? lo : hi;
           const uint32_t in_tree = (uint32_t)(word >> (x & 63)) | (uint32_t)x >> 31;
-          const uint32_t in_run = (uint32_t)(key - limit[n]) >> 31;
+          const uint32_t in_run = (uint32_t)(key - limit) >> 31;
           seen[n] |= ((runs ? in_run : in_tree) & (uint32_t)(key - key1) >> 31 & 1u) << e;
         }
       }
@@ -329,37 +335,39 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
         vscale[e] = bad ? 0.f : vscale[e];
       }
     }
-    float smax[NT];
+    float p[NT][8], psum[NT];
+    auto weigh = [&](int n) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[n][e] = fast_exp2(fmaf(s[n][e], sl2, -m_run[n]));
+      psum[n] = ((p[n][0] + p[n][1]) + (p[n][2] + p[n][3])) + ((p[n][4] + p[n][5]) + (p[n][6] + p[n][7]));
+    };
     bool grows = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      smax[n] = maximum(maximum(maximum(s[n][0], s[n][1]), s[n][2]), maximum(maximum(s[n][3], s[n][4]), s[n][5]));
-      smax[n] = maximum(maximum(smax[n], s[n][6]), s[n][7]);
-      grows |= smax[n] * sl2 > m_run[n] + kRescaleSlack;
+      weigh(n);
+      grows |= psum[n] > kMostSum;
     }
     if (__ballot(grows)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float m_new = maximum(m_run[n], max_groups(smax[n]) * sl2);
-        const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(m_run[n] - m_new);
+        float most = maximum(maximum(maximum(s[n][0], s[n][1]), s[n][2]), maximum(maximum(s[n][3], s[n][4]), s[n][5]));
+        most = maximum(maximum(most, s[n][6]), s[n][7]);
+        const float m_new = maximum(m_run[n], max_groups(most) * sl2);
+        const float alpha = fast_exp2(m_run[n] - m_new);
         l_run[n] *= alpha;
 #pragma unroll
         for (int i = 0; i < NB; ++i) o[n][i] *= alpha;
         m_run[n] = m_new;
+        weigh(n);
       }
     }
     i32x4 pb[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float mb = m_run[n] == -INFINITY ? 0.f : m_run[n];
-      float psum = 0.f;
+      l_run[n] += psum[n];
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float p0 = fast_exp2(fmaf(s[n][e], sl2, -mb)), p1 = fast_exp2(fmaf(s[n][e + 1], sl2, -mb));
-        psum += p0 + p1;
-        pb[n][e >> 1] = (int)pack_bf16(p0 * vscale[e], p1 * vscale[e + 1]);
-      }
-      l_run[n] += psum;
+      for (int e = 0; e < 8; e += 2)
+        pb[n][e >> 1] = (int)pack_bf16(p[n][e] * vscale[e], p[n][e + 1] * vscale[e + 1]);
       // [tile 0: groups' keys 0-3, 4-7, 8-11, 12-15; tile 1: 16-19, ..] -> group g: keys 8 g .. 8 g + 7
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -406,6 +414,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
     if (t == 0) step(b0, 0);
   }
 
+  asm("" : "+v"(r) : "v"(l_run[0]));            // nor of this
   // o[n][i][j]: dim 16 i + 4 g + j of row row0 + 16 n + r.  Row r of tile n, normalised by
   // its sum l: to the output, or to its key range's partial state.
   const bool split = it.nsplit > 1;
@@ -414,7 +423,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
       const size_t row = (size_t)(it.part + (NT * pair + n) * it.nsplit) * 16 + r;
       *(f32x4*)(a.part_o + row * HD + 16 * i + 4 * g) = x;
     } else {
-      bf16* dst = a.out + ((size_t)(si.tok0 + node[n]) * a.n_heads + head[n]) * HD + 16 * i + 4 * g;
+      bf16* dst = a.out + ((size_t)(si.tok0 + node_at(n)) * a.n_heads + head_at(n)) * HD + 16 * i + 4 * g;
       *(i32x2*)dst = i32x2{(int)pack_bf16(x[0], x[1]), (int)pack_bf16(x[2], x[3])};
     }
   };
@@ -426,7 +435,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float l = sum_groups(l_run[n]), inv = l == 0.f ? 0.f : 1.f / l;
-      if (node[n] >= si.ntok) continue;
+      if (node_at(n) >= si.ntok) continue;
       put_ml(n, m_run[n], l);
 #pragma unroll
       for (int i = 0; i < NB; ++i) put(n, i, o[n][i] * inv);
@@ -459,12 +468,12 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
 #pragma unroll
     for (int k = 0; k < kWaves; ++k)
       if (k < KS) {
-        ml[k].x = ml[k].x == -INFINITY ? 0.f : fast_exp2(ml[k].x - m);
+        ml[k].x = fast_exp2(ml[k].x - m);
         l += ml[k].x * ml[k].y;
       }
     l = sum_groups(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (node[n] >= si.ntok) continue;
+    if (node_at(n) >= si.ntok) continue;
     if (part == 0) put_ml(n, m, l);
     for (int i = part * NB / KS; i < (part + 1) * NB / KS; ++i) {
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -499,7 +508,7 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   for (int sp = lane; sp < ns; sp += LPR) {
     const size_t slot = (size_t)(ci.part0 + sp) * 16 + row;
     const float ms = a.part_ml[slot * 2];
-    const float f = ms == -INFINITY ? 0.f : fast_exp2(ms - M) * a.part_ml[slot * 2 + 1];
+    const float f = fast_exp2(ms - M) * a.part_ml[slot * 2 + 1];
     wgt[rr][sp] = f;
     L += f;
   }
