@@ -13,7 +13,7 @@ using namespace spec;
 
 namespace {
 
-constexpr int kPartCap = 16384;         // partial tiles of 16 rows per step
+constexpr int kPartCap = 8192;          // partial tiles of 16 rows per step
 constexpr int kTargetGroups1 = 512;     // attention work-groups aimed for, a wave on one row tile
 constexpr int kTargetGroups2 = 768;     // and on two
 constexpr int kPairRows = 128;          // rows per KV head from which on a wave takes two tiles
@@ -49,8 +49,8 @@ StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, 
   const int64_t octets = rows / 8 + 2 * batch;
   const size_t blob = align_up(batch * sizeof(SampleInfo)) + align_up(rows * 4) + align_up(pages * 4) +
                       align_up(c->head_dim / 2 * sizeof(double)) + align_up(octets * sizeof(Kv4Octet)) +
-                      align_up(items * sizeof(AttnItem)) +
-                      align_up(kPartCap * sizeof(CombineItem));
+                      align_up(items * sizeof(Kv4Item)) +
+                      align_up(kPartCap * sizeof(Kv4Merge));
   StepLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -67,11 +67,11 @@ StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, 
   return L;
 }
 
-// The attention work of a step: items (AttnItem::pad is Kv4Item::waves) and the
-// combine jobs of split key ranges.
+// The attention work of a step: work-groups, as they go to the XCDs, and the merges of
+// split key ranges.
 struct AttnPlan {
-  std::vector<AttnItem> items;
-  std::vector<CombineItem> comb;
+  std::vector<Kv4Item> items;
+  std::vector<Kv4Merge> comb;
   int wave_tiles = 1;
 };
 
@@ -133,23 +133,34 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
     if (slots <= kPartCap) break;
     unit = unit * 1.25 + 128;
   }
+  std::vector<AttnItem> list;      // its `pad` is Kv4Item::waves
   int slot = 0;
   for (const Group& g : groups) {
     const int64_t ch = chunk_of(g, unit);
     const int ns = splits_of(g, unit);
     for (int kvh = 0; kvh < nkv; ++kvh) {
       for (int k = 0; k < ns; ++k)
-        plan->items.push_back(AttnItem{g.b, kvh, g.tile0 * 16, (int)(k * ch),
-                                       (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns, ns > 1 ? slot + k : 0,
-                                       waves_of(g.tiles)});
+        list.push_back(AttnItem{g.b, kvh, g.tile0 * 16, (int)(k * ch),
+                                (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns, ns > 1 ? slot + k : 0,
+                                waves_of(g.tiles)});
       if (ns > 1) {
         for (int t = 0; t < g.tiles; ++t)
-          plan->comb.push_back(CombineItem{g.b, kvh, (g.tile0 + t) * 16, ns, slot + t * ns, 0, 0, 0});
+          plan->comb.push_back(Kv4Merge{kvh, (g.tile0 + t) * 16, ns, slot + t * ns, si[g.b].tok0, si[g.b].ntok, {}});
         slot += ns * g.tiles;
       }
     }
   }
-  deal_items(plan->items);
+  deal_items(list);
+  plan->items.reserve(list.size());
+  for (const AttnItem& x : list) {
+    if (x.sample < 0) {              // padding of a shorter per-XCD list
+      plan->items.push_back(Kv4Item{});
+      continue;
+    }
+    const SampleInfo& b = si[x.sample];
+    plan->items.push_back(Kv4Item{x.kvh, x.row0, x.key0, x.key1, x.nsplit, x.part, x.pad, b.seq_len, b.tok0, b.ntok,
+                                  (uint32_t)b.kv_base, {}});
+  }
 }
 
 }  // namespace
@@ -246,8 +257,8 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   const size_t o_table = put(table.data(), table.size() * 4);
   const size_t o_freq = put(freq.data(), freq.size() * sizeof(double));
   const size_t o_oct = put(octets.data(), octets.size() * sizeof(Kv4Octet));
-  const size_t o_items = put(plan.items.data(), plan.items.size() * sizeof(AttnItem));
-  const size_t o_comb = put(plan.comb.data(), plan.comb.size() * sizeof(CombineItem));
+  const size_t o_items = put(plan.items.data(), plan.items.size() * sizeof(Kv4Item));
+  const size_t o_comb = put(plan.comb.data(), plan.comb.size() * sizeof(Kv4Merge));
   char* ws = (char*)workspace;
   char* d = ws + L.blob;
   if (int rc = kv->ring.upload(blob.data(), blob.size(), d, s)) return rc;
@@ -275,7 +286,7 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   a.n_heads = c.n_heads;
   a.group = c.n_heads / c.n_kv_heads;
   a.group_inv = (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
-  a.comb = (const CombineItem*)(d + o_comb);
+  a.comb = (const Kv4Merge*)(d + o_comb);
   a.n_comb = (int)plan.comb.size();
   return SPEC_OK;
 }

@@ -60,13 +60,24 @@ hipError_t launch_kv4_append(const Kv4RowArgs& a, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4RowArgs& a, hipStream_t s);
 
 // One attention work-group: four waves on up to 4 * wave_tiles tiles of 16 query rows
-// of one (sample, kv head), from row row0 on, against keys [key0, key1).  It takes
-// AttnItem's place in the dealing, whose last field is free.
+// of one (sample, kv head), from row row0 on, against keys [key0, key1).  It holds what
+// the kernel needs of the sample, so that the first keys are two dependent loads away.
 struct Kv4Item {
-  int32_t sample, kvh, row0, key0, key1, nsplit, part;
-  int32_t waves;                 // waves that share wave_tiles row tiles: 4, 2 or 1
+  int32_t kvh, row0, key0, key1, nsplit, part;
+  int32_t waves;                 // waves that share wave_tiles row tiles: 4, 2 or 1; 0: no work
+  int32_t seq_len, tok0, ntok;   // the sample's
+  uint32_t pages;                // its first entry in the table
+  int32_t pad[5];
 };
-static_assert(sizeof(Kv4Item) == sizeof(AttnItem), "dealt as AttnItem");
+static_assert(sizeof(Kv4Item) == 64, "Kv4Item layout");
+
+// The key ranges of one row tile, to be merged.
+struct Kv4Merge {
+  int32_t kvh, row0, nsplit, part0;
+  int32_t tok0, ntok;            // the sample's
+  int32_t pad[2];
+};
+static_assert(sizeof(Kv4Merge) == 32, "Kv4Merge layout");
 
 struct Kv4AttnArgs {
   Kv4View v;
@@ -82,7 +93,7 @@ struct Kv4AttnArgs {
   int n_heads;
   int group;                     // query heads per KV head
   uint32_t group_inv;            // ceil(2^32 / group): row / group = high word of row * group_inv
-  const CombineItem* comb;
+  const Kv4Merge* comb;
   int n_comb;
 };
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, hipStream_t s);

@@ -121,15 +121,20 @@ struct Query {
   i32x8 q[HD / 64];
   int scale;               // exponent + 127; 255 for a row with an infinity or NaN
 
-  __device__ __forceinline__ void load(const bf16* row, int g, bool live) {
-    constexpr int N = HD / 4;                 // numbers of this lane
+  static constexpr int N = HD / 4;            // numbers of a lane
+  struct Raw {
+    i32x4 x[N / 8];
+  };
+  static __device__ __forceinline__ Raw load(const bf16* row, int g) {
+    Raw raw;
+#pragma unroll
+    for (int c = 0; c < N / 8; ++c) raw.x[c] = *(const i32x4*)(row + 16 * g + (c & 1) * 8 + (c >> 1) * 64);
+    return raw;
+  }
+  __device__ __forceinline__ void convert(const Raw& raw, bool live) {
     uint32_t x[N / 2];
 #pragma unroll
-    for (int c = 0; c < N / 8; ++c) {
-      const i32x4 v = *(const i32x4*)(row + 16 * g + (c & 1) * 8 + (c >> 1) * 64);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * c + i] = live ? (uint32_t)v[i] : 0u;
-    }
+    for (int c = 0; c < N / 2; ++c) x[c] = live ? (uint32_t)raw.x[c >> 2][c & 3] : 0u;
     typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
     u16x2 most = {0, 0};
 #pragma unroll
@@ -199,8 +204,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   const int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
   if (item >= a.n_items) return;
   const Kv4Item it = a.items[item];
-  if (it.sample < 0) return;                  // padding of a shorter per-XCD list
-  const SampleInfo si = a.v.samples[it.sample];
+  if (it.waves == 0) return;                  // padding of a shorter per-XCD list
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int r = lane & 15;
   const int g = lane >> 4;
@@ -214,26 +218,34 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   // The node and query head of the lane's row in tile n.
   auto node_at = [&](int n) { return node_of(row0 + 16 * n + r); };
   auto head_at = [&](int n) { return it.kvh * G + row0 + 16 * n + r - node_at(n) * G; };
-  Query<HD> qf[NT];
+  typename Query<HD>::Raw raw[NT];
+  uint64_t anc0[NT];                           // of a tree the ancestors among the first 64 nodes
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const bool ok = node_at(n) < si.ntok;
-    qf[n].load(a.q + (size_t)(si.tok0 + (ok ? node_at(n) : 0)) * a.q_stride + (ok ? head_at(n) : 0) * HD, g, ok);
+    const bool ok = node_at(n) < it.ntok;
+    anc0[n] = runs ? 0 : a.anc[(size_t)(it.tok0 + min(node_at(n), it.ntok - 1)) * kAncWords];
+    raw[n] = Query<HD>::load(a.q + (size_t)(it.tok0 + (ok ? node_at(n) : 0)) * a.q_stride + (ok ? head_at(n) : 0) * HD, g);
   }
+  Query<HD> qf[NT];
+  auto convert = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) qf[n].convert(raw[n], node_at(n) < it.ntok);
+  };
+  if constexpr (NT > 1) convert();             // two tiles' raw numbers would stay in registers too long
 
   // The wave's keys end with its last row's, and blocks past `mask_from` are masked.
-  int key1 = it.key1, mask_from = si.seq_len;
+  int key1 = it.key1, mask_from = it.seq_len;
   if (runs) {
-    const int last = min(node_of(row0 + 16 * NT - 1), si.ntok - 1);
-    key1 = min(key1, si.seq_len + last + 1);
-    mask_from = si.seq_len + min(node_of(row0), si.ntok - 1) + 1;
+    const int last = min(node_of(row0 + 16 * NT - 1), it.ntok - 1);
+    key1 = min(key1, it.seq_len + last + 1);
+    mask_from = it.seq_len + min(node_of(row0), it.ntok - 1) + 1;
   }
   mask_from = min(mask_from, key1);
   const int nblk = key1 > it.key0 ? (key1 - it.key0 + KBLK - 1) / KBLK : 0;
   const int mine = nblk > part ? (nblk - part + KS - 1) / KS : 0;
 
   const char* in_page = a.v.pool + ((int64_t)a.v.layer * a.v.n_kv_heads + it.kvh) * kv4_head_bytes(HD);
-  const uint32_t* table = a.v.table + si.kv_base;
+  const uint32_t* table = a.v.table + it.pages;
   const int chunk = HD == 128 ? g : g & 1;
   const uint32_t k_off = chunk * 512 + r * 16, ks_off = kv4_kscale_at(HD) + r * (HD / 32) + chunk;
   const uint32_t v_off = kv4_value_at(HD) + g * kv4_octet_bytes(HD) + r * (HD / 8);
@@ -305,33 +317,32 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
       int at_lane = lane;                      // nothing of this is worth a register between blocks
       asm("" : "+v"(at_lane) : "s"(kb));
       const int r = at_lane & 15, g = at_lane >> 4;
-      const int x0 = kb - si.seq_len;          // the block's nodes lie in at most two words
-      uint32_t seen[NT];                       // bit e
+      auto below = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; };   // bits 0 .. n - 1
+      uint32_t seen[NT];                       // bit e, of keys e = 4 .. 7 bit 12 + e
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int node = min(node_of(row0 + 16 * n + r), si.ntok - 1), limit = si.seq_len + node + 1;
-        uint64_t lo = 0, hi = 0;               // of a tree its ancestors; a run sees the keys before `limit`
-        if (!runs) {
-          const uint64_t* anc = a.anc + (size_t)(si.tok0 + node) * kAncWords;
-          lo = anc[min(max(x0 >> 6, 0), kAncWords - 1)];
-          hi = anc[min(max((x0 + 31) >> 6, 0), kAncWords - 1)];
+        const int node = min(node_of(row0 + 16 * n + r), it.ntok - 1), x0 = kb - it.seq_len;
+        uint32_t see;                          // bit k: key kb + k
+        if (runs) {
+          see = below(node + 1 - x0);
+        } else if (x0 < 0) {                   // committed keys, all seen, then the first nodes
+          see = x0 <= -32 ? ~0u : (uint32_t)(anc0[n] << -x0) | below(-x0);
+        } else {
+          const uint64_t* anc = a.anc + (size_t)(it.tok0 + node) * kAncWords;
+          const int i = x0 >> 6, shift = x0 & 63;
+          const uint64_t lo = i == 0 ? anc0[n] : i < kAncWords ? anc[i] : 0;
+          see = (uint32_t)(lo >> shift);
+          if (shift > 32 && i + 1 < kAncWords) see |= (uint32_t)(anc[i + 1] << (64 - shift));
         }
-        seen[n] = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3), x = key - si.seq_len;
-          const uint64_t word = (x >> 6) == (x0 >> 6) ? lo : hi;
-          const uint32_t in_tree = (uint32_t)(word >> (x & 63)) | (uint32_t)x >> 31;
-          const uint32_t in_run = (uint32_t)(key - limit) >> 31;
-          seen[n] |= ((runs ? in_run : in_tree) & (uint32_t)(key - key1) >> 31 & 1u) << e;
-        }
+        see &= below(key1 - kb);
+        seen[n] = see >> (4 * g);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool bad = (__float_as_uint(vscale[e]) & 0x7f800000u) == 0x7f800000u;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          s[n][e] = !(seen[n] >> e & 1u) ? -INFINITY : bad ? __uint_as_float(0x7fc00000u) : s[n][e];
+          s[n][e] = !(seen[n] >> (e < 4 ? e : 12 + e) & 1u) ? -INFINITY : bad ? __uint_as_float(0x7fc00000u) : s[n][e];
         vscale[e] = bad ? 0.f : vscale[e];
       }
     }
@@ -405,6 +416,8 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
     };
     fill(b0, t);
     fill(b1, max(t - 1, 0));
+    if constexpr (NT == 1) convert();          // while the first keys are on their way
+    __builtin_amdgcn_sched_barrier(0);
     for (; t > 0; t -= 2) {
       step(b0, t);
       __builtin_amdgcn_sched_barrier(0);       // the registers of two blocks' steps at once are too many
@@ -423,7 +436,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
       const size_t row = (size_t)(it.part + (NT * pair + n) * it.nsplit) * 16 + r;
       *(f32x4*)(a.part_o + row * HD + 16 * i + 4 * g) = x;
     } else {
-      bf16* dst = a.out + ((size_t)(si.tok0 + node_at(n)) * a.n_heads + head_at(n)) * HD + 16 * i + 4 * g;
+      bf16* dst = a.out + ((size_t)(it.tok0 + node_at(n)) * a.n_heads + head_at(n)) * HD + 16 * i + 4 * g;
       *(i32x2*)dst = i32x2{(int)pack_bf16(x[0], x[1]), (int)pack_bf16(x[2], x[3])};
     }
   };
@@ -435,7 +448,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const float l = sum_groups(l_run[n]), inv = l == 0.f ? 0.f : 1.f / l;
-      if (node_at(n) >= si.ntok) continue;
+      if (node_at(n) >= it.ntok) continue;
       put_ml(n, m_run[n], l);
 #pragma unroll
       for (int i = 0; i < NB; ++i) put(n, i, o[n][i] * inv);
@@ -455,7 +468,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   __syncthreads();
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    if (row0 + 16 * n >= si.ntok * G) break;   // wave-uniform: no row in the tile
+    if (row0 + 16 * n >= it.ntok * G) break;   // wave-uniform: no row in the tile
     const float* p = smem + (w - part) * NT * STATE + n * STATE;
     float2 ml[kWaves];
     float m = -INFINITY, l = 0.f;
@@ -473,7 +486,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
       }
     l = sum_groups(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (node_at(n) >= si.ntok) continue;
+    if (node_at(n) >= it.ntok) continue;
     if (part == 0) put_ml(n, m, l);
     for (int i = part * NB / KS; i < (part + 1) * NB / KS; ++i) {
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -492,13 +505,12 @@ template <int HD>
 __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   constexpr int LPR = HD / 4, RPB = 256 / LPR, MAXS = 64;
   __shared__ float wgt[RPB][MAXS];
-  const CombineItem ci = a.comb[blockIdx.x];        // a tile of 16 rows
+  const Kv4Merge ci = a.comb[blockIdx.x];        // a tile of 16 rows
   const int lane = threadIdx.x % LPR, rr = threadIdx.x / LPR;
   const int row = blockIdx.y * RPB + rr;
-  const SampleInfo si = a.v.samples[ci.sample];
-  const int G = a.n_heads / a.v.n_kv_heads;
+  const int G = a.group;
   const int gr = ci.row0 + row, nd = gr / G;
-  if (nd >= si.ntok) return;                   // a row's lanes lie in one wave: nobody waits for them
+  if (nd >= ci.ntok) return;                   // a row's lanes lie in one wave: nobody waits for them
   const int ns = ci.nsplit;
   float M = -INFINITY;
   for (int sp = lane; sp < ns; sp += LPR) M = maximum(M, a.part_ml[((size_t)(ci.part0 + sp) * 16 + row) * 2]);
@@ -532,7 +544,7 @@ __global__ __launch_bounds__(256) void kv4_combine_kernel(Kv4AttnArgs a) {
   bf16x4 v;
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = (bf16)(O[j] * inv);
-  *(bf16x4*)(a.out + ((size_t)(si.tok0 + nd) * a.n_heads + ci.kvh * G + gr % G) * HD + 4 * lane) = v;
+  *(bf16x4*)(a.out + ((size_t)(ci.tok0 + nd) * a.n_heads + ci.kvh * G + gr % G) * HD + 4 * lane) = v;
 }
 
 template <int HD, int NT>
