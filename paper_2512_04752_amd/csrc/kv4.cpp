@@ -73,6 +73,7 @@ struct AttnPlan {
   std::vector<Kv4Item> items;
   std::vector<Kv4Merge> comb;
   int wave_tiles = 1;
+  bool once = false;
 };
 
 // A (sample, kv head) has ceil(T G / 16) row tiles.  A wave takes one (three waves per
@@ -99,6 +100,7 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
   int64_t most_rows = 0;
   for (const SampleInfo& x : si) most_rows = std::max(most_rows, (int64_t)x.ntok * G);
   plan->wave_tiles = most_rows <= kPairRows ? 1 : 2;
+  plan->once = most_rows <= 16;               // one row tile
   const int wt = plan->wave_tiles;
   auto waves_of = [&](int tiles) { return tiles <= wt ? 4 : tiles <= 2 * wt ? 2 : 1; };
   auto weight = [&](int tiles) { return 4 / waves_of(tiles); };
@@ -281,6 +283,7 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
   a.items = (const Kv4Item*)(d + o_items);
   a.n_items = (int)plan.items.size();
   a.wave_tiles = plan.wave_tiles;
+  a.once = plan.once;
   a.part_o = (float*)(ws + L.part_o);
   a.part_ml = (float*)(ws + L.part_ml);
   a.n_heads = c.n_heads;

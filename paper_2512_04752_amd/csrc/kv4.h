@@ -87,6 +87,7 @@ struct Kv4AttnArgs {
   const Kv4Item* items;
   int n_items;
   int wave_tiles;                // row tiles of a wave: 1 or 2
+  int once;                      // one row tile per sample and KV head: no key is read by two waves
   float* part_o;                 // [slots][16][head_dim], divided by its l
   float* part_ml;                // [slots][16][2]
   bf16* out;                     // [N][n_heads*head_dim]
