@@ -533,6 +533,15 @@ def _kv4_rows(step, t, heads, what):
     return t.stride(0) if step.n_rows > 1 else heads * d
 
 
+def _kv4_ints(pool, **tensors):
+    """Each name=(tensor, numbers) must be a contiguous int32 tensor on the pool's device that
+    holds that many."""
+    for name, (t, n) in tensors.items():
+        if (t.dtype != torch.int32 or t.device != pool.buf.device or not t.is_contiguous()
+                or t.numel() < n):
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} on the pool's device")
+
+
 def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
     """Write the rows' K and V ([rows, kv heads, head_dim], rows may be strided) into the cache,
     rotating k by position unless it has been."""
@@ -584,6 +593,8 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
     pars, p_pars = _i32(tree_parents)
     lens, p_lens = _i32(seq_lens)
     samp = _sampling(cfg, int(offs[-1]), temperature, eos_token, draft_probs, uniforms)
+    _kv4_ints(pool, accepted_len=(accepted_len, len(ids)), next_token=(next_token, len(ids)),
+              accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
     dbg = None
     if debug:
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
@@ -600,6 +611,8 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
                     stream=None):
     ids, p_ids = _i32(sample_ids)
     lens, p_lens = _i32(seq_lens)
+    _kv4_ints(pool, accepted_len=(accepted_len, len(ids)), new_seq_lens=(new_seq_lens, len(ids)),
+              accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
     with _on(pool.buf.device):
         _check(lib().spec_kv4_commit(pool.handle, len(ids), p_ids, p_lens, _ptr(accepted_len),
                                      _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))

@@ -21,8 +21,11 @@
 // decodes them.  Its other operand has 8 bits at most, so a query number is held
 // as the sum of two e4m3 numbers of four significant bits each, which carries
 // bf16's eight; both share a power of two per row that puts the row's largest
-// magnitude in [128, 256).  What that loses is below 2^-18 of the row's largest
-// magnitude (numbers more than 2^10 below it run into e4m3's smallest step).
+// magnitude in [128, 256).  Numbers more than 2^10 below the largest run into e4m3's
+// smallest step and are off by up to 2^-17 of the largest: by 2^-12 of the row's mean
+// magnitude at most, below bf16's own rounding of a query.  Rows whose largest is more
+// than 32 times their mean ("wide": an outlier) get the remainders as two more e4m3
+// numbers, and two more products, which leaves 2^-34 of the largest.
 //
 // V's codes are turned into bf16 (one conversion per byte), without their power of
 // two: it is the same for all dims of a key and scales the key's probability
@@ -119,7 +122,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
 template <int HD>
 struct Query {
   i32x8 q[HD / 64];
-  int scale;               // exponent + 127; 255 for a row with an infinity or NaN
+  i32x8 rest[HD / 64];     // what q leaves, likewise, times 2^17; zero in a row that is not wide
+  int scale, rest_scale;   // exponents + 127; 255 for a row with an infinity or NaN
 
   static constexpr int N = HD / 4;            // numbers of a lane
   struct Raw {
@@ -131,56 +135,106 @@ struct Query {
     for (int c = 0; c < N / 8; ++c) raw.x[c] = *(const i32x4*)(row + 16 * g + (c & 1) * 8 + (c >> 1) * 64);
     return raw;
   }
-  __device__ __forceinline__ void convert(const Raw& raw, bool live) {
+
+  // Four numbers f[0 .. 3] / s as two words of e4m3, high parts and low; f keeps the remainder.
+  static __device__ __forceinline__ void split(float (&f)[4], float s, int& hi, int& lo) {
+    auto parts = [&]() __attribute__((always_inline)) {
+      typedef __attribute__((ext_vector_type(2))) short i16x2;
+      i16x2 w = {0, 0};
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, f[0], f[1], s, false);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, f[2], f[3], s, true);
+      const int v = __builtin_bit_cast(int, w);
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, s, false);
+      const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, s, true);
+      f[0] -= a[0];
+      f[1] -= a[1];
+      f[2] -= b[0];
+      f[3] -= b[1];
+      return v;
+    };
+    hi = parts();
+    lo = parts();
+  }
+
+  // Returns whether some row of the wave is wide.
+  __device__ __forceinline__ bool convert(const Raw& raw, bool live) {
     uint32_t x[N / 2];
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) x[c] = live ? (uint32_t)raw.x[c >> 2][c & 3] : 0u;
-    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
-    u16x2 most = {0, 0};
+    float most = 0.f, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i)
-      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
-    uint32_t top = max((uint32_t)most[0], (uint32_t)most[1]);
-    uint2 other = with16(top);
-    other = with32(max(other.x, other.y));
-    top = max(other.x, other.y);
-    const int e = (int)(top >> 7);            // a NaN or infinity has 255
+    for (int c = 0; c < N / 2; ++c) {
+      const float a = fabsf(__uint_as_float(x[c] << 16)), b = fabsf(__uint_as_float(x[c] & 0xffff0000u));
+      most = maximum(maximum(most, a), b);
+      sum += a + b;
+    }
+    most = max_groups(most);
+    sum = sum_groups(sum);
+    const int e = (int)(__float_as_uint(most) >> 23 & 255);   // a NaN or infinity has 255
     scale = e == 255 ? 255 : max(e - 7, 1);
+    rest_scale = e == 255 ? 255 : max(scale - 17, 1);
+    const bool wide = e != 255 && sum < most * (HD * 0.03125f);
     const float f = __uint_as_float((uint32_t)min(scale, 247) << 23);
+    const float fr = __uint_as_float((uint32_t)min(rest_scale, 247) << 23);
+    auto four = [&](int c, int i, float (&v)[4]) __attribute__((always_inline)) {
+      const uint32_t w0 = x[8 * c + 2 * i], w1 = x[8 * c + 2 * i + 1];
+      v[0] = __uint_as_float(w0 << 16);
+      v[1] = __uint_as_float(w0 & 0xffff0000u);
+      v[2] = __uint_as_float(w1 << 16);
+      v[3] = __uint_as_float(w1 & 0xffff0000u);
+    };
     i32x4 hi[HD / 64], lo[HD / 64];
+    auto join = [&](i32x8 (&to)[HD / 64]) __attribute__((always_inline)) {
+      if constexpr (HD == 128) {
+        to[0] = __builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        to[1] = __builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        to[0] = __builtin_shufflevector(hi[0], lo[0], 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    };
 #pragma unroll
     for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        typedef __attribute__((ext_vector_type(2))) short i16x2;
-        i16x2 h = {0, 0}, l = {0, 0};
-        const uint32_t w0 = x[8 * c + 2 * i], w1 = x[8 * c + 2 * i + 1];
-        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, w0), f, false);
-        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, w1), f, true);
-        hi[c][i] = __builtin_bit_cast(int, h);
-        const f32x2 b0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[c][i], f, false);
-        const f32x2 b1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[c][i], f, true);
-        l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, __uint_as_float(w0 << 16) - b0[0],
-                                                     __uint_as_float(w0 & 0xffff0000u) - b0[1], f, false);
-        l = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(l, __uint_as_float(w1 << 16) - b1[0],
-                                                     __uint_as_float(w1 & 0xffff0000u) - b1[1], f, true);
-        lo[c][i] = __builtin_bit_cast(int, l);
+        float v[4];
+        int h, l;
+        four(c, i, v);
+        split(v, f, h, l);
+        hi[c][i] = h;
+        lo[c][i] = l;
       }
-    if constexpr (HD == 128) {
-      q[0] = __builtin_shufflevector(hi[0], hi[1], 0, 1, 2, 3, 4, 5, 6, 7);
-      q[1] = __builtin_shufflevector(lo[0], lo[1], 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-      q[0] = __builtin_shufflevector(hi[0], lo[0], 0, 1, 2, 3, 4, 5, 6, 7);
+    join(q);
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c) rest[c] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+    const bool any = __ballot(wide) != 0;
+    if (any) {
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v[4];
+          int h, l;
+          four(c, i, v);
+          split(v, f, h, l);
+          split(v, fr, h, l);
+          hi[c][i] = wide ? h : 0;
+          lo[c][i] = wide ? l : 0;
+        }
+      join(rest);
     }
+    return any;
   }
 
-  // Scores of 16 keys (codes k, scale byte ks) in the lane's row.
-  __device__ __forceinline__ f32x4 scores(i32x4 k, int ks) const {
+  // Scores of 16 keys (codes k, scale byte ks) in the lane's row; what the remainders add.
+  __device__ __forceinline__ f32x4 scores(i32x4 k, int ks) const { return product(k, ks, q, scale, f32x4{0.f, 0.f, 0.f, 0.f}); }
+  __device__ __forceinline__ f32x4 add_rest(i32x4 k, int ks, f32x4 s) const { return product(k, ks, rest, rest_scale, s); }
+
+ private:
+  static __device__ __forceinline__ f32x4 product(i32x4 k, int ks, const i32x8 (&x)[HD / 64], int xs, f32x4 s) {
     const i32x8 a = __builtin_shufflevector(k, k, 0, 1, 2, 3, -1, -1, -1, -1);
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < HD / 64; ++i)
-      s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[i], s, 4, 0, 0, ks, 0, scale);   // E2M1 . E4M3
+      s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, x[i], s, 4, 0, 0, ks, 0, xs);   // E2M1 . E4M3
     return s;
   }
 };
@@ -236,9 +290,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
     raw[n] = Query<HD>::load(a.q + (size_t)(it.tok0 + (ok ? node_at(n) : 0)) * a.q_stride + (ok ? head_at(n) : 0) * HD, g);
   }
   Query<HD> qf[NT];
+  bool wide = false;                           // wave-uniform
   auto convert = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) qf[n].convert(raw[n], node_at(n) < it.ntok);
+    for (int n = 0; n < NT; ++n) wide |= qf[n].convert(raw[n], node_at(n) < it.ntok);
   };
   if constexpr (NT > 1) convert();             // two tiles' raw numbers would stay in registers too long
 
@@ -303,15 +358,21 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : 2) void kv4_attention_kernel(Kv4
   // again when there is none: the waits below count on them).
   auto step = [&](Block<HD>& b, int t) __attribute__((always_inline)) {
     const int kb = (int)first_key(t);
-    float s[NT][8];                            // s[n][e]: key kb + 16 (e / 4) + 4 g + e % 4
+    f32x4 x[NT][2];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const f32x4 x = qf[n].scores(b.k[j], b.ks[j]);
+      for (int n = 0; n < NT; ++n) x[n][j] = qf[n].scores(b.k[j], b.ks[j]);
+    if (wide)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][4 * j + i] = x[i];
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) x[n][j] = qf[n].add_rest(b.k[j], b.ks[j], x[n][j]);
+    float s[NT][8];                            // s[n][e]: key kb + 16 (e / 4) + 4 g + e % 4
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[n][e] = x[n][e >> 2][e & 3];
     load_k(b, max(t - 2, 0));
     float vscale[8];
 #pragma unroll

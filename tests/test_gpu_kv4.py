@@ -16,7 +16,10 @@ last bit counted in B); each enters the numerator and the denominator, so
 parts: 2 (n + 70) v A.  Numbers below 2^-126 may be flushed to zero: a probability
 (at most 2^-126 |V| lost, the row's sum being at least 1), its product with the
 value's power of two (whose code is at most 6) and the output, together
-(n + 1) 2^-126 (max |V| + 6).
+(n + 1) 2^-126 (max |V| + 6).  A query number enters as a sum of e4m3 parts: off by at
+most 2^-17 of its row's largest where it is more than 2^10 below that one, by 2^-34 of it
+in a row whose largest is above 32 times its mean; a score so by that times
+sum |k| / sqrt(d) at most, the output by 2 A of it (added where rows have outliers).
 """
 
 import numpy as np
@@ -213,7 +216,7 @@ def test_rotated_extremes(top):
 
 # ---- attention ---------------------------------------------------------------
 
-def check_attend(cfg, q, out, prefix, own, lens, rows, parents, samples=None):
+def check_attend(cfg, q, out, prefix, own, lens, rows, parents, samples=None, q_off=0.0):
     at = 0
     d = cfg.head_dim
     q = q.double().cpu().numpy().reshape(-1, cfg.n_heads, d)
@@ -230,6 +233,7 @@ def check_attend(cfg, q, out, prefix, own, lens, rows, parents, samples=None):
         v = 2.0 ** -24
         tol = 2.0 ** -8 * (A + np.abs(o)) + (2 * ((d + 6) * v * B + 4 * v) + 2 * (s + r + 70) * v) * A
         tol = tol + (s + r + 1) * 2.0 ** -126 * (np.abs(V).max() + 6)
+        tol = tol + 2 * q_off * np.abs(q[sl]).max() * np.abs(K).sum(-1).max() / np.sqrt(d) * A
         err = np.abs(out[sl] - o)
         assert (err <= tol).all(), f"sample {b}: error {err.max()} over {(err - tol).max()} past its bound"
 
@@ -295,6 +299,36 @@ def test_attend_many_samples():
 def test_attend_large_scores():
     """Scores of several hundred: one key takes all."""
     attend_case((8, 2, 128), [500, 64], [8, 20], False, seed=11, std=8.0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", [5, 40, 90])
+def test_attend_queries_with_outliers(d, rows):
+    """Rows of which one number dwarfs the others, in a dimension where the keys are zero; rows of tiny
+    numbers, of zeros, and ordinary ones between them, which come out as they do without those."""
+    cfg = config(8, 2, d)
+    rng = np.random.default_rng(rows)
+    c = Cache(cfg, [0], [rows])
+    k = bf16(rng.normal(size=(rows, 2, d)))
+    k[:, :, 5] = 0
+    v = bf16(rng.normal(size=(rows, 2, d))).cuda()
+    step = c.append(0, [0], [0], k.cuda(), v, [rows], rotate=False)
+    ko, vo = (torch.empty(rows, 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sv.spec_kv4_read(step, 0, ko, vo)
+    assert (ko[:, :, 5] == 0).all()
+    plain = rng.normal(size=(rows, 8, d))
+    q = plain.copy()
+    q[::3, :, 5] = 5000.0
+    q[1::6] *= 2.0 ** -100
+    q[1::6, :, 5] = 2.0 ** -80
+    q[4::6] = 0
+    out, alone = (torch.empty(rows, 8, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sv.spec_kv4_attend(step, 0, bf16(q).cuda(), out)
+    sv.spec_kv4_attend(step, 0, bf16(plain).cuda(), alone)
+    assert torch.equal(out[2::3], alone[2::3])
+    own = tuple(t.double().cpu().numpy() for t in (ko, vo))
+    none = [(np.empty((0, 2, d)),) * 2]
+    check_attend(cfg, bf16(q), out, none, own, [0], [rows], None, q_off=2.0 ** -34)
 
 
 def test_attend_at_32k_keys():
@@ -552,7 +586,20 @@ def test_launch_refusals():
         sv.KV4Step(c.pool, [0, 1], [0, 6, 9], parents[:5], [150, 10])
     with pytest.raises(sv.SpecError, match="workspace"):
         sv.KV4Step(c.pool, [0, 1], [0, 6, 9], parents, [150, 10], workspace=step.workspace[:4096])
+    for bad in (torch.empty(1 << 26, dtype=torch.int32, device="cuda"), torch.empty(1 << 26, dtype=torch.uint8),
+                torch.empty(2, 1 << 26, dtype=torch.uint8, device="cuda")[:, ::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            sv.KV4Step(c.pool, [0, 1], [0, 6, 9], parents, [150, 10], workspace=bad)
+    lens, new = (torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(2))
+    nodes = torch.zeros(2, sv.SPEC_MAX_TREE, dtype=torch.int32, device="cuda")
+    for a, b, d in ((lens.cpu(), nodes, new), (lens.long(), nodes, new), (lens, nodes[:, ::2], new),
+                    (lens, nodes[:1], new), (lens, nodes, new[:1])):
+        with pytest.raises(ValueError):
+            sv.spec_kv4_commit(c.pool, [0, 1], [150, 10], a, b, d)
     assert np.array_equal(c.bytes(), before)
+    c.pool.close()
+    with pytest.raises(ValueError, match="closed"):
+        sv.spec_kv4_append(step, 0, k, v)
 
 
 # ---- together ------------------------------------------------------------------

@@ -220,3 +220,63 @@ def test_null_handles():
     assert L.spec_kv4_read(None, 0, dev, 128, dev, 128, None) == -1
     assert L.spec_kv4_attend(None, 0, dev, 256, dev, None) == -1
     assert ctypes.sizeof(POINTER(c_int32)) == 8
+
+
+def test_largest_pool_and_run(fake):
+    """Page places and row numbers are 32-bit: what would pass them is refused."""
+    kv, fake.kv = fake.kv, c_void_p()
+    try:
+        big = B.make_config(wl.LLAMA_8B)
+        page = sv.spec_kv4_page_bytes(wl.LLAMA_8B)
+        most = 0xffffffff // (page // 128)
+        need = sv.spec_kv4_bytes(wl.LLAMA_8B, 1, most + 1)
+        assert fake.alloc(1, most + 1, FAKE_DEV, need, big) == -6 and "512 GB" in fake.error()
+        # 4 query heads per KV head: rows * 16 in 32 bits
+        few = B.make_config(wl.ModelConfig(1, 512, 8, 2, 64, 1024, 1024))
+        assert fake.alloc(1, 1, FAKE_DEV, 1 << 30, few) == 0
+        assert fake.begin([0], [0, 1 << 28], None, [0], ws_bytes=0) == -6 and "rows" in fake.error()
+        assert fake.begin([0], [0, (1 << 28) - 1], None, [0], ws_bytes=0) == -3       # then its pages
+    finally:
+        fake.L.spec_kv4_free(fake.kv)
+        fake.kv = kv
+
+
+def verify(fake, ids=(0, 1), offs=(0, 3, 6), toks=(1, 2, 3, 4, 5, 6), parents=tuple(TREE + TREE), lens=(10, 20),
+           ws=FAKE_DEV, ws_bytes=0, cfg=None, samp=None):
+    n = CFG.n_layers
+    arrays = {k: (c_void_p * n)(*[FAKE_DEV] * n) for k in B.Weights.LAYER_FIELDS}
+    w = B.spec_weights(FAKE_DEV, FAKE_DEV, FAKE_DEV,
+                       *[ctypes.cast(arrays[k], POINTER(c_void_p)) for k in B.Weights.LAYER_FIELDS])
+    args = [B._i32(x) for x in (ids, offs, toks, parents, lens)]
+    dev = c_void_p(FAKE_DEV)
+    return fake.L.spec_verify_kv4(byref(cfg or fake.c), byref(w), fake.kv, len(ids), *[a[1] for a in args],
+                                  c_void_p(ws), ws_bytes, None, samp, dev, dev, dev, None)
+
+
+def test_verify_refusals(fake):
+    assert verify(fake) == -5 and "workspace" in fake.error()             # all else is in order
+    assert verify(fake, ids=(1, 1)) == -1
+    assert verify(fake, ids=(0, 3)) == -1
+    assert verify(fake, lens=(126, 20)) == -3                               # 128 positions, 129 needed
+    assert verify(fake, lens=(-1, 20)) == -1
+    assert verify(fake, parents=(-1, 0, 2, -1, 0, 0)) == -2
+    assert verify(fake, parents=(0, 0, 0, -1, 0, 0)) == -2
+    assert verify(fake, toks=(1, 2, CFG.vocab, 4, 5, 6)) == -2
+    assert verify(fake, toks=(1, 2, -1, 4, 5, 6)) == -2
+    assert verify(fake, offs=(0, 3, 3), lens=(10, 20)) == -2
+    assert verify(fake, ws=FAKE_DEV + 128, ws_bytes=1 << 30) == -1
+    other = B.make_config(wl.ModelConfig(CFG.n_layers, CFG.hidden, CFG.n_heads, CFG.n_kv_heads, CFG.head_dim,
+                                         CFG.ffn + 128, CFG.vocab))
+    assert verify(fake, cfg=other) == -1 and "config" in fake.error()
+    assert fake.L.spec_kv4_map(fake.kv, 2, 1, i32(4)) == 0                  # page 4 is sample 0's too
+    assert verify(fake) == -1 and "page 4" in fake.error()
+
+
+def test_verify_workspace_bytes():
+    one = sv.spec_workspace_bytes_kv4(CFG, 1, 8, 4)
+    assert 0 < one < sv.spec_workspace_bytes_kv4(CFG, 4, 800, 40)
+    assert one <= sv.spec_workspace_bytes_kv4(CFG, 1, 8, 4, sampled=True)
+    assert one >= sv.spec_kv4_step_bytes(CFG, 1, 8, 4)
+    for args in ((0, 8, 4), (2, 1, 4), (1, 8, 0)):
+        assert sv.spec_workspace_bytes_kv4(CFG, *args) == 0
+    assert sv.spec_workspace_bytes_kv4(wl.ModelConfig(2, 256, 4, 2, 32, 1024, 1024), 1, 8, 4) == 0
