@@ -18,6 +18,7 @@ constexpr int kTargetGroups1 = 512;     // attention work-groups aimed for, a wa
 constexpr int kTargetGroups2 = 768;     // and on two
 constexpr int kPairRows = 128;          // rows per KV head from which on a wave takes two tiles
 constexpr int kMinWork = 2048;          // keys x (row tile share) of a work-group, lower bound
+constexpr int kUnsplit = 2816;          // nothing is split when no range is above this
 constexpr int kMaxSplits = 64;          // key ranges per row tile (combine kernel's table)
 
 int64_t page_bytes_of(const spec_model_config* c) {
@@ -81,16 +82,18 @@ struct AttnPlan {
 // decoded once for both).  A work-group's four waves share the keys of the first tile
 // (pair) by four, of two by two, or have one each; more tiles go to more work-groups.
 // A group's key range is cut into chunks of about the same work (keys x waves' share),
-// so that the step has about kTargetGroups work-groups, but of at least kMinWork: below
-// that a split's merge launch costs more than it saves.  Measured, us, 8B heads:
+// so that the step has about kTargetGroups work-groups, but of at least kMinWork; with no
+// range above kUnsplit nothing is cut, which saves the merge's launch.  Measured, us, 8B
+// heads:
 //                                   one tile per wave   two tiles
-//   128 samples, 175K keys, 32 rows        59.6            65.0
-//   4 samples, 15K keys, 64 rows           17.4            21.9
-//   4 samples, 101K keys, 256 rows         139             127
-//   prompt pieces of 500 - 1170 rows       173             158
-// and work-groups aimed for 384 / 512 / 768 / 1024, one tile: 256 samples, 227K keys,
-// 4 rows 51.9 / 51.7 / 55.8 / 55.6; two tiles: the third row 144 / 133 / 127 / 132, the
-// fourth 154 / 161 / 158 / 161.  One sample of 580 keys: 10.5 unsplit, 14.5 in chunks of 256.
+//   128 samples, 176K keys, 32 rows        58.5            62.1
+//   4 samples, 15K keys, 64 rows           16.7            20.5
+//   4 samples, 101K keys, 256 rows         139             124
+//   prompt pieces of 500 - 1170 rows       173             157
+// Work-groups aimed for 384 / 512 / 768 / 1024: one tile, 256 samples, 227K keys, 4 rows
+// 46 / 45.5 / 48.7 / 48.7; two tiles, the third row 144 / 133 / 124 / 128.  At least 1024
+// / 2048 per work-group: the second row 19.8 / 17.4.  A range of 2100 (of 4064) in one
+// piece 11.4 (17.7), in pieces of 2048 14.2 (14.3).
 void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, AttnPlan* plan) {
   const int G = c->n_heads / c->n_kv_heads, nkv = c->n_kv_heads;
   struct Group {
@@ -105,6 +108,7 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
   auto waves_of = [&](int tiles) { return tiles <= wt ? 4 : tiles <= 2 * wt ? 2 : 1; };
   auto weight = [&](int tiles) { return 4 / waves_of(tiles); };
   double work = 0.0;
+  int64_t longest = 0;
   for (int b = 0; b < (int)si.size(); ++b) {
     const int64_t rows = (int64_t)si[b].ntok * G;
     const int tiles = (int)((rows + 15) / 16);
@@ -114,6 +118,7 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
       const int keys = si[b].seq_len + (runs ? (int)(last / G) + 1 : si[b].ntok);
       groups.push_back(Group{b, t, n, keys});
       work += (double)nkv * keys * weight(n);
+      longest = std::max(longest, (int64_t)keys * weight(n));
     }
   }
   auto chunk_of = [&](const Group& g, double unit) {
@@ -125,7 +130,8 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
     const int64_t ch = chunk_of(g, unit);
     return (int)((g.keys + ch - 1) / ch);
   };
-  double unit = std::max<double>(kMinWork, work / (wt == 1 ? kTargetGroups1 : kTargetGroups2));
+  double unit = std::max<double>(longest <= kUnsplit ? kUnsplit : kMinWork,
+                                 work / (wt == 1 ? kTargetGroups1 : kTargetGroups2));
   for (;;) {      // ends: with units beyond the longest range times four nothing is split
     int64_t slots = 0;
     for (const Group& g : groups) {
