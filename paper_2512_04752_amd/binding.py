@@ -406,9 +406,9 @@ def spec_kv4_step_bytes(cfg, max_batch, max_rows, max_pages) -> int:
 _NOTHING = contextlib.nullcontext()
 
 
-def _on(device):
-    """torch.cuda.device(device), which costs nothing when that is the current one."""
-    return _NOTHING if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _on(index):
+    """torch.cuda.device(index), which costs nothing when that is the current one."""
+    return _NOTHING if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
 class KV4Pool:
@@ -429,9 +429,10 @@ class KV4Pool:
         elif buf.dtype != torch.uint8 or not buf.is_cuda or not buf.is_contiguous():
             raise ValueError("buf must be a contiguous uint8 device tensor")
         self.buf = buf
+        self.index = buf.get_device()
         c = make_config(cfg)
         h = c_void_p()
-        with _on(buf.device):
+        with _on(self.index):
             _check(lib().spec_kv4_alloc(ctypes.byref(c), self.n_samples, self.n_pages,
                                         c_void_p(buf.data_ptr()), buf.numel(), ctypes.byref(h)))
         self.handle = h
@@ -474,20 +475,19 @@ class KV4Step:
         if len(ids) and pars is not None and len(pars) != int(offs[-1]):
             raise ValueError("parents must have one entry per row")
         self.n_rows = int(offs[-1])
-        self._made_on = False                # or the stream of a workspace of the step's own
+        self._made_on = None                 # the stream of a workspace of the step's own
         if workspace is None:
             pages = int(((lens.astype(np.int64) + np.diff(offs) + SPEC_KV4_PAGE - 1)
                          // SPEC_KV4_PAGE).sum())
             nbytes = spec_kv4_step_bytes(pool.cfg, len(ids), self.n_rows, max(pages, 1))
             workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
-            with _on(pool.buf.device):
-                self._made_on = _stream(None).value
+            self._made_on = torch._C._cuda_getCurrentRawStream(pool.index)
         elif (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
               or not workspace.is_contiguous()):
             raise ValueError("workspace must be a contiguous uint8 tensor on the pool's device")
         self.workspace = workspace
         h = c_void_p()
-        with _on(pool.buf.device):
+        with _on(pool.index):
             _check(lib().spec_kv4_step_begin(pool.handle, len(ids), p_ids, p_offs, p_pars, p_lens,
                                              _ptr(workspace),
                                              workspace.numel() * workspace.element_size(),
@@ -499,8 +499,9 @@ class KV4Step:
         stream has passed its use."""
         if self.pool.handle is None:
             raise ValueError("the step's pool is closed")
-        s = _stream(stream)
-        if self._made_on is not False and s.value != self._made_on:
+        s = (torch._C._cuda_getCurrentRawStream(self.pool.index) if stream is None
+             else stream.cuda_stream)
+        if self._made_on is not None and s != self._made_on:
             self.workspace.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return s
 
@@ -520,8 +521,8 @@ def _kv4_rows(step, t, heads, what):
     """Row stride of a bf16 device tensor [rows, heads, head_dim] or [rows, heads * head_dim] whose
     rows are contiguous."""
     d = step.pool.cfg.head_dim
-    if t.shape == (step.n_rows, heads, d) and t.is_contiguous() and t.dtype == torch.bfloat16 \
-            and t.device == step.pool.buf.device:
+    if t.shape == (step.n_rows, heads, d) and t.is_contiguous() and t.dtype is torch.bfloat16 \
+            and t.get_device() == step.pool.index:
         return heads * d
     flat = t.dim() == 2 and t.shape[1] == heads * d and t.stride(1) == 1
     split = (t.dim() == 3 and tuple(t.shape[1:]) == (heads, d) and t.stride(2) == 1
@@ -547,17 +548,17 @@ def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
     rotating k by position unless it has been."""
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with _on(step.pool.buf.device):
-        _check(lib().spec_kv4_append(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs, int(rotate),
-                                     step._on_stream(stream)))
+    with _on(step.pool.index):
+        _check(lib().spec_kv4_append(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs,
+                                     int(rotate), step._on_stream(stream)))
 
 
 def spec_kv4_read(step: KV4Step, layer, k, v, stream=None):
     """Write what the cache holds for the step's rows into k and v (as in spec_kv4_append)."""
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with _on(step.pool.buf.device):
-        _check(lib().spec_kv4_read(step.handle, int(layer), _ptr(k), ks, _ptr(v), vs,
+    with _on(step.pool.index):
+        _check(lib().spec_kv4_read(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs,
                                    step._on_stream(stream)))
 
 
@@ -569,8 +570,8 @@ def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
     _kv4_rows(step, out, n, "out")
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    with _on(step.pool.buf.device):
-        _check(lib().spec_kv4_attend(step.handle, int(layer), _ptr(q), qs, _ptr(out),
+    with _on(step.pool.index):
+        _check(lib().spec_kv4_attend(step.handle, int(layer), q.data_ptr(), qs, out.data_ptr(),
                                      step._on_stream(stream)))
 
 
@@ -599,7 +600,7 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
     if debug:
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
                            for k in ("logits", "argmax", "depth", "pos", "anc")])
-    with _on(pool.buf.device):
+    with _on(pool.index):
         _check(lib().spec_verify_kv4(ctypes.byref(c), ctypes.byref(weights.struct), pool.handle,
                                      len(ids), p_ids, p_offs, p_toks, p_pars, p_lens, _ptr(workspace),
                                      workspace.numel() * workspace.element_size(), _stream(stream),
@@ -613,7 +614,7 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
     lens, p_lens = _i32(seq_lens)
     _kv4_ints(pool, accepted_len=(accepted_len, len(ids)), new_seq_lens=(new_seq_lens, len(ids)),
               accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
-    with _on(pool.buf.device):
+    with _on(pool.index):
         _check(lib().spec_kv4_commit(pool.handle, len(ids), p_ids, p_lens, _ptr(accepted_len),
                                      _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))
 
