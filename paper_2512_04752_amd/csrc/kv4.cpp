@@ -14,8 +14,10 @@ using namespace spec;
 namespace {
 
 constexpr int kPartCap = 8192;          // partial tiles of 16 rows per step
-constexpr int kTargetGroups1 = 512;     // attention work-groups aimed for, a wave on one row tile
-constexpr int kTargetGroups2 = 768;     // and on two
+constexpr int kResident1 = 768;         // attention work-groups that fit the chip, a wave on one row tile
+constexpr int kResident2 = 512;         // and on two
+constexpr double kUneven1 = 2.25;       // largest work of one over the average of that many
+constexpr double kUneven2 = 1.5;
 constexpr int kPairRows = 128;          // rows per KV head from which on a wave takes two tiles
 constexpr int kMinWork = 2048;          // keys x (row tile share) of a work-group, lower bound
 constexpr int kUnsplit = 2816;          // nothing is split when no range is above this
@@ -81,19 +83,22 @@ struct AttnPlan {
 // SIMD) or, when some sample has more than kPairRows rows, two (two per SIMD, and V is
 // decoded once for both).  A work-group's four waves share the keys of the first tile
 // (pair) by four, of two by two, or have one each; more tiles go to more work-groups.
-// A group's key range is cut into chunks of about the same work (keys x waves' share),
-// so that the step has about kTargetGroups work-groups, but of at least kMinWork; with no
-// range above kUnsplit nothing is cut, which saves the merge's launch.  Measured, us, 8B
-// heads:
+// A group's key range is cut evenly, so that the step's work-groups (work: keys x waves'
+// share) fit the chip at once, kResident, unless one would then have kUneven times the
+// average; but none below kMinWork is made, and with no range above kUnsplit nothing is
+// cut, which saves the merge's launch.  Measured, us, 8B heads:
 //                                   one tile per wave   two tiles
-//   128 samples, 176K keys, 32 rows        58.5            62.1
-//   4 samples, 15K keys, 64 rows           16.7            20.5
-//   4 samples, 101K keys, 256 rows         139             124
-//   prompt pieces of 500 - 1170 rows       173             157
-// Work-groups aimed for 384 / 512 / 768 / 1024: one tile, 256 samples, 227K keys, 4 rows
-// 46 / 45.5 / 48.7 / 48.7; two tiles, the third row 144 / 133 / 124 / 128.  At least 1024
-// / 2048 per work-group: the second row 19.8 / 17.4.  A range of 2100 (of 4064) in one
-// piece 11.4 (17.7), in pieces of 2048 14.2 (14.3).
+//   128 samples, 176K keys, 32 rows        55.7            62.1
+//   4 samples, 15K keys, 64 rows           17.0            20.5
+//   4 samples, 101K keys, 256 rows         139             120
+//   prompt pieces of 500 - 1170 rows       173             153
+// kUneven 1 / 1.5 / 2 / 2.25 / 4: first row 60.0 / 58.5 / 57.7 / 55.6 / 55.7, third 143 /
+// 121 / 121 / 120 / 119, fourth 158 / 155 / 153 / 153 / 153; but with one sample of 30000
+// keys among 100 of 64 rows and 1000 keys 66.9 / 90 for the last two, and among 8 of 1024
+// rows 211 / 306 (192 at 1.5; a work-group that is left alone runs faster where three share a CU than
+// where two do).  Chunks of one length for all, 1.5 rounds of them: 58.8, 124, 157, 70, 179.
+// At least 1024 / 2048 per work-group: the second row 19.8 / 17.4.  A range of 2100 (of
+// 4064) in one piece 11.4 (17.7), in two 14.2 (14.3).
 void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, AttnPlan* plan) {
   const int G = c->n_heads / c->n_kv_heads, nkv = c->n_kv_heads;
   struct Group {
@@ -121,31 +126,30 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
       longest = std::max(longest, (int64_t)keys * weight(n));
     }
   }
-  auto chunk_of = [&](const Group& g, double unit) {
-    const int64_t least = ((int64_t)g.keys + kMaxSplits - 1) / kMaxSplits;
-    const int64_t want = std::max<int64_t>(least, (int64_t)(unit / weight(g.tiles)));
-    return (want + 127) / 128 * 128;
-  };
   auto splits_of = [&](const Group& g, double unit) {
-    const int64_t ch = chunk_of(g, unit);
-    return (int)((g.keys + ch - 1) / ch);
+    const double per = std::max(128.0, unit / weight(g.tiles));
+    return (int)std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (int64_t)std::ceil(g.keys / per)));
   };
-  double unit = std::max<double>(longest <= kUnsplit ? kUnsplit : kMinWork,
-                                 work / (wt == 1 ? kTargetGroups1 : kTargetGroups2));
+  auto chunk_of = [&](const Group& g, int ns) { return ((int64_t)g.keys + 128 * ns - 1) / (128 * ns) * 128; };
+  const int slots_at_once = wt == 1 ? kResident1 : kResident2;
+  const double least = longest <= kUnsplit ? kUnsplit : kMinWork, even = work / slots_at_once;
+  const double uneven = wt == 1 ? kUneven1 : kUneven2;
+  double unit = std::max(least, even);
   for (;;) {      // ends: with units beyond the longest range times four nothing is split
-    int64_t slots = 0;
+    int64_t slots = 0, wgs = 0;
     for (const Group& g : groups) {
       const int ns = splits_of(g, unit);
+      wgs += (int64_t)ns * nkv;
       if (ns > 1) slots += (int64_t)ns * nkv * g.tiles;
     }
-    if (slots <= kPartCap) break;
-    unit = unit * 1.25 + 128;
+    if (slots <= kPartCap && (wgs <= slots_at_once || slots == 0 || unit > uneven * even)) break;
+    unit *= 1.03;
   }
   std::vector<AttnItem> list;      // its `pad` is Kv4Item::waves
   int slot = 0;
   for (const Group& g : groups) {
-    const int64_t ch = chunk_of(g, unit);
-    const int ns = splits_of(g, unit);
+    const int64_t ch = chunk_of(g, splits_of(g, unit));
+    const int ns = (int)((g.keys + ch - 1) / ch);
     for (int kvh = 0; kvh < nkv; ++kvh) {
       for (int k = 0; k < ns; ++k)
         list.push_back(AttnItem{g.b, kvh, g.tile0 * 16, (int)(k * ch),
