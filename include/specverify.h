@@ -375,8 +375,9 @@ size_t spec_kv4_step_bytes(const spec_model_config* cfg, int32_t max_batch, int3
  *                                S_b + i and sees the keys [0, S_b + i]
  *   seq_lens     host [batch]    S_b >= 0, S_b + T_b <= 64 * (pages of the sample)
  *   workspace    device, 256-byte aligned; the step's until its last launch is done
- * *out receives the plan; spec_kv4_step_free releases it (host memory only: call it
- * once no more launches are to be made). */
+ * The plan is uploaded on `stream`: launches on another stream are the caller's to order
+ * after it.  *out receives the plan; spec_kv4_step_free releases it (host memory only: call
+ * it once no more launches are to be made). */
 int spec_kv4_step_begin(spec_kv4* kv, int32_t batch, const int32_t* sample_ids,
                         const int32_t* row_offsets, const int32_t* parents, const int32_t* seq_lens,
                         void* workspace, size_t ws_bytes, void* stream, spec_kv4_step** out);

@@ -40,14 +40,18 @@
 // A work-group has four waves: one, two or four share a row tile (pair)'s keys, block
 // by block, and merge through LDS at the end.
 //
-// What bounds it: up to about 16 rows per KV head the cache's bytes (256 samples, 227K
-// keys of 8 heads, 243 MB: 51 us, 4.8 TB/s, what a copy reaches); above that the vector
-// instructions of a block (the softmax and V's conversions), which do not overlap the
-// MFMAs of their own wave.  A first form, 32 rows by v_mfma_f32_32x32x16_bf16 with K
-// decoded to bf16 as well and the blocks' scores in 32 keys x 32 rows, took (this form in
-// brackets, us): one sample of 1100 keys 12.5 (9.4); 4 x 16 nodes, 15K keys 21.6 (16.5);
-// 1B heads, 32 x 15 nodes 25.4 (20.7); 128 x 8 nodes, 175K keys 62.8 (58.8); 256 x 1
-// 67 (51.2); 4 x 64 nodes, 101K keys 151 (123); prompt pieces of 500 - 1170 rows 181 (158).
+// What bounds it: up to 16 rows per KV head the cache's bytes (256 samples, 227K keys of 8
+// heads, 243 MB: 46 us, 5.3 TB/s, above a copy's rate); above that the vector instructions
+// (4 x 64 nodes at 16K - 32K keys: 67 % of the cycles, the matrix cores 43 %); below some
+// 3000 keys per work-group its own latency, about 1000 cycles per block of a wave that has
+// its SIMD alone, and 4 us of a merge's launch.  A first form, 32 rows by
+// v_mfma_f32_32x32x16_bf16 with K decoded to bf16 as well, took (this form in brackets, us):
+// one sample of 580 keys 12.5 (6.9); 4 x 16 nodes, 15K keys 21.6 (17.1); 1B heads, 32 x 15
+// nodes 25.4 (20.7); 128 x 8 nodes, 176K keys 62.8 (55.9); 256 x 1 67 (46); 4 x 64 nodes, 101K
+// keys 151 (120); prompt pieces of 500 - 1170 rows 181 (155).  Tried and slower: the next
+// block's scores multiplied ahead of a block's softmax (tail 127, prompt 163 against 120, 152
+// then); three blocks of loads under way (no change); the merge by the last work-group of
+// a row group (its device-wide stores: 4 x 16 nodes 37.8, tail 170).
 #include <math.h>
 
 #include <atomic>

@@ -141,7 +141,7 @@ __device__ __forceinline__ int octet_of_block() {
 // keep their codes.
 //
 // Bound by bytes and vector instructions about alike: 29.7K rows of 8 heads of 128 (122
-// MB in, 32 MB out, 32 us at a copy's rate) take 38 us with some 450 instructions per
+// MB in, 32 MB out, 32 us at a copy's rate) take 38 us with some 500 instructions per
 // octet and head.  With the library's sincos, a conversion of both numbers of a pair in
 // both of their lanes, and no load under way it was 44 us and 665; a wave per head and no
 // second one to load for, 48 us.  One row: 3.6 us (5.1).
