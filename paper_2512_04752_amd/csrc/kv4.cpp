@@ -47,8 +47,8 @@ struct StepLayout {
 
 StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, int64_t pages) {
   const int64_t G = c->n_heads / c->n_kv_heads;
-  const int64_t groups = (int64_t)c->n_kv_heads * ((rows * G + 15) / 16 + batch);   // row groups, at most
-  const int64_t items = 8 * (groups + kPartCap);                                    // padded per XCD
+  const int64_t groups = (int64_t)c->n_kv_heads * (rows * G / 64 + batch);   // of four row tiles at least, or a sample's last
+  const int64_t items = 8 * (groups + kPartCap);                             // padded per XCD
   const int64_t octets = rows / 8 + 2 * batch;
   const size_t blob = align_up(batch * sizeof(SampleInfo)) + align_up(rows * 4) + align_up(pages * 4) +
                       align_up(c->head_dim / 2 * sizeof(double)) + align_up(octets * sizeof(Kv4Octet)) +
@@ -145,34 +145,32 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
     if (slots <= kPartCap && (wgs <= slots_at_once || slots == 0 || unit > uneven * even)) break;
     unit *= 1.03;
   }
-  std::vector<AttnItem> list;      // its `pad` is Kv4Item::waves
+  std::vector<Kv4Item> list;
+  std::vector<AttnItem> order;     // with ranges as long as the work; `pad` is an index into `list`
   int slot = 0;
   for (const Group& g : groups) {
     const int64_t ch = chunk_of(g, splits_of(g, unit));
     const int ns = (int)((g.keys + ch - 1) / ch);
+    const SampleInfo& b = si[g.b];
     for (int kvh = 0; kvh < nkv; ++kvh) {
-      for (int k = 0; k < ns; ++k)
-        list.push_back(AttnItem{g.b, kvh, g.tile0 * 16, (int)(k * ch),
-                                (int)std::min<int64_t>(g.keys, (k + 1) * ch), ns, ns > 1 ? slot + k : 0,
-                                waves_of(g.tiles)});
+      for (int k = 0; k < ns; ++k) {
+        const int key0 = (int)(k * ch), key1 = (int)std::min<int64_t>(g.keys, (k + 1) * ch);
+        const int64_t end = key0 + (int64_t)(key1 - key0) * weight(g.tiles);
+        order.push_back(AttnItem{g.b, kvh, 0, key0, (int)std::min<int64_t>(end, 0x7fffffff), 0, 0, (int)list.size()});
+        list.push_back(Kv4Item{kvh, g.tile0 * 16, key0, key1, ns, ns > 1 ? slot + k : 0, waves_of(g.tiles), b.seq_len,
+                               b.tok0, b.ntok, (uint32_t)b.kv_base, {}});
+      }
       if (ns > 1) {
         for (int t = 0; t < g.tiles; ++t)
-          plan->comb.push_back(Kv4Merge{kvh, (g.tile0 + t) * 16, ns, slot + t * ns, si[g.b].tok0, si[g.b].ntok, {}});
+          plan->comb.push_back(Kv4Merge{kvh, (g.tile0 + t) * 16, ns, slot + t * ns, b.tok0, b.ntok, {}});
         slot += ns * g.tiles;
       }
     }
   }
-  deal_items(list);
-  plan->items.reserve(list.size());
-  for (const AttnItem& x : list) {
-    if (x.sample < 0) {              // padding of a shorter per-XCD list
-      plan->items.push_back(Kv4Item{});
-      continue;
-    }
-    const SampleInfo& b = si[x.sample];
-    plan->items.push_back(Kv4Item{x.kvh, x.row0, x.key0, x.key1, x.nsplit, x.part, x.pad, b.seq_len, b.tok0, b.ntok,
-                                  (uint32_t)b.kv_base, {}});
-  }
+  deal_items(order);
+  plan->items.reserve(order.size());
+  for (const AttnItem& x : order)  // sample -1: padding of a shorter per-XCD list
+    plan->items.push_back(x.sample < 0 ? Kv4Item{} : list[x.pad]);
 }
 
 }  // namespace
