@@ -546,33 +546,45 @@ def _kv4_ints(pool, **tensors):
 def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
     """Write the rows' K and V ([rows, kv heads, head_dim], rows may be strided) into the cache,
     rotating k by position unless it has been."""
+    if torch.cuda.current_device() != step.pool.index:
+        with torch.cuda.device(step.pool.index):
+            return spec_kv4_append(step, layer, k, v, rotate, stream)
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with _on(step.pool.index):
-        _check(lib().spec_kv4_append(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs,
-                                     int(rotate), step._on_stream(stream)))
+    rc = lib().spec_kv4_append(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs, bool(rotate),
+                               step._on_stream(stream))
+    if rc:
+        _check(rc)
 
 
 def spec_kv4_read(step: KV4Step, layer, k, v, stream=None):
     """Write what the cache holds for the step's rows into k and v (as in spec_kv4_append)."""
+    if torch.cuda.current_device() != step.pool.index:
+        with torch.cuda.device(step.pool.index):
+            return spec_kv4_read(step, layer, k, v, stream)
     n = step.pool.cfg.n_kv_heads
     ks, vs = _kv4_rows(step, k, n, "k"), _kv4_rows(step, v, n, "v")
-    with _on(step.pool.index):
-        _check(lib().spec_kv4_read(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs,
-                                   step._on_stream(stream)))
+    rc = lib().spec_kv4_read(step.handle, int(layer), k.data_ptr(), ks, v.data_ptr(), vs,
+                             step._on_stream(stream))
+    if rc:
+        _check(rc)
 
 
 def spec_kv4_attend(step: KV4Step, layer, q, out, stream=None):
     """Attention of the step's rows: q [rows, heads, head_dim] (rows may be strided), rotated;
     out [rows, heads * head_dim], contiguous."""
+    if torch.cuda.current_device() != step.pool.index:
+        with torch.cuda.device(step.pool.index):
+            return spec_kv4_attend(step, layer, q, out, stream)
     n = step.pool.cfg.n_heads
     qs = _kv4_rows(step, q, n, "q")
     _kv4_rows(step, out, n, "out")
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    with _on(step.pool.index):
-        _check(lib().spec_kv4_attend(step.handle, int(layer), q.data_ptr(), qs, out.data_ptr(),
-                                     step._on_stream(stream)))
+    rc = lib().spec_kv4_attend(step.handle, int(layer), q.data_ptr(), qs, out.data_ptr(),
+                               step._on_stream(stream))
+    if rc:
+        _check(rc)
 
 
 def spec_workspace_bytes_kv4(cfg, max_batch, max_tokens, max_pages, sampled=False) -> int:
