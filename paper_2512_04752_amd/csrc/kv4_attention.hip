@@ -50,7 +50,8 @@
 // nodes 25.4 (20.7); 128 x 8 nodes, 176K keys 62.8 (55.9); 256 x 1 67 (46); 4 x 64 nodes, 101K
 // keys 151 (120); prompt pieces of 500 - 1170 rows 181 (155).  Tried and slower: the next
 // block's scores multiplied ahead of a block's softmax (tail 127, prompt 163 against 120, 152
-// then); three blocks of loads under way (no change); the merge by the last work-group of
+// then); three blocks of loads under way (no change); eight waves per work-group where each has
+// a CU to itself (4 x 16 nodes 17.5 against 17.2); the merge by the last work-group of
 // a row group (its device-wide stores: 4 x 16 nodes 37.8, tail 170).
 #include <math.h>
 
