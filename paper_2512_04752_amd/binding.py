@@ -480,8 +480,11 @@ class KV4Step:
             pages = int(((lens.astype(np.int64) + np.diff(offs) + SPEC_KV4_PAGE - 1)
                          // SPEC_KV4_PAGE).sum())
             nbytes = spec_kv4_step_bytes(pool.cfg, len(ids), self.n_rows, max(pages, 1))
-            workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
-            self._made_on = torch._C._cuda_getCurrentRawStream(pool.index)
+            # of that stream, where nothing before it can still use the memory
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
+            self._made_on = (torch._C._cuda_getCurrentRawStream(pool.index) if stream is None
+                             else stream.cuda_stream)
         elif (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
               or not workspace.is_contiguous()):
             raise ValueError("workspace must be a contiguous uint8 tensor on the pool's device")

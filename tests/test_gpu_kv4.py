@@ -511,6 +511,28 @@ def test_other_stream():
                  [150, 10], [6, 3], parents)
 
 
+def test_step_made_on_another_stream():
+    """Steps that are planned, run and dropped on a side stream, while memory is freed and taken on the
+    current one: their workspaces are the side stream's."""
+    cfg, c, prefix, parents, x, _ = _small(4)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    want = None
+    for i in range(6):
+        busy = torch.full((1 << 26,), 0xFF, dtype=torch.uint8, device="cuda")
+        del busy
+        step = sv.KV4Step(c.pool, [0, 1], [0, 6, 9], parents, [150, 10], stream=s)
+        assert step._made_on == s.cuda_stream
+        out = torch.empty(9, 1024, dtype=torch.bfloat16, device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        sv.spec_kv4_append(step, 0, x[:, 1024:1280], x[:, 1280:], stream=s)
+        sv.spec_kv4_attend(step, 0, x[:, :1024], out, stream=s)
+        del step
+        s.synchronize()
+        want = out if want is None else want
+        assert torch.equal(out, want)
+
+
 def test_captured_and_replayed():
     """append, read and attend in a graph, replayed on new inputs, with eager work between the replays."""
     cfg, c, prefix, parents, x, step = _small(2)
