@@ -406,9 +406,10 @@ int spec_kv4_read(const spec_kv4_step* step, int32_t layer, void* k, int64_t k_s
  *        (q_stride a multiple of 8, 16-byte aligned)
  *   out  device bf16 [N][n_heads * head_dim], 16-byte aligned
  * K and V enter as the numbers they stand for; probabilities are rounded to bf16,
- * sums and softmax statistics are fp32.  A query number more than 2^10 below its
- * row's largest is off by at most 2^-12 of the row's mean magnitude (2^-34 of the
- * largest in rows with one above 32 times their mean).  V is summed before the
+ * sums and softmax statistics are fp32.  Query numbers less than 2^9 below their
+ * row's largest are exact; what the others are off by (2^-17 of the largest each at
+ * most) comes, summed, to at most 2^-12 of the row's numbers that are more than 16
+ * times below the largest, or is 2^-34 of the largest at most each.  V is summed before the
  * division by the softmax's sum: values past 2^96 may overflow fp32 there.  Bitwise
  * the same for the same step, one attend of which runs at a time. */
 int spec_kv4_attend(const spec_kv4_step* step, int32_t layer, const void* q, int64_t q_stride,

@@ -108,3 +108,50 @@ def attend(q, K, V, visible):
         p /= p.sum(axis=1, keepdims=True)
         out[:, i], spread[:, i] = p @ v, p @ np.abs(v)
     return out, spread
+
+
+def e4m3(x):
+    """x rounded to e4m3 (4 significant bits, steps of 2^-9 at least), |x| < 448."""
+    x = np.asarray(x, np.float64)
+    e = np.maximum(np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -20))), -6)
+    return np.round(x * 2.0 ** (3 - e)) * 2.0 ** (e - 3)
+
+
+def query_loss(q):
+    """What each number of bf16 queries q [..., d] may be off by where the attention holds it as
+    two e4m3 numbers of the row's power of two, or, in rows that lose more than 2^-12 of the
+    numbers below a sixteenth of their largest, as four."""
+    q = np.asarray(q, np.float64)
+    top = np.abs(q).max(-1, keepdims=True)
+    s = 2.0 ** np.maximum(np.floor(np.log2(np.maximum(top, 2.0 ** -140))) - 7, -126)
+    rest = q / s
+    for _ in range(2):
+        rest = rest - e4m3(rest)
+    lost = np.abs(rest) * s
+    small = np.where(np.abs(q) < top / 16, np.abs(q), 0.0)
+    wide = lost.sum(-1, keepdims=True) > 2.0 ** -12 * small.sum(-1, keepdims=True)
+    return np.where(wide, np.minimum(lost, 2.0 ** -34 * top), lost)
+
+
+def attend_bound(q, K, V, visible, out, spread):
+    """How far the attention's output (rounded to bf16) may be from out = attend()[0], element by
+    element, by its roundings; spread = attend()[1], arguments as there.
+
+    Per row and head, with v = 2^-24 (fp32, half a step, relative): the score of a key is a sum of d
+    products, off by at most (d + 2) v B, B = sum |q k| / sqrt(d) of that key; the scale and the
+    subtraction of the reference add 4 v B, exp2 4 v; the query's parts what query_loss() says times
+    |k| / sqrt(d).  The largest of it over the visible keys is e: the probabilities of a row change
+    by factors within exp(+-2 e) against each other, the output by expm1(2 e) spread.  Rounding the
+    probabilities to bf16 adds 2^-8 spread, sums over n keys and merges 2 (n + 70) v spread, numbers
+    flushed below 2^-126 (n + 1) 2^-126 (max |V| + 6), and rounding the output 2^-8 of it."""
+    rows, heads, d = q.shape
+    group = heads // K.shape[1]
+    bound = np.empty(out.shape)
+    v, aq, lost = 2.0 ** -24, np.abs(q), query_loss(q)
+    n = visible.sum(1)[:, None]
+    for i in range(heads):
+        k = np.abs(K[:, i // group]).T / np.sqrt(d)
+        e = np.where(visible, (d + 6) * v * (aq[:, i] @ k) + lost[:, i] @ k, 0.0).max(1) + 4 * v
+        bound[:, i] = (np.expm1(2 * e)[:, None] + 2.0 ** -8 + 2 * (n + 70) * v) * spread[:, i]
+        bound[:, i] += (n + 1) * 2.0 ** -126 * (np.abs(V[:, i // group]).max() + 6)
+    return bound + 2.0 ** -8 * (np.abs(out) + bound)

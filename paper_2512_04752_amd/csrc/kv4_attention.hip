@@ -21,11 +21,15 @@
 // decodes them.  Its other operand has 8 bits at most, so a query number is held
 // as the sum of two e4m3 numbers of four significant bits each, which carries
 // bf16's eight; both share a power of two per row that puts the row's largest
-// magnitude in [128, 256).  Numbers more than 2^10 below the largest run into e4m3's
-// smallest step and are off by up to 2^-17 of the largest: by 2^-12 of the row's mean
-// magnitude at most, below bf16's own rounding of a query.  Rows whose largest is more
-// than 32 times their mean ("wide": an outlier) get the remainders as two more e4m3
-// numbers, and two more products, which leaves 2^-34 of the largest.
+// magnitude in [128, 256).  Numbers more than 2^9 below the largest run into e4m3's
+// smallest step and are off by up to 2^-17 of the largest, which is nothing beside the
+// largest's own rounding but may be much of such a number.  Rows where that matters
+// ("wide": what is lost comes, summed, to more than 2^-12 of the numbers that are more
+// than 16 times below the largest, a sixteenth of what rounding them to bf16 may cost)
+// get the remainders as two more e4m3 numbers, and two more products, which leaves
+// 2^-34 of the largest.  Weighing the loss against the row's mean instead misses two
+// equal outliers of 64 numbers, or four of 128.  Random normal rows are wide once in
+// 2800 (64 numbers) or less (128).
 //
 // V's codes are turned into bf16 (one conversion per byte), without their power of
 // two: it is the same for all dims of a key and scales the key's probability
@@ -166,19 +170,16 @@ struct Query {
     uint32_t x[N / 2];
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) x[c] = live ? (uint32_t)raw.x[c >> 2][c & 3] : 0u;
-    float most = 0.f, sum = 0.f;
+    float most = 0.f;
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) {
       const float a = fabsf(__uint_as_float(x[c] << 16)), b = fabsf(__uint_as_float(x[c] & 0xffff0000u));
       most = maximum(maximum(most, a), b);
-      sum += a + b;
     }
     most = max_groups(most);
-    sum = sum_groups(sum);
     const int e = (int)(__float_as_uint(most) >> 23 & 255);   // a NaN or infinity has 255
     scale = e == 255 ? 255 : max(e - 7, 1);
     rest_scale = e == 255 ? 255 : max(scale - 17, 1);
-    const bool wide = e != 255 && sum < most * (HD * 0.03125f);
     const float f = __uint_as_float((uint32_t)min(scale, 247) << 23);
     const float fr = __uint_as_float((uint32_t)min(rest_scale, 247) << 23);
     auto four = [&](int c, int i, float (&v)[4]) __attribute__((always_inline)) {
@@ -188,6 +189,8 @@ struct Query {
       v[2] = __uint_as_float(w1 << 16);
       v[3] = __uint_as_float(w1 & 0xffff0000u);
     };
+    const float small = most * 0.0625f;
+    float lost = 0.f, below = 0.f;             // sums: what two parts lose; the numbers below `small`
     i32x4 hi[HD / 64], lo[HD / 64];
     auto join = [&](i32x8 (&to)[HD / 64]) __attribute__((always_inline)) {
       if constexpr (HD == 128) {
@@ -204,11 +207,15 @@ struct Query {
         float v[4];
         int h, l;
         four(c, i, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) below += fabsf(v[j]) < small ? fabsf(v[j]) : 0.f;
         split(v, f, h, l);
+        lost += (fabsf(v[0]) + fabsf(v[1])) + (fabsf(v[2]) + fabsf(v[3]));
         hi[c][i] = h;
         lo[c][i] = l;
       }
     join(q);
+    const bool wide = e != 255 && sum_groups(fmaf(below, -0x1p-12f, lost)) > 0.f;
 #pragma unroll
     for (int c = 0; c < HD / 64; ++c) rest[c] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
     const bool any = __ballot(wide) != 0;

@@ -1,0 +1,52 @@
+"""GPU parity of the 4-bit cache's attention against the float64 oracle within
+oracle.kv4.attend_bound: element by element, every term from the row and the
+keys that it sees."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_04752_amd as sv
+from oracle import kv4 as O
+from tests.test_gpu_kv4 import Cache, bf16, config, random_tree
+
+pytestmark = pytest.mark.gpu
+
+
+def read(step, layer, n, kv, d):
+    ko, vo = (torch.empty(n, kv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sv.spec_kv4_read(step, layer, ko, vo)
+    return tuple(t.double().cpu().numpy() for t in (ko, vo))
+
+
+def check(q, out, K, V, visible, what):
+    o, spread = O.attend(q, K, V, visible)
+    err, tol = np.abs(out - o), O.attend_bound(q, K, V, visible, o, spread)
+    assert (err <= tol).all(), f"{what}: error {err.max():.3g}, {(err / tol).max():.2f} of its bound"
+
+
+@pytest.mark.parametrize("d,dims", [(64, (5, 37)), (64, tuple(range(0, 64, 2))), (64, tuple(range(60))),
+                                    (128, (5, 69)), (128, (5, 37, 69, 101)), (128, tuple(range(1, 128, 2)))],
+                         ids=lambda x: str(x if isinstance(x, int) else len(x)))
+@pytest.mark.parametrize("ratio", [100.0, 1000.0, 5000.0, 20000.0, 2.0 ** 20])
+def test_queries_with_several_outliers(d, dims, ratio):
+    """Rows whose outliers, several of one size, lie where the keys are zero: the scores are those of the
+    other numbers.  Ordinary rows between them come out as they do alone."""
+    rows, dims = 24, list(dims)
+    cfg = config(8, 2, d)
+    rng = np.random.default_rng(len(dims) + int(ratio))
+    c = Cache(cfg, [0], [rows])
+    k = rng.normal(size=(rows, 2, d)) * 2
+    k[:, :, dims] = 0
+    step = c.append(0, [0], [0], bf16(k).cuda(), bf16(rng.normal(size=(rows, 2, d))).cuda(), [rows], rotate=False)
+    K, V = read(step, 0, rows, 2, d)
+    assert (K[:, :, dims] == 0).all()
+    plain = rng.normal(size=(rows, 8, d))
+    q = plain.copy()
+    q[::2, :, dims] = ratio * rng.choice([-1.0, 1.0], size=q[::2, :, dims].shape)
+    out, alone = (torch.empty(rows, 8 * d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sv.spec_kv4_attend(step, 0, bf16(q).cuda(), out)
+    sv.spec_kv4_attend(step, 0, bf16(plain).cuda(), alone)
+    assert torch.equal(out[1::2], alone[1::2])
+    check(bf16(q).double().numpy(), out.double().cpu().numpy().reshape(q.shape), K, V,
+          np.tril(np.ones((rows, rows), bool)), f"d {d}, {len(dims)} outliers of {ratio}")
