@@ -455,6 +455,25 @@ class KV4Pool:
             pass
 
 
+def _kv4_arrays(sample_ids, row_offsets, seq_lens, **per_row):
+    """The int32 arrays and pointers of a step's host arguments, which the library reads by
+    the lengths of sample_ids and the last offset."""
+    ids, offs, lens = (_i32(x) for x in (sample_ids, row_offsets, seq_lens))
+    if len(offs[0]) != len(ids[0]) + 1 or len(lens[0]) != len(ids[0]):
+        raise ValueError("row_offsets must have one entry more than sample_ids, seq_lens as many")
+    rows = {name: (None, None) if x is None else _i32(x) for name, x in per_row.items()}
+    for name, (arr, _) in rows.items():
+        if len(ids[0]) and arr is not None and len(arr) != int(offs[0][-1]):
+            raise ValueError(f"{name} must have one entry per row")
+    return (ids, offs, lens, *rows.values())
+
+
+def _kv4_workspace(pool, workspace):
+    if (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
+            or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the pool's device")
+
+
 class KV4Step:
     """The plan of one step over a KV4Pool (spec_kv4_step_begin).
 
@@ -466,14 +485,8 @@ class KV4Step:
                  stream=None):
         self.handle = None
         self.pool = pool
-        ids, p_ids = _i32(sample_ids)
-        offs, p_offs = _i32(row_offsets)
-        lens, p_lens = _i32(seq_lens)
-        pars, p_pars = (None, None) if parents is None else _i32(parents)
-        if len(offs) != len(ids) + 1 or len(lens) != len(ids):
-            raise ValueError("row_offsets must have one entry more than sample_ids, seq_lens as many")
-        if len(ids) and pars is not None and len(pars) != int(offs[-1]):
-            raise ValueError("parents must have one entry per row")
+        (ids, p_ids), (offs, p_offs), (lens, p_lens), (pars, p_pars) = _kv4_arrays(
+            sample_ids, row_offsets, seq_lens, parents=parents)
         self.n_rows = int(offs[-1])
         self._made_on = None                 # the stream of a workspace of the step's own
         if workspace is None:
@@ -485,9 +498,8 @@ class KV4Step:
                 workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=pool.buf.device)
             self._made_on = (torch._C._cuda_getCurrentRawStream(pool.index) if stream is None
                              else stream.cuda_stream)
-        elif (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
-              or not workspace.is_contiguous()):
-            raise ValueError("workspace must be a contiguous uint8 tensor on the pool's device")
+        else:
+            _kv4_workspace(pool, workspace)
         self.workspace = workspace
         h = c_void_p()
         with _on(pool.index):
@@ -537,13 +549,14 @@ def _kv4_rows(step, t, heads, what):
     return t.stride(0) if step.n_rows > 1 else heads * d
 
 
-def _kv4_ints(pool, **tensors):
-    """Each name=(tensor, numbers) must be a contiguous int32 tensor on the pool's device that
-    holds that many."""
+def _kv4_tensors(pool, dtype, **tensors):
+    """Each name=(tensor, numbers) must be a contiguous tensor of that type on the pool's device
+    that holds that many."""
     for name, (t, n) in tensors.items():
-        if (t.dtype != torch.int32 or t.device != pool.buf.device or not t.is_contiguous()
+        if (t.dtype != dtype or t.device != pool.buf.device or not t.is_contiguous()
                 or t.numel() < n):
-            raise ValueError(f"{name} must be a contiguous int32 tensor of {n} on the pool's device")
+            kind = str(dtype).split(".")[-1]
+            raise ValueError(f"{name} must be a contiguous {kind} tensor of {n} on the pool's device")
 
 
 def spec_kv4_append(step: KV4Step, layer, k, v, rotate=True, stream=None):
@@ -603,16 +616,22 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
     """spec_verify (or, with a temperature or an EOS token, spec_verify_sampled) over a 4-bit
     pool."""
     c = make_config(cfg)
-    ids, p_ids = _i32(sample_ids)
-    offs, p_offs = _i32(tree_offsets)
-    toks, p_toks = _i32(tree_tokens)
-    pars, p_pars = _i32(tree_parents)
-    lens, p_lens = _i32(seq_lens)
-    samp = _sampling(cfg, int(offs[-1]), temperature, eos_token, draft_probs, uniforms)
-    _kv4_ints(pool, accepted_len=(accepted_len, len(ids)), next_token=(next_token, len(ids)),
-              accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
+    (ids, p_ids), (offs, p_offs), (lens, p_lens), (_, p_toks), (_, p_pars) = _kv4_arrays(
+        sample_ids, tree_offsets, seq_lens, tree_tokens=tree_tokens, tree_parents=tree_parents)
+    n = int(offs[-1])
+    _kv4_workspace(pool, workspace)
+    samp = _sampling(cfg, n, temperature, eos_token, draft_probs, uniforms)
+    if temperature > 0:
+        _kv4_tensors(pool, torch.float32, draft_probs=(draft_probs, n * cfg.vocab), uniforms=(uniforms, 2 * n))
+    _kv4_tensors(pool, torch.int32, accepted_len=(accepted_len, len(ids)), next_token=(next_token, len(ids)),
+                 accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
     dbg = None
     if debug:
+        for name, dtype, width in (("logits", torch.float32, cfg.vocab), ("argmax", torch.int32, 1),
+                                   ("depth", torch.int32, 1), ("pos", torch.int32, 1),
+                                   ("anc", torch.int64, SPEC_ANC_WORDS)):
+            if debug.get(name) is not None:
+                _kv4_tensors(pool, dtype, **{name: (debug[name], n * width)})
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
                            for k in ("logits", "argmax", "depth", "pos", "anc")])
     with _on(pool.index):
@@ -627,8 +646,10 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
                     stream=None):
     ids, p_ids = _i32(sample_ids)
     lens, p_lens = _i32(seq_lens)
-    _kv4_ints(pool, accepted_len=(accepted_len, len(ids)), new_seq_lens=(new_seq_lens, len(ids)),
-              accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
+    if len(lens) != len(ids):
+        raise ValueError("seq_lens must have as many entries as sample_ids")
+    _kv4_tensors(pool, torch.int32, accepted_len=(accepted_len, len(ids)), new_seq_lens=(new_seq_lens, len(ids)),
+                 accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
     with _on(pool.index):
         _check(lib().spec_kv4_commit(pool.handle, len(ids), p_ids, p_lens, _ptr(accepted_len),
                                      _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))
