@@ -83,6 +83,13 @@ def decode_page(page, n_layers, n_kv_heads, d):
     return K, V
 
 
+def negative_zeros(page, n_layers, n_kv_heads, d):
+    """How many numbers of a page's bytes have the code 8, which nothing is stored as."""
+    heads = page[:n_layers * n_kv_heads * PAGE * (d + d // 32 + 2)].reshape(n_layers * n_kv_heads, -1)
+    codes = heads[:, :PAGE * d]
+    return int((codes & 15 == 8).sum() + (codes >> 4 == 8).sum())
+
+
 def sees(parents, rows):
     """[rows, rows] whether row i sees row j, and the rows' depths; parents None: a run."""
     if parents is None:

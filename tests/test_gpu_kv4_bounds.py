@@ -50,3 +50,30 @@ def test_queries_with_several_outliers(d, dims, ratio):
     assert torch.equal(out[1::2], alone[1::2])
     check(bf16(q).double().numpy(), out.double().cpu().numpy().reshape(q.shape), K, V,
           np.tril(np.ones((rows, rows), bool)), f"d {d}, {len(dims)} outliers of {ratio}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rotate", [True, False])
+def test_no_negative_zero_is_stored(d, rotate):
+    """Negative numbers too small for their group's steps, and -0: code 0, in every page and head, and
+    read back as +0, in K and V."""
+    rows, kv = 90, 256 // d
+    cfg = config(kv, kv, d, layers=2)
+    rng = np.random.default_rng(d)
+    x = rng.normal(size=(2, rows, kv, d))
+    x[rng.random(x.shape) < 0.5] *= 1e-3
+    x[rng.random(x.shape) < 0.1] = -0.0
+    x[:, 5] = -0.0
+    x = bf16(x).cuda()
+    c = Cache(cfg, [3], [rows])
+    step = c.append(1, [0], [3], x[0], x[1], [rows], rotate=rotate)
+    ko, vo = (torch.empty(rows, kv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sv.spec_kv4_read(step, 1, ko, vo)
+    raw = c.bytes()
+    assert sum(O.negative_zeros(page, 2, kv, d) for page in raw) == 0
+    want = O.stored(x[0].double().cpu().numpy(), x[1].double().cpu().numpy(),
+                    range(3, 3 + rows) if rotate else None, 1e4)
+    for got, w, from_ in zip((ko, vo), want, x.double().cpu().numpy()):
+        assert ((w == 0) & (from_ < 0)).sum() > rows * kv * d / 20           # there are many
+        bits = got.view(torch.int16).cpu().numpy()
+        assert (bits[w == 0] == 0).all() and (bits[w != 0] != 0).all()

@@ -55,3 +55,15 @@ def test_bound_of_two_part_queries(d):
     tol = O.attend_bound(q, K, V, visible, o, spread)
     assert not (np.abs(O.attend(two, K, V, visible)[0] - o) <= tol).all()
     assert (np.abs(bf16(o) - o) <= tol).all()
+
+
+def test_negative_zeros_are_counted():
+    """A code 8 in either half of any code byte of K or V; scales that hold an 8 are none."""
+    d, size = 64, 64 * (64 + 2 + 2)
+    page = np.full(2 * 3 * size, 0xFF, np.uint8)
+    heads = page.reshape(6, size)
+    heads[:, 64 * d:] = 8
+    assert O.negative_zeros(page, 2, 3, d) == 0
+    heads[4, 7] = 0x81
+    heads[5, 64 * d - 1] = 0x18
+    assert O.negative_zeros(page, 2, 3, d) == 2
