@@ -77,3 +77,39 @@ def test_no_negative_zero_is_stored(d, rotate):
         assert ((w == 0) & (from_ < 0)).sum() > rows * kv * d / 20           # there are many
         bits = got.view(torch.int16).cpu().numpy()
         assert (bits[w == 0] == 0).all() and (bits[w != 0] != 0).all()
+
+
+# ---- the element-wise bound over the kernel's shapes -----------------------------------
+
+@pytest.mark.parametrize("shape,lens,rows,chain,std", [
+    ((8, 2, 128), [500, 64], [8, 20], False, 8.0),        # scores of several hundred
+    ((8, 2, 64), [500, 64], [8, 20], False, 8.0),
+    ((8, 2, 128), [700], [40], False, 30.0),              # of several thousand
+    ((32, 8, 128), [65, 0], [17, 9], False, 1.3),
+    ((4, 2, 64), [0, 1, 63, 200], [1, 9, 33, 40], True, 1.3),
+    ((3, 3, 128), [64, 130], [2, 70], True, 3.0),
+    ((14, 2, 128), [257], [33], False, 3.0),
+    ((8, 4, 64), [9001, 40], [3, 5], False, 3.0),         # split ranges
+    ((8, 2, 128), [300], [400], True, 3.0),
+], ids=str)
+def test_attend_element_by_element(shape, lens, rows, chain, std):
+    cfg = config(*shape)
+    rng = np.random.default_rng(sum(rows))
+    n, kv, d = sum(rows), cfg.n_kv_heads, cfg.head_dim
+    hq = cfg.n_heads * d
+    c = Cache(cfg, lens, rows, seed=n)
+    prefix = c.prefix(0, std=std)
+    parents = None if chain else [p for r in rows for p in random_tree(rng, r)]
+    x = torch.from_numpy(rng.normal(size=(n, hq + 2 * kv * d)) * std).to(torch.bfloat16).cuda()
+    step = c.append(0, range(len(lens)), lens, x[:, hq:hq + kv * d], x[:, hq + kv * d:], rows, parents)
+    own = read(step, 0, n, kv, d)
+    out = torch.full((n, hq), float("nan"), dtype=torch.bfloat16, device="cuda")
+    sv.spec_kv4_attend(step, 0, x[:, :hq], out)
+    q, out = (t.double().cpu().numpy().reshape(n, -1, d) for t in (x[:, :hq], out))
+    at = 0
+    for b, (s, r) in enumerate(zip(lens, rows)):
+        sl = slice(at, at + r)
+        at += r
+        m, _ = O.sees(None if chain else parents[sl], r)
+        check(q[sl], out[sl], *(np.concatenate([prefix[b][i], own[i][sl]]) for i in (0, 1)),
+              np.concatenate([np.ones((r, s), bool), m], 1), f"sample {b}")

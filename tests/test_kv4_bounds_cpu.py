@@ -67,3 +67,21 @@ def test_negative_zeros_are_counted():
     heads[4, 7] = 0x81
     heads[5, 64 * d - 1] = 0x18
     assert O.negative_zeros(page, 2, 3, d) == 2
+
+
+def test_bound_at_large_scores():
+    """Scores of several hundred, off by 0.02 here and there: past the bound, which the exact output
+    rounded to bf16 is not."""
+    q, K, V, visible = case(128, rows=8, keys=508, std=8.0, seed=11)
+    o, spread = O.attend(q, K, V, visible)
+    tol = O.attend_bound(q, K, V, visible, o, spread)
+    assert (np.abs(bf16(o) - o) <= tol).all()
+    rng = np.random.default_rng(0)
+    worst = 0.0
+    for i in range(8):
+        z = np.where(visible, q[:, i] @ K[:, i // 4].T / np.sqrt(128), -np.inf)
+        z += 0.02 * rng.choice([-1.0, 1.0], size=z.shape)
+        p = np.exp(z - z.max(1, keepdims=True))
+        off = (p / p.sum(1, keepdims=True)) @ V[:, i // 4]
+        worst = max(worst, (np.abs(off - o[:, i]) / tol[:, i]).max())
+    assert worst > 1
