@@ -79,6 +79,47 @@ def test_no_negative_zero_is_stored(d, rotate):
         assert (bits[w == 0] == 0).all() and (bits[w != 0] != 0).all()
 
 
+# ---- the same rows in other company ------------------------------------------------
+
+def test_rows_alone_and_among_others():
+    """A sample's rows by themselves, by one-row steps' kernels, and in batches whose other samples bring
+    two row tiles per wave, split ranges or both: the same cache, keys and queries, so the outputs lie
+    within their bound of each other's exact value."""
+    cfg = config(8, 2, 128)
+    kv, d, hq = 2, 128, 1024
+    rng = np.random.default_rng(17)
+    lens, rows = [129, 12000, 1, 700], [3, 5, 1, 90]
+    for first in (3, 1):                                  # 12 rows per KV head; 4
+        rows[0] = first
+        c = Cache(cfg, lens, rows, seed=first)
+        prefix = c.prefix(0)
+        x = torch.from_numpy(rng.normal(size=(sum(rows), hq + 2 * kv * d))).to(torch.bfloat16).cuda()
+        parents = [random_tree(rng, r) for r in rows]
+        at = np.concatenate([[0], np.cumsum(rows)])
+        outs, held = [], []
+        for ids in ([0], [0, 1], [0, 2], [3, 0], [0, 1, 2, 3]):
+            part = torch.cat([x[at[b]:at[b + 1]] for b in ids])
+            step = sv.KV4Step(c.pool, ids, np.concatenate([[0], np.cumsum([rows[b] for b in ids])]),
+                              sum((parents[b] for b in ids), []), [lens[b] for b in ids])
+            sv.spec_kv4_append(step, 0, part[:, hq:hq + kv * d], part[:, hq + kv * d:])
+            out = torch.empty(len(part), hq, dtype=torch.bfloat16, device="cuda")
+            sv.spec_kv4_attend(step, 0, part[:, :hq], out)
+            mine = sum(rows[b] for b in ids[:ids.index(0)])
+            outs.append(out[mine:mine + first].double().cpu().numpy().reshape(first, 8, d))
+            K, V = read(step, 0, len(part), kv, d)
+            held.append((K[mine:mine + first], V[mine:mine + first]))
+        for K, V in held[1:]:
+            assert np.array_equal(K, held[0][0]) and np.array_equal(V, held[0][1])
+        K, V = (np.concatenate([prefix[0][i], held[0][i]]) for i in (0, 1))
+        visible = np.concatenate([np.ones((first, lens[0]), bool), O.sees(parents[0], first)[0]], 1)
+        q = x[:first, :hq].double().cpu().numpy().reshape(first, 8, d)
+        o, spread = O.attend(q, K, V, visible)
+        tol = O.attend_bound(q, K, V, visible, o, spread)
+        for out in outs:
+            assert (np.abs(out - o) <= tol).all()
+            assert (np.abs(out - outs[0]) <= 2 * tol).all()
+
+
 # ---- the element-wise bound over the kernel's shapes -----------------------------------
 
 @pytest.mark.parametrize("shape,lens,rows,chain,std", [
