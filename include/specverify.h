@@ -304,7 +304,7 @@ int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int3
  * reads as NaN, and rows that see it attend to NaN or infinities.
  * Every reader sees the same numbers, whether a key is a tree node of this
  * step or was committed long ago, so a verified tree gives what one-token
- * steps over the same cache give.
+ * steps over the same cache give, up to the attention's roundings.
  *
  * Pages.  Page p lies at byte p * spec_kv4_page_bytes(cfg); in it, layer l
  * and KV head g take 64 * (head_dim + head_dim / 32 + 2) bytes at

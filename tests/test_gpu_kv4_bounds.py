@@ -120,6 +120,48 @@ def test_rows_alone_and_among_others():
             assert (np.abs(out - outs[0]) <= 2 * tol).all()
 
 
+@pytest.mark.parametrize("shape", [(8, 2, 128), (12, 4, 64)], ids=str)
+def test_tree_equals_one_token_steps(shape):
+    """The rows of a tree's branches, attended at once, and one at a time by one-row steps over the same
+    prefix, each of which sees what the ones before it appended: the same numbers in the cache, outputs
+    within their bound of one exact value."""
+    cfg = config(*shape, theta=5e5)
+    kv, d, hq = cfg.n_kv_heads, cfg.head_dim, cfg.n_heads * cfg.head_dim
+    rng = np.random.default_rng(23)
+    S, n = 203, 40
+    parents = random_tree(rng, n)
+    sees, depth = O.sees(parents, n)
+    leaves = [i for i in range(n) if i not in parents][-3:] + [int(depth.argmax())]
+    paths = [np.nonzero(sees[i])[0] for i in leaves]
+    c = Cache(cfg, [S] * (1 + len(paths)), [n] * (1 + len(paths)), seed=2)
+    p = torch.from_numpy(rng.normal(size=(2, S, kv, d)) * 1.3).to(torch.bfloat16).cuda()
+    for b in range(1 + len(paths)):                       # one prefix for all
+        step = c.append(0, [b], [0], p[0], p[1], [S])
+    prefix = read(step, 0, S, kv, d)
+    x = torch.from_numpy(rng.normal(size=(n, hq + 2 * kv * d)) * 1.3).to(torch.bfloat16).cuda()
+    k, v = x[:, hq:hq + kv * d], x[:, hq + kv * d:]
+    step = c.append(0, [0], [S], k, v, [n], parents)
+    own = read(step, 0, n, kv, d)
+    out = torch.empty(n, hq, dtype=torch.bfloat16, device="cuda")
+    sv.spec_kv4_attend(step, 0, x[:, :hq], out)
+    out = out.double().cpu().numpy().reshape(n, -1, d)
+    for b, path in enumerate(paths, 1):
+        for t, node in enumerate(path):
+            row = x[node:node + 1]
+            step = c.append(0, [b], [S + t], row[:, hq:hq + kv * d], row[:, hq + kv * d:], [1])
+            K, V = read(step, 0, 1, kv, d)
+            assert np.array_equal(K[0], own[0][node]) and np.array_equal(V[0], own[1][node])
+            one = torch.empty(1, hq, dtype=torch.bfloat16, device="cuda")
+            sv.spec_kv4_attend(step, 0, row[:, :hq], one)
+            q = row[:, :hq].double().cpu().numpy().reshape(1, -1, d)
+            K, V = (np.concatenate([prefix[i], own[i][path[:t + 1]]]) for i in (0, 1))
+            seen = np.ones((1, S + t + 1), bool)
+            o, spread = O.attend(q, K, V, seen)
+            tol = O.attend_bound(q, K, V, seen, o, spread)[0]
+            assert (np.abs(one.double().cpu().numpy().reshape(-1, d) - o[0]) <= tol).all()
+            assert (np.abs(out[node] - o[0]) <= tol).all()
+
+
 # ---- the element-wise bound over the kernel's shapes -----------------------------------
 
 @pytest.mark.parametrize("shape,lens,rows,chain,std", [
