@@ -13,7 +13,7 @@ using namespace spec;
 
 namespace {
 
-constexpr int kPartCap = 8192;          // partial tiles of 16 rows per step
+constexpr int kPartCap = 8192;          // partial tiles of 16 rows per step, at most
 constexpr int kResident1 = 768;         // attention work-groups that fit the chip, a wave on one row tile
 constexpr int kResident2 = 512;         // and on two
 constexpr double kUneven1 = 2.25;       // largest work of one over the average of that many
@@ -41,6 +41,14 @@ int check_unshared(const spec_kv4* kv, int sample, int64_t begin, int64_t end) {
   return SPEC_OK;
 }
 
+// Partial tiles that the plan of such a step may have: every row tile in as many key ranges
+// as the shortest range, kMinWork shared by a work-group's four tiles, leaves of its keys.
+int64_t part_cap(const spec_model_config* c, int64_t batch, int64_t rows, int64_t pages) {
+  const int64_t tiles = rows * (c->n_heads / c->n_kv_heads) / 16 + batch;
+  const int64_t ranges = std::min<int64_t>(kMaxSplits, (pages * kKv4Page + kMinWork / 4 - 1) / (kMinWork / 4));
+  return std::min<int64_t>(kPartCap, c->n_kv_heads * tiles * ranges);
+}
+
 struct StepLayout {
   size_t blob, toks, anc, part_o, part_ml, total;
 };
@@ -48,12 +56,13 @@ struct StepLayout {
 StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, int64_t pages) {
   const int64_t G = c->n_heads / c->n_kv_heads;
   const int64_t groups = (int64_t)c->n_kv_heads * (rows * G / 64 + batch);   // of four row tiles at least, or a sample's last
-  const int64_t items = 8 * (groups + kPartCap);                             // padded per XCD
+  const int64_t parts = part_cap(c, batch, rows, pages);
+  const int64_t items = 8 * (groups + parts);                                // padded per XCD
   const int64_t octets = rows / 8 + 2 * batch;
   const size_t blob = align_up(batch * sizeof(SampleInfo)) + align_up(rows * 4) + align_up(pages * 4) +
                       align_up(c->head_dim / 2 * sizeof(double)) + align_up(octets * sizeof(Kv4Octet)) +
                       align_up(items * sizeof(Kv4Item)) +
-                      align_up(kPartCap * sizeof(Kv4Merge));
+                      align_up(parts * sizeof(Kv4Merge));
   StepLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -64,8 +73,8 @@ StepLayout step_layout(const spec_model_config* c, int64_t batch, int64_t rows, 
   L.blob = take(blob);
   L.toks = take(rows * sizeof(TokInfo));
   L.anc = take(rows * 8 * kAncWords);
-  L.part_o = take((size_t)kPartCap * 16 * c->head_dim * 4);
-  L.part_ml = take((size_t)kPartCap * 16 * 2 * 4);
+  L.part_o = take((size_t)parts * 16 * c->head_dim * 4);
+  L.part_ml = take((size_t)parts * 16 * 2 * 4);
   L.total = off;
   return L;
 }
@@ -99,7 +108,8 @@ struct AttnPlan {
 // where two do).  Chunks of one length for all, 1.5 rounds of them: 58.8, 124, 157, 70, 179.
 // At least 1024 / 2048 per work-group: the second row 19.8 / 17.4.  A range of 2100 (of
 // 4064) in one piece 11.4 (17.7), in two 14.2 (14.3).
-void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, AttnPlan* plan) {
+void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& si, bool runs, int64_t parts,
+                    AttnPlan* plan) {
   const int G = c->n_heads / c->n_kv_heads, nkv = c->n_kv_heads;
   struct Group {
     int b, tile0, tiles, keys;
@@ -142,7 +152,7 @@ void plan_attention(const spec_model_config* c, const std::vector<SampleInfo>& s
       wgs += (int64_t)ns * nkv;
       if (ns > 1) slots += (int64_t)ns * nkv * g.tiles;
     }
-    if (slots <= kPartCap && (wgs <= slots_at_once || slots == 0 || unit > uneven * even)) break;
+    if (slots <= parts && (wgs <= slots_at_once || slots == 0 || unit > uneven * even)) break;
     unit *= 1.03;
   }
   std::vector<Kv4Item> list;
@@ -248,7 +258,7 @@ int kv4_plan_step(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, const 
                                 offsets[b] + (o - S), offsets[b], T, 0});
   }
   AttnPlan plan;
-  plan_attention(&c, si, runs, &plan);
+  plan_attention(&c, si, runs, part_cap(&c, batch, N, pages), &plan);
   std::vector<double> freq(c.head_dim / 2);
   for (int j = 0; j < c.head_dim / 2; ++j)
     freq[j] = std::pow((double)c.rope_theta, -2.0 * j / c.head_dim);

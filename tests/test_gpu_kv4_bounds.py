@@ -196,3 +196,40 @@ def test_attend_element_by_element(shape, lens, rows, chain, std):
         m, _ = O.sees(None if chain else parents[sl], r)
         check(q[sl], out[sl], *(np.concatenate([prefix[b][i], own[i][sl]]) for i in (0, 1)),
               np.concatenate([np.ones((r, s), bool), m], 1), f"sample {b}")
+
+
+# ---- workspaces of just the bytes that a step needs -----------------------------------
+
+@pytest.mark.parametrize("shape,lens,rows,chain", [
+    ((8, 2, 128), [0], [1], True), ((8, 2, 128), [3000], [1], False), ((8, 2, 128), [3000, 5, 2900], [40, 1, 9], False),
+    ((4, 2, 64), [20000], [33], True), ((32, 8, 128), [700, 3], [300, 2], True), ((8, 4, 64), [511, 512, 6000], [1, 1, 1], True),
+], ids=str)
+def test_workspace_of_exactly_the_step(shape, lens, rows, chain):
+    """The bytes behind it stay as they are, and the attention is right."""
+    cfg = config(*shape)
+    rng = np.random.default_rng(len(lens))
+    n, kv, d = sum(rows), cfg.n_kv_heads, cfg.head_dim
+    hq = cfg.n_heads * d
+    c = Cache(cfg, lens, rows)
+    prefix = c.prefix(0)
+    parents = None if chain else [p for r in rows for p in random_tree(rng, r)]
+    need = sv.spec_kv4_step_bytes(cfg, len(lens), n, sum((s + r + 63) // 64 for s, r in zip(lens, rows)))
+    whole = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    offsets = np.concatenate([[0], np.cumsum(rows)])
+    with pytest.raises(sv.SpecError, match="workspace"):
+        sv.KV4Step(c.pool, range(len(lens)), offsets, parents, lens, workspace=whole[:need - 1])
+    step = sv.KV4Step(c.pool, range(len(lens)), offsets, parents, lens, workspace=whole[:need])
+    x = torch.from_numpy(rng.normal(size=(n, hq + 2 * kv * d))).to(torch.bfloat16).cuda()
+    sv.spec_kv4_append(step, 0, x[:, hq:hq + kv * d], x[:, hq + kv * d:])
+    own = read(step, 0, n, kv, d)
+    out = torch.empty(n, hq, dtype=torch.bfloat16, device="cuda")
+    sv.spec_kv4_attend(step, 0, x[:, :hq], out)
+    assert (whole[need:] == 0xA5).all()
+    q, out = (t.double().cpu().numpy().reshape(n, -1, d) for t in (x[:, :hq], out))
+    at = 0
+    for b, (s, r) in enumerate(zip(lens, rows)):
+        sl = slice(at, at + r)
+        at += r
+        m, _ = O.sees(None if chain else parents[sl], r)
+        check(q[sl], out[sl], *(np.concatenate([prefix[b][i], own[i][sl]]) for i in (0, 1)),
+              np.concatenate([np.ones((r, s), bool), m], 1), f"sample {b}")
