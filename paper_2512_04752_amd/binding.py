@@ -425,6 +425,8 @@ class KV4Pool:
         if nbytes == 0:
             raise SpecError(-1, "invalid KV pool request")
         if buf is None:
+            if torch.device(device).type != "cuda":
+                raise ValueError(f"a KV pool lies in device memory, not on {device!r}")
             buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
         elif buf.dtype != torch.uint8 or not buf.is_cuda or not buf.is_contiguous():
             raise ValueError("buf must be a contiguous uint8 device tensor")

@@ -98,3 +98,11 @@ def test_commit_refusals(calls, changed):
 def test_step_refusals(offsets, parents, lens):
     with pytest.raises(ValueError):
         sv.KV4Step(pool(), [0], offsets, parents, lens, workspace=torch.empty(64, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("device", ["cpu", "meta", torch.device("cpu")], ids=str)
+def test_pool_off_the_device(device):
+    with pytest.raises(ValueError, match="device memory"):
+        sv.KV4Pool(CFG, 1, 2, device=device)
+    with pytest.raises(ValueError):
+        sv.KV4Pool(CFG, 1, 2, buf=torch.empty(1 << 20, dtype=torch.uint8))
