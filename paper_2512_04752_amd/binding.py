@@ -470,6 +470,11 @@ def _kv4_arrays(sample_ids, row_offsets, seq_lens, **per_row):
     return (ids, offs, lens, *rows.values())
 
 
+def _kv4_stream(pool, stream):
+    if stream is not None and stream.device.index != pool.index:
+        raise ValueError(f"the stream is on {stream.device}, the pool on device {pool.index}")
+
+
 def _kv4_workspace(pool, workspace):
     if (workspace.dtype != torch.uint8 or workspace.device != pool.buf.device
             or not workspace.is_contiguous()):
@@ -489,6 +494,7 @@ class KV4Step:
         self.pool = pool
         (ids, p_ids), (offs, p_offs), (lens, p_lens), (pars, p_pars) = _kv4_arrays(
             sample_ids, row_offsets, seq_lens, parents=parents)
+        _kv4_stream(pool, stream)
         self.n_rows = int(offs[-1])
         self._made_on = None                 # the stream of a workspace of the step's own
         if workspace is None:
@@ -516,8 +522,11 @@ class KV4Step:
         stream has passed its use."""
         if self.pool.handle is None:
             raise ValueError("the step's pool is closed")
-        s = (torch._C._cuda_getCurrentRawStream(self.pool.index) if stream is None
-             else stream.cuda_stream)
+        if stream is None:
+            s = torch._C._cuda_getCurrentRawStream(self.pool.index)
+        else:
+            _kv4_stream(self.pool, stream)
+            s = stream.cuda_stream
         if self._made_on is not None and s != self._made_on:
             self.workspace.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return s
@@ -621,6 +630,7 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
     (ids, p_ids), (offs, p_offs), (lens, p_lens), (_, p_toks), (_, p_pars) = _kv4_arrays(
         sample_ids, tree_offsets, seq_lens, tree_tokens=tree_tokens, tree_parents=tree_parents)
     n = int(offs[-1])
+    _kv4_stream(pool, stream)
     _kv4_workspace(pool, workspace)
     samp = _sampling(cfg, n, temperature, eos_token, draft_probs, uniforms)
     if temperature > 0:
@@ -650,6 +660,7 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
     lens, p_lens = _i32(seq_lens)
     if len(lens) != len(ids):
         raise ValueError("seq_lens must have as many entries as sample_ids")
+    _kv4_stream(pool, stream)
     _kv4_tensors(pool, torch.int32, accepted_len=(accepted_len, len(ids)), new_seq_lens=(new_seq_lens, len(ids)),
                  accepted_nodes=(accepted_nodes, len(ids) * SPEC_MAX_TREE))
     with _on(pool.index):

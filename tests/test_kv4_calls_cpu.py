@@ -106,3 +106,21 @@ def test_pool_off_the_device(device):
         sv.KV4Pool(CFG, 1, 2, device=device)
     with pytest.raises(ValueError):
         sv.KV4Pool(CFG, 1, 2, buf=torch.empty(1 << 20, dtype=torch.uint8))
+
+
+def test_streams_of_another_device(calls):
+    """Launched there, the kernels would take the pool's addresses for their own device's."""
+    here, there = (SimpleNamespace(cuda_stream=7, device=torch.device("cuda", i)) for i in (0, 1))
+    for call in (verify, commit):
+        with pytest.raises(ValueError, match="stream"):
+            call(stream=there)
+        call(stream=here)
+    assert calls == ["verify", "commit"]
+    with pytest.raises(ValueError, match="stream"):
+        sv.KV4Step(pool(), [0], [0, 1], None, [5], stream=there)
+    step = sv.KV4Step.__new__(sv.KV4Step)
+    step.handle, step.pool, step._made_on = None, pool(), None
+    step.pool.handle = 1
+    assert step._on_stream(here) == 7
+    with pytest.raises(ValueError, match="stream"):
+        step._on_stream(there)
