@@ -233,3 +233,28 @@ def test_workspace_of_exactly_the_step(shape, lens, rows, chain):
         m, _ = O.sees(None if chain else parents[sl], r)
         check(q[sl], out[sl], *(np.concatenate([prefix[b][i], own[i][sl]]) for i in (0, 1)),
               np.concatenate([np.ones((r, s), bool), m], 1), f"sample {b}")
+
+
+def test_a_query_that_is_not_finite_is_its_rows_alone():
+    """A NaN or infinity in one row and head: that row and head come out as NaN, the others as they do
+    without it, in one tile and in two, with ranges that are split."""
+    cfg = config(8, 2, 128)
+    rng = np.random.default_rng(5)
+    for lens, rows in (([40], [6]), ([9000, 3], [50, 2])):
+        n = sum(rows)
+        c = Cache(cfg, lens, rows)
+        c.prefix(0)
+        x = torch.from_numpy(rng.normal(size=(n, 1024 + 512))).to(torch.bfloat16).cuda()
+        step = c.append(0, range(len(lens)), lens, x[:, 1024:1280], x[:, 1280:], rows,
+                        [p for r in rows for p in random_tree(rng, r)])
+        q = x[:, :1024].clone().view(n, 8, 128)
+        plain, out = (torch.empty(n, 1024, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        sv.spec_kv4_attend(step, 0, q, plain)
+        bad = torch.zeros(n, 8, dtype=torch.bool)
+        for r, h, d, v in ((0, 3, 7, float("nan")), (4, 0, 127, float("inf")), (n - 1, 7, 64, float("-inf"))):
+            q[r, h, d] = v
+            bad[r, h] = True
+        sv.spec_kv4_attend(step, 0, q, out)
+        out, plain = out.view(n, 8, 128).cpu(), plain.view(n, 8, 128).cpu()
+        assert torch.isfinite(plain).all() and torch.equal(out[~bad], plain[~bad])
+        assert torch.isnan(out[bad]).all()
