@@ -95,7 +95,7 @@ struct AttnPlan {
 // A group's key range is cut evenly, so that the step's work-groups (work: keys x waves'
 // share) fit the chip at once, kResident, unless one would then have kUneven times the
 // average; but none below kMinWork is made, and with no range above kUnsplit nothing is
-// cut, which saves the merge's launch.  Measured, us, 8B heads:
+// cut, which saves the merge's launch.  Measured side by side when the rules were set, us, 8B heads:
 //                                   one tile per wave   two tiles
 //   128 samples, 176K keys, 32 rows        55.7            62.1
 //   4 samples, 15K keys, 64 rows           17.0            20.5

@@ -45,18 +45,19 @@
 // by block, and merge through LDS at the end.
 //
 // What bounds it: up to 16 rows per KV head the cache's bytes (256 samples, 227K keys of 8
-// heads, 243 MB: 46 us, 5.3 TB/s, above a copy's rate); above that the vector instructions
-// (4 x 64 nodes at 16K - 32K keys: 67 % of the cycles, the matrix cores 43 %); below some
-// 3000 keys per work-group its own latency, about 1000 cycles per block of a wave that has
-// its SIMD alone, and 4 us of a merge's launch.  A first form, 32 rows by
-// v_mfma_f32_32x32x16_bf16 with K decoded to bf16 as well, took (this form in brackets, us):
-// one sample of 580 keys 12.5 (6.9); 4 x 16 nodes, 15K keys 21.6 (17.1); 1B heads, 32 x 15
-// nodes 25.4 (20.7); 128 x 8 nodes, 176K keys 62.8 (55.9); 256 x 1 67 (46); 4 x 64 nodes, 101K
-// keys 151 (120); prompt pieces of 500 - 1170 rows 181 (155).  Tried and slower: the next
-// block's scores multiplied ahead of a block's softmax (tail 127, prompt 163 against 120, 152
-// then); three blocks of loads under way (no change); eight waves per work-group where each has
-// a CU to itself (4 x 16 nodes 17.5 against 17.2); the merge by the last work-group of
-// a row group (its device-wide stores: 4 x 16 nodes 37.8, tail 170).
+// heads, 248 MB: 45 us, 5.5 TB/s; a plain read of as many reaches 5.8); above that the vector
+// instructions (4 x 64 nodes at 16K - 32K keys: 68 % of the cycles) and the matrix products (43 %),
+// which two waves per SIMD do not overlap; below some 3000 keys per work-group its own latency,
+// about 1000 cycles per block of a wave that has its SIMD alone, and 4 us of a merge's launch.
+// Weighing what two parts lose takes four vector instructions per query number, 0.5 - 1 % of the
+// time.  A first form, 32 rows by v_mfma_f32_32x32x16_bf16 with K decoded to bf16 as well, took
+// (this form in brackets, us): one sample of 580 keys 12.5 (6.9); 4 x 16 nodes, 15K keys 21.6
+// (16.8); 1B heads, 32 x 15 nodes 25.4 (19.6); 128 x 8 nodes, 176K keys 62.8 (55.1); 256 x 1 67
+// (45.4); 4 x 64 nodes, 101K keys 151 (118); prompt pieces of 500 - 1170 rows 181 (156).  Tried and
+// slower, each beside the form of its time: the next block's scores multiplied ahead of a block's
+// softmax (tail 127, prompt 163 against 120, 152); three blocks of loads under way (no change);
+// eight waves per work-group where each has a CU to itself (4 x 16 nodes 17.5 against 17.2); the
+// merge by the last work-group of a row group (its device-wide stores: 4 x 16 nodes 37.8, tail 170).
 #include <math.h>
 
 #include <atomic>

@@ -25,7 +25,8 @@ class Verifier:
                  cache="bf16"):
         """sampling=True sizes the workspace for verify_sampled at temperature > 0.  cache="kv4"
         holds K and V in the 4-bit paged pool, every sample with pages of its own for its
-        capacity (remap them with self.kv.map)."""
+        capacity (remap them with self.kv.map; the workspace holds steps whose samples' positions
+        take no more pages than the max_batch largest capacities do)."""
         self.cfg = cfg
         self.cache = cache
         self.weights = B.Weights(W)
