@@ -372,7 +372,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4RowArgs a, int heads_p
 // goes up in d.  What it overwrites lies at d, what it still has to read at
 // path[d'] > d' > d, so nothing is lost and no thread waits for another.
 // Bound by that thread's chain of loads, PER of the keys and 8 of the values under way:
-// 127 rows moved in 128 samples, 32 layers of 8 heads of 128 (8.7 MB in and out) take 79 us.
+// 127 rows moved in 128 samples, 32 layers of 8 heads of 128 (8.7 MB in and out) take 80 us.
 template <int HD>
 __global__ __launch_bounds__(128) void kv4_compact_kernel(const Kv4CommitInfo* info, char* pool,
                                                           int64_t page_bytes, int n_kv_heads,
