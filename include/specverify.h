@@ -286,6 +286,116 @@ int spec_kv_pack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int32_
 int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int32_t* tok_begin,
                    const int32_t* tok_end, const void* buf, size_t buf_bytes, void* stream);
 
+/* ---- Products with weights in 4 bits -----------------------------------
+ *
+ * Few rows through a model cost the bytes of its weights.  These products take
+ * them in 4.25 bits per number, for a draft model, or for a target model's
+ * matrices outside spec_verify: x . W^T as every GEMM here, with W quantised once.
+ *
+ * Numbers.  E2M1 codes times a power of two 2^e that 32 consecutive numbers of a
+ * row share, as in the 4-bit cache below, with e >= -120: the smallest exponent in
+ * [-120, 125] with which no magnitude of the group exceeds 6 * 2^e (125 if none is;
+ * larger numbers take 6 * 2^125), the nearest code, the even one of two equally
+ * near, and code 0 for zero.  A group with an infinity or NaN reads as NaN.
+ *
+ * Layout (spec_w4_bytes).  Rows in tiles of 16, columns in tiles of 128, both
+ * padded with zeros.  A row tile holds, for its T column tiles,
+ *   codes   [T][64 lanes][16 bytes]: lane l has row l % 16, columns 32 (l / 16)
+ *           .. + 31 of the tile, column 2n and 2n + 1 in the low and high half of
+ *           byte n: what a lane of the matrix cores takes, in one load
+ *   scales  [ceil(T / 4)][64 lanes][4] bytes e + 127 (255: none), of column tiles
+ *           4 i .. 4 i + 3 */
+typedef struct {
+  const void* data;       /* device, spec_w4_bytes(rows, cols), 256-byte aligned */
+  int32_t rows, cols;     /* W is [rows][cols]: cols inputs, rows outputs */
+} spec_w4;
+
+/* Bytes of a [rows][cols] matrix in 4 bits; 0 if an argument is invalid (rows >= 1,
+ * cols a positive multiple of 32, both at most 2^24). */
+size_t spec_w4_bytes(int32_t rows, int32_t cols);
+
+/* Quantise w (device bf16, row r at r * stride; stride in values, a multiple of 8;
+ * 16-byte aligned) into data (device, 256-byte aligned, bytes >= spec_w4_bytes). */
+int spec_w4_pack(const void* w, int64_t stride, int32_t rows, int32_t cols, void* data, size_t bytes,
+                 void* stream);
+
+/* What the matrix stands for, exactly, as bf16 rows of w (as in spec_w4_pack). */
+int spec_w4_unpack(const spec_w4* m, void* w, int64_t stride, void* stream);
+
+enum {
+  SPEC_W4_BF16 = 0,       /* out = bf16(x W^T) */
+  SPEC_W4_F32 = 1,        /* out = x W^T, fp32 (logits) */
+  SPEC_W4_ADD = 2         /* out += x W^T, fp32 (a residual stream) */
+};
+
+/* Workspace bytes that a product of up to max_n rows of x with one such matrix (or, in
+ * spec_w4_gate_up, with two) may need.  May be 0, also if an argument is invalid. */
+size_t spec_w4_workspace_bytes(int32_t rows, int32_t cols, int32_t max_n);
+
+/* Products of n >= 0 rows.  The weights enter as the numbers they stand for, sums are
+ * fp32, in an order that depends on the shapes and n alone.
+ *   x          device bf16 [n][cols], row i at i * x_stride (a multiple of 8; 16-byte
+ *              aligned)
+ *   out        device, row i at i * out_stride (in values, any stride >= rows; aligned
+ *              as its type), of type `kind`
+ *   workspace  device, 256-byte aligned; may be NULL where no bytes are needed.  Calls
+ *              that can run at once need workspaces of their own.
+ * A row of x with an infinity or NaN changes no other row's outputs.  Only launches
+ * kernels: can be captured into a graph. */
+int spec_w4_linear(const spec_w4* m, const void* x, int64_t x_stride, int32_t n, void* out,
+                   int64_t out_stride, int32_t kind, void* workspace, size_t ws_bytes, void* stream);
+
+/* out = bf16(silu(x Wg^T) * (x Wu^T)), out [n][rows]: an FFN's first half.  Both
+ * matrices have the same shape; the rest as above. */
+int spec_w4_gate_up(const spec_w4* gate, const spec_w4* up, const void* x, int64_t x_stride, int32_t n,
+                    void* out, int64_t out_stride, void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- The choice of beams ------------------------------------------------
+ *
+ * One step of beam search, or the next level of a draft tree: of `groups` samples,
+ * each with `width` beams (or tree nodes) that have a score and logits, the k best
+ * continuations.
+ *   logits       device [groups * width] rows of vocab values, row r at r * row_stride
+ *                (in values, >= vocab), fp32 (bf16 = 0) or bf16 (1)
+ *   scores       device fp32 [groups][width], e.g. log probabilities so far
+ *   last_tokens  device int32 [groups][width], or NULL: the beams' last tokens, read
+ *                when eos_token >= 0
+ * Candidate (w, y) scores scores[w] + log softmax(logits of w)[y], computed in fp64.  A
+ * beam whose last token is eos_token has ended: it offers (w, eos_token) alone, at
+ * scores[w].  No candidates: tokens whose logit is -infinity; beams whose score is not
+ * finite; live beams with a logit that is NaN or +infinity.
+ * Outputs, per group the k best, best first, the lower (w, y) of equal scores first:
+ *   parents      device int32 [groups][k]  w
+ *   tokens       device int32 [groups][k]  y
+ *   new_scores   device fp32 [groups][k]   (rounded to fp32 once)
+ * Where a group has fewer candidates, the rest is -1, -1 and -infinity.  new_scores may
+ * be scores and tokens last_tokens (k == width).
+ * 1 <= k <= SPEC_MAX_BEAMS, 1 <= width <= SPEC_MAX_BEAMS, eos_token < vocab.  Only
+ * launches kernels; the workspace (device, 256-byte aligned, spec_beam_workspace_bytes) is
+ * the call's until they are done. */
+#define SPEC_MAX_BEAMS 64
+
+size_t spec_beam_workspace_bytes(int32_t groups, int32_t width, int32_t vocab, int32_t k);
+int spec_beam_select(const void* logits, int64_t row_stride, int32_t bf16, int32_t groups, int32_t width,
+                     int32_t vocab, const float* scores, const int32_t* last_tokens, int32_t eos_token,
+                     int32_t k, int32_t* parents, int32_t* tokens, float* new_scores, void* workspace,
+                     size_t ws_bytes, void* stream);
+
+/* ---- The cache rows that follow the beams ------------------------------
+ *
+ * Beam j of group g, pool sample sample_ids[g][j], continues beam p = parents[g][j]:
+ * the K/V of its positions [begin[g], end[g]), all layers, become what sample
+ * sample_ids[g][p] holds there before the call, all beams at once (p may be any beam of
+ * the group, the same for several).  A p outside [0, width), as spec_beam_select gives
+ * where there is no candidate, or equal to j leaves the beam as it is.  Positions before
+ * begin (a prompt that all beams share) are not touched.
+ *   sample_ids  host [groups][width]   distinct
+ *   begin, end  host [groups]          0 <= begin <= end <= every beam's capacity
+ *   parents     device int32 [groups][width]
+ * 1 <= width <= SPEC_MAX_BEAMS.  Descriptors are uploaded: a capturing stream is refused. */
+int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
+                    const int32_t* begin, const int32_t* end, const int32_t* parents, void* stream);
+
 /* ---- A KV cache in 4 bits, in pages ------------------------------------
  *
  * The bf16 pool above gives every sample one block of fixed capacity.  This
@@ -437,6 +547,15 @@ int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, cons
                     const int32_t* accepted_len, const int32_t* accepted_nodes,
                     int32_t* new_seq_lens, void* stream);
 
+/* spec_kv_reorder for this pool: codes and scales move.  The pages of positions
+ * [begin[g], end[g]) of every beam must not be shared (SPEC_ERR_INVALID).
+ *   workspace  device, 256-byte aligned, spec_kv4_reorder_bytes(groups, width, pages) with
+ *              pages >= those that any group's range touches; the call's until it has run */
+size_t spec_kv4_reorder_bytes(int32_t groups, int32_t width, int32_t max_pages);
+int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
+                     const int32_t* begin, const int32_t* end, const int32_t* parents, void* workspace,
+                     size_t ws_bytes, void* stream);
+
 /* ---- Drafting-strategy selection (Section 5) ----------------------------
  *
  * Verification-cost predictor (Section 5.2, "the execution time"): a
@@ -507,7 +626,10 @@ enum {
   SPEC_K_TRANSFER = 7,   /* spec_kv_pack / spec_kv_unpack */
   SPEC_K_ACCEPT = 8,     /* tree acceptance: greedy, greedy with EOS, or sampled */
   SPEC_K_KV4_APPEND = 9, /* spec_kv4_append (SPEC_K_ATTENTION: spec_kv4_attend too) */
-  SPEC_K_COUNT = 10
+  SPEC_K_W4 = 10,        /* spec_w4_linear / spec_w4_gate_up */
+  SPEC_K_BEAM = 11,      /* spec_beam_select */
+  SPEC_K_REORDER = 12,   /* spec_kv_reorder / spec_kv4_reorder */
+  SPEC_K_COUNT = 13
 };
 int spec_profile_begin(int32_t kernel_class, int32_t max_launches);
 int spec_profile_end(float* total_ms, int32_t* launches);

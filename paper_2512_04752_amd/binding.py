@@ -24,6 +24,7 @@ KERNEL_CLASS = {"gemm_qkv": 0, "attention": 1, "gemm_o": 2, "gemm_gate_up": 3, "
                 "lm_head": 5, "commit": 6, "accept": 8}   # the kernel classes of one verify step
 TRANSFER_CLASS = 7                                    # spec_kv_pack / spec_kv_unpack
 KV4_APPEND_CLASS = 9                                  # spec_kv4_append
+OPERATOR_CLASS = {"transfer": TRANSFER_CLASS, "kv4_append": KV4_APPEND_CLASS, "w4": 10, "beam": 11, "reorder": 12}
 
 # Every symbol the public header declares.
 EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout",
@@ -35,9 +36,14 @@ EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_lay
            "spec_kv4_bytes", "spec_kv4_alloc", "spec_kv4_free", "spec_kv4_map",
            "spec_kv4_step_bytes", "spec_kv4_step_begin", "spec_kv4_step_free", "spec_kv4_append",
            "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit",
-           "spec_workspace_bytes_kv4", "spec_verify_kv4")
+           "spec_workspace_bytes_kv4", "spec_verify_kv4", "spec_w4_bytes", "spec_w4_pack",
+           "spec_w4_unpack", "spec_w4_workspace_bytes", "spec_w4_linear", "spec_w4_gate_up",
+           "spec_beam_workspace_bytes", "spec_beam_select", "spec_kv_reorder",
+           "spec_kv4_reorder_bytes", "spec_kv4_reorder")
 SPEC_KV4_PAGE = 64                # positions per page of the 4-bit pool
 SPEC_NOALLOC_SCRATCH_BYTES = 320 << 20
+SPEC_MAX_BEAMS = 64               # beams of a group, and continuations of a choice
+SPEC_W4_BF16, SPEC_W4_F32, SPEC_W4_ADD = 0, 1, 2      # outputs of spec_w4_linear
 
 
 class SpecError(RuntimeError):
@@ -68,6 +74,10 @@ class spec_cost_coeffs(ctypes.Structure):
 class spec_sampling(ctypes.Structure):
     _fields_ = [("temperature", c_float), ("eos_token", c_int32), ("draft_probs", c_void_p),
                 ("uniforms", c_void_p)]
+
+
+class spec_w4(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("rows", c_int32), ("cols", c_int32)]
 
 
 class spec_debug(ctypes.Structure):
@@ -149,7 +159,27 @@ def lib():
                                            c_int32]
     L.spec_workspace_bytes_kv4.restype = c_size_t
     L.spec_verify_kv4.argtypes = L.spec_verify_sampled.argtypes
-    for name in ("spec_verify_kv4", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
+    w4 = POINTER(spec_w4)
+    L.spec_w4_bytes.argtypes = [c_int32, c_int32]
+    L.spec_w4_workspace_bytes.argtypes = [c_int32, c_int32, c_int32]
+    L.spec_w4_pack.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_size_t, c_void_p]
+    L.spec_w4_unpack.argtypes = [w4, c_void_p, c_int64, c_void_p]
+    L.spec_w4_linear.argtypes = [w4, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int32, c_void_p,
+                                 c_size_t, c_void_p]
+    L.spec_w4_gate_up.argtypes = [w4, w4, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p,
+                                  c_size_t, c_void_p]
+    L.spec_beam_workspace_bytes.argtypes = [c_int32] * 4
+    L.spec_beam_select.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                                   c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                   c_void_p]
+    L.spec_kv_reorder.argtypes = [c_void_p, c_int32, c_int32, i32p, i32p, i32p, c_void_p, c_void_p]
+    L.spec_kv4_reorder_bytes.argtypes = [c_int32] * 3
+    L.spec_kv4_reorder.argtypes = [c_void_p, c_int32, c_int32, i32p, i32p, i32p, c_void_p, c_void_p, c_size_t,
+                                   c_void_p]
+    for name in ("spec_w4_bytes", "spec_w4_workspace_bytes", "spec_beam_workspace_bytes", "spec_kv4_reorder_bytes"):
+        getattr(L, name).restype = c_size_t
+    for name in ("spec_w4_pack", "spec_w4_unpack", "spec_w4_linear", "spec_w4_gate_up", "spec_beam_select",
+                 "spec_kv_reorder", "spec_kv4_reorder", "spec_verify_kv4", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
                  "spec_kv_commit", "spec_profile_begin", "spec_profile_end", "spec_kv_pack",
                  "spec_kv_unpack", "spec_cost_model_create", "spec_cost_model_free",
                  "spec_cost_model_stats", "spec_select_draft_count", "spec_verify_sampled",
@@ -677,6 +707,237 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
                                      _ptr(accepted_nodes), _ptr(new_seq_lens), _stream(stream)))
 
 
+# ---- products with weights in 4 bits ----
+
+def spec_w4_bytes(rows, cols) -> int:
+    return int(lib().spec_w4_bytes(rows, cols))
+
+
+def spec_w4_workspace_bytes(rows, cols, max_n) -> int:
+    return int(lib().spec_w4_workspace_bytes(rows, cols, max_n))
+
+
+def _device_rows(t, dtype, rows, cols, what, index=None):
+    """Row stride of a device tensor [rows, cols] whose rows are contiguous."""
+    if t.dtype is not dtype or not t.is_cuda or t.dim() != 2 or t.shape[1] != cols \
+            or (rows is not None and t.shape[0] != rows) or (t.stride(1) != 1 and cols > 1) \
+            or (index is not None and t.get_device() != index):
+        kind = str(dtype).split(".")[-1]
+        where = "device" if index is None else f"cuda:{index}"
+        raise ValueError(f"{what} must be a {kind} [{'n' if rows is None else rows}, {cols}] tensor on {where} with "
+                         "contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(cols, (cols + 7) // 8 * 8)
+
+
+def _device_stream(index, stream):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    if stream.device.index != index:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on device {index}")
+    return stream.cuda_stream
+
+
+def _device_workspace(workspace, index):
+    """(pointer, bytes) of a workspace tensor."""
+    if workspace.dtype is not torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the tensors' device")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _made_workspace(nbytes, index, stream):
+    """A workspace that lives until `stream` has passed what is launched on it next."""
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
+
+
+def spec_w4_pack(w, data, stream=None):
+    """Quantise w (bf16 [rows, cols], rows may be strided) into data (uint8, spec_w4_bytes)."""
+    rows, cols = w.shape if w.dim() == 2 else (0, 0)
+    stride = _device_rows(w, torch.bfloat16, rows, cols, "w")
+    index = w.get_device()
+    p, n = _device_workspace(data, index)
+    with _on(index):
+        _check(lib().spec_w4_pack(w.data_ptr(), stride, rows, cols, p, n, _device_stream(index, stream)))
+
+
+def spec_w4_unpack(data, w, stream=None):
+    """Write what data (of spec_w4_pack) stands for into w (bf16 [rows, cols])."""
+    rows, cols = w.shape if w.dim() == 2 else (0, 0)
+    stride = _device_rows(w, torch.bfloat16, rows, cols, "w")
+    index = w.get_device()
+    p, n = _device_workspace(data, index)
+    if n < spec_w4_bytes(rows, cols):
+        raise ValueError(f"data holds {n} bytes, a matrix of {rows} x {cols} {spec_w4_bytes(rows, cols)}")
+    m = spec_w4(p, rows, cols)
+    with _on(index):
+        _check(lib().spec_w4_unpack(m, w.data_ptr(), stride, _device_stream(index, stream)))
+
+
+class W4Matrix:
+    """A weight matrix [rows, cols] in 4 bits, quantised from a bf16 device tensor."""
+
+    def __init__(self, w, stream=None):
+        if w.dim() != 2 or not w.is_cuda:
+            raise ValueError("a weight matrix is a bfloat16 [rows, cols] device tensor")
+        self.rows, self.cols = w.shape
+        self.index = w.get_device()
+        nbytes = spec_w4_bytes(self.rows, self.cols)
+        if nbytes == 0:
+            raise SpecError(-6, f"a matrix of {self.rows} x {self.cols}: columns must be a multiple of 32")
+        self.data = _made_workspace(nbytes, self.index, stream)
+        spec_w4_pack(w, self.data, stream)
+        self.struct = spec_w4(self.data.data_ptr(), self.rows, self.cols)
+
+    def unpack(self, out=None, stream=None):
+        """What the matrix stands for, as bf16."""
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16, device=self.data.device)
+        spec_w4_unpack(self.data, out, stream)
+        return out
+
+
+def _w4_workspace(m, n, workspace, stream):
+    if workspace is not None:
+        return _device_workspace(workspace, m.index)
+    nbytes = lib().spec_w4_workspace_bytes(m.rows, m.cols, n)
+    if nbytes == 0:
+        return None, 0
+    workspace = _made_workspace(nbytes, m.index, stream)
+    return workspace.data_ptr(), nbytes
+
+
+def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
+    """out = x W^T: x bf16 [n, cols] (rows may be strided), out bf16 or float32 [n, rows]; add: float32
+    out += x W^T.  workspace: a uint8 tensor of spec_w4_workspace_bytes (allocated when None)."""
+    if torch.cuda.current_device() != m.index:
+        with torch.cuda.device(m.index):
+            return spec_w4_linear(m, x, out, add, workspace, stream)
+    xs = _device_rows(x, torch.bfloat16, None, m.cols, "x", m.index)
+    n = x.shape[0]
+    kind = SPEC_W4_BF16 if out.dtype is torch.bfloat16 and not add else SPEC_W4_ADD if add else SPEC_W4_F32
+    os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", m.index)
+    if n == 0:
+        return
+    p, nbytes = _w4_workspace(m, n, workspace, stream)
+    rc = lib().spec_w4_linear(m.struct, x.data_ptr(), xs, n, out.data_ptr(), os, kind, p, nbytes,
+                              _device_stream(m.index, stream))
+    if rc:
+        _check(rc)
+
+
+def spec_w4_gate_up(gate: W4Matrix, up: W4Matrix, x, out, workspace=None, stream=None):
+    """out = silu(x Wg^T) * (x Wu^T), bf16 [n, rows]; the rest as in spec_w4_linear."""
+    if torch.cuda.current_device() != gate.index:
+        with torch.cuda.device(gate.index):
+            return spec_w4_gate_up(gate, up, x, out, workspace, stream)
+    if up.index != gate.index:
+        raise ValueError("gate and up are on different devices")
+    xs = _device_rows(x, torch.bfloat16, None, gate.cols, "x", gate.index)
+    n = x.shape[0]
+    os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", gate.index)
+    if n == 0:
+        return
+    p, nbytes = _w4_workspace(gate, n, workspace, stream)
+    rc = lib().spec_w4_gate_up(gate.struct, up.struct, x.data_ptr(), xs, n, out.data_ptr(), os, p, nbytes,
+                               _device_stream(gate.index, stream))
+    if rc:
+        _check(rc)
+
+
+# ---- the choice of beams, and the cache rows that follow ----
+
+def spec_beam_workspace_bytes(groups, width, vocab, k) -> int:
+    return int(lib().spec_beam_workspace_bytes(groups, width, vocab, k))
+
+
+def _beam_tensor(t, dtype, shape, index, what):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+        kind = str(dtype).split(".")[-1]
+        raise ValueError(f"{what} must be a contiguous {kind} tensor of {tuple(shape)} on the logits' device")
+    return t.data_ptr()
+
+
+def spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens=None, eos_token=-1, workspace=None,
+                     stream=None):
+    """The k best continuations of every group's beams.  logits float32 or bfloat16
+    [groups, width, vocab] (rows may be strided, evenly); scores float32 and last_tokens int32
+    [groups, width]; parents, tokens int32 and new_scores float32 [groups, k] are written."""
+    if logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda or logits.dim() != 3 \
+            or parents.dim() != 2:
+        raise ValueError("logits must be a float32 or bfloat16 [groups, width, vocab] device tensor, parents [groups, k]")
+    groups, width, vocab = logits.shape
+    index = logits.get_device()
+    if torch.cuda.current_device() != index:
+        with torch.cuda.device(index):
+            return spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens, eos_token, workspace,
+                                    stream)
+    by_group, by_row, by_token = logits.stride()
+    row = by_row if width > 1 else by_group if groups > 1 else vocab
+    if (by_token != 1 and vocab > 1) or (width > 1 and groups > 1 and by_group != width * by_row):
+        raise ValueError("logits must have contiguous rows at one stride")
+    k = parents.shape[1]
+    beams, kept = torch.Size((groups, width)), torch.Size((groups, k))
+    i32, f32 = torch.int32, torch.float32
+    pointers = (_beam_tensor(scores, f32, beams, index, "scores"),
+                None if last_tokens is None else _beam_tensor(last_tokens, i32, beams, index, "last_tokens"),
+                int(eos_token), k, _beam_tensor(parents, i32, kept, index, "parents"),
+                _beam_tensor(tokens, i32, kept, index, "tokens"),
+                _beam_tensor(new_scores, f32, kept, index, "new_scores"))
+    if workspace is None:
+        workspace = _made_workspace(max(256, lib().spec_beam_workspace_bytes(groups, width, vocab, k)), index, stream)
+    p, nbytes = _device_workspace(workspace, index)
+    rc = lib().spec_beam_select(logits.data_ptr(), row, logits.dtype is torch.bfloat16, groups, width, vocab, *pointers,
+                                p, nbytes, _device_stream(index, stream))
+    if rc:
+        _check(rc)
+
+
+def _reorder_arrays(pool_index, sample_ids, begin, end, parents):
+    ids = np.ascontiguousarray(np.asarray(sample_ids, dtype=np.int32))
+    if ids.ndim != 2:
+        raise ValueError("sample_ids must be [groups, width]")
+    (b, p_b), (e, p_e) = _i32(begin), _i32(end)
+    if b.shape != ids.shape[:1] or e.shape != b.shape:
+        raise ValueError("begin and end must have one entry per group")
+    if parents.dtype is not torch.int32 or parents.shape != torch.Size(ids.shape) or not parents.is_contiguous() \
+            or parents.get_device() != pool_index:
+        raise ValueError(f"parents must be a contiguous int32 tensor of {ids.shape} on the pool's device")
+    return ids, p_b, p_e, (b, e)
+
+
+def spec_kv_reorder(pool: KVPool, sample_ids, begin, end, parents, stream=None):
+    """Beam j of group g (sample sample_ids[g][j]) takes what beam parents[g][j] holds at positions
+    [begin[g], end[g])."""
+    index = pool.buf.get_device()
+    ids, p_b, p_e, kept = _reorder_arrays(index, sample_ids, begin, end, parents)
+    if pool.handle is None:
+        raise ValueError("the pool is closed")
+    with _on(index):
+        _check(lib().spec_kv_reorder(pool.handle, *ids.shape, _pointer(ids, c_int32), p_b, p_e, parents.data_ptr(),
+                                     _device_stream(index, stream)))
+
+
+def spec_kv4_reorder_bytes(groups, width, max_pages) -> int:
+    return int(lib().spec_kv4_reorder_bytes(groups, width, max_pages))
+
+
+def spec_kv4_reorder(pool: KV4Pool, sample_ids, begin, end, parents, workspace=None, stream=None):
+    """spec_kv_reorder for a 4-bit pool; workspace: a uint8 tensor of spec_kv4_reorder_bytes
+    (allocated when None)."""
+    ids, p_b, p_e, (b, e) = _reorder_arrays(pool.index, sample_ids, begin, end, parents)
+    if pool.handle is None:
+        raise ValueError("the pool is closed")
+    if workspace is None:
+        pages = int(np.max((e.astype(np.int64) + SPEC_KV4_PAGE - 1) // SPEC_KV4_PAGE - b // SPEC_KV4_PAGE, initial=1))
+        nbytes = lib().spec_kv4_reorder_bytes(*ids.shape, max(1, min(pages, pool.n_pages)))
+        workspace = _made_workspace(max(256, nbytes), pool.index, stream)
+    p, nbytes = _device_workspace(workspace, pool.index)
+    with _on(pool.index):
+        _check(lib().spec_kv4_reorder(pool.handle, *ids.shape, _pointer(ids, c_int32), p_b, p_e, parents.data_ptr(), p,
+                                      nbytes, _device_stream(pool.index, stream)))
+
+
 class CostModel:
     """The library's verification-cost predictor (spec_cost_model_*)."""
 
@@ -731,12 +992,10 @@ def spec_select_draft_count(model: CostModel, seq_lens, tree_offsets, parents, w
 
 
 def spec_profile_begin(kernel_class, max_launches):
-    if kernel_class == "transfer":
-        k = TRANSFER_CLASS
-    elif kernel_class == "kv4_append":
-        k = KV4_APPEND_CLASS
+    if isinstance(kernel_class, str):
+        k = OPERATOR_CLASS[kernel_class] if kernel_class in OPERATOR_CLASS else KERNEL_CLASS[kernel_class]
     else:
-        k = KERNEL_CLASS[kernel_class] if isinstance(kernel_class, str) else int(kernel_class)
+        k = int(kernel_class)
     _check(lib().spec_profile_begin(k, max_launches))
 
 

@@ -15,7 +15,8 @@ OUT = os.path.join(PKG, "libspecverify.so")
 BUILD = os.path.join(PKG, "_build")
 SOURCES = ["api.cpp", "gemm.hip", "attention.hip", "elementwise.hip", "migrate.hip",
            "strategy.cpp", "sampling.hip", "noalloc.hip", "kv4.cpp", "kv4_cache.hip",
-           "kv4_attention.hip"]
+           "kv4_attention.hip", "w4.cpp", "w4_pack.hip", "w4_gemm.hip", "beam.cpp", "beam_search.hip",
+           "reorder.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-x", "hip", "-std=c++17", "-O3", "--offload-arch=gfx950", "-fPIC",

@@ -13,6 +13,7 @@
 
 #include "common.h"
 #include "kv4_host.h"
+#include "reorder.h"
 #include "specverify.h"
 
 using namespace spec;
@@ -179,6 +180,20 @@ int check_samples(const spec_kv* kv, int32_t batch, const int32_t* ids) {
 }  // namespace
 
 namespace spec {
+
+int check_reorder(int n, int32_t groups, int32_t width, const int32_t* ids, const int32_t* begin,
+                  const int32_t* end, const int32_t* parents) {
+  if (!ids || !begin || !end || !parents) return fail(SPEC_ERR_INVALID, "null argument");
+  if (width < 1 || width > kMaxReorder) return fail(SPEC_ERR_INVALID, "width %d outside 1 .. %d", width, kMaxReorder);
+  if (groups < 1 || (int64_t)groups * width > n)
+    return fail(SPEC_ERR_INVALID, "%d groups of %d beams over %d samples", groups, width, n);
+  if (groups > 65535) return fail(SPEC_ERR_UNSUPPORTED, "%d groups, at most 65535", groups);
+  if ((uintptr_t)parents % 4) return fail(SPEC_ERR_INVALID, "parents not 4-byte aligned");
+  for (int g = 0; g < groups; ++g)
+    if (begin[g] < 0 || end[g] < begin[g])
+      return fail(SPEC_ERR_INVALID, "group %d: positions [%d, %d)", g, begin[g], end[g]);
+  return check_sample_ids(n, groups * width, ids);
+}
 
 int check_sample_ids(int n, int32_t batch, const int32_t* ids) {
   std::vector<char> seen(n, 0);
@@ -772,6 +787,38 @@ SPEC_API int spec_kv_commit(spec_kv* kv, int32_t batch, const int32_t* sample_id
           }),
           "compact");
   return SPEC_OK;
+}
+
+SPEC_API int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
+                             const int32_t* begin, const int32_t* end, const int32_t* parents, void* stream) {
+  return guarded([&]() -> int {
+    if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
+    if (int rc = check_reorder(kv->n, groups, width, sample_ids, begin, end, parents)) return rc;
+    std::vector<ReorderBeam> info((size_t)groups * width);
+    int most = 0;
+    for (int g = 0; g < groups; ++g) {
+      most = std::max(most, end[g] - begin[g]);
+      for (int j = 0; j < width; ++j) {
+        const int id = sample_ids[g * width + j];
+        if (end[g] > kv->cap[id])
+          return fail(SPEC_ERR_CAPACITY, "group %d: positions up to %d exceed sample %d's capacity %d", g, end[g], id,
+                      kv->cap[id]);
+        info[g * width + j] = ReorderBeam{kv->base[id], kv->cap[id], begin[g], end[g], {}};
+      }
+    }
+    if (int rc = refuse_capture(stream)) return rc;
+    if (most == 0 || width == 1) return SPEC_OK;
+    hipStream_t s = (hipStream_t)stream;
+    void* ctl = (char*)kv->pool + kv->ctl_off;
+    if (int rc = kv->ring.upload(info.data(), info.size() * sizeof(ReorderBeam), ctl, s)) return rc;
+    const spec_model_config& c = kv->cfg;
+    HIP_TRY(timed(SPEC_K_REORDER, s, [&] {
+              return launch_reorder((const ReorderBeam*)ctl, groups, width, most, kv->pool, c.n_layers, c.n_kv_heads,
+                                    c.head_dim, parents, s);
+            }),
+            "reorder");
+    return SPEC_OK;
+  });
 }
 
 namespace {

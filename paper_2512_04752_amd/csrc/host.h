@@ -34,6 +34,9 @@ bool config_ok(const spec_model_config* c, std::string* why);
 bool same_config(const spec_model_config* a, const spec_model_config* b);
 // Sample ids of a call: distinct and in [0, n).
 int check_sample_ids(int n, int32_t batch, const int32_t* ids);
+// What both pools' reorder calls check alike; n: the pool's samples.
+int check_reorder(int n, int32_t groups, int32_t width, const int32_t* ids, const int32_t* begin,
+                  const int32_t* end, const int32_t* parents);
 
 // Order attention items longest-first per XCD.  A kernel hands XCD x the items
 // [x*per, (x+1)*per) in order.  Deal the groups of items that share a key range

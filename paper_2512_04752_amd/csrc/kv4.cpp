@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "kv4_host.h"
+#include "reorder.h"
 
 using namespace spec;
 
@@ -549,6 +550,64 @@ SPEC_API int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_
                                         c.n_kv_heads, c.head_dim, accepted_len, accepted_nodes, new_seq_lens, s);
             }),
             "kv4 compact");
+    return SPEC_OK;
+  });
+}
+
+namespace {
+
+size_t reorder_bytes(int64_t groups, int64_t width, int64_t pages) {
+  return align_up(groups * sizeof(ReorderGroup)) + align_up(groups * width * pages * 4);
+}
+
+}  // namespace
+
+SPEC_API size_t spec_kv4_reorder_bytes(int32_t groups, int32_t width, int32_t max_pages) {
+  if (groups < 1 || width < 1 || width > kMaxReorder || max_pages < 1) return 0;
+  return reorder_bytes(groups, width, max_pages);
+}
+
+SPEC_API int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
+                              const int32_t* begin, const int32_t* end, const int32_t* parents, void* workspace,
+                              size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    if (!kv || !workspace) return fail(SPEC_ERR_INVALID, "null argument");
+    if (int rc = check_reorder(kv->n, groups, width, sample_ids, begin, end, parents)) return rc;
+    std::vector<ReorderGroup> info(groups);
+    std::vector<int32_t> table;
+    int64_t most = 0;
+    for (int g = 0; g < groups; ++g) {
+      const int64_t p0 = begin[g] / kKv4Page, p1 = ((int64_t)end[g] + kKv4Page - 1) / kKv4Page;
+      const int64_t pages = begin[g] < end[g] ? p1 - p0 : 0;
+      most = std::max(most, pages);
+      info[g] = ReorderGroup{begin[g], end[g], (int32_t)pages, (int32_t)table.size()};
+      for (int j = 0; j < width; ++j) {
+        const int id = sample_ids[g * width + j];
+        if (end[g] > mapped(kv, id))
+          return fail(SPEC_ERR_CAPACITY, "group %d: positions up to %d exceed the %lld of sample %d's pages", g, end[g],
+                      (long long)mapped(kv, id), id);
+        if (pages == 0) continue;
+        if (int rc = check_unshared(kv, id, begin[g], end[g])) return rc;
+        table.insert(table.end(), kv->pages[id].begin() + p0, kv->pages[id].begin() + p1);
+      }
+    }
+    if (most > 65535) return fail(SPEC_ERR_UNSUPPORTED, "a range of %lld pages, at most 65535", (long long)most);
+    if ((uintptr_t)workspace % kAlign) return fail(SPEC_ERR_INVALID, "workspace not 256-byte aligned");
+    const size_t head = align_up(groups * sizeof(ReorderGroup)), need = head + table.size() * 4;
+    if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
+    if (int rc = refuse_capture(stream)) return rc;
+    if (most == 0 || width == 1) return SPEC_OK;
+    std::vector<char> blob(need, 0);
+    memcpy(blob.data(), info.data(), groups * sizeof(ReorderGroup));
+    memcpy(blob.data() + head, table.data(), table.size() * 4);
+    hipStream_t s = (hipStream_t)stream;
+    if (int rc = kv->ring.upload(blob.data(), need, workspace, s)) return rc;
+    const spec_model_config& c = kv->cfg;
+    HIP_TRY(timed(SPEC_K_REORDER, s, [&] {
+              return launch_kv4_reorder((const ReorderGroup*)workspace, (const int32_t*)((char*)workspace + head), groups,
+                                        width, (int)most, kv->pool, page_bytes_of(&c), c.head_dim, parents, s);
+            }),
+            "kv4 reorder");
     return SPEC_OK;
   });
 }

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <math.h>
 
+#include "e2m1.h"
 #include "kv4.h"
 
 namespace spec {
@@ -81,44 +82,11 @@ __device__ __forceinline__ double2 cos_sin(double x) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// e + 127 for a group whose largest magnitude has the fp32 bits `top`; 255 when
-// the group holds an infinity or NaN.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-  if (top >= 0x7f800000u) return 255u;
-  // top = 1.m 2^(E - 127) <= 6 2^e = 1.5 2^(e + 2)
-  return (uint32_t)min(max(((int)top + 0x3fffff - (2 << 23)) >> 23, 1), 252);
-}
-
-// N (4 or 8) E2M1 codes of f / 2^(byte - 127), dim n in bits 4n .. 4n + 3; 0 for a
-// group without a scale, and 0 rather than -0.
-template <int N>
-__device__ __forceinline__ uint32_t pack_codes(const float* f, uint32_t byte) {
-  const float s = __uint_as_float(byte << 23);
-  uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], s, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], s, 1);
-  if constexpr (N == 8) {
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], s, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], s, 3);
-  }
-  const uint32_t some = ((w & 0x77777777u) + 0x77777777u) & 0x88888888u;   // magnitude bits set
-  w &= some | 0x77777777u;
-  return byte == 255u ? 0u : w;
-}
-
 // The number of a code: its exponent and mantissa bits read as fp32's are 2^-126
 // times the E2M1 number, subnormals included.
 __device__ __forceinline__ float code_value(uint32_t code, float s) {
   const float m = __uint_as_float((code & 7u) << 22) * 0x1p126f;
   return (code & 8u ? -m : m) * s;
-}
-
-// Eight numbers of a word of codes, s a power of two, as bf16.
-__device__ __forceinline__ i32x4 numbers(uint32_t w, float s) {
-  return i32x4{__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)),
-               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1)),
-               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)),
-               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
 }
 
 // A row's lanes: HD / 8 lanes, so a wave holds 64 / (HD / 8) rows at a time and takes an

@@ -1,0 +1,33 @@
+// The cache rows that follow the beams: descriptors and launcher prototypes.
+#pragma once
+
+#include "common.h"
+
+namespace spec {
+
+constexpr int kMaxReorder = SPEC_MAX_BEAMS;      // beams of a group
+
+// One beam over the bf16 pool.
+struct ReorderBeam {
+  int64_t kv_base;      // element offset of the sample's block
+  int32_t cap;          // positions per (layer, K/V, kv head)
+  int32_t begin, end;   // its group's range
+  int32_t pad[3];
+};
+static_assert(sizeof(ReorderBeam) == 32, "ReorderBeam layout");
+
+// One group over the 4-bit pool.
+struct ReorderGroup {
+  int32_t begin, end;
+  int32_t pages;        // that the range touches, of every beam
+  int32_t table;        // its first entry in the table: [width][pages] page ids
+};
+static_assert(sizeof(ReorderGroup) == 16, "ReorderGroup layout");
+
+// most: tokens of the longest range, or pages.
+hipError_t launch_reorder(const ReorderBeam* beams, int groups, int width, int most, bf16* pool, int n_layers,
+                          int n_kv_heads, int head_dim, const int32_t* parents, hipStream_t s);
+hipError_t launch_kv4_reorder(const ReorderGroup* info, const int32_t* table, int groups, int width, int most,
+                              char* pool, int64_t page_bytes, int head_dim, const int32_t* parents, hipStream_t s);
+
+}  // namespace spec
