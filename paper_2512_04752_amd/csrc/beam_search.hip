@@ -20,30 +20,46 @@ namespace {
 
 constexpr int64_t kMaxGrid = 0xffffffffll / 1024;
 
-// 2^t for -1100 <= t <= 1000, relative error below 1e-14: 2^n times the series of
-// exp(f ln 2), |f| <= 1/2, cut where the next term, (ln 2 / 2)^12 / 12!, is 6e-15.
-__device__ __forceinline__ double exp2_double(double t) {
-  constexpr double L = 0.69314718055994530942;
-  constexpr double C[12] = {1.0,
-                            L,
-                            L * L / 2,
-                            L * L * L / 6,
-                            L * L * L * L / 24,
-                            L * L * L * L * L / 120,
-                            L * L * L * L * L * L / 720,
-                            L * L * L * L * L * L * L / 5040,
-                            L * L * L * L * L * L * L * L / 40320,
-                            L * L * L * L * L * L * L * L * L / 362880,
-                            L * L * L * L * L * L * L * L * L * L / 3628800,
-                            L * L * L * L * L * L * L * L * L * L * L / 39916800};
-  const double n = rint(t), f = t - n;
-  double y = C[11];
+// e^d for -1000 <= d <= 690, relative error below 3e-10: 2^n times the series of exp(f ln 2),
+// d log2 e = n + f, |f| <= 1/2, cut where the next term, (ln 2 / 2)^9 / 9!, is 2e-10 (and of
+// a sum of many far less).  n comes out of an addition that leaves it in the low bits, and
+// goes into the exponent by an integer one: all of it at the rate of fp64 additions.  The
+// constants are held in scalar registers (of constants that the compiler knows, it copies
+// each into the result first and then accumulates, twice the instructions).
+struct Exp {
+  double log2e, big, c[9];
+  __device__ __forceinline__ Exp() {
+    constexpr double L = 0.69314718055994530942;
+    log2e = 1.44269504088896340736;
+    // 1.5 * 2^52, and 2^12 that the shift drops: without it the low word is 0, and then this
+    // compiler (ROCm 7.2) loads it by s_mov_b64 with a 64-bit literal, which there is none of.
+    big = 6755399441055744.0 + 4096.0;
+    double t = L;
 #pragma unroll
-  for (int i = 10; i >= 0; --i) y = fma(y, f, C[i]);
-  return ldexp(y, (int)n);
-}
+    for (int i = 1; i < 9; ++i) {
+      c[i] = t;                              // ln 2^i / i!
+      t *= L / (i + 1);
+    }
+    asm volatile("" : "+s"(log2e), "+s"(big), "+v"(c[8]));         // an instruction reads one scalar pair
+#pragma unroll
+    for (int i = 1; i < 8; ++i) asm volatile("" : "+s"(c[i]));
+  }
+  __device__ __forceinline__ double operator()(double d) const {
+    const double m = fma(d, log2e, big), f = fma(d, log2e, big - m);
+    double y = fma(f, c[8], c[7]);
+#pragma unroll
+    for (int i = 6; i >= 1; --i) y = fma(y, f, c[i]);
+    y = fma(y, f, 1.0);
+    i32x2 b = __builtin_bit_cast(i32x2, y);
+    b[1] += __builtin_bit_cast(i32x2, m)[0] << 20;
+    return __builtin_bit_cast(double, b);
+  }
+  // x e^d, d <= 690; a NaN for a NaN; 0 where that is below e^-690 of x.
+  __device__ __forceinline__ double scaled(double x, double d) const {
+    return d != d ? d : d < -690.0 ? 0.0 : x * (*this)(d);
+  }
+};
 
-constexpr double kLog2e = 1.44269504088896340736;
 constexpr float kLowest = -3.4028234663852886e38f;
 
 // A wave's running list of the k best, one entry per lane, best first; entries past the
@@ -62,14 +78,78 @@ __device__ __forceinline__ float lane_value(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
 
-// Put (z, y) into the list, behind entries that are as good: a caller that comes to tokens in
-// ascending order so keeps the lower one of equal logits first.
+// The largest float below x; -infinity and NaN stay.
+__device__ __forceinline__ float float_below(float x) {
+  const int b = __float_as_int(x);
+  return !(x > -INFINITY) ? x : b == 0 ? -1e-45f : __int_as_float(b > 0 ? b - 1 : b + 1);
+}
+
+// A bound that at least k of the wave's N x 64 numbers are not below, within 2^-11 of the
+// k-th largest (k <= 64 N): the leading 20 bits of its place in the order of floats, found
+// from the top by counting.  -infinity where it is that.
+template <int N>
+__device__ __forceinline__ float kth_bound(const float (&x)[N], int k) {
+  uint32_t u[N], t = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t b = __float_as_uint(x[i]);
+    u[i] = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+  }
+#pragma unroll
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t with = t | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(u[i] >= with));
+    if (n >= k) t = with;
+  }
+  return t <= 0x007fffffu ? -INFINITY : __uint_as_float(t & 0x80000000u ? t ^ 0x80000000u : ~t);
+}
+
+// Put (z, y) into the list: behind larger logits, and behind equal ones of lower tokens.
 __device__ __forceinline__ void insert(List& l, float z, int y, int lane) {
-  const int pos = __popcll(__ballot(l.z >= z));
+  const int pos = __popcll(__ballot(l.z > z) | (__ballot(l.z == z) & __ballot(l.y < y)));
   const float zb = __int_as_float(from_below(__float_as_int(l.z)));
   const int yb = from_below(l.y);
   l.z = lane < pos ? l.z : lane == pos ? z : zb;
   l.y = lane < pos ? l.y : lane == pos ? y : yb;
+}
+
+// LDS written by lanes of a wave is there for its other lanes.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Put n <= 64 more entries into the list, by counting for each what is better: about 13
+// instructions per new entry and 6 per old one, where insert() takes 35 for each.
+constexpr int kFew = 5;
+__device__ __forceinline__ bool before(const List& p, const List& q) {
+  return (p.z > q.z) | ((p.z == q.z) & (p.y < q.y));
+}
+__device__ __forceinline__ void merge(List& l, const List* found, List* merged, int n, int k, int lane) {
+  List x = found[lane];
+  if (lane >= n) x = List{-INFINITY, 0x7fffffff};
+  int rank = 0, old = lane;
+  merged[lane] = l;
+  wave_sync();
+#pragma unroll 4
+  for (int q = 0; q < n; ++q) {
+    const List f = found[q];
+    rank += before(f, x);
+    old += before(f, l);
+  }
+  if (lane_value(l.z, 0) > -INFINITY) {
+#pragma unroll 4
+    for (int q = 0; q < k; ++q) rank += before(merged[q], x);
+  }
+  wave_sync();
+  merged[lane] = List{-INFINITY, -1};
+  wave_sync();
+  if (lane < k && l.z > -INFINITY && old < k) merged[old] = l;
+  if (lane < n && rank < k) merged[rank] = x;
+  wave_sync();
+  l = merged[lane];
 }
 
 // Whether a beam is read at all: its score is finite and it has not ended.
@@ -86,99 +166,165 @@ struct Vectors {
   typedef i32x4 __attribute__((aligned(2))) Loose;
   const T* row;
   int vocab;
-  // Elements v * PER ..; what is past the row reads as -infinity.
-  __device__ __forceinline__ void load(int v, float* z) const {
+  // Elements v * PER ..; what is past the row, or vector v1, reads as -infinity.
+  __device__ __forceinline__ i32x4 load(int v, int v1) const {
+    constexpr int NONE = PER == 4 ? (int)0xff800000 : (int)0xff80ff80;
     const int e0 = v * PER;
-    if (e0 + PER <= vocab) {
-      const i32x4 x = *(const Loose*)(row + e0);
+    i32x4 x{NONE, NONE, NONE, NONE};
+    if (v < v1) {
+      if (e0 + PER <= vocab) {
+        x = *(const Loose*)(row + e0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (PER == 4) {
-          z[i] = __uint_as_float((uint32_t)x[i]);
-        } else {
-          z[2 * i] = __uint_as_float((uint32_t)x[i] << 16);
-          z[2 * i + 1] = __uint_as_float((uint32_t)x[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < PER - 1; ++i)
+          if (e0 + i < vocab) {
+            const T t = row[e0 + i];
+            if constexpr (PER == 4) x[i] = __builtin_bit_cast(int, t);
+            else {
+              const uint32_t b = (uint32_t)__builtin_bit_cast(uint16_t, t), at = 16 * (i & 1);
+              x[i / 2] = (int)(((uint32_t)x[i / 2] & ~(0xffffu << at)) | b << at);
+            }
+          }
       }
-    } else {
+    }
+    return x;
+  }
+  static __device__ __forceinline__ void numbers(const i32x4& x, float* z) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) z[i] = e0 + i < vocab ? (float)row[e0 + i] : -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (PER == 4) {
+        z[i] = __uint_as_float((uint32_t)x[i]);
+      } else {
+        z[2 * i] = __uint_as_float((uint32_t)x[i] << 16);
+        z[2 * i + 1] = __uint_as_float((uint32_t)x[i] & 0xffff0000u);
+      }
     }
   }
 };
 
+// A wave goes through its segment in batches of kVecs vectors per lane, the next batch on
+// its way while one is worked on.  Per number: 18 instructions of fp64 rate for its term,
+// one comparison with the k-th best so far, and the few that pass go into the list one by
+// one (k ln(n / k) of n in random order).  The first batch gives the list a lower bound to
+// start with.
 template <class T>
-__global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
-  constexpr int PER = Vectors<T>::PER;
+__global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
+  constexpr int PER = Vectors<T>::PER, kVecs = 16 / PER;
+  __shared__ List found[4][64], merged[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
   const int row = (int)(id / a.segs), seg = (int)(id % a.segs);
   if (row >= a.groups * a.width || !beam_live(a, row)) return;
-  const T* p = (const T*)a.logits + row * a.row_stride;
-  const Vectors<T> vec{p, a.vocab};
-  const int vectors = (a.vocab + PER - 1) / PER;
-  const int v0 = seg * a.seg, v1 = min(vectors, v0 + a.seg);
-  float top = kLowest;          // the lane's reference: at least a logit of its own less 600
+  const Vectors<T> vec{(const T*)a.logits + row * a.row_stride, a.vocab};
+  const int v0 = seg * a.seg, v1 = min((a.vocab + PER - 1) / PER, v0 + a.seg);
+  float top = kLowest;          // the lane's reference: its largest logit so far, less 600 at most
+  const Exp exp;
   double sum = 0.0;
   List best{-INFINITY, -1};
-  float least = -INFINITY;      // of the k best
-  for (int v = v0; v < v1; v += 64) {
-    float z[PER];
-    if (v + lane < v1) {
-      vec.load(v + lane, z);
-    } else {
+  float least = -INFINITY;      // only what is above, or as good with a token below, can be one of the k best
+  int least_y = -1;
+  bool first = true;
+  constexpr int kStep = 64 * kVecs;
+  const T* at_lane = vec.row + (int64_t)(v0 + lane) * PER;
+  i32x4 next[kVecs];
+  for (int v = v0 - kStep; v < v1; v += kStep) {       // batch v, and loads of the one after it
+    float z[kVecs][PER], m[kVecs];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) z[i] = -INFINITY;
+    for (int j = 0; j < kVecs; ++j) Vectors<T>::numbers(next[j], z[j]);
+    const int after = v + kStep;
+    if (after + kStep <= v1 && (int64_t)(after + kStep) * PER <= a.vocab) {
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) next[j] = *(const typename Vectors<T>::Loose*)(at_lane + j * 64 * PER);
+    } else if (after < v1) {
+      int l = lane;
+      asm volatile("" : "+v"(l));              // its addresses are not kept in registers over the loop
+      for (int j = 0; j < kVecs; ++j) next[j] = vec.load(after + 64 * j + l, v1);
     }
-    float m = z[0];
+    at_lane += kStep * PER;
+    if (v < v0) continue;
 #pragma unroll
-    for (int i = 1; i < PER; ++i) m = __builtin_elementwise_maximum(m, z[i]);   // a NaN when there is one
-    // Terms relative to `top`: doubles hold e^600, and what is e^-690 of `top` counts as that.
-    if (__ballot(!(m <= top + 600.f) || top < -1e37f)) {
-      if (!(m <= top)) {
-        sum = m - top > 690.f ? 0.0 : sum * exp2_double(((double)top - (double)m) * kLog2e);
-        top = m;
-      }
+    for (int j = 0; j < kVecs; ++j) {
+      m[j] = z[j][0];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const double d = (double)z[i] - (double)top;
-        sum += d != d ? d : d < -690.0 ? 0.0 : exp2_double(d * kLog2e);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        sum += exp2_double(((double)fmaxf(z[i], top - 690.f) - (double)top) * kLog2e);
+      for (int i = 1; i < PER; ++i) m[j] = __builtin_elementwise_maximum(m[j], z[j][i]);   // a NaN when there is one
     }
-    uint64_t pass = __ballot(m > least || m != m);
-    while (pass) {
-      const int l = __ffsll((unsigned long long)pass) - 1;
-      pass &= pass - 1;
+    float most = m[0];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const float x = lane_value(z[i], l);
-        if (x > least) {
-          insert(best, x, (v + l) * PER + i, lane);
-          least = lane_value(best.z, a.k - 1);
+    for (int j = 1; j < kVecs; ++j) most = __builtin_elementwise_maximum(most, m[j]);
+    // Terms relative to `top`: doubles hold e^600, and what is below e^-690 of it counts as
+    // that.  A NaN makes the sum one, an infinity `top`.
+    if (__ballot(!(most <= top + 600.f))) {
+      if (!(most <= top)) {
+        sum = exp.scaled(sum, (double)top - (double)most);
+        top = most;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sum += exp(fmax((double)z[j][i] - (double)top, -690.0));
+      __builtin_amdgcn_sched_barrier(0);       // else all terms at once, in more registers than there are
+    }
+    if (first) {
+      first = false;
+      // k of the maxima of halves of the lanes' numbers are not below it.  What equals it has to pass.
+      float half[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) half[i & 1] = fmaxf(half[i & 1], z[j][i]);
+      least = float_below(kth_bound(half, a.k));
+    }
+    if (__ballot(most >= least) == 0) continue;
+    // What can be among the k best, side by side, and into the list.
+    int n = 0;
+    auto flush = [&]() {
+      wave_sync();
+      if (n > kFew) {
+        merge(best, found[wave], merged[wave], n, a.k, lane);
+      } else {
+        for (int q = 0; q < n; ++q) {
+          const List x = found[wave][q];
+          insert(best, x.z, x.y, lane);
         }
       }
+      n = 0;
+      const float kth = lane_value(best.z, a.k - 1);
+      if (kth >= least) {
+        least = kth;
+        least_y = __builtin_amdgcn_readlane(best.y, a.k - 1);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      if (__ballot(m[j] >= least) == 0) continue;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int y = (v + 64 * j + lane) * PER + i;
+        auto passing = [&]() {
+          return __ballot(z[j][i] > least) | (__ballot(z[j][i] == least) & __ballot(y < least_y));
+        };
+        uint64_t pass = passing();
+        if (n + __popcll(pass) > 64) {
+          flush();
+          pass = passing();
+        }
+        if (pass >> lane & 1) found[wave][n + __popcll(pass & ((1ull << lane) - 1))] = List{z[j][i], y};
+        n += __popcll(pass);
+      }
     }
+    flush();
   }
   // over the wave
+  float all = top;
 #pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) {
-    const float t = __shfl_xor(top, x);
-    const double s = __shfl_xor(sum, x);
-    const float m = __builtin_elementwise_maximum(top, t);
-    auto scaled = [&](double q, float from) {
-      const double d = (double)from - (double)m;
-      return d != d ? d : d < -690.0 ? 0.0 : q * exp2_double(d * kLog2e);
-    };
-    sum = scaled(sum, top) + scaled(s, t);
-    top = m;
-  }
+  for (int x = 32; x >= 1; x >>= 1) all = __builtin_elementwise_maximum(all, __shfl_xor(all, x));
+  sum = exp.scaled(sum, (double)top - (double)all);
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
   const int64_t at = (int64_t)row * a.segs + seg;
   if (lane == 0) {
-    a.tops[at] = top;
+    a.tops[at] = all;
     a.sums[at] = sum;
   }
   if (lane < a.k) {
@@ -187,118 +333,206 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   }
 }
 
-// A candidate of the last stage: better is a higher score, then a lower beam, then a lower token.
+// A candidate of the last stage: a higher score is better, then a lower id, which is the
+// beam above the token; score -infinity: none.
 struct Cand {
   double s;
-  int w, y;
+  uint64_t id;
 };
 __device__ __forceinline__ bool better(const Cand& p, const Cand& q) {
-  return p.s > q.s || (p.s == q.s && (p.w < q.w || (p.w == q.w && p.y < q.y)));
+  return (p.s > q.s) | ((p.s == q.s) & (p.id < q.id));
 }
-__device__ __forceinline__ double readlane_double(double x, int lane) {
+__device__ __forceinline__ uint64_t id_of(int w, int y) { return (uint64_t)(uint32_t)w << 32 | (uint32_t)y; }
+template <class X>
+__device__ __forceinline__ X lane_value64(X x, int lane) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ double double_from_below(double x) {
+template <class X>
+__device__ __forceinline__ X from_below64(X x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
   const uint32_t lo = from_below((int)(uint32_t)b), hi = from_below((int)(uint32_t)(b >> 32));
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
 }
 
-constexpr int kPickWaves = 8;
+constexpr int kPick = 512;         // threads
+constexpr int kHeads = kPick / 2;  // candidates that bound the k-th best
+constexpr int kListed = 1024;      // candidates that can be ranked side by side
+static_assert(kHeads == 4 * 64, "four per lane");
+constexpr int kMaxLists = 4096;    // lists of a group: plan_beam()
+static_assert(kPick / 64 * kMaxBeams <= kListed && kMaxBeams <= kHeads, "the waves' lists, and the bound's rank");
 
-__global__ __launch_bounds__(64 * kPickWaves) void beam_pick_kernel(BeamArgs a) {
+// -infinity by way of vector registers: as a scalar one this compiler (ROCm 7.2) makes it
+// s_mov_b64 with a 64-bit literal, which the instruction does not have, and it arrives as 0.
+__device__ __forceinline__ double no_score() {
+  double x = -INFINITY;
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The normalisers, then the k best of the rows' lists.  Bound by latency, a few loads one
+// after the other, so candidates are only looked at where they can be chosen: every thread
+// takes the best of some lists' first entries; the k-th best of these bounds the group's
+// k-th best from below, and only lists that begin at or above it are read.  All that these
+// hold bounds it again (one beam far ahead of the others has k better ones than the second
+// beam's best), and what is not below (about k, unless many are equal) is ranked by counting.  Where that is more
+// than fits, each wave keeps a sorted list instead, and these are ranked.
+__global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
+  constexpr int kWaves = kPick / 64;
   __shared__ double lse[kMaxBeams];              // NaN: the beam offers nothing
-  __shared__ Cand lists[kPickWaves * kMaxBeams];
-  __shared__ int count;
-  __shared__ Cand kth[kPickWaves];
+  __shared__ float score[kMaxBeams];
+  __shared__ Cand listed[kListed];
+  __shared__ __attribute__((aligned(16))) float heads[kHeads];
+  __shared__ uint16_t open[kMaxLists];
+  __shared__ int count, opened;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, k = a.k;
-  if (threadIdx.x == 0) count = 0;
-  // normalisers
-  for (int w = wave; w < a.width; w += kPickWaves) {
-    const int row = g * a.width + w;
-    double v = NAN;
-    if (beam_live(a, row)) {
-      const float* tops = a.tops + (int64_t)row * a.segs;
-      const double* sums = a.sums + (int64_t)row * a.segs;
-      float top = -INFINITY;
-      for (int i = lane; i < a.segs; i += 64) top = __builtin_elementwise_maximum(top, tops[i]);
-#pragma unroll
-      for (int x = 32; x >= 1; x >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, x));
-      double sum = 0.0;
-      for (int i = lane; i < a.segs; i += 64) {
-        const double d = (double)tops[i] - (double)top;
-        sum += d != d ? d : d < -690.0 ? 0.0 : sums[i] * exp2_double(d * kLog2e);
-      }
-#pragma unroll
-      for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-      v = top < INFINITY ? (double)top + log(sum) : NAN;
-    }
-    if (lane == 0) lse[w] = v;
-  }
-  __syncthreads();
-  // each wave's k best
-  // -infinity by way of vector registers: as a scalar one this compiler (ROCm 7.2) makes it
-  // s_mov_b64 with a 64-bit literal, which the instruction does not have, and it arrives as 0.
-  double none = -INFINITY;
-  asm volatile("" : "+v"(none));
-  Cand best{none, 0x7fffffff, 0x7fffffff}, least = best;
-  auto offer = [&](const Cand& c, bool some) {
-    uint64_t pass = __ballot(some && better(c, least));
-    while (pass) {
-      const int l = __ffsll((unsigned long long)pass) - 1;
-      pass &= pass - 1;
-      const Cand n{readlane_double(c.s, l), __builtin_amdgcn_readlane(c.w, l), __builtin_amdgcn_readlane(c.y, l)};
-      if (!better(n, least)) continue;
-      const int pos = __popcll(__ballot(better(best, n)));
-      const Cand b{double_from_below(best.s), from_below(best.w), from_below(best.y)};
-      if (lane >= pos) best = lane == pos ? n : b;
-      least = Cand{readlane_double(best.s, k - 1), __builtin_amdgcn_readlane(best.w, k - 1),
-                   __builtin_amdgcn_readlane(best.y, k - 1)};
-    }
+  const int per_row = a.segs * k, lists = a.width * a.segs, total = a.width * per_row;
+  const int64_t first = (int64_t)g * a.width * per_row;
+  // Candidate e of list l.
+  auto entry = [&](int l, int e) { return first + l * k + e; };
+  auto candidate = [&](int w, float z, int y) {
+    Cand c{no_score(), id_of(w, y)};
+    const double norm = lse[w];
+    if (norm == norm && y >= 0) c.s = (double)score[w] + ((double)z - norm);
+    return c;
   };
-  const int per_row = a.segs * k, total = a.width * per_row;
-  for (int i = wave * 64; i < total; i += 64 * kPickWaves) {
-    const int at = i + lane, w = min(at, total - 1) / per_row, row = g * a.width + w;
-    Cand c{};
-    bool some = false;
-    if (at < total && lse[w] == lse[w]) {
-      const int64_t from = (int64_t)row * per_row + at - w * per_row;
-      const float z = a.cand_z[from];
-      c = Cand{(double)a.scores[row] + ((double)z - lse[w]), w, a.cand_y[from]};
-      some = z > -INFINITY;
+  auto ended = [&](int w) {                      // a beam that has ended, as a candidate
+    Cand c{no_score(), id_of(w, a.eos)};
+    if (a.eos >= 0 && w < a.width) {
+      const float s = a.scores[g * a.width + w];
+      if (fabsf(s) < INFINITY && a.last[g * a.width + w] == a.eos) c.s = s;
     }
-    offer(c, some);
-  }
-  if (a.eos >= 0 && wave == 0) {                 // beams that have ended
-    const int row = g * a.width + min(lane, a.width - 1);
+    return c;
+  };
+  // Threads' own entries, in the order of all lists' first entries, then all second ones ..
+  const int mine = min((int)threadIdx.x, total - 1), l0 = mine % lists, e0 = mine / lists;
+  const float z0 = a.cand_z[entry(l0, e0)];
+  const int y0 = a.cand_y[entry(l0, e0)];
+  if (threadIdx.x == 0) count = opened = 0;
+  // normalisers: as many lanes per row as there are for all rows at once
+  const Exp exp;
+  int lanes = 64;
+  while (lanes > 1 && (lanes / 2 >= a.segs || lanes * a.width > kPick)) lanes /= 2;
+  const int rows_at_once = 64 / lanes, sub = lane & (lanes - 1);
+  for (int w0 = wave * rows_at_once; w0 < a.width; w0 += kWaves * rows_at_once) {
+    const int w = w0 + lane / lanes, row = g * a.width + min(w, a.width - 1);
+    const bool live = beam_live(a, row);
     const float s = a.scores[row];
-    offer(Cand{(double)s, lane, a.eos}, lane < a.width && fabsf(s) < INFINITY && a.last[row] == a.eos);
+    float top = -INFINITY;
+    // of a beam that is not live this is not written, and not used
+#pragma unroll 4
+    for (int i = sub; i < a.segs; i += lanes) top = __builtin_elementwise_maximum(top, a.tops[(int64_t)row * a.segs + i]);
+    for (int x = lanes / 2; x >= 1; x >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, x));
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = sub; i < a.segs; i += lanes)
+      sum += exp.scaled(a.sums[(int64_t)row * a.segs + i], (double)a.tops[(int64_t)row * a.segs + i] - (double)top);
+    for (int x = lanes / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+    if (sub == 0 && w < a.width) {
+      lse[w] = live && top < INFINITY ? (double)top + log(sum) : NAN;
+      score[w] = s;
+    }
   }
-  // The best k-th of any wave bounds the group's from below; what passes is ranked.
-  if (lane == 0) kth[wave] = least;
   __syncthreads();
-  Cand floor = kth[0];
-#pragma unroll
-  for (int i = 1; i < kPickWaves; ++i)
-    if (better(kth[i], floor)) floor = kth[i];
-  if (lane < k && best.s > -INFINITY && !better(floor, best)) lists[atomicAdd(&count, 1)] = best;
+  double head = no_score();
+  if ((int)threadIdx.x < total) head = candidate(l0 / a.segs, z0, y0).s;
+  const double own = head;
+  for (int l = threadIdx.x + kPick; l < lists; l += kPick)
+    head = fmax(head, candidate(l / a.segs, a.cand_z[entry(l, 0)], a.cand_y[entry(l, 0)]).s);
+  // A bound that k of the threads' candidates are not below, from the maxima of pairs.
+  auto kth_of = [&](double x) {
+    float h = (float)x;                          // not above the double
+    if ((double)h > x) h = float_below(h);
+    h = fmaxf(h, __shfl_xor(h, 1));
+    __syncthreads();
+    if ((lane & 1) == 0) heads[threadIdx.x / 2] = h;
+    __syncthreads();
+    const f32x4 o = *(const f32x4*)(heads + 4 * lane);
+    const float all[4] = {o[0], o[1], o[2], o[3]};
+    return (double)kth_bound(all, k);
+  };
+  double least_score = kth_of(head);
+  for (int l = threadIdx.x; l < lists; l += kPick) {
+    const double s = l < kPick && e0 == 0 ? own : candidate(l / a.segs, a.cand_z[entry(l, 0)], a.cand_y[entry(l, 0)]).s;
+    if (s >= least_score && s > -INFINITY) open[atomicAdd(&opened, 1)] = (uint16_t)l;
+  }
+  if (wave == 0 && a.eos >= 0) {
+    const Cand c = ended(lane);
+    if (fabs(c.s) < INFINITY) listed[atomicAdd(&count, 1)] = c;
+  }
   __syncthreads();
-  const int n = count;
-  for (int i = threadIdx.x; i < n; i += 64 * kPickWaves) {
-    const Cand c = lists[i];
+  // The open lists in blocks of `deep` entries of each, as many as there are threads for.
+  const int lists_open = opened, deep = max(1, kPick / max(1, lists_open)), block = lists_open * deep;
+  auto opened_entry = [&](int i, int at) {
+    const int l = open[i % lists_open], e = at + i / lists_open;
+    if (e >= k) return Cand{no_score(), 0};
+    return candidate(l / a.segs, a.cand_z[entry(l, e)], a.cand_y[entry(l, e)]);
+  };
+  if (lists_open * k > 2 * kMaxBeams) {          // a closer bound
+    head = no_score();
+    for (int i = threadIdx.x; i < block; i += kPick) head = fmax(head, opened_entry(i, 0).s);
+    least_score = fmax(least_score, kth_of(head));
+  }
+  for (int at = 0; at < k && lists_open > 0; at += deep) {
+    bool some = false;
+    for (int i = threadIdx.x; i < block; i += kPick) {
+      const Cand c = opened_entry(i, at);
+      if (c.s >= least_score && c.s > -INFINITY) {
+        some = true;
+        const int to = atomicAdd(&count, 1);
+        if (to < kListed) listed[to] = c;
+      }
+    }
+    if (!__syncthreads_or(some)) break;          // the lists are sorted
+  }
+  __syncthreads();
+  int n = count;
+  if (n > kListed) {
+    __syncthreads();
+    if (threadIdx.x == 0) count = 0;
+    Cand best{no_score(), ~0ull}, least = best;
+    auto offer = [&](const Cand& c, bool some) {
+      uint64_t pass = __ballot(some && better(c, least));
+      while (pass) {
+        const int l = __ffsll((unsigned long long)pass) - 1;
+        pass &= pass - 1;
+        const Cand x{lane_value64(c.s, l), lane_value64(c.id, l)};
+        if (!better(x, least)) continue;
+        const int pos = __popcll(__ballot(better(best, x)));
+        const Cand b{from_below64(best.s), from_below64(best.id)};
+        if (lane >= pos) best = lane == pos ? x : b;
+        least = Cand{lane_value64(best.s, k - 1), lane_value64(best.id, k - 1)};
+      }
+    };
+    for (int i = wave * 64; i < total; i += kPick) {
+      const int at = min(i + lane, total - 1);
+      const Cand c = candidate(at / per_row, a.cand_z[first + at], a.cand_y[first + at]);
+      offer(c, i + lane < total && c.s > -INFINITY);
+    }
+    if (a.eos >= 0 && wave == 0) {
+      const Cand c = ended(lane);
+      offer(c, fabs(c.s) < INFINITY);
+    }
+    __syncthreads();
+    if (lane < k && fabs(best.s) < INFINITY) listed[atomicAdd(&count, 1)] = best;
+    __syncthreads();
+    n = count;
+  }
+  for (int i = threadIdx.x; i < n; i += kPick) {
+    const Cand c = listed[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += better(lists[j], c);
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += better(listed[j], c);
     if (rank < k) {
       const int64_t at = (int64_t)g * k + rank;
-      a.parents[at] = c.w;
-      a.tokens[at] = c.y;
+      a.parents[at] = (int32_t)(c.id >> 32);
+      a.tokens[at] = (int32_t)c.id;
       a.new_scores[at] = (float)c.s;
     }
   }
-  for (int i = n + threadIdx.x; i < k; i += 64 * kPickWaves) {
+  for (int i = n + threadIdx.x; i < k; i += kPick) {
     const int64_t at = (int64_t)g * k + i;
     a.parents[at] = a.tokens[at] = -1;
     a.new_scores[at] = -INFINITY;
@@ -341,7 +575,7 @@ hipError_t launch_beam(const BeamArgs& a, hipStream_t s) {
   if (a.is_bf16) beam_scan_kernel<bf16><<<grid, 256, 0, s>>>(a);
   else beam_scan_kernel<float><<<grid, 256, 0, s>>>(a);
   if (const hipError_t e = hipGetLastError()) return e;
-  beam_pick_kernel<<<a.groups, 64 * kPickWaves, 0, s>>>(a);
+  beam_pick_kernel<<<a.groups, kPick, 0, s>>>(a);
   return hipGetLastError();
 }
 
