@@ -303,8 +303,7 @@ int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int3
  *   codes   [T][64 lanes][16 bytes]: lane l has row l % 16, columns 32 (l / 16)
  *           .. + 31 of the tile, column 2n and 2n + 1 in the low and high half of
  *           byte n: what a lane of the matrix cores takes, in one load
- *   scales  [ceil(T / 4)][64 lanes][4] bytes e + 127 (255: none), of column tiles
- *           4 i .. 4 i + 3 */
+ *   scales  [T][64 lanes] bytes e + 127 (255: none), padded to 256 */
 typedef struct {
   const void* data;       /* device, spec_w4_bytes(rows, cols), 256-byte aligned */
   int32_t rows, cols;     /* W is [rows][cols]: cols inputs, rows outputs */

@@ -12,7 +12,7 @@ constexpr int kW4Lowest = 7;                    // lowest scale byte: 2^-120, no
 constexpr __host__ __device__ int w4_col_tiles(int cols) { return (cols + kW4Cols - 1) / kW4Cols; }
 constexpr __host__ __device__ int64_t w4_codes_bytes(int col_tiles) { return (int64_t)col_tiles * 1024; }
 constexpr __host__ __device__ int64_t w4_tile_bytes(int col_tiles) {
-  return w4_codes_bytes(col_tiles) + (int64_t)((col_tiles + 3) / 4) * 256;
+  return w4_codes_bytes(col_tiles) + (int64_t)((col_tiles + 3) / 4) * 256;      // of 64 bytes per column tile
 }
 
 // w[0, rows) x [0, cols) <-> data.
@@ -20,10 +20,11 @@ hipError_t launch_w4_pack(const bf16* w, int64_t stride, int rows, int cols, cha
 hipError_t launch_w4_unpack(const char* data, int rows, int cols, bf16* w, int64_t stride, hipStream_t s);
 
 // How a product runs: rows of x and row tiles of W per work-group, and K splits.
+enum W4Shape { W4_STREAM, W4_TILE32, W4_TILE32W, W4_TILE64, W4_TILE64W, W4_TILE128, W4_TILE256 };
 struct W4Plan {
-  int mb;          // blocks of 16 rows of x
-  int nb;          // row tiles of W (of each matrix)
-  int splits;
+  W4Shape shape;   // the stream kernel, or a tile's rows of x (W: with more of W)
+  int wide;        // W4_STREAM: waves that share the columns
+  int splits;      // of the columns, over work-groups
 };
 
 struct W4Args {

@@ -11,6 +11,7 @@
 // The products are taken as D = W . x^T: a lane's four accumulators of a block are four
 // consecutive outputs of one row of x.
 #include <algorithm>
+#include <atomic>
 
 #include "e2m1.h"
 #include "gemm_tile.h"
@@ -21,7 +22,12 @@ namespace spec {
 namespace {
 
 constexpr int64_t kMaxGrid = 0xffffffffll / 512;
-constexpr size_t kPartialCap = 64ull << 20;
+
+// Direct global -> LDS load of 16 bytes per lane from the lane's own address to the
+// wave-uniform LDS address `lds` + 16 * lane; see dma16(base, voff, lds).
+__device__ __forceinline__ void dma16_at(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds) : "memory", "m0");
+}
 
 // A group's scale; the infinity that byte 255 becomes makes every code a NaN.
 __device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
@@ -56,91 +62,301 @@ __device__ __forceinline__ f32x4 gated(f32x4 g, f32x4 u) {
   return f32x4{silu(g[0]) * u[0], silu(g[1]) * u[1], silu(g[2]) * u[2], silu(g[3]) * u[3]};
 }
 
-constexpr int kWaves = 8;
+// Four sums (of each matrix) of row `row`, columns col .. col + 3, of one split.
+template <bool PAIR>
+__device__ __forceinline__ void finish(const W4Args& a, int split, int row, int col, const f32x4 (&v)[PAIR ? 2 : 1]) {
+  constexpr int MATS = PAIR ? 2 : 1;
+  if (a.plan.splits > 1) {
+    const int padded = (a.rows + 15) / 16 * 16;
+#pragma unroll
+    for (int k = 0; k < MATS; ++k)
+      *(f32x4*)(a.partial + ((int64_t)(split * MATS + k) * a.n + row) * padded + col) = v[k];
+  } else {
+    store4(a, row, col, PAIR ? gated(v[0], v[MATS - 1]) : v[0]);
+  }
+}
 
-// Few rows.  A work-group takes 16 MB rows of x and NB row tiles of W (of both
-// matrices of a gate/up pair); its waves take column tiles in turn, and their sums meet in
-// LDS, in the waves' order.
-template <int MB, int NB, bool PAIR>
-__global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Args a) {
-  constexpr int MATS = PAIR ? 2 : 1, WB = NB * MATS;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
+// Accumulators that a loop goes on with, held in registers from here on.  (Of zeros that it
+// may make again where they are used, this compiler, ROCm 7.2, has left out two of the four.)
+__device__ __forceinline__ f32x4 zeros() {
+  f32x4 v{};
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// Few rows (up to 16): bound by the weights' bytes, and so by how many of them are on their
+// way at a time (some 10 MB over the chip).  The rows of x, or their columns of this split,
+// lie in LDS as a whole; after that a wave only loads weights, up to 2 D column tiles of a row
+// tile (of both matrices) ahead, and meets no barrier.  The sixteen waves of a work-group take KG ranges of
+// the columns for 16 / KG groups of row tiles (KG > 1: their sums meet in LDS, in order) and go
+// on with the next such set until there is none.  (Per wave and column tile 4 KB of x come
+// out of LDS for 1 KB of weights out of HBM; read from L2 instead, x takes more of the
+// load path than the weights, and its loads, waited for in order, hold theirs up.)
+constexpr int kStreamWaves = 16;
+template <bool PAIR>
+__global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args a) {
+  constexpr int NB = PAIR ? 2 : 1, D = 4 / NB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row_tiles = (a.rows + 15) / 16, T = w4_col_tiles(a.cols);
-  const int groups = (row_tiles + NB - 1) / NB;
-  const int group = blockIdx.x % groups, split = blockIdx.x / groups;
-  const int m0 = blockIdx.y * 16 * MB;
-  const int t0 = (int)((int64_t)T * split / a.plan.splits), t1 = (int)((int64_t)T * (split + 1) / a.plan.splits);
-  const char* w[WB];
-#pragma unroll
-  for (int j = 0; j < WB; ++j)
-    w[j] = (j < NB ? a.w0 : a.w1) + (int64_t)min(group * NB + j % NB, row_tiles - 1) * w4_tile_bytes(T);
+  const int KG = a.plan.wide, CG = kStreamWaves / KG, kg = wave % KG, cg = wave / KG;
+  const int split = blockIdx.x % a.plan.splits, first = blockIdx.x / a.plan.splits, wgs = gridDim.x / a.plan.splits;
+  const int s0 = T * split / a.plan.splits, s1 = T * (split + 1) / a.plan.splits;
+  const int longest = (T + a.plan.splits - 1) / a.plan.splits, pitch = (longest + 3) / 4 * 1024;
   const int r = lane & 15, g = lane >> 4;
-  const bf16* x[MB];
-  bool live[MB];
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    live[i] = m0 + 16 * i + r < a.n;
-    x[i] = a.x + (live[i] ? m0 + 16 * i + r : 0) * a.x_stride + 32 * g;
+  // x into LDS: wave-load = 64 chunks of 16 bytes of one row, chunk c at place c ^ row of its 16.
+  {
+    const int per_row = pitch / 1024, loads = a.n * per_row, valid = (a.cols - s0 * kW4Cols) / 8;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+    for (int l = wave; l < loads; l += kStreamWaves) {
+      const int row = l / per_row, c = l % per_row * 64 + (lane ^ (row & 15));
+      const bf16* p = a.x + row * a.x_stride + (int64_t)s0 * kW4Cols;
+      dma16_at(p + (c < valid ? 8 * c : 0), lds0 + row * pitch + l % per_row * 1024);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (s1 == T && (a.cols & (kW4Cols - 1)))                   // columns that the matrix does not have
+      for (int l = wave; l < loads; l += kStreamWaves) {
+        const int row = l / per_row, c = l % per_row * 64 + (lane ^ (row & 15));
+        if (c >= valid) *(i32x4*)(smem + row * pitch + l % per_row * 1024 + lane * 16) = i32x4{0, 0, 0, 0};
+      }
+    __syncthreads();
   }
-  f32x4 acc[MB][WB];
+  const char* xrow = smem + min(r, a.n - 1) * pitch;
+  const int swz = min(r, a.n - 1) & 15;
+  f32x4* sums = (f32x4*)(smem + a.n * pitch);
+  const int len = s1 - s0, t0 = s0 + len * kg / KG, t1 = s0 + len * (kg + 1) / KG;
+  struct Tiles {
+    i32x4 c[D][NB];
+    uint32_t e[D][NB];
+  };
+  for (int set = first; set * CG < row_tiles; set += wgs) {
+    const int tile = set * CG + cg;
+    const char* w[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) w[j] = (j == 0 ? a.w0 : a.w1) + (int64_t)min(tile, row_tiles - 1) * w4_tile_bytes(T);
+    f32x4 acc[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j] = zeros();
+    auto load = [&](Tiles& b, int t) {
+#pragma unroll
+      for (int u = 0; u < D; ++u) {
+        const int tu = min(t + u, t1 - 1);       // never conditional: the compiler's waits count the loads
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          b.c[u][j] = *(const i32x4*)(w[j] + (int64_t)tu * 1024 + lane * 16);
+          b.e[u][j] = *((const uint8_t*)w[j] + w4_codes_bytes(T) + tu * 64 + lane);
+        }
+      }
+    };
+    auto multiply = [&](Tiles& b, int t) {
+#pragma unroll
+      for (int u = 0; u < D; ++u) {
+        if (t + u >= t1) break;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(b.c[u][j]), "+v"(b.e[u][j]));      // waited for here
+        const char* p = xrow + (t + u - s0) * 256;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8 f = *(const bf16x8*)(p + (((4 * g + q) ^ swz) << 4));
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weights_of((uint32_t)b.c[u][j][q], scale_of(b.e[u][j])), f,
+                                                             acc[j], 0, 0, 0);
+        }
+      }
+    };
+    if (t0 < t1) {
+      Tiles b0, b1;
+      load(b0, t0);
+      for (int t = t0;;) {
+        if (t + D >= t1) {
+          multiply(b0, t);
+          break;
+        }
+        load(b1, t + D);
+        multiply(b0, t);
+        t += D;
+        if (t + D >= t1) {
+          multiply(b1, t);
+          break;
+        }
+        load(b0, t + D);
+        multiply(b1, t);
+        t += D;
+      }
+    }
+    if (KG > 1) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) sums[(wave * NB + j) * 64 + lane] = acc[j];
+      __syncthreads();
+      if (kg == 0) {
+        for (int k = 1; k < KG; ++k)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[j] += sums[((wave + k) * NB + j) * 64 + lane];
+      }
+      __syncthreads();
+      if (kg > 0) continue;
+    }
+    if (tile < row_tiles && r < a.n) finish<PAIR>(a, split, r, tile * 16 + 4 * g, acc);
+  }
+}
+
+// Many rows: bound by the matrix cores.  A work-group of WM x WN waves (times KG that share
+// out the column tiles) takes BM = 16 MB WM rows of x and 16 NB WN rows of W (of a gate/up
+// pair, half of them each one's); a wave 16 MB x 16 NB.  x moves into LDS by direct loads, a
+// column tile (256 bytes of every row) at a time, the 16-byte chunk of a row XOR-ed with the row,
+// so that the operand reads (16 rows, one chunk) hit all 64 banks once.  The weights go
+// straight to registers.  Both are loaded for the next column tile while one is multiplied:
+// one barrier per tile, at which the loads issued a whole tile ago have arrived.
+template <int MB, int NB, int WM, int WN, int KG, bool PAIR>
+__global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_kernel(W4Args a) {
+  constexpr int BM = 16 * MB * WM, BT = NB * WN / (PAIR ? 2 : 1), STAGE = BM * 256, LOADS = BM / 4 / (WM * WN);
+  static_assert(LOADS * 4 * WM * WN == BM && (!PAIR || NB % 2 == 0), "whole loads, whole pairs");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = wave / (WM * WN), wm = wave % (WM * WN) / WN, wn = wave % WN;
+  const int row_tiles = (a.rows + 15) / 16, T = w4_col_tiles(a.cols);
+  const int ntm = (a.n + BM - 1) / BM, ntn = (row_tiles + BT - 1) / BT, tiles = ntm * ntn;
+  const int bid = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int split = bid / tiles;
+  int tm, tn;
+  tile_at(bid % tiles, ntm, ntn, &tm, &tn);
+  const int t0 = T * split / a.plan.splits, t1 = T * (split + 1) / a.plan.splits;
+  const int r = lane & 15, g = lane >> 4;
+  const char* w[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    constexpr int HALF = PAIR ? NB / 2 : NB;
+    const int tile = min(tn * BT + wn * HALF + j % HALF, row_tiles - 1);
+    w[j] = (j < HALF ? a.w0 : a.w1) + (int64_t)tile * w4_tile_bytes(T);
+  }
+  // Wave-load l: 4 rows, lane at row lane / 16, chunk lane % 16 of its stage; it fetches the
+  // chunk that belongs there, from a scalar base (the first of the four rows) and an offset
+  // of the lane's.  Rows past the last repeat it (never stored); chunks past the last column
+  // repeat the row's first ones and are cleared in LDS.
+  const int last = (a.cols - (T - 1) * kW4Cols) / 8;             // chunks of the last column tile
+  const int lw = wave % (WM * WN);
+  const char* x[LOADS];
+  uint32_t off[LOADS];
+#pragma unroll
+  for (int l = 0; l < LOADS; ++l) {
+    const int row0 = tm * BM + (lw * LOADS + l) * 4, base = min(row0, a.n - 1);
+    x[l] = (const char*)(a.x + base * a.x_stride);
+    off[l] = (uint32_t)((min(row0 + g, a.n - 1) - base) * a.x_stride * 2 + 16 * (r ^ ((row0 + g) & 15)));
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem + kg * 2 * STAGE + lw * LOADS * 1024;
+  char* stage0 = smem + kg * 2 * STAGE;
+  auto chunk_of = [&](int l) { return r ^ (((lw * LOADS + l) * 4 + g) & 15); };
+  auto load_x = [&](int t, int buf) {
+    if (last < 16 && t == T - 1) {
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) {
+        const int c = chunk_of(l);
+        dma16(x[l] + (int64_t)t * 256, off[l] - (c < last ? 0 : 16 * (c - c % last)), lds0 + buf * STAGE + l * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) dma16(x[l] + (int64_t)t * 256, off[l], lds0 + buf * STAGE + l * 1024);
+    }
+  };
+  auto clear_x = [&](int buf) {          // of the last column tile
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l)
+      if (chunk_of(l) >= last)
+        *(i32x4*)(stage0 + buf * STAGE + (lw * LOADS + l) * 1024 + lane * 16) = i32x4{0, 0, 0, 0};
+  };
+  struct Weights {
+    i32x4 c[NB];
+    uint32_t e[NB];
+  };
+  auto load_w = [&](Weights& b, int t) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      b.c[j] = *(const i32x4*)(w[j] + (int64_t)t * 1024 + lane * 16);
+      b.e[j] = *((const uint8_t*)w[j] + w4_codes_bytes(T) + t * 64 + lane);
+    }
+  };
+  f32x4 acc[MB][NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int j = 0; j < WB; ++j) acc[i][j] = f32x4{};
-  for (int t = t0 + wave; t < t1; t += kWaves) {
-    i32x4 c[WB];
-    uint32_t e[WB];
-    bf16x8 f[MB][4];
+    for (int j = 0; j < NB; ++j) acc[i][j] = zeros();
+  const char* arow = stage0 + (wm * 16 * MB + r) * 256;
+  auto multiply = [&](const Weights& b, int buf) {
 #pragma unroll
-    for (int j = 0; j < WB; ++j) {
-      c[j] = *(const i32x4*)(w[j] + (int64_t)t * 1024 + lane * 16);
-      e[j] = *(const uint8_t*)(w[j] + w4_codes_bytes(T) + (t >> 2) * 256 + lane * 4 + (t & 3));
+    for (int q = 0; q < 4; ++q) {
+      bf16x8 f[MB], v[NB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) f[i] = *(const bf16x8*)(arow + buf * STAGE + i * 16 * 256 + (((4 * g + q) ^ r) << 4));
+#pragma unroll
+      for (int j = 0; j < NB; ++j) v[j] = weights_of((uint32_t)b.c[j][q], scale_of(b.e[j]));
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], f[i], acc[i][j], 0, 0, 0);
     }
-    const bool inside = t * kW4Cols + 32 * g < a.cols;
+  };
+  // Every group runs the same number of steps; one past its last tile multiplies nothing.
+  const int steps = (t1 - t0 + KG - 1) / KG;
+  Weights wa, wb;
+  auto step = [&](int i, int buf, Weights& now, Weights& next) {
+    const int t = t0 + i * KG + kg;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // Here and not where they are first used, behind the next loads; nor does anything of
+    // theirs (the shift of the scales) move up to those.
+#pragma unroll
+    for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(now.c[j]), "+v"(now.e[j]));
+    if (last < 16 && t == T - 1) {
+      clear_x(buf);
+      wait_lds();
+    }
+    phase_barrier();
+    if (i + 1 < steps) {
+      load_x(min(t + KG, t1 - 1), buf ^ 1);
+      load_w(next, min(t + KG, t1 - 1));
+    }
+    if (t < t1) multiply(now, buf);
+  };
+  if (steps > 0) {
+    load_x(min(t0 + kg, t1 - 1), 0);
+    load_w(wa, min(t0 + kg, t1 - 1));
+  }
+  for (int i = 0; i < steps; i += 2) {
+    step(i, 0, wa, wb);
+    if (i + 1 < steps) step(i + 1, 1, wb, wa);
+  }
+  if constexpr (KG > 1) {                // the groups' sums meet in LDS, in their order
+    constexpr int BLOCKS = MB * NB;
+    static_assert((KG - 1) * WM * WN * BLOCKS * 1024 <= KG * 2 * STAGE, "sums fit");
+    __syncthreads();
+    f32x4* sums = (f32x4*)smem;
+    if (kg > 0)
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[(((kg - 1) * WM * WN + lw) * BLOCKS + i * NB + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    if (kg > 0) return;
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        f[i][q] = live[i] && inside ? *(const bf16x8*)(x[i] + t * kW4Cols + 8 * q) : bf16x8{};
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int j = 0; j < WB; ++j) {
-      const float s = scale_of(e[j]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bf16x8 b = weights_of((uint32_t)c[j][q], s);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, f[i][q], acc[i][j], 0, 0, 0);
-      }
-    }
+        for (int k = 1; k < KG; ++k) acc[i][j] += sums[(((k - 1) * WM * WN + lw) * BLOCKS + i * NB + j) * 64 + lane];
   }
-  // [block][wave][lane] of four sums
-  f32x4* part = (f32x4*)smem;
+  constexpr int MATS = PAIR ? 2 : 1, HALF = NB / MATS;
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int j = 0; j < WB; ++j) part[((i * WB + j) * kWaves + wave) * 64 + lane] = acc[i][j];
-  __syncthreads();
-  auto total = [&](int i, int j) {
-    f32x4 v = part[(i * WB + j) * kWaves * 64 + lane];
+    for (int j = 0; j < HALF; ++j) {
+      const int row = tm * BM + (wm * MB + i) * 16 + r, tile = tn * BT + wn * HALF + j;
+      if (tile >= row_tiles || row >= a.n) continue;
+      f32x4 v[MATS];
 #pragma unroll
-    for (int k = 1; k < kWaves; ++k) v += part[((i * WB + j) * kWaves + k) * 64 + lane];
-    return v;
-  };
-  for (int b = wave; b < MB * NB; b += kWaves) {
-    const int i = b / NB, j = b % NB, tile = group * NB + j;
-    const int row = m0 + 16 * i + r, col = tile * 16 + 4 * g;
-    if (tile >= row_tiles || row >= a.n) continue;
-    if (a.plan.splits > 1) {
-#pragma unroll
-      for (int k = 0; k < MATS; ++k)
-        *(f32x4*)(a.partial + ((int64_t)(split * MATS + k) * a.n + row) * (row_tiles * 16) + col) = total(i, j + k * NB);
-    } else if (PAIR) {
-      store4(a, row, col, gated(total(i, j), total(i, j + NB)));
-    } else {
-      store4(a, row, col, total(i, j));
+      for (int k = 0; k < MATS; ++k) v[k] = acc[i][j + k * HALF];
+      finish<PAIR>(a, split, row, tile * 16 + 4 * g, v);
     }
-  }
 }
 
 // Sum the splits, in their order, and store.
@@ -162,24 +378,66 @@ __global__ __launch_bounds__(256) void w4_reduce_kernel(W4Args a) {
   store4(a, (int)row, col, PAIR ? gated(v[0], v[MATS - 1]) : v[0]);
 }
 
-template <int MB, int NB, bool PAIR>
-hipError_t launch_rows(const W4Args& a, hipStream_t s) {
-  const int64_t groups = ((a.rows + 15) / 16 + NB - 1) / NB, blocks = (a.n + 16 * MB - 1) / (16 * MB);
-  if (groups * a.plan.splits * blocks > kMaxGrid || blocks > 65535) return hipErrorInvalidValue;
-  constexpr int smem = MB * NB * (PAIR ? 2 : 1) * kWaves * 1024;
-  static_assert(smem <= 64 * 1024, "LDS without an attribute");
-  w4_rows_kernel<MB, NB, PAIR><<<dim3((unsigned)(groups * a.plan.splits), (unsigned)blocks), 64 * kWaves, smem, s>>>(a);
+constexpr int kLds = 160 * 1024;         // of a CU
+constexpr size_t kPartialCap = 64ull << 20;
+
+// Let a kernel have that much LDS, once per device (a call takes a microsecond).
+hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>* ready) {
+  int dev = -1;
+  if (const hipError_t e = hipGetDevice(&dev)) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (ready->load(std::memory_order_relaxed) & bit) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) ready->fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+// LDS that the stream kernel needs.
+int stream_lds(int cols, int n, int nb, const W4Plan& p) {
+  const int T = w4_col_tiles(cols), longest = (T + p.splits - 1) / p.splits;
+  return n * ((longest + 3) / 4 * 1024) + (p.wide > 1 ? kStreamWaves * nb * 1024 : 0);
+}
+
+template <bool PAIR>
+hipError_t launch_stream(const W4Args& a, hipStream_t s) {
+  const auto kernel = w4_stream_kernel<PAIR>;
+  const int smem = stream_lds(a.cols, a.n, PAIR ? 2 : 1, a.plan);
+  static std::atomic<uint64_t> ready{0};
+  if (const hipError_t e = allow_lds((const void*)kernel, kLds, &ready)) return e;
+  const int per = kStreamWaves / a.plan.wide, sets = ((a.rows + 15) / 16 + per - 1) / per;
+  kernel<<<(unsigned)(std::min(sets, std::max(1, 256 / a.plan.splits)) * a.plan.splits), 64 * kStreamWaves, smem, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int MB, int NB, int WM, int WN, int KG, bool PAIR>
+hipError_t launch_tile(const W4Args& a, hipStream_t s) {
+  constexpr int BM = 16 * MB * WM, BT = NB * WN / (PAIR ? 2 : 1), SMEM = KG * 2 * BM * 256;
+  const auto kernel = w4_tile_kernel<MB, NB, WM, WN, KG, PAIR>;
+  static std::atomic<uint64_t> ready{0};
+  if (const hipError_t e = allow_lds((const void*)kernel, SMEM, &ready)) return e;
+  const int64_t tiles = (int64_t)((a.n + BM - 1) / BM) * (((a.rows + 15) / 16 + BT - 1) / BT);
+  if (tiles * a.plan.splits > kMaxGrid) return hipErrorInvalidValue;
+  kernel<<<(unsigned)(tiles * a.plan.splits), 64 * WM * WN * KG, SMEM, s>>>(a);
   return hipGetLastError();
 }
 
 template <bool PAIR>
-hipError_t launch_pair(const W4Args& a, hipStream_t s) {
-  hipError_t e;
-  switch (a.plan.mb) {
-    case 1: e = launch_rows<1, 1, PAIR>(a, s); break;
-    case 2: e = launch_rows<2, 1, PAIR>(a, s); break;
-    default: e = launch_rows<4, 1, PAIR>(a, s); break;
+hipError_t launch_shape(const W4Args& a, hipStream_t s) {
+  switch (a.plan.shape) {
+    case W4_STREAM: return launch_stream<PAIR>(a, s);
+    case W4_TILE32: return launch_tile<2, 2, 1, 4, 2, PAIR>(a, s);
+    case W4_TILE32W: return launch_tile<2, 4, 1, 8, 1, PAIR>(a, s);
+    case W4_TILE64: return launch_tile<4, 2, 1, 4, 2, PAIR>(a, s);
+    case W4_TILE64W: return launch_tile<4, 2, 1, 8, 1, PAIR>(a, s);
+    case W4_TILE128: return launch_tile<4, 4, 2, 4, 1, PAIR>(a, s);
+    case W4_TILE256: return launch_tile<8, 4, 2, 4, 1, PAIR>(a, s);
   }
+  return hipErrorInvalidValue;
+}
+
+template <bool PAIR>
+hipError_t launch_pair(const W4Args& a, hipStream_t s) {
+  const hipError_t e = launch_shape<PAIR>(a, s);
   if (e != hipSuccess || a.plan.splits == 1) return e;
   const int64_t threads = (int64_t)a.n * ((a.rows + 15) / 16 * 4);
   if ((threads + 255) / 256 > kMaxGrid) return hipErrorInvalidValue;
@@ -189,11 +447,67 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 
 }  // namespace
 
+// Up to 16 rows: the stream kernel, x in LDS over as few column splits as its place there
+// allows, and as many waves to a row tile as still leave one round of work-groups.  (us, the
+// splits cold: 1 row 4096 x 14336, 16 / 8 / 4 / 2 waves 9.3 / 9.9 / 12.6 / 19.5; gate/up of 4 rows,
+// 14336 x 4096, 17.9 / 14.8 / 14.0 / 15.3; head of 1 row, 128256 x 4096, 73 / 54 / 52 / 50 and
+// alone 49; 16 rows 4096 x 14336 in 4 splits 16.2 / 14.3 / 13.8 / 14.4, in 8 no better.)
+//
+// More rows: the cost model below, in us.  Work-groups run `slots` to a CU; k of them on one
+// take max(alone, k * each) per step of a column tile (the kernel's KG at a time), `fixed`
+// more per round; weights stream at `tbs` TB/s; the larger of both, an eighth of the smaller
+// (they overlap imperfectly), 5.7 for a launch in a graph and, where columns are split, 2.1 and
+// the partials written and read at 5 TB/s for the reduction.  Fitted to 2550 launches (8
+// matrices of the 1B and 8B shapes, 17 to 2048 rows, all tiles, 1 to 16 splits, weights from
+// HBM): 9 % rms, and the choice is on average 1.7 % slower than the best of them, at worst
+// 19 % (4096 x 4096, 768 rows).
 W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
-  (void)rows;
-  (void)cols;
-  (void)gate_up;
-  return W4Plan{n <= 16 ? 1 : n <= 32 ? 2 : 4, 1, 1};
+  const int tiles = (rows + 15) / 16, mats = gate_up ? 2 : 1, T = w4_col_tiles(cols);
+  if (n <= 16) {
+    W4Plan p{W4_STREAM, kStreamWaves, 1};
+    while (stream_lds(cols, n, mats, p) > kLds) ++p.splits;
+    while (p.wide > 1 && (int64_t)tiles * p.wide * p.splits > 256 * kStreamWaves) p.wide /= 2;
+    return p;
+  }
+  struct Tile {
+    W4Shape shape;
+    int bm, bt, kg, slots;
+    double alone, each, fixed, tbs;
+  };
+  static constexpr Tile shapes[] = {{W4_TILE32, 32, 8, 2, 3, 0.548, 0.512, 0.0, 4.74},
+                                    {W4_TILE32W, 32, 32, 1, 1, 0.988, 0, 0.16, 5.13},
+                                    {W4_TILE64, 64, 8, 2, 2, 0.907, 0.845, 0.03, 3.84},
+                                    {W4_TILE64W, 64, 16, 1, 2, 0.843, 0.317, 0.38, 4.03},
+                                    {W4_TILE128, 128, 16, 1, 1, 1.507, 0, 0.41, 2.80},
+                                    {W4_TILE256, 256, 16, 1, 1, 2.732, 0, 1.29, 1e9}};
+  W4Plan best{W4_TILE64, 1, 1};
+  double best_us = 1e30;
+  for (const Tile& s : shapes) {
+    if (s.shape == W4_TILE32W && n > s.bm) continue;      // its weights would pass once per 32 rows
+    const int64_t count = ((int64_t)n + s.bm - 1) / s.bm * (((int64_t)tiles * mats + s.bt - 1) / s.bt);
+    for (int splits = 1; splits <= 16; ++splits) {
+      const double part = 4.0 * splits * mats * n * tiles * 16;
+      if (splits > 1 && (T / splits < 4 || part > kPartialCap)) break;
+      const int64_t wgs = count * splits;
+      const double steps = (T + splits * s.kg - 1) / (splits * s.kg), at_once = 256.0 * s.slots;
+      auto step = [&](int k) { return k == 0 ? 0.0 : std::max(s.alone, k * s.each); };
+      double work;
+      if (wgs > 3 * at_once) {
+        work = wgs / at_once * (steps * step(s.slots) + s.fixed);
+      } else {
+        const int64_t full = wgs / (256 * s.slots), rest = wgs % (256 * s.slots);
+        work = steps * (full * step(s.slots) + step((int)((rest + 255) / 256))) + (full + (rest > 0)) * s.fixed;
+      }
+      const double stream = mats * (double)rows * cols * 17 / 32 / s.tbs / 1e6;
+      double us = std::max(work, stream) + 0.13 * std::min(work, stream);
+      if (splits > 1) us += 2.1 + 2 * part / 5e6;
+      if (us < best_us) {
+        best_us = us;
+        best = W4Plan{s.shape, 1, splits};
+      }
+    }
+  }
+  return best;
 }
 
 size_t w4_partial_bytes(int rows, int cols, int n, bool gate_up) {

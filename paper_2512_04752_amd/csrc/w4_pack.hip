@@ -37,7 +37,7 @@ __device__ __forceinline__ Place place(int rows, int cols) {
 
 // Word of the codes that lane (row r, chunk c) has in a tile, and its group's scale.
 __device__ __forceinline__ int word_at(int r, int c) { return (r + 16 * (c >> 2)) * 16 + (c & 3) * 4; }
-__device__ __forceinline__ int scale_at(int r, int c) { return (r + 16 * (c >> 2)) * 4; }
+__device__ __forceinline__ int scale_at(int r, int c) { return r + 16 * (c >> 2); }
 
 __global__ __launch_bounds__(256) void w4_pack_kernel(const bf16* w, int64_t stride, int rows, int cols,
                                                       char* data) {
@@ -52,10 +52,10 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const bf16* w, int64_t str
       v[i][j] = row < rows && col < cols ? *(const i32x4*)(w + row * stride + col) : i32x4{0, 0, 0, 0};
     }
   char* tile = data + p.rt * w4_tile_bytes(p.tiles);
+  uint8_t* scales = (uint8_t*)tile + w4_codes_bytes(p.tiles);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 4 * i + p.r4;
-    uint32_t scales = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float f[8];
@@ -71,11 +71,10 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const bf16* w, int64_t str
       top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, true));   // quad_perm 2 3 0 1
       const uint32_t e = scale_byte(top, kW4Lowest);
       const uint32_t codes = pack_codes<8>(f, e);
-      if (p.kt0 + j < p.tiles) *(uint32_t*)(tile + (int64_t)(p.kt0 + j) * 1024 + word_at(r, p.chunk)) = codes;
-      scales |= e << (8 * j);
+      if (p.kt0 + j >= p.tiles) continue;
+      *(uint32_t*)(tile + (int64_t)(p.kt0 + j) * 1024 + word_at(r, p.chunk)) = codes;
+      if ((p.chunk & 3) == 0) scales[(p.kt0 + j) * 64 + scale_at(r, p.chunk)] = (uint8_t)e;
     }
-    if ((p.chunk & 3) == 0)
-      *(uint32_t*)(tile + w4_codes_bytes(p.tiles) + (int64_t)(p.kt0 / 4) * 256 + scale_at(r, p.chunk)) = scales;
   }
 }
 
@@ -84,24 +83,25 @@ __global__ __launch_bounds__(256) void w4_unpack_kernel(const char* data, int ro
   const Place p = place(rows, cols);
   if (!p.some) return;
   const char* tile = data + p.rt * w4_tile_bytes(p.tiles);
-  uint32_t codes[4][4], scales[4];
+  const uint8_t* scales = (const uint8_t*)tile + w4_codes_bytes(p.tiles);
+  uint32_t codes[4][4], exps[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 4 * i + p.r4;
-    scales[i] = *(const uint32_t*)(tile + w4_codes_bytes(p.tiles) + (int64_t)(p.kt0 / 4) * 256 + scale_at(r, p.chunk));
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      codes[i][j] = p.kt0 + j < p.tiles
-                        ? *(const uint32_t*)(tile + (int64_t)(p.kt0 + j) * 1024 + word_at(r, p.chunk)) : 0;
+    for (int j = 0; j < 4; ++j) {
+      const int t = min(p.kt0 + j, p.tiles - 1);
+      codes[i][j] = *(const uint32_t*)(tile + (int64_t)t * 1024 + word_at(r, p.chunk));
+      exps[i][j] = scales[t * 64 + scale_at(r, p.chunk)];
+    }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int row = p.rt * 16 + 4 * i + p.r4, col = (p.kt0 + j) * kW4Cols + 8 * p.chunk;
-      const uint32_t e = scales[i] >> (8 * j) & 255u;
-      i32x4 v = numbers(codes[i][j], __uint_as_float(e << 23));
-      if (e == 255u) v = i32x4{0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0};
+      // (byte 255 becomes an infinity, with which every code is a NaN)
+      const i32x4 v = numbers(codes[i][j], __uint_as_float(exps[i][j] << 23));
       if (row < rows && col < cols) *(i32x4*)(w + row * stride + col) = v;
     }
 }
