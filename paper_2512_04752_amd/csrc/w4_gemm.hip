@@ -36,6 +36,20 @@ __device__ __forceinline__ bf16x8 weights_of(uint32_t word, float s) {
   return __builtin_bit_cast(bf16x8, numbers(word, s));
 }
 
+// A row tile of a matrix as a buffer: places in it are a lane's constant offset and a scalar
+// one.  (Of pointers the compiler keeps a 64-bit address per load and lane over the loops.)
+struct RowTile {
+  __amdgpu_buffer_rsrc_t buf;
+  __device__ __forceinline__ RowTile() {}
+  __device__ __forceinline__ RowTile(const char* w, int tile, int T)
+      : buf(__builtin_amdgcn_make_buffer_rsrc((void*)(w + tile * w4_tile_bytes(T)), 0, (int)w4_tile_bytes(T), 0x27000)) {}
+  // A lane's codes and scale of column tile t.
+  __device__ __forceinline__ void load(int T, int t, int lane, i32x4* c, uint32_t* e) const {
+    *c = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, lane * 16, t * 1024, 0));
+    *e = __builtin_amdgcn_raw_buffer_load_b8(buf, lane, (int)w4_codes_bytes(T) + t * 64, 0);
+  }
+};
+
 // Four outputs of one row of x, columns col .. col + 3.
 __device__ __forceinline__ void store4(const W4Args& a, int row, int col, f32x4 v) {
   const int64_t at = row * a.out_stride + col;
@@ -104,7 +118,27 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
   const int s0 = T * split / a.plan.splits, s1 = T * (split + 1) / a.plan.splits;
   const int longest = (T + a.plan.splits - 1) / a.plan.splits, pitch = (longest + 3) / 4 * 1024;
   const int r = lane & 15, g = lane >> 4;
+  const int len = s1 - s0, t0 = s0 + len * kg / KG, t1 = s0 + len * (kg + 1) / KG;
+  RowTile w[NB];
+  auto weights_at = [&](int tile) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) w[j] = RowTile(j == 0 ? a.w0 : a.w1, min(tile, row_tiles - 1), T);
+  };
+  struct Tiles {
+    i32x4 c[D][NB];
+    uint32_t e[D][NB];
+  };
+  auto load = [&](Tiles& b, int t) {
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+      const int tu = min(t + u, t1 - 1);         // never conditional: the compiler's waits count the loads
+#pragma unroll
+      for (int j = 0; j < NB; ++j) w[j].load(T, tu, lane, &b.c[u][j], &b.e[u][j]);
+    }
+  };
+  Tiles b0, b1;
   // x into LDS: wave-load = 64 chunks of 16 bytes of one row, chunk c at place c ^ row of its 16.
+  // The first weights go out behind it, and are not waited for with it.
   {
     const int per_row = pitch / 1024, loads = a.n * per_row, valid = (a.cols - s0 * kW4Cols) / 8;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
@@ -113,41 +147,29 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
       const bf16* p = a.x + row * a.x_stride + (int64_t)s0 * kW4Cols;
       dma16_at(p + (c < valid ? 8 * c : 0), lds0 + row * pitch + l % per_row * 1024);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    weights_at(first * CG + cg);
+    if (t0 < t1) {
+      load(b0, t0);
+      wait_vm<2 * D * NB>();
+    } else {
+      wait_vm<0>();
+    }
     if (s1 == T && (a.cols & (kW4Cols - 1)))                   // columns that the matrix does not have
       for (int l = wave; l < loads; l += kStreamWaves) {
         const int row = l / per_row, c = l % per_row * 64 + (lane ^ (row & 15));
         if (c >= valid) *(i32x4*)(smem + row * pitch + l % per_row * 1024 + lane * 16) = i32x4{0, 0, 0, 0};
       }
-    __syncthreads();
+    wait_lds();
+    phase_barrier();
   }
   const char* xrow = smem + min(r, a.n - 1) * pitch;
   const int swz = min(r, a.n - 1) & 15;
   f32x4* sums = (f32x4*)(smem + a.n * pitch);
-  const int len = s1 - s0, t0 = s0 + len * kg / KG, t1 = s0 + len * (kg + 1) / KG;
-  struct Tiles {
-    i32x4 c[D][NB];
-    uint32_t e[D][NB];
-  };
   for (int set = first; set * CG < row_tiles; set += wgs) {
     const int tile = set * CG + cg;
-    const char* w[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) w[j] = (j == 0 ? a.w0 : a.w1) + (int64_t)min(tile, row_tiles - 1) * w4_tile_bytes(T);
     f32x4 acc[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[j] = zeros();
-    auto load = [&](Tiles& b, int t) {
-#pragma unroll
-      for (int u = 0; u < D; ++u) {
-        const int tu = min(t + u, t1 - 1);       // never conditional: the compiler's waits count the loads
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          b.c[u][j] = *(const i32x4*)(w[j] + (int64_t)tu * 1024 + lane * 16);
-          b.e[u][j] = *((const uint8_t*)w[j] + w4_codes_bytes(T) + tu * 64 + lane);
-        }
-      }
-    };
     auto multiply = [&](Tiles& b, int t) {
 #pragma unroll
       for (int u = 0; u < D; ++u) {
@@ -163,11 +185,10 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
             acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weights_of((uint32_t)b.c[u][j][q], scale_of(b.e[u][j])), f,
                                                              acc[j], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);       // not all tiles' reads of x at once: more registers than there are
       }
     };
     if (t0 < t1) {
-      Tiles b0, b1;
-      load(b0, t0);
       for (int t = t0;;) {
         if (t + D >= t1) {
           multiply(b0, t);
@@ -184,17 +205,23 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
         multiply(b1, t);
         t += D;
       }
+      if ((set + wgs) * CG < row_tiles) {        // the next set's first weights, behind this one's sums
+        weights_at((set + wgs) * CG + cg);
+        load(b0, t0);
+      }
     }
     if (KG > 1) {
 #pragma unroll
       for (int j = 0; j < NB; ++j) sums[(wave * NB + j) * 64 + lane] = acc[j];
-      __syncthreads();
+      wait_lds();
+      phase_barrier();
       if (kg == 0) {
         for (int k = 1; k < KG; ++k)
 #pragma unroll
           for (int j = 0; j < NB; ++j) acc[j] += sums[((wave + k) * NB + j) * 64 + lane];
       }
-      __syncthreads();
+      wait_lds();
+      phase_barrier();
       if (kg > 0) continue;
     }
     if (tile < row_tiles && r < a.n) finish<PAIR>(a, split, r, tile * 16 + 4 * g, acc);
@@ -223,12 +250,11 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_k
   tile_at(bid % tiles, ntm, ntn, &tm, &tn);
   const int t0 = T * split / a.plan.splits, t1 = T * (split + 1) / a.plan.splits;
   const int r = lane & 15, g = lane >> 4;
-  const char* w[NB];
+  RowTile w[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
     constexpr int HALF = PAIR ? NB / 2 : NB;
-    const int tile = min(tn * BT + wn * HALF + j % HALF, row_tiles - 1);
-    w[j] = (j < HALF ? a.w0 : a.w1) + (int64_t)tile * w4_tile_bytes(T);
+    w[j] = RowTile(j < HALF ? a.w0 : a.w1, min(tn * BT + wn * HALF + j % HALF, row_tiles - 1), T);
   }
   // Wave-load l: 4 rows, lane at row lane / 16, chunk lane % 16 of its stage; it fetches the
   // chunk that belongs there, from a scalar base (the first of the four rows) and an offset
@@ -271,10 +297,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_k
   };
   auto load_w = [&](Weights& b, int t) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      b.c[j] = *(const i32x4*)(w[j] + (int64_t)t * 1024 + lane * 16);
-      b.e[j] = *((const uint8_t*)w[j] + w4_codes_bytes(T) + t * 64 + lane);
-    }
+    for (int j = 0; j < NB; ++j) w[j].load(T, t, lane, &b.c[j], &b.e[j]);
   };
   f32x4 acc[MB][NB];
 #pragma unroll
