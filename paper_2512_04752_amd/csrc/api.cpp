@@ -794,7 +794,11 @@ SPEC_API int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const i
   return guarded([&]() -> int {
     if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
     if (int rc = check_reorder(kv->n, groups, width, sample_ids, begin, end, parents)) return rc;
-    std::vector<ReorderBeam> info((size_t)groups * width);
+    ReorderBeams beams;
+    std::vector<ReorderBeam> many;
+    const bool small = groups * width <= kInlineBeams;
+    if (!small) many.resize((size_t)groups * width);
+    ReorderBeam* info = small ? beams.here : many.data();
     int most = 0;
     for (int g = 0; g < groups; ++g) {
       most = std::max(most, end[g] - begin[g]);
@@ -810,10 +814,12 @@ SPEC_API int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const i
     if (most == 0 || width == 1) return SPEC_OK;
     hipStream_t s = (hipStream_t)stream;
     void* ctl = (char*)kv->pool + kv->ctl_off;
-    if (int rc = kv->ring.upload(info.data(), info.size() * sizeof(ReorderBeam), ctl, s)) return rc;
+    beams.device = small ? nullptr : (const ReorderBeam*)ctl;
+    if (!small)
+      if (int rc = kv->ring.upload(many.data(), many.size() * sizeof(ReorderBeam), ctl, s)) return rc;
     const spec_model_config& c = kv->cfg;
     HIP_TRY(timed(SPEC_K_REORDER, s, [&] {
-              return launch_reorder((const ReorderBeam*)ctl, groups, width, most, kv->pool, c.n_layers, c.n_kv_heads,
+              return launch_reorder(beams, groups, width, most, kv->pool, c.n_layers, c.n_kv_heads,
                                     c.head_dim, parents, s);
             }),
             "reorder");

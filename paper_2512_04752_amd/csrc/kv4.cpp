@@ -597,15 +597,24 @@ SPEC_API int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const
     if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
     if (int rc = refuse_capture(stream)) return rc;
     if (most == 0 || width == 1) return SPEC_OK;
-    std::vector<char> blob(need, 0);
-    memcpy(blob.data(), info.data(), groups * sizeof(ReorderGroup));
-    memcpy(blob.data() + head, table.data(), table.size() * 4);
     hipStream_t s = (hipStream_t)stream;
-    if (int rc = kv->ring.upload(blob.data(), need, workspace, s)) return rc;
+    ReorderPages pages;
+    if (groups <= kInlineGroups && table.size() <= kInlinePages && kv->uses.size() <= 65536) {
+      pages.groups = nullptr;
+      std::copy(info.begin(), info.end(), pages.groups_here);
+      std::copy(table.begin(), table.end(), pages.table_here);
+    } else {
+      std::vector<char> blob(need, 0);
+      memcpy(blob.data(), info.data(), groups * sizeof(ReorderGroup));
+      memcpy(blob.data() + head, table.data(), table.size() * 4);
+      if (int rc = kv->ring.upload(blob.data(), need, workspace, s)) return rc;
+      pages.groups = (const ReorderGroup*)workspace;
+      pages.table = (const int32_t*)((char*)workspace + head);
+    }
     const spec_model_config& c = kv->cfg;
     HIP_TRY(timed(SPEC_K_REORDER, s, [&] {
-              return launch_kv4_reorder((const ReorderGroup*)workspace, (const int32_t*)((char*)workspace + head), groups,
-                                        width, (int)most, kv->pool, page_bytes_of(&c), c.head_dim, parents, s);
+              return launch_kv4_reorder(pages, groups, width, (int)most, kv->pool, page_bytes_of(&c), c.head_dim, parents,
+                                        s);
             }),
             "kv4 reorder");
     return SPEC_OK;

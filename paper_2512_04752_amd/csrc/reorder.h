@@ -24,10 +24,25 @@ struct ReorderGroup {
 };
 static_assert(sizeof(ReorderGroup) == 16, "ReorderGroup layout");
 
+// Descriptors of a small call go along as kernel arguments (an upload takes the host 5 us, and
+// the stream as long); of a larger one they lie in device memory.
+constexpr int kInlineBeams = 96, kInlineGroups = 32, kInlinePages = 1440;
+struct ReorderBeams {
+  const ReorderBeam* device;             // NULL: here
+  ReorderBeam here[kInlineBeams];
+};
+struct ReorderPages {
+  const ReorderGroup* groups;            // NULL: here
+  const int32_t* table;
+  ReorderGroup groups_here[kInlineGroups];
+  uint16_t table_here[kInlinePages];
+};
+static_assert(sizeof(ReorderBeams) < 3500 && sizeof(ReorderPages) < 3500, "kernel arguments");
+
 // most: tokens of the longest range, or pages.
-hipError_t launch_reorder(const ReorderBeam* beams, int groups, int width, int most, bf16* pool, int n_layers,
+hipError_t launch_reorder(const ReorderBeams& beams, int groups, int width, int most, bf16* pool, int n_layers,
                           int n_kv_heads, int head_dim, const int32_t* parents, hipStream_t s);
-hipError_t launch_kv4_reorder(const ReorderGroup* info, const int32_t* table, int groups, int width, int most,
-                              char* pool, int64_t page_bytes, int head_dim, const int32_t* parents, hipStream_t s);
+hipError_t launch_kv4_reorder(const ReorderPages& info, int groups, int width, int most, char* pool,
+                              int64_t page_bytes, int head_dim, const int32_t* parents, hipStream_t s);
 
 }  // namespace spec

@@ -8,6 +8,7 @@
 // parent is read once (a second beam's read of it hits the caches) and every moving beam
 // written once; beams that stay cost nothing.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.h"
 #include "reorder.h"
@@ -18,52 +19,57 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The moving beams of group g into LDS, as (source, destination) beams of the group; their number.
-__device__ __forceinline__ int moving_beams(const int32_t* parents, int g, int width, int* src, int* dst, int* count) {
+// The moving beams of a group into LDS, as byte places of what they read and write
+// (place(beam)); their number.  One wave's work: a parent, its and the beam's descriptor.
+struct Moves {
+  int64_t from[64], to[64];
+  int count;
+};
+template <class F>
+__device__ __forceinline__ int moving_beams(const int32_t* parents, int width, Moves* m, F&& place) {
   if (threadIdx.x < 64) {
     const int j = threadIdx.x;
-    const int p = j < width ? parents[(int64_t)g * width + j] : -1;
+    const int p = j < width ? parents[j] : -1;
     const bool moves = p >= 0 && p < width && p != j;
-    const uint64_t m = __ballot(moves);
+    const uint64_t all = __ballot(moves);
     if (moves) {
-      const int at = __popcll(m & ((1ull << j) - 1));
-      src[at] = p;
-      dst[at] = j;
+      const int at = __popcll(all & ((1ull << j) - 1));
+      m->from[at] = place(p);
+      m->to[at] = place(j);
     }
-    if (j == 0) *count = __popcll(m);
+    if (j == 0) m->count = __popcll(all);
   }
   __syncthreads();
-  return *count;
+  return __builtin_amdgcn_readfirstlane(m->count);
+}
+
+// A value that all lanes have, as a scalar.
+__device__ __forceinline__ int64_t scalar(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 template <int W, class Unit>
-__global__ __launch_bounds__(kThreads) void reorder_kernel(const ReorderBeam* beams, int width, bf16* pool, int head_dim,
+__global__ __launch_bounds__(kThreads, W <= 8 ? 8 : W <= 16 ? 5 : 3) void reorder_kernel(ReorderBeams beams, int width, char* pool, int head_dim,
                                                            const int32_t* parents) {
-  __shared__ int src[64], dst[64], count;
-  __shared__ int64_t from[64], to[64];
-  constexpr int PER = sizeof(Unit) / 2;
+  __shared__ Moves m;
   const int g = blockIdx.z, run = blockIdx.y;
-  const ReorderBeam* b = beams + (int64_t)g * width;
+  const ReorderBeam* b = (beams.device ? beams.device : beams.here) + (int64_t)g * width;
   const int begin = b->begin;
-  const int64_t units = (int64_t)(b->end - begin) * head_dim / PER;
-  if ((int64_t)blockIdx.x * kThreads >= units) return;
-  const int n = moving_beams(parents, g, width, src, dst, &count);
-  if (n == 0) return;
-  if (threadIdx.x < n) {
-    const ReorderBeam s = b[src[threadIdx.x]], d = b[dst[threadIdx.x]];
-    from[threadIdx.x] = s.kv_base + ((int64_t)run * s.cap + begin) * head_dim;
-    to[threadIdx.x] = d.kv_base + ((int64_t)run * d.cap + begin) * head_dim;
-  }
-  __syncthreads();
-  const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (u >= units) return;
+  const int64_t bytes = (int64_t)(b->end - begin) * head_dim * 2, block = (int64_t)blockIdx.x * kThreads * sizeof(Unit);
+  if (block >= bytes) return;
+  const int n = moving_beams(parents + (int64_t)g * width, width, &m, [&](int j) {
+    return (b[j].kv_base + ((int64_t)run * b[j].cap + begin) * head_dim) * 2;
+  });
+  const uint32_t at = threadIdx.x * sizeof(Unit);
+  if (block + at >= bytes) return;
   Unit v[W];
 #pragma unroll
   for (int i = 0; i < W; ++i)
-    if (i < n) v[i] = *(const Unit*)(pool + from[i] + u * PER);
+    if (i < n) v[i] = *(const Unit*)(pool + scalar(m.from[i]) + block + at);
 #pragma unroll
   for (int i = 0; i < W; ++i)
-    if (i < n) *(Unit*)(pool + to[i] + u * PER) = v[i];
+    if (i < n) *(Unit*)(pool + scalar(m.to[i]) + block + at) = v[i];
 }
 
 // Which bits of word w (of a 16-byte unit `u` of a head's bytes in a page) belong to
@@ -88,29 +94,25 @@ __device__ __forceinline__ uint32_t bits_of(int u, int w, int lo, int hi) {
 }
 
 template <int W, class Unit, int HD>
-__global__ __launch_bounds__(kThreads) void kv4_reorder_kernel(const ReorderGroup* info, const int32_t* table, int width,
-                                                               char* pool, int64_t page_bytes,
-                                                               const int32_t* parents) {
-  __shared__ int src[64], dst[64], count;
-  __shared__ int64_t from[64], to[64];
+__global__ __launch_bounds__(kThreads, W <= 8 ? 8 : W <= 16 ? 5 : 3) void kv4_reorder_kernel(ReorderPages info, int width, char* pool,
+                                                               int64_t page_bytes, const int32_t* parents) {
+  __shared__ Moves m;
   constexpr int BYTES = sizeof(Unit), WORDS = BYTES / 4;
   const int g = blockIdx.z, page = blockIdx.y;
-  const ReorderGroup r = info[g];
+  const ReorderGroup r = (info.groups ? info.groups : info.groups_here)[g];
   if (page >= r.pages) return;
-  const int n = moving_beams(parents, g, width, src, dst, &count);
-  if (n == 0) return;
-  if (threadIdx.x < n) {
-    from[threadIdx.x] = table[r.table + src[threadIdx.x] * r.pages + page] * page_bytes;
-    to[threadIdx.x] = table[r.table + dst[threadIdx.x] * r.pages + page] * page_bytes;
-  }
-  __syncthreads();
-  const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * BYTES;
-  if (at >= page_bytes) return;
+  const int n = moving_beams(parents + (int64_t)g * width, width, &m, [&](int j) {
+    const int64_t at = r.table + (int64_t)j * r.pages + page;
+    return (info.groups ? info.table[at] : (int32_t)info.table_here[at]) * page_bytes;
+  });
+  const int64_t block = (int64_t)blockIdx.x * kThreads * BYTES;
+  const uint32_t at = threadIdx.x * BYTES;
+  if (block + at >= page_bytes) return;
   const int pos0 = (r.begin / kKv4Page + page) * kKv4Page;
   const int lo = max(0, r.begin - pos0), hi = min(kKv4Page, r.end - pos0);
   uint32_t mask[WORDS], all = ~0u, some = ~0u;
   if (lo > 0 || hi < kKv4Page) {
-    const int in_head = (int)(at % kv4_head_bytes(HD));
+    const int in_head = (int)((block + at) % kv4_head_bytes(HD));
     some = 0;
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) {
@@ -123,18 +125,22 @@ __global__ __launch_bounds__(kThreads) void kv4_reorder_kernel(const ReorderGrou
   Unit v[W];
 #pragma unroll
   for (int i = 0; i < W; ++i)
-    if (i < n) v[i] = *(const Unit*)(pool + from[i] + at);
+    if (i < n) v[i] = *(const Unit*)(pool + scalar(m.from[i]) + block + at);
+  if (all == ~0u) {
 #pragma unroll
-  for (int i = 0; i < W; ++i)
-    if (i < n) {
-      Unit* p = (Unit*)(pool + to[i] + at);
-      if (all != ~0u) {
+    for (int i = 0; i < W; ++i)
+      if (i < n) *(Unit*)(pool + scalar(m.to[i]) + block + at) = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (i < n) {
+        Unit* p = (Unit*)(pool + scalar(m.to[i]) + block + at);
         const Unit old = *p;
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) v[i][w] = (int)((uint32_t)old[w] & ~mask[w] | (uint32_t)v[i][w] & mask[w]);
+        *p = v[i];
       }
-      *p = v[i];
-    }
+  }
 }
 
 // Units of 16 bytes, of 8 where 64 beams' would not fit the registers.
@@ -154,23 +160,21 @@ hipError_t grid_of(int64_t x, int64_t y, int64_t z, dim3* grid) {
 
 }  // namespace
 
-hipError_t launch_reorder(const ReorderBeam* beams, int groups, int width, int most, bf16* pool, int n_layers,
+hipError_t launch_reorder(const ReorderBeams& beams, int groups, int width, int most, bf16* pool, int n_layers,
                           int n_kv_heads, int head_dim, const int32_t* parents, hipStream_t s) {
-  if (most == 0 || width == 1) return hipSuccess;
   return by_width(width, [&](auto w, auto unit) {
     using Unit = decltype(unit);
     const int64_t units = (int64_t)most * head_dim * 2 / sizeof(Unit);
     dim3 grid;
     if (const hipError_t e = grid_of((units + kThreads - 1) / kThreads, (int64_t)n_layers * 2 * n_kv_heads, groups, &grid))
       return e;
-    reorder_kernel<decltype(w)::value, Unit><<<grid, kThreads, 0, s>>>(beams, width, pool, head_dim, parents);
+    reorder_kernel<decltype(w)::value, Unit><<<grid, kThreads, 0, s>>>(beams, width, (char*)pool, head_dim, parents);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_kv4_reorder(const ReorderGroup* info, const int32_t* table, int groups, int width, int most,
-                              char* pool, int64_t page_bytes, int head_dim, const int32_t* parents, hipStream_t s) {
-  if (most == 0 || width == 1) return hipSuccess;
+hipError_t launch_kv4_reorder(const ReorderPages& info, int groups, int width, int most, char* pool,
+                              int64_t page_bytes, int head_dim, const int32_t* parents, hipStream_t s) {
   return by_width(width, [&](auto w, auto unit) {
     using Unit = decltype(unit);
     constexpr int W = decltype(w)::value;
@@ -178,9 +182,9 @@ hipError_t launch_kv4_reorder(const ReorderGroup* info, const int32_t* table, in
     const int64_t units = page_bytes / sizeof(Unit);
     if (const hipError_t e = grid_of((units + kThreads - 1) / kThreads, most, groups, &grid)) return e;
     if (head_dim == 128)
-      kv4_reorder_kernel<W, Unit, 128><<<grid, kThreads, 0, s>>>(info, table, width, pool, page_bytes, parents);
+      kv4_reorder_kernel<W, Unit, 128><<<grid, kThreads, 0, s>>>(info, width, pool, page_bytes, parents);
     else if (head_dim == 64)
-      kv4_reorder_kernel<W, Unit, 64><<<grid, kThreads, 0, s>>>(info, table, width, pool, page_bytes, parents);
+      kv4_reorder_kernel<W, Unit, 64><<<grid, kThreads, 0, s>>>(info, width, pool, page_bytes, parents);
     else
       return hipErrorInvalidValue;
     return hipGetLastError();
