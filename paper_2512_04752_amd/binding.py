@@ -206,7 +206,7 @@ def _pointer(arr, kind):
 
 
 def _i32(a):
-    arr = np.ascontiguousarray(np.asarray(a, dtype=np.int32))
+    arr = np.ascontiguousarray(a, dtype=np.int32)
     return arr, _pointer(arr, c_int32)
 
 
@@ -719,11 +719,15 @@ def spec_w4_workspace_bytes(rows, cols, max_n) -> int:
 
 def _device_rows(t, dtype, rows, cols, what, index=None):
     """Row stride of a device tensor [rows, cols] whose rows are contiguous."""
+    shape = t.shape
+    if t.dtype is dtype and t.is_cuda and len(shape) == 2 and shape[1] == cols and not cols & 7 \
+            and t.get_device() == index and (rows is None or shape[0] == rows) and t.is_contiguous():
+        return cols
     if t.dtype is not dtype or not t.is_cuda or t.dim() != 2 or t.shape[1] != cols \
             or (rows is not None and t.shape[0] != rows) or (t.stride(1) != 1 and cols > 1) \
             or (index is not None and t.get_device() != index):
         kind = str(dtype).split(".")[-1]
-        where = "device" if index is None else f"cuda:{index}"
+        where = "a device" if index is None or index < 0 else f"cuda:{index}"
         raise ValueError(f"{what} must be a {kind} [{'n' if rows is None else rows}, {cols}] tensor on {where} with "
                          "contiguous rows")
     return t.stride(0) if t.shape[0] > 1 else max(cols, (cols + 7) // 8 * 8)
@@ -753,24 +757,27 @@ def _made_workspace(nbytes, index, stream):
 def spec_w4_pack(w, data, stream=None):
     """Quantise w (bf16 [rows, cols], rows may be strided) into data (uint8, spec_w4_bytes)."""
     rows, cols = w.shape if w.dim() == 2 else (0, 0)
-    stride = _device_rows(w, torch.bfloat16, rows, cols, "w")
     index = w.get_device()
+    stride = _device_rows(w, torch.bfloat16, rows, cols, "w", index)
     p, n = _device_workspace(data, index)
     with _on(index):
-        _check(lib().spec_w4_pack(w.data_ptr(), stride, rows, cols, p, n, _device_stream(index, stream)))
+        rc = lib().spec_w4_pack(w.data_ptr(), stride, rows, cols, p, n, _device_stream(index, stream))
+    if rc:
+        _check(rc)
 
 
 def spec_w4_unpack(data, w, stream=None):
     """Write what data (of spec_w4_pack) stands for into w (bf16 [rows, cols])."""
     rows, cols = w.shape if w.dim() == 2 else (0, 0)
-    stride = _device_rows(w, torch.bfloat16, rows, cols, "w")
     index = w.get_device()
+    stride = _device_rows(w, torch.bfloat16, rows, cols, "w", index)
     p, n = _device_workspace(data, index)
-    if n < spec_w4_bytes(rows, cols):
+    if n < lib().spec_w4_bytes(rows, cols):
         raise ValueError(f"data holds {n} bytes, a matrix of {rows} x {cols} {spec_w4_bytes(rows, cols)}")
-    m = spec_w4(p, rows, cols)
     with _on(index):
-        _check(lib().spec_w4_unpack(m, w.data_ptr(), stride, _device_stream(index, stream)))
+        rc = lib().spec_w4_unpack(spec_w4(p, rows, cols), w.data_ptr(), stride, _device_stream(index, stream))
+    if rc:
+        _check(rc)
 
 
 class W4Matrix:
@@ -810,37 +817,39 @@ def _w4_workspace(m, n, workspace, stream):
 def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
     """out = x W^T: x bf16 [n, cols] (rows may be strided), out bf16 or float32 [n, rows]; add: float32
     out += x W^T.  workspace: a uint8 tensor of spec_w4_workspace_bytes (allocated when None)."""
-    if torch.cuda.current_device() != m.index:
-        with torch.cuda.device(m.index):
+    index = m.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
             return spec_w4_linear(m, x, out, add, workspace, stream)
-    xs = _device_rows(x, torch.bfloat16, None, m.cols, "x", m.index)
-    n = x.shape[0]
-    kind = SPEC_W4_BF16 if out.dtype is torch.bfloat16 and not add else SPEC_W4_ADD if add else SPEC_W4_F32
-    os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", m.index)
+    xs = _device_rows(x, torch.bfloat16, None, m.cols, "x", index)
+    n = len(x)
+    kind = SPEC_W4_ADD if add else SPEC_W4_BF16 if out.dtype is torch.bfloat16 else SPEC_W4_F32
+    os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", index)
     if n == 0:
         return
     p, nbytes = _w4_workspace(m, n, workspace, stream)
     rc = lib().spec_w4_linear(m.struct, x.data_ptr(), xs, n, out.data_ptr(), os, kind, p, nbytes,
-                              _device_stream(m.index, stream))
+                              _device_stream(index, stream))
     if rc:
         _check(rc)
 
 
 def spec_w4_gate_up(gate: W4Matrix, up: W4Matrix, x, out, workspace=None, stream=None):
     """out = silu(x Wg^T) * (x Wu^T), bf16 [n, rows]; the rest as in spec_w4_linear."""
-    if torch.cuda.current_device() != gate.index:
-        with torch.cuda.device(gate.index):
+    index = gate.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
             return spec_w4_gate_up(gate, up, x, out, workspace, stream)
-    if up.index != gate.index:
+    if up.index != index:
         raise ValueError("gate and up are on different devices")
-    xs = _device_rows(x, torch.bfloat16, None, gate.cols, "x", gate.index)
-    n = x.shape[0]
-    os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", gate.index)
+    xs = _device_rows(x, torch.bfloat16, None, gate.cols, "x", index)
+    n = len(x)
+    os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", index)
     if n == 0:
         return
     p, nbytes = _w4_workspace(gate, n, workspace, stream)
     rc = lib().spec_w4_gate_up(gate.struct, up.struct, x.data_ptr(), xs, n, out.data_ptr(), os, p, nbytes,
-                               _device_stream(gate.index, stream))
+                               _device_stream(index, stream))
     if rc:
         _check(rc)
 
@@ -868,7 +877,7 @@ def spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens=No
         raise ValueError("logits must be a float32 or bfloat16 [groups, width, vocab] device tensor, parents [groups, k]")
     groups, width, vocab = logits.shape
     index = logits.get_device()
-    if torch.cuda.current_device() != index:
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens, eos_token, workspace,
                                     stream)
@@ -894,7 +903,7 @@ def spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens=No
 
 
 def _reorder_arrays(pool_index, sample_ids, begin, end, parents):
-    ids = np.ascontiguousarray(np.asarray(sample_ids, dtype=np.int32))
+    ids = np.ascontiguousarray(sample_ids, dtype=np.int32)
     if ids.ndim != 2:
         raise ValueError("sample_ids must be [groups, width]")
     (b, p_b), (e, p_e) = _i32(begin), _i32(end)

@@ -5,6 +5,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2512_04752_amd as sv
 import workload as wl
@@ -87,6 +88,15 @@ def test_pack_refusals():
     unpack = B.lib().spec_w4_unpack
     assert unpack(None, P, 64, None) == INVALID and unpack(ctypes.byref(m), P, 60, None) == INVALID
     assert unpack(ctypes.byref(m), None, 64, None) == INVALID
+
+
+def test_tensors_off_the_device():
+    w, data = torch.zeros(48, 64, dtype=torch.bfloat16), torch.zeros(sv.spec_w4_bytes(48, 64), dtype=torch.uint8)
+    for call in (lambda: sv.spec_w4_pack(w, data), lambda: sv.spec_w4_unpack(data, w), lambda: sv.W4Matrix(w),
+                 lambda: sv.spec_beam_select(torch.zeros(1, 2, 9), torch.zeros(1, 2), *[torch.zeros(1, 2).int()] * 2,
+                                             torch.zeros(1, 2))):
+        with pytest.raises(ValueError, match="device"):
+            call()
 
 
 def beam(logits=P, stride=100, bf16=0, groups=2, width=3, vocab=100, scores=P, last=None, eos=-1, k=4, parents=P,
