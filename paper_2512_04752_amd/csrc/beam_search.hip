@@ -62,12 +62,17 @@ struct Exp {
 
 constexpr float kLowest = -3.4028234663852886e38f;
 
-// A wave's running list of the k best, one entry per lane, best first; entries past the
-// filled ones hold -infinity.
-struct List {
-  float z;
-  int y;
-};
+// A logit and its token as one number, larger for a higher logit, then for a lower token; 0:
+// none.
+__device__ __forceinline__ uint64_t key_of(float z, int y) {
+  const uint32_t b = __float_as_uint(z + 0.0f);              // -0 as 0
+  return (uint64_t)(b ^ ((uint32_t)((int)b >> 31) | 0x80000000u)) << 32 | (uint32_t)~y;
+}
+__device__ __forceinline__ float logit_of(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return key == 0 ? -INFINITY : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+__device__ __forceinline__ int token_of(uint64_t key) { return (int)~(uint32_t)key; }
 
 // Lane i gets lane i - 1's x.
 __device__ __forceinline__ int from_below(int x) {
@@ -76,6 +81,19 @@ __device__ __forceinline__ int from_below(int x) {
 
 __device__ __forceinline__ float lane_value(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+
+template <class X>
+__device__ __forceinline__ X lane_value64(X x, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
+}
+template <class X>
+__device__ __forceinline__ X from_below64(X x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = from_below((int)(uint32_t)b), hi = from_below((int)(uint32_t)(b >> 32));
+  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
 }
 
 // The largest float below x; -infinity and NaN stay.
@@ -106,47 +124,42 @@ __device__ __forceinline__ float kth_bound(const float (&x)[N], int k) {
   return t <= 0x007fffffu ? -INFINITY : __uint_as_float(t & 0x80000000u ? t ^ 0x80000000u : ~t);
 }
 
-// Put (z, y) into the list: behind larger logits, and behind equal ones of lower tokens.
-__device__ __forceinline__ void insert(List& l, float z, int y, int lane) {
-  const int pos = __popcll(__ballot(l.z > z) | (__ballot(l.z == z) & __ballot(l.y < y)));
-  const float zb = __int_as_float(from_below(__float_as_int(l.z)));
-  const int yb = from_below(l.y);
-  l.z = lane < pos ? l.z : lane == pos ? z : zb;
-  l.y = lane < pos ? l.y : lane == pos ? y : yb;
-}
-
 // LDS written by lanes of a wave is there for its other lanes.
 __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
-// Put n <= 64 more entries into the list, by counting for each what is better: about 13
-// instructions per new entry and 6 per old one, where insert() takes 35 for each.
-constexpr int kFew = 5;
-__device__ __forceinline__ bool before(const List& p, const List& q) {
-  return (p.z > q.z) | ((p.z == q.z) & (p.y < q.y));
+// A wave's list of the k best is one key per lane, best first, 0 past the last.
+// Put one more into it.
+__device__ __forceinline__ void insert(uint64_t& l, uint64_t key, int lane) {
+  const int pos = __popcll(__ballot(l > key));
+  const uint64_t b = from_below64(l);
+  l = lane < pos ? l : lane == pos ? key : b;
 }
-__device__ __forceinline__ void merge(List& l, const List* found, List* merged, int n, int k, int lane) {
-  List x = found[lane];
-  if (lane >= n) x = List{-INFINITY, 0x7fffffff};
+
+// Put n <= 64 more into it, by counting for each what is better: about 5 instructions per new
+// entry and 3 per old one, where insert() takes 20 for each.
+constexpr int kFew = 5;
+__device__ __forceinline__ void merge(uint64_t& l, const uint64_t* found, uint64_t* merged, int n, int k, int lane) {
+  const uint64_t x = lane < n ? found[lane] : 0;
   int rank = 0, old = lane;
   merged[lane] = l;
   wave_sync();
 #pragma unroll 4
   for (int q = 0; q < n; ++q) {
-    const List f = found[q];
-    rank += before(f, x);
-    old += before(f, l);
+    const uint64_t f = found[q];
+    rank += f > x;
+    old += f > l;
   }
-  if (lane_value(l.z, 0) > -INFINITY) {
+  if (lane_value64(l, 0) != 0) {
 #pragma unroll 4
-    for (int q = 0; q < k; ++q) rank += before(merged[q], x);
+    for (int q = 0; q < k; ++q) rank += merged[q] > x;
   }
   wave_sync();
-  merged[lane] = List{-INFINITY, -1};
+  merged[lane] = 0;
   wave_sync();
-  if (lane < k && l.z > -INFINITY && old < k) merged[old] = l;
+  if (lane < k && l != 0 && old < k) merged[old] = l;
   if (lane < n && rank < k) merged[rank] = x;
   wave_sync();
   l = merged[lane];
@@ -210,7 +223,7 @@ struct Vectors {
 template <class T>
 __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int PER = Vectors<T>::PER, kVecs = 16 / PER;
-  __shared__ List found[4][64], merged[4][64];
+  __shared__ uint64_t found[4][64], merged[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
   const int row = (int)(id / a.segs), seg = (int)(id % a.segs);
@@ -220,9 +233,8 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
   float top = kLowest;          // the lane's reference: its largest logit so far, less 600 at most
   const Exp exp;
   double sum = 0.0;
-  List best{-INFINITY, -1};
-  float least = -INFINITY;      // only what is above, or as good with a token below, can be one of the k best
-  int least_y = -1;
+  uint64_t best = 0;
+  float least = -INFINITY;      // only what is above can be one of the k best: tokens come in ascending order
   bool first = true;
   constexpr int kStep = 64 * kVecs;
   const T* at_lane = vec.row + (int64_t)(v0 + lane) * PER;
@@ -275,45 +287,40 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
         for (int i = 0; i < PER; ++i) half[i & 1] = fmaxf(half[i & 1], z[j][i]);
       least = float_below(kth_bound(half, a.k));
     }
-    if (__ballot(most >= least) == 0) continue;
-    // What can be among the k best, side by side, and into the list.
+    if (__ballot(most > least) == 0) continue;
+    // What can be among the k best, side by side, and into the list.  Within a batch the
+    // order is another: once the bound has risen in it, what equals the bound passes too.
     int n = 0;
+    float kth = least;
     auto flush = [&]() {
       wave_sync();
       if (n > kFew) {
         merge(best, found[wave], merged[wave], n, a.k, lane);
       } else {
-        for (int q = 0; q < n; ++q) {
-          const List x = found[wave][q];
-          insert(best, x.z, x.y, lane);
-        }
+        for (int q = 0; q < n; ++q) insert(best, found[wave][q], lane);
       }
       n = 0;
-      const float kth = lane_value(best.z, a.k - 1);
-      if (kth >= least) {
-        least = kth;
-        least_y = __builtin_amdgcn_readlane(best.y, a.k - 1);
-      }
+      kth = fmaxf(least, logit_of(lane_value64(best, a.k - 1)));
     };
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-      if (__ballot(m[j] >= least) == 0) continue;
+      if (__ballot(m[j] > least) == 0) continue;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int y = (v + 64 * j + lane) * PER + i;
-        auto passing = [&]() {
-          return __ballot(z[j][i] > least) | (__ballot(z[j][i] == least) & __ballot(y < least_y));
-        };
-        uint64_t pass = passing();
+        uint64_t pass = __ballot(z[j][i] > least);
+        if (pass == 0) continue;
         if (n + __popcll(pass) > 64) {
           flush();
-          pass = passing();
+          least = float_below(kth);
+          pass = __ballot(z[j][i] > least);
         }
-        if (pass >> lane & 1) found[wave][n + __popcll(pass & ((1ull << lane) - 1))] = List{z[j][i], y};
+        const int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(pass >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)pass, n));
+        if (pass >> lane & 1) found[wave][at] = key_of(z[j][i], (v + 64 * j + lane) * PER + i);
         n += __popcll(pass);
       }
     }
     flush();
+    least = kth;
   }
   // over the wave
   float all = top;
@@ -328,8 +335,8 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
     a.sums[at] = sum;
   }
   if (lane < a.k) {
-    a.cand_z[at * a.k + lane] = best.z;
-    a.cand_y[at * a.k + lane] = best.y;
+    a.cand_z[at * a.k + lane] = logit_of(best);
+    a.cand_y[at * a.k + lane] = best ? token_of(best) : -1;
   }
 }
 
@@ -343,19 +350,6 @@ __device__ __forceinline__ bool better(const Cand& p, const Cand& q) {
   return (p.s > q.s) | ((p.s == q.s) & (p.id < q.id));
 }
 __device__ __forceinline__ uint64_t id_of(int w, int y) { return (uint64_t)(uint32_t)w << 32 | (uint32_t)y; }
-template <class X>
-__device__ __forceinline__ X lane_value64(X x, int lane) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
-  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
-}
-template <class X>
-__device__ __forceinline__ X from_below64(X x) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = from_below((int)(uint32_t)b), hi = from_below((int)(uint32_t)(b >> 32));
-  return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
-}
-
 constexpr int kPick = 512;         // threads
 constexpr int kHeads = kPick / 2;  // candidates that bound the k-th best
 constexpr int kListed = 1024;      // candidates that can be ranked side by side
