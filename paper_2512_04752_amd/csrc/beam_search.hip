@@ -412,16 +412,18 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   const int rows_at_once = 64 / lanes, sub = lane & (lanes - 1);
   for (int w0 = wave * rows_at_once; w0 < a.width; w0 += kWaves * rows_at_once) {
     const int w = w0 + lane / lanes, row = g * a.width + min(w, a.width - 1);
+    // The first segment of every lane before anything waits, then the others.  (What is read
+    // of a beam that is not live is not used.)
+    const int i0 = min(sub, a.segs - 1);
+    const float s = a.scores[row], t0 = a.tops[(int64_t)row * a.segs + i0];
+    const double x0 = a.sums[(int64_t)row * a.segs + i0];
     const bool live = beam_live(a, row);
-    const float s = a.scores[row];
-    float top = -INFINITY;
-    // of a beam that is not live this is not written, and not used
-#pragma unroll 4
-    for (int i = sub; i < a.segs; i += lanes) top = __builtin_elementwise_maximum(top, a.tops[(int64_t)row * a.segs + i]);
+    float top = t0;
+    for (int i = sub + lanes; i < a.segs; i += lanes)
+      top = __builtin_elementwise_maximum(top, a.tops[(int64_t)row * a.segs + i]);
     for (int x = lanes / 2; x >= 1; x >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, x));
-    double sum = 0.0;
-#pragma unroll 4
-    for (int i = sub; i < a.segs; i += lanes)
+    double sum = sub < a.segs ? exp.scaled(x0, (double)t0 - (double)top) : 0.0;
+    for (int i = sub + lanes; i < a.segs; i += lanes)
       sum += exp.scaled(a.sums[(int64_t)row * a.segs + i], (double)a.tops[(int64_t)row * a.segs + i] - (double)top);
     for (int x = lanes / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
     if (sub == 0 && w < a.width) {
@@ -470,16 +472,16 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     least_score = fmax(least_score, kth_of(head));
   }
   for (int at = 0; at < k && lists_open > 0; at += deep) {
-    bool some = false;
+    bool more = false;                           // a list's last entry here passes
     for (int i = threadIdx.x; i < block; i += kPick) {
       const Cand c = opened_entry(i, at);
       if (c.s >= least_score && c.s > -INFINITY) {
-        some = true;
+        more |= i >= block - lists_open;
         const int to = atomicAdd(&count, 1);
         if (to < kListed) listed[to] = c;
       }
     }
-    if (!__syncthreads_or(some)) break;          // the lists are sorted
+    if (!__syncthreads_or(more)) break;          // the lists are sorted
   }
   __syncthreads();
   int n = count;
