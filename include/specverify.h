@@ -328,13 +328,14 @@ enum {
 };
 
 /* Workspace bytes that a product of up to max_n rows of x with one such matrix (or, in
- * spec_w4_gate_up, with two) may need.  May be 0, also if an argument is invalid. */
+ * spec_w4_gate_up, with two) may need.  May be 0, also if an argument is invalid.  (A search
+ * over n, up to a millisecond: for setting up, not for every call.) */
 size_t spec_w4_workspace_bytes(int32_t rows, int32_t cols, int32_t max_n);
 
-/* Products of n >= 0 rows.  The weights enter as the numbers they stand for, sums are
+/* Products of 0 <= n <= 2^20 rows (n * rows <= 2^34).  The weights enter as the numbers they stand for, sums are
  * fp32, in an order that depends on the shapes and n alone.
- *   x          device bf16 [n][cols], row i at i * x_stride (a multiple of 8; 16-byte
- *              aligned)
+ *   x          device bf16 [n][cols], row i at i * x_stride (a multiple of 8, at most 2^28;
+ *              16-byte aligned)
  *   out        device, row i at i * out_stride (in values, any stride >= rows; aligned
  *              as its type), of type `kind`
  *   workspace  device, 256-byte aligned; may be NULL where no bytes are needed.  Calls
@@ -359,8 +360,8 @@ int spec_w4_gate_up(const spec_w4* gate, const spec_w4* up, const void* x, int64
  *   scores       device fp32 [groups][width], e.g. log probabilities so far
  *   last_tokens  device int32 [groups][width], or NULL: the beams' last tokens, read
  *                when eos_token >= 0
- * Candidate (w, y) scores scores[w] + log softmax(logits of w)[y], computed in fp64.  A
- * beam whose last token is eos_token has ended: it offers (w, eos_token) alone, at
+ * Candidate (w, y) scores scores[w] + log softmax(logits of w)[y], in fp64, the logarithm
+ * of the sum to 1e-9 (and the same for equal rows).  A beam whose last token is eos_token has ended: it offers (w, eos_token) alone, at
  * scores[w].  No candidates: tokens whose logit is -infinity; beams whose score is not
  * finite; live beams with a logit that is NaN or +infinity.
  * Outputs, per group the k best, best first, the lower (w, y) of equal scores first:

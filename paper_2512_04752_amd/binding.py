@@ -794,6 +794,7 @@ class W4Matrix:
         self.data = _made_workspace(nbytes, self.index, stream)
         spec_w4_pack(w, self.data, stream)
         self.struct = spec_w4(self.data.data_ptr(), self.rows, self.cols)
+        self.needs = {}                      # workspace bytes by rows of x
 
     def unpack(self, out=None, stream=None):
         """What the matrix stands for, as bf16."""
@@ -807,7 +808,9 @@ class W4Matrix:
 def _w4_workspace(m, n, workspace, stream):
     if workspace is not None:
         return _device_workspace(workspace, m.index)
-    nbytes = lib().spec_w4_workspace_bytes(m.rows, m.cols, n)
+    nbytes = m.needs.get(n)
+    if nbytes is None:                       # asked once: the library searches
+        nbytes = m.needs[n] = lib().spec_w4_workspace_bytes(m.rows, m.cols, n)
     if nbytes == 0:
         return None, 0
     workspace = _made_workspace(nbytes, m.index, stream)

@@ -11,6 +11,7 @@ using namespace spec;
 namespace {
 
 constexpr int kMaxDim = 1 << 24, kMaxN = 1 << 20;
+constexpr int64_t kMaxStride = 1 << 28, kMaxOut = 1ll << 34;     // values
 
 bool dims_ok(int32_t rows, int32_t cols) {
   return rows >= 1 && cols >= 1 && cols % 32 == 0 && rows <= kMaxDim && cols <= kMaxDim;
@@ -54,6 +55,10 @@ int product(const spec_w4* m, const spec_w4* up, const void* x, int64_t x_stride
   if (n < 0) return fail(SPEC_ERR_INVALID, "n = %d", n);
   if (n > kMaxN) return fail(SPEC_ERR_UNSUPPORTED, "%d rows, at most %d in one call", n, kMaxN);
   if (int rc = check_rows("x", x, x_stride, m->cols)) return rc;
+  if (x_stride > kMaxStride)
+    return fail(SPEC_ERR_UNSUPPORTED, "x: row stride %lld, at most %lld", (long long)x_stride, (long long)kMaxStride);
+  if ((int64_t)n * m->rows > kMaxOut)
+    return fail(SPEC_ERR_UNSUPPORTED, "%d x %d outputs, at most %lld in one call", n, m->rows, (long long)kMaxOut);
   if (out_stride < m->rows) return fail(SPEC_ERR_INVALID, "out: row stride %lld below %d", (long long)out_stride, m->rows);
   if ((uintptr_t)out % (kind == SPEC_W4_BF16 ? 2 : 4)) return fail(SPEC_ERR_INVALID, "out not aligned to its type");
   const size_t need = w4_partial_bytes(m->rows, m->cols, n, up != nullptr);
@@ -112,7 +117,7 @@ SPEC_API int spec_w4_unpack(const spec_w4* m, void* w, int64_t stride, void* str
 SPEC_API size_t spec_w4_workspace_bytes(int32_t rows, int32_t cols, int32_t max_n) {
   if (!dims_ok(rows, cols) || max_n < 1) return 0;
   size_t most = 0;
-  for (int n = 1; n <= max_n; ++n)
+  for (int n = 1; n <= std::min<int>(max_n, kMostSplitRows); ++n)
     for (const bool pair : {false, true}) most = std::max(most, w4_partial_bytes(rows, cols, n, pair));
   return align_up(most);
 }

@@ -471,7 +471,7 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 }  // namespace
 
 // Up to 16 rows: the stream kernel, x in LDS over as few column splits as its place there
-// allows, and as many waves to a row tile as still leave one round of work-groups.  (us, the
+// allows (unless these are many), and as many waves to a row tile as still leave one round of work-groups.  (us, the
 // splits cold: 1 row 4096 x 14336, 16 / 8 / 4 / 2 waves 9.3 / 9.9 / 12.6 / 19.5; gate/up of 4 rows,
 // 14336 x 4096, 17.9 / 14.8 / 14.0 / 15.3; head of 1 row, 128256 x 4096, 73 / 54 / 52 / 50 and
 // alone 49; 16 rows 4096 x 14336 in 4 splits 16.2 / 14.3 / 13.8 / 14.4, in 8 no better.)
@@ -486,11 +486,12 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 // 19 % (4096 x 4096, 768 rows).
 W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   const int tiles = (rows + 15) / 16, mats = gate_up ? 2 : 1, T = w4_col_tiles(cols);
+  auto partials = [&](int splits) { return 4.0 * splits * mats * n * tiles * 16; };      // bytes
   if (n <= 16) {
     W4Plan p{W4_STREAM, kStreamWaves, 1};
-    while (stream_lds(cols, n, mats, p) > kLds) ++p.splits;
+    while (p.splits <= 16 && stream_lds(cols, n, mats, p) > kLds) ++p.splits;
     while (p.wide > 1 && (int64_t)tiles * p.wide * p.splits > 256 * kStreamWaves) p.wide /= 2;
-    return p;
+    if (p.splits <= 16 && (p.splits == 1 || partials(p.splits) <= kPartialCap)) return p;
   }
   struct Tile {
     W4Shape shape;
@@ -508,8 +509,8 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   for (const Tile& s : shapes) {
     if (s.shape == W4_TILE32W && n > s.bm) continue;      // its weights would pass once per 32 rows
     const int64_t count = ((int64_t)n + s.bm - 1) / s.bm * (((int64_t)tiles * mats + s.bt - 1) / s.bt);
-    for (int splits = 1; splits <= 16; ++splits) {
-      const double part = 4.0 * splits * mats * n * tiles * 16;
+    for (int splits = 1; splits <= (n <= kMostSplitRows ? 16 : 1); ++splits) {
+      const double part = partials(splits);
       if (splits > 1 && (T / splits < 4 || part > kPartialCap)) break;
       const int64_t wgs = count * splits;
       const double steps = (T + splits * s.kg - 1) / (splits * s.kg), at_once = 256.0 * s.slots;

@@ -45,7 +45,8 @@ def linear(m=(P, 48, 64), x=P, x_stride=64, n=3, out=P, out_stride=48, kind=1, w
     (dict(m=(P + 128, 48, 64)), INVALID), (dict(m=(P, 0, 64)), INVALID), (dict(m=(P, 48, 40)), UNSUPPORTED),
     (dict(x=P + 8), INVALID), (dict(x_stride=63), INVALID), (dict(x_stride=68), INVALID), (dict(x_stride=56), INVALID),
     (dict(n=-1), INVALID), (dict(n=(1 << 20) + 1), UNSUPPORTED), (dict(out=P + 2), INVALID), (dict(out_stride=47), INVALID),
-    (dict(kind=0, out=P + 1), INVALID), (dict(kind=3), INVALID), (dict(kind=-1), INVALID)])
+    (dict(x_stride=(1 << 28) + 8), UNSUPPORTED),
+    (dict(m=(P, 1 << 24, 64), n=1025, out_stride=1 << 24), UNSUPPORTED), (dict(kind=0, out=P + 1), INVALID), (dict(kind=3), INVALID), (dict(kind=-1), INVALID)])
 def test_linear_refusals(changed, code):
     assert linear(**changed) == code
     assert B.lib().spec_last_error()

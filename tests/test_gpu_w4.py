@@ -162,6 +162,34 @@ def test_gate_up(shape, n):
     check(out, want, bound * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want))
 
 
+@pytest.mark.parametrize("rows,cols,n", [(40, 70016, 16), (17, 70016, 1), (24, 300000, 16), (5, 131072, 3), (33, 64, 5000),
+                                         (64, 4096, 4097)])
+def test_long_and_tall(rows, cols, n):
+    """Columns that take many pieces of LDS, or more than it has; rows in the thousands."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    m = sv.W4Matrix(torch.empty(rows, cols, device="cuda").normal_(0, 0.02, generator=gen).bfloat16())
+    x = torch.empty(n, cols, device="cuda").normal_(0, 1, generator=gen).bfloat16()
+    held = m.unpack().double().T.contiguous()
+    want, A = x.double() @ held, x.double().abs() @ held.abs()
+    out = torch.empty(n, rows, device="cuda")
+    sv.spec_w4_linear(m, x, out)
+    check(out, want.cpu().numpy(), sum_bound(cols, A.cpu().numpy()))
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_rows_gigabytes_apart(n):
+    """The last token's state of long samples: one row of every 128 MB."""
+    rows, cols = 96, 256
+    m = sv.W4Matrix(numbers(1, rows, cols, std=0.02).cuda())
+    big = torch.empty(n, 1 << 26, dtype=torch.bfloat16, device="cuda")
+    x = big[:, 4096:4096 + cols]
+    x.copy_(numbers(n, n, cols))
+    out = torch.empty(n, rows, device="cuda")
+    sv.spec_w4_linear(m, x, out)
+    want, A = O.linear(x.double().cpu().numpy(), unpacked(m))
+    check(out, want, sum_bound(cols, A))
+
+
 @pytest.mark.parametrize("n", [1, 20, 70, 300])
 def test_strided_and_unaligned(n):
     """Rows of a fused projection's output in, columns of a wider buffer out, at odd places."""
