@@ -392,7 +392,8 @@ int spec_beam_select(const void* logits, int64_t row_stride, int32_t bf16, int32
  *   sample_ids  host [groups][width]   distinct
  *   begin, end  host [groups]          0 <= begin <= end <= every beam's capacity
  *   parents     device int32 [groups][width]
- * 1 <= width <= SPEC_MAX_BEAMS.  Descriptors are uploaded: a capturing stream is refused. */
+ * 1 <= width <= SPEC_MAX_BEAMS.  A large call uploads descriptors: a capturing stream is
+ * refused. */
 int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
                     const int32_t* begin, const int32_t* end, const int32_t* parents, void* stream);
 
@@ -549,9 +550,10 @@ int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_ids, cons
 
 /* spec_kv_reorder for this pool: codes and scales move.  The pages of positions
  * [begin[g], end[g]) of every beam must not be shared (SPEC_ERR_INVALID).
- *   workspace  device, 256-byte aligned, spec_kv4_reorder_bytes(groups, width, pages) with
- *              pages >= those that any group's range touches; the call's until it has run */
-size_t spec_kv4_reorder_bytes(int32_t groups, int32_t width, int32_t max_pages);
+ *   workspace  device, 256-byte aligned, spec_kv4_reorder_bytes(kv, groups, width, pages) with
+ *              pages >= those that any group's range touches (0 for a small call: it may
+ *              be NULL then); the call's until it has run */
+size_t spec_kv4_reorder_bytes(const spec_kv4* kv, int32_t groups, int32_t width, int32_t max_pages);
 int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
                      const int32_t* begin, const int32_t* end, const int32_t* parents, void* workspace,
                      size_t ws_bytes, void* stream);

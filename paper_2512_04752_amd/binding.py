@@ -172,10 +172,10 @@ def lib():
     L.spec_beam_select.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p,
                                    c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
                                    c_void_p]
-    L.spec_kv_reorder.argtypes = [c_void_p, c_int32, c_int32, i32p, i32p, i32p, c_void_p, c_void_p]
-    L.spec_kv4_reorder_bytes.argtypes = [c_int32] * 3
-    L.spec_kv4_reorder.argtypes = [c_void_p, c_int32, c_int32, i32p, i32p, i32p, c_void_p, c_void_p, c_size_t,
-                                   c_void_p]
+    L.spec_kv_reorder.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    L.spec_kv4_reorder_bytes.argtypes = [c_void_p, c_int32, c_int32, c_int32]
+    L.spec_kv4_reorder.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_size_t, c_void_p]
     for name in ("spec_w4_bytes", "spec_w4_workspace_bytes", "spec_beam_workspace_bytes", "spec_kv4_reorder_bytes"):
         getattr(L, name).restype = c_size_t
     for name in ("spec_w4_pack", "spec_w4_unpack", "spec_w4_linear", "spec_w4_gate_up", "spec_beam_select",
@@ -906,48 +906,57 @@ def spec_beam_select(logits, scores, parents, tokens, new_scores, last_tokens=No
 
 
 def _reorder_arrays(pool_index, sample_ids, begin, end, parents):
-    ids = np.ascontiguousarray(sample_ids, dtype=np.int32)
+    """int32 arrays of a reorder call's host arguments."""
+    ids, b, e = (np.ascontiguousarray(x, dtype=np.int32) for x in (sample_ids, begin, end))
     if ids.ndim != 2:
         raise ValueError("sample_ids must be [groups, width]")
-    (b, p_b), (e, p_e) = _i32(begin), _i32(end)
     if b.shape != ids.shape[:1] or e.shape != b.shape:
         raise ValueError("begin and end must have one entry per group")
-    if parents.dtype is not torch.int32 or parents.shape != torch.Size(ids.shape) or not parents.is_contiguous() \
+    if parents.dtype is not torch.int32 or parents.shape != ids.shape or not parents.is_contiguous() \
             or parents.get_device() != pool_index:
         raise ValueError(f"parents must be a contiguous int32 tensor of {ids.shape} on the pool's device")
-    return ids, p_b, p_e, (b, e)
+    return ids, b, e
 
 
 def spec_kv_reorder(pool: KVPool, sample_ids, begin, end, parents, stream=None):
     """Beam j of group g (sample sample_ids[g][j]) takes what beam parents[g][j] holds at positions
     [begin[g], end[g])."""
     index = pool.buf.get_device()
-    ids, p_b, p_e, kept = _reorder_arrays(index, sample_ids, begin, end, parents)
+    ids, b, e = _reorder_arrays(index, sample_ids, begin, end, parents)
     if pool.handle is None:
         raise ValueError("the pool is closed")
     with _on(index):
-        _check(lib().spec_kv_reorder(pool.handle, *ids.shape, _pointer(ids, c_int32), p_b, p_e, parents.data_ptr(),
-                                     _device_stream(index, stream)))
+        rc = lib().spec_kv_reorder(pool.handle, *ids.shape, ids.ctypes.data, b.ctypes.data, e.ctypes.data,
+                                   parents.data_ptr(), _device_stream(index, stream))
+    if rc:
+        _check(rc)
 
 
-def spec_kv4_reorder_bytes(groups, width, max_pages) -> int:
-    return int(lib().spec_kv4_reorder_bytes(groups, width, max_pages))
+def spec_kv4_reorder_bytes(pool: KV4Pool, groups, width, max_pages) -> int:
+    return int(lib().spec_kv4_reorder_bytes(pool.handle, groups, width, max_pages))
 
 
 def spec_kv4_reorder(pool: KV4Pool, sample_ids, begin, end, parents, workspace=None, stream=None):
     """spec_kv_reorder for a 4-bit pool; workspace: a uint8 tensor of spec_kv4_reorder_bytes
-    (allocated when None)."""
-    ids, p_b, p_e, (b, e) = _reorder_arrays(pool.index, sample_ids, begin, end, parents)
+    (allocated when None and needed)."""
+    index = pool.index
+    ids, b, e = _reorder_arrays(index, sample_ids, begin, end, parents)
     if pool.handle is None:
         raise ValueError("the pool is closed")
-    if workspace is None:
-        pages = int(np.max((e.astype(np.int64) + SPEC_KV4_PAGE - 1) // SPEC_KV4_PAGE - b // SPEC_KV4_PAGE, initial=1))
-        nbytes = lib().spec_kv4_reorder_bytes(*ids.shape, max(1, min(pages, pool.n_pages)))
-        workspace = _made_workspace(max(256, nbytes), pool.index, stream)
-    p, nbytes = _device_workspace(workspace, pool.index)
-    with _on(pool.index):
-        _check(lib().spec_kv4_reorder(pool.handle, *ids.shape, _pointer(ids, c_int32), p_b, p_e, parents.data_ptr(), p,
-                                      nbytes, _device_stream(pool.index, stream)))
+    p, nbytes = None, 0
+    if workspace is not None:
+        p, nbytes = _device_workspace(workspace, index)
+    elif ids.size:
+        pages = min((int(e.max()) - 1) // SPEC_KV4_PAGE - int(b.min()) // SPEC_KV4_PAGE + 1, pool.n_pages)
+        nbytes = lib().spec_kv4_reorder_bytes(pool.handle, *ids.shape, max(1, pages))
+        if nbytes:
+            workspace = _made_workspace(nbytes, index, stream)
+            p = workspace.data_ptr()
+    with _on(index):
+        rc = lib().spec_kv4_reorder(pool.handle, *ids.shape, ids.ctypes.data, b.ctypes.data, e.ctypes.data,
+                                    parents.data_ptr(), p, nbytes, _device_stream(index, stream))
+    if rc:
+        _check(rc)
 
 
 class CostModel:

@@ -795,28 +795,33 @@ SPEC_API int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const i
     if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
     if (int rc = check_reorder(kv->n, groups, width, sample_ids, begin, end, parents)) return rc;
     ReorderBeams beams;
-    std::vector<ReorderBeam> many;
-    const bool small = groups * width <= kInlineBeams;
-    if (!small) many.resize((size_t)groups * width);
-    ReorderBeam* info = small ? beams.here : many.data();
+    const int total = groups * width;
+    const bool small = groups <= kInlineGroups && total <= kInlineBeams;
+    // [groups], [groups * width]: at most 24 bytes per sample, which the control area has
+    std::vector<char> blob(small ? 0 : groups * sizeof(ReorderGroup) + total * sizeof(ReorderBeam));
+    ReorderGroup* group = small ? beams.groups_here : (ReorderGroup*)blob.data();
+    ReorderBeam* beam = small ? beams.beams_here : (ReorderBeam*)(group + groups);
     int most = 0;
     for (int g = 0; g < groups; ++g) {
       most = std::max(most, end[g] - begin[g]);
+      group[g] = ReorderGroup{begin[g], end[g], 0, 0};
       for (int j = 0; j < width; ++j) {
         const int id = sample_ids[g * width + j];
         if (end[g] > kv->cap[id])
           return fail(SPEC_ERR_CAPACITY, "group %d: positions up to %d exceed sample %d's capacity %d", g, end[g], id,
                       kv->cap[id]);
-        info[g * width + j] = ReorderBeam{kv->base[id], kv->cap[id], begin[g], end[g], {}};
+        if (kv->base[id] / 128 > 0xffffffffll) return fail(SPEC_ERR_UNSUPPORTED, "a pool of more than 1 TB");
+        beam[g * width + j] = ReorderBeam{(uint32_t)(kv->base[id] / 128), kv->cap[id]};
       }
     }
     if (int rc = refuse_capture(stream)) return rc;
     if (most == 0 || width == 1) return SPEC_OK;
     hipStream_t s = (hipStream_t)stream;
-    void* ctl = (char*)kv->pool + kv->ctl_off;
-    beams.device = small ? nullptr : (const ReorderBeam*)ctl;
+    char* ctl = (char*)kv->pool + kv->ctl_off;
+    beams.groups = small ? nullptr : (const ReorderGroup*)ctl;
+    beams.beams = small ? nullptr : (const ReorderBeam*)(ctl + groups * sizeof(ReorderGroup));
     if (!small)
-      if (int rc = kv->ring.upload(many.data(), many.size() * sizeof(ReorderBeam), ctl, s)) return rc;
+      if (int rc = kv->ring.upload(blob.data(), blob.size(), ctl, s)) return rc;
     const spec_model_config& c = kv->cfg;
     HIP_TRY(timed(SPEC_K_REORDER, s, [&] {
               return launch_reorder(beams, groups, width, most, kv->pool, c.n_layers, c.n_kv_heads,

@@ -556,22 +556,24 @@ SPEC_API int spec_kv4_commit(spec_kv4* kv, int32_t batch, const int32_t* sample_
 
 namespace {
 
-size_t reorder_bytes(int64_t groups, int64_t width, int64_t pages) {
-  return align_up(groups * sizeof(ReorderGroup)) + align_up(groups * width * pages * 4);
+// Whether a call's descriptors go along as kernel arguments.
+bool reorder_inline(const spec_kv4* kv, int64_t groups, int64_t pages_in_all) {
+  return groups <= kInlineGroups && pages_in_all <= kInlinePages && kv->uses.size() <= 65536;
 }
 
 }  // namespace
 
-SPEC_API size_t spec_kv4_reorder_bytes(int32_t groups, int32_t width, int32_t max_pages) {
-  if (groups < 1 || width < 1 || width > kMaxReorder || max_pages < 1) return 0;
-  return reorder_bytes(groups, width, max_pages);
+SPEC_API size_t spec_kv4_reorder_bytes(const spec_kv4* kv, int32_t groups, int32_t width, int32_t max_pages) {
+  if (!kv || groups < 1 || width < 1 || width > kMaxReorder || max_pages < 1) return 0;
+  const int64_t pages = (int64_t)groups * width * max_pages;
+  return reorder_inline(kv, groups, pages) ? 0 : align_up(groups * sizeof(ReorderGroup)) + align_up(pages * 4);
 }
 
 SPEC_API int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
                               const int32_t* begin, const int32_t* end, const int32_t* parents, void* workspace,
                               size_t ws_bytes, void* stream) {
   return guarded([&]() -> int {
-    if (!kv || !workspace) return fail(SPEC_ERR_INVALID, "null argument");
+    if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
     if (int rc = check_reorder(kv->n, groups, width, sample_ids, begin, end, parents)) return rc;
     std::vector<ReorderGroup> info(groups);
     std::vector<int32_t> table;
@@ -592,14 +594,16 @@ SPEC_API int spec_kv4_reorder(spec_kv4* kv, int32_t groups, int32_t width, const
       }
     }
     if (most > 65535) return fail(SPEC_ERR_UNSUPPORTED, "a range of %lld pages, at most 65535", (long long)most);
+    const bool small = reorder_inline(kv, groups, (int64_t)table.size());
+    const size_t head = align_up(groups * sizeof(ReorderGroup)), need = small ? 0 : head + table.size() * 4;
+    if (need && (!workspace || ws_bytes < need))
+      return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", workspace ? ws_bytes : 0, need);
     if ((uintptr_t)workspace % kAlign) return fail(SPEC_ERR_INVALID, "workspace not 256-byte aligned");
-    const size_t head = align_up(groups * sizeof(ReorderGroup)), need = head + table.size() * 4;
-    if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
     if (int rc = refuse_capture(stream)) return rc;
     if (most == 0 || width == 1) return SPEC_OK;
     hipStream_t s = (hipStream_t)stream;
     ReorderPages pages;
-    if (groups <= kInlineGroups && table.size() <= kInlinePages && kv->uses.size() <= 65536) {
+    if (small) {
       pages.groups = nullptr;
       std::copy(info.begin(), info.end(), pages.groups_here);
       std::copy(table.begin(), table.end(), pages.table_here);

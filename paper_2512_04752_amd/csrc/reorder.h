@@ -9,27 +9,26 @@ constexpr int kMaxReorder = SPEC_MAX_BEAMS;      // beams of a group
 
 // One beam over the bf16 pool.
 struct ReorderBeam {
-  int64_t kv_base;      // element offset of the sample's block
+  uint32_t block;       // the sample's block, in units of 256 bytes
   int32_t cap;          // positions per (layer, K/V, kv head)
-  int32_t begin, end;   // its group's range
-  int32_t pad[3];
 };
-static_assert(sizeof(ReorderBeam) == 32, "ReorderBeam layout");
 
-// One group over the 4-bit pool.
+// One group.
 struct ReorderGroup {
   int32_t begin, end;
-  int32_t pages;        // that the range touches, of every beam
+  int32_t pages;        // 4-bit pool: that the range touches, of every beam
   int32_t table;        // its first entry in the table: [width][pages] page ids
 };
 static_assert(sizeof(ReorderGroup) == 16, "ReorderGroup layout");
 
 // Descriptors of a small call go along as kernel arguments (an upload takes the host 5 us, and
 // the stream as long); of a larger one they lie in device memory.
-constexpr int kInlineBeams = 96, kInlineGroups = 32, kInlinePages = 1440;
+constexpr int kInlineBeams = 288, kInlineGroups = 64, kInlinePages = 1216;
 struct ReorderBeams {
-  const ReorderBeam* device;             // NULL: here
-  ReorderBeam here[kInlineBeams];
+  const ReorderGroup* groups;            // NULL: here
+  const ReorderBeam* beams;
+  ReorderGroup groups_here[kInlineGroups];
+  ReorderBeam beams_here[kInlineBeams];
 };
 struct ReorderPages {
   const ReorderGroup* groups;            // NULL: here

@@ -130,7 +130,7 @@ def test_beam_workspace():
 
 def arrays(ids, begin, end):
     out = [np.ascontiguousarray(x, dtype=np.int32) for x in (ids, begin, end)]
-    return out, [x.ctypes.data_as(B.POINTER(B.c_int32)) for x in out]
+    return out, [x.ctypes.data for x in out]
 
 
 REORDERS = [
@@ -159,22 +159,34 @@ def test_reorder_refusals(changed, code):
         assert L.spec_kv4_map(h, s, 2, (ctypes.c_int32 * 2)(2 * s, 2 * s + 1)) == 0
     call = (a["groups"], a["width"], ids, begin, end, a["parents"])
     assert L.spec_kv4_reorder(h, *call, P, 1 << 20, None) == code
-    if code == CAPACITY:                 # pages that are not there, or another sample's too
-        _, (ids, begin, end) = kept, arrays([0, 1, 2, 3], [0, 64], [64, 65])[1]
-        assert L.spec_kv4_reorder(h, 2, 2, ids, begin, end, P, P, 256, None) == WORKSPACE
+    if code == CAPACITY:                 # another sample's page too; the right workspace only
+        kept, (ids, begin, end) = arrays([0, 1, 2, 3], [0, 64], [64, 65])
         assert L.spec_kv4_reorder(h, 2, 2, ids, begin, end, P, P + 16, 1 << 20, None) == INVALID
-        assert L.spec_kv4_reorder(h, 2, 2, ids, begin, end, P, None, 1 << 20, None) == INVALID
         assert L.spec_kv4_map(h, 3, 2, (ctypes.c_int32 * 2)(6, 5)) == 0      # page 5: position 64 .. of sample 2
         assert L.spec_kv4_reorder(h, 2, 2, ids, begin, end, P, P, 1 << 20, None) == INVALID
         assert b"mapped to 2" in L.spec_last_error()
     L.spec_kv4_free(h)
 
 
-def test_kv4_reorder_bytes():
-    assert sv.spec_kv4_reorder_bytes(2, 3, 5) == 256 + 256
-    assert sv.spec_kv4_reorder_bytes(100, 8, 100) == 1792 + 100 * 8 * 100 * 4
-    for bad in ((0, 1, 1), (1, 0, 1), (1, 65, 1), (1, 1, 0)):
-        assert sv.spec_kv4_reorder_bytes(*bad) == 0
+def test_kv4_reorder_workspace():
+    """Small calls' descriptors go along as kernel arguments; others need room for theirs."""
+    L, h, c = B.lib(), ctypes.c_void_p(), B.make_config(wl.TINY)
+    n = 140
+    assert L.spec_kv4_alloc(ctypes.byref(c), n, 10 * n, P, 1 << 40, ctypes.byref(h)) == 0
+    size = L.spec_kv4_reorder_bytes
+    assert size(h, 2, 2, 10) == size(h, 64, 1, 19) == 0
+    assert size(h, 65, 1, 1) == 1280 + 512
+    assert size(h, 100, 8, 100) == 1792 + 100 * 8 * 100 * 4
+    for bad in ((None, 1, 1, 1), (h, 0, 1, 1), (h, 1, 0, 1), (h, 1, 65, 1), (h, 1, 1, 0)):
+        assert size(*bad) == 0
+    for s in range(n):
+        assert L.spec_kv4_map(h, s, 10, (ctypes.c_int32 * 10)(*range(10 * s, 10 * s + 10))) == 0
+    kept, (ids, begin, end) = arrays(range(n), [0] * 7, [640] * 7)
+    need = size(h, 7, 20, 10)
+    assert need >= 256 + 7 * 20 * 10 * 4
+    for ws, nbytes in ((None, 1 << 20), (P, 256)):
+        assert L.spec_kv4_reorder(h, 7, 20, ids, begin, end, P, ws, nbytes, None) == WORKSPACE
+    L.spec_kv4_free(h)
 
 
 # ---- the oracle itself -------------------------------------------------------

@@ -41,7 +41,7 @@ KINDS = ["any", "cycle", "one", "stay", "none"]
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("kv_heads,d,layers,groups,width", [
     (2, 64, 1, 1, 1), (2, 64, 2, 3, 2), (1, 128, 2, 2, 8), (2, 64, 1, 2, 9), (3, 128, 1, 2, 17), (1, 128, 1, 2, 33),
-    (2, 64, 1, 1, 64), (2, 64, 1, 40, 5)], ids=str)
+    (2, 64, 1, 1, 64), (2, 64, 1, 60, 5), (2, 64, 1, 70, 2)], ids=str)
 def test_bf16_pool(kv_heads, d, layers, groups, width, kind):
     rng = np.random.default_rng(width)
     cfg = config(kv_heads, d, layers)
@@ -76,7 +76,7 @@ def test_bf16_pool(kv_heads, d, layers, groups, width, kind):
 @pytest.mark.parametrize("kv_heads,d,layers,groups,width,begin,end", [
     (2, 64, 1, 2, 2, 0, 1), (2, 64, 2, 3, 3, 5, 64), (1, 128, 2, 2, 8, 63, 65), (2, 64, 1, 1, 9, 64, 128),
     (2, 128, 1, 1, 17, 1, 200), (1, 128, 1, 1, 33, 130, 139), (2, 64, 1, 1, 64, 37, 100), (1, 128, 1, 2, 4, 70, 70),
-    (2, 64, 1, 34, 2, 60, 70), (2, 64, 1, 23, 20, 3, 190)], ids=str)
+    (2, 64, 1, 66, 2, 60, 70), (2, 64, 1, 23, 20, 3, 190)], ids=str)
 def test_kv4_pool(kv_heads, d, layers, groups, width, begin, end, kind):
     """Each head's bytes, position by position, from the layout."""
     rng = np.random.default_rng(width + end)
@@ -149,6 +149,6 @@ def test_refusals():
     with pytest.raises(sv.SpecError, match="mapped to 2"):
         sv.spec_kv4_reorder(kv4, ids, [0, 0], [1, 1], p)
     sv.spec_kv4_reorder(kv4, ids, [64, 0], [65, 1], p)
-    with pytest.raises(sv.SpecError, match="workspace"):
-        sv.spec_kv4_reorder(kv4, ids, [64, 0], [65, 1], p, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError, match="workspace"):
+        sv.spec_kv4_reorder(kv4, ids, [64, 0], [65, 1], p, workspace=torch.empty(256, device="cuda"))
     torch.cuda.synchronize()
