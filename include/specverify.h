@@ -289,8 +289,8 @@ int spec_kv_unpack(spec_kv* kv, int32_t n, const int32_t* sample_ids, const int3
 /* ---- Products with weights in 4 bits -----------------------------------
  *
  * Few rows through a model cost the bytes of its weights.  These products take
- * them in 4.25 bits per number, for a draft model, or for a target model's
- * matrices outside spec_verify: x . W^T as every GEMM here, with W quantised once.
+ * them in 4.25 bits per number: x . W^T as every GEMM here, with W quantised once.
+ * spec_verify_w4, below, runs a whole step with them.
  *
  * Numbers.  E2M1 codes times a power of two 2^e that 32 consecutive numbers of a
  * row share, as in the 4-bit cache below, with e >= -120: the smallest exponent in
@@ -540,6 +540,40 @@ int spec_verify_kv4(const spec_model_config* cfg, const spec_weights* w, spec_kv
                     const int32_t* tree_parents, const int32_t* seq_lens, void* workspace,
                     size_t ws_bytes, void* stream, const spec_sampling* samp, int32_t* accepted_len,
                     int32_t* next_token, int32_t* accepted_nodes, const spec_debug* dbg);
+
+/* ---- The verify step with weights in 4 bits ----------------------------
+ *
+ * spec_verify's step with these products in place of the bf16 ones: a draft model's
+ * steps, or a target's where its weights' bytes are the cost.  Norm gains and the
+ * embedding stay bf16.  Pointers of matrices as in spec_weights, 256-byte aligned. */
+typedef struct {
+  const void* tok_embed;        /* device bf16 [vocab][hidden] */
+  const void* final_norm;       /* device bf16 [hidden] */
+  spec_w4 lm_head;              /* [vocab][hidden] */
+  const void* const* attn_norm; /* host [n_layers] of device bf16 [hidden] */
+  const spec_w4* wqkv;          /* host [n_layers]: [(n_heads + 2 n_kv_heads) * head_dim][hidden],
+                                   the rows of q, then of k, then of v */
+  const spec_w4* wo;            /* host [n_layers]: [hidden][n_heads*head_dim] */
+  const void* const* ffn_norm;  /* host [n_layers] of device bf16 [hidden] */
+  const spec_w4* w_gate;        /* host [n_layers]: [ffn][hidden] */
+  const spec_w4* w_up;          /* host [n_layers]: [ffn][hidden] */
+  const spec_w4* w_down;        /* host [n_layers]: [hidden][ffn] */
+} spec_weights_w4;
+
+/* Workspace bytes spec_verify_w4 needs: max_pages 0 for a bf16 pool, otherwise as in
+ * spec_workspace_bytes_kv4; 0 if an argument is invalid. */
+size_t spec_workspace_bytes_w4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
+                               int32_t max_pages, int32_t sampled);
+
+/* spec_verify (samp NULL) or spec_verify_sampled with w, over the bf16 pool kv (kv4
+ * NULL) or the 4-bit one kv4 (kv NULL): otherwise the same arguments, outputs and
+ * commit as theirs or spec_verify_kv4's.  Refuses a capturing stream. */
+int spec_verify_w4(const spec_model_config* cfg, const spec_weights_w4* w, spec_kv* kv, spec_kv4* kv4,
+                   int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets,
+                   const int32_t* tree_tokens, const int32_t* tree_parents, const int32_t* seq_lens,
+                   void* workspace, size_t ws_bytes, void* stream, const spec_sampling* samp,
+                   int32_t* accepted_len, int32_t* next_token, int32_t* accepted_nodes,
+                   const spec_debug* dbg);
 
 /* spec_kv_commit for this pool: the codes and scales of node accepted_nodes[b][d]
  * move to position S_b + d for d = 1 .. accepted_len[b], all layers, and

@@ -36,8 +36,9 @@ EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_lay
            "spec_kv4_bytes", "spec_kv4_alloc", "spec_kv4_free", "spec_kv4_map",
            "spec_kv4_step_bytes", "spec_kv4_step_begin", "spec_kv4_step_free", "spec_kv4_append",
            "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit",
-           "spec_workspace_bytes_kv4", "spec_verify_kv4", "spec_w4_bytes", "spec_w4_pack",
-           "spec_w4_unpack", "spec_w4_workspace_bytes", "spec_w4_linear", "spec_w4_gate_up",
+           "spec_workspace_bytes_kv4", "spec_verify_kv4", "spec_workspace_bytes_w4",
+           "spec_verify_w4", "spec_w4_bytes", "spec_w4_pack", "spec_w4_unpack",
+           "spec_w4_workspace_bytes", "spec_w4_linear", "spec_w4_gate_up",
            "spec_beam_workspace_bytes", "spec_beam_select", "spec_kv_reorder",
            "spec_kv4_reorder_bytes", "spec_kv4_reorder")
 SPEC_KV4_PAGE = 64                # positions per page of the 4-bit pool
@@ -78,6 +79,13 @@ class spec_sampling(ctypes.Structure):
 
 class spec_w4(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("rows", c_int32), ("cols", c_int32)]
+
+
+class spec_weights_w4(ctypes.Structure):
+    _fields_ = [("tok_embed", c_void_p), ("final_norm", c_void_p), ("lm_head", spec_w4),
+                ("attn_norm", POINTER(c_void_p)), ("wqkv", POINTER(spec_w4)), ("wo", POINTER(spec_w4)),
+                ("ffn_norm", POINTER(c_void_p)), ("w_gate", POINTER(spec_w4)), ("w_up", POINTER(spec_w4)),
+                ("w_down", POINTER(spec_w4))]
 
 
 class spec_debug(ctypes.Structure):
@@ -159,6 +167,10 @@ def lib():
                                            c_int32]
     L.spec_workspace_bytes_kv4.restype = c_size_t
     L.spec_verify_kv4.argtypes = L.spec_verify_sampled.argtypes
+    L.spec_workspace_bytes_w4.argtypes = L.spec_workspace_bytes_kv4.argtypes
+    L.spec_workspace_bytes_w4.restype = c_size_t
+    L.spec_verify_w4.argtypes = [POINTER(spec_model_config), POINTER(spec_weights_w4), c_void_p,
+                                 *L.spec_verify_sampled.argtypes[2:]]
     w4 = POINTER(spec_w4)
     L.spec_w4_bytes.argtypes = [c_int32, c_int32]
     L.spec_w4_workspace_bytes.argtypes = [c_int32, c_int32, c_int32]
@@ -179,7 +191,8 @@ def lib():
     for name in ("spec_w4_bytes", "spec_w4_workspace_bytes", "spec_beam_workspace_bytes", "spec_kv4_reorder_bytes"):
         getattr(L, name).restype = c_size_t
     for name in ("spec_w4_pack", "spec_w4_unpack", "spec_w4_linear", "spec_w4_gate_up", "spec_beam_select",
-                 "spec_kv_reorder", "spec_kv4_reorder", "spec_verify_kv4", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
+                 "spec_kv_reorder", "spec_kv4_reorder", "spec_verify_kv4", "spec_verify_w4",
+                 "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_layout", "spec_verify",
                  "spec_kv_commit", "spec_profile_begin", "spec_profile_end", "spec_kv_pack",
                  "spec_kv_unpack", "spec_cost_model_create", "spec_cost_model_free",
                  "spec_cost_model_stats", "spec_select_draft_count", "spec_verify_sampled",
@@ -264,6 +277,7 @@ class KVPool:
         if nbytes == 0:
             raise SpecError(-1, "invalid KV pool request")
         self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.index = self.buf.get_device()
         self.handle = spec_kv_alloc(cfg, self.capacity, self.buf)
 
     def sample_view(self, sample):
@@ -665,6 +679,15 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
                     stream=None):
     """spec_verify (or, with a temperature or an EOS token, spec_verify_sampled) over a 4-bit
     pool."""
+    _verify_pool(lib().spec_verify_kv4, (ctypes.byref(weights.struct), pool.handle), cfg, pool, sample_ids,
+                 tree_offsets, tree_tokens, tree_parents, seq_lens, workspace, accepted_len, next_token,
+                 accepted_nodes, temperature, eos_token, draft_probs, uniforms, debug, stream)
+
+
+def _verify_pool(call, handles, cfg, pool, sample_ids, tree_offsets, tree_tokens, tree_parents, seq_lens,
+                 workspace, accepted_len, next_token, accepted_nodes, temperature, eos_token, draft_probs,
+                 uniforms, debug, stream):
+    """call, one of the verify steps, after checks of every array and tensor that it reads."""
     c = make_config(cfg)
     (ids, p_ids), (offs, p_offs), (lens, p_lens), (_, p_toks), (_, p_pars) = _kv4_arrays(
         sample_ids, tree_offsets, seq_lens, tree_tokens=tree_tokens, tree_parents=tree_parents)
@@ -686,11 +709,10 @@ def spec_verify_kv4(cfg, weights: Weights, pool: KV4Pool, sample_ids, tree_offse
         dbg = spec_debug(*[debug[k].data_ptr() if debug.get(k) is not None else None
                            for k in ("logits", "argmax", "depth", "pos", "anc")])
     with _on(pool.index):
-        _check(lib().spec_verify_kv4(ctypes.byref(c), ctypes.byref(weights.struct), pool.handle,
-                                     len(ids), p_ids, p_offs, p_toks, p_pars, p_lens, _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(), _stream(stream),
-                                     ctypes.byref(samp), _ptr(accepted_len), _ptr(next_token),
-                                     _ptr(accepted_nodes), ctypes.byref(dbg) if dbg else None))
+        _check(call(ctypes.byref(c), *handles, len(ids), p_ids, p_offs, p_toks, p_pars, p_lens, _ptr(workspace),
+                    workspace.numel() * workspace.element_size(), _stream(stream), ctypes.byref(samp),
+                    _ptr(accepted_len), _ptr(next_token), _ptr(accepted_nodes),
+                    ctypes.byref(dbg) if dbg else None))
 
 
 def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_nodes, new_seq_lens,
@@ -803,6 +825,58 @@ class W4Matrix:
                 out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16, device=self.data.device)
         spec_w4_unpack(self.data, out, stream)
         return out
+
+
+class W4Weights:
+    """A model's weights with its matrices in 4 bits, quantised from those that Weights takes
+    (W["layers"] may be an iterator, so that a layer's bf16 matrices need not outlive it)."""
+
+    MATRICES = ("wqkv", "wo", "w_gate", "w_up", "w_down")
+
+    def __init__(self, W, stream=None):
+        self.lm_head = W4Matrix(W["lm_head"], stream)
+        self.index = self.lm_head.index
+        self.tok_embed, self.final_norm = W["tok_embed"], W["final_norm"]
+        self.norms, self.matrices = {"attn_norm": [], "ffn_norm": []}, {k: [] for k in self.MATRICES}
+        with torch.cuda.stream(stream):
+            for lw in W["layers"]:
+                for k, rows in self.norms.items():
+                    rows.append(lw[k])
+                for k, layers in self.matrices.items():
+                    w = torch.cat([lw["wq"], lw["wk"], lw["wv"]]) if k == "wqkv" else lw[k]
+                    layers.append(W4Matrix(w, stream))
+        for t in (self.tok_embed, self.final_norm, *self.norms["attn_norm"], *self.norms["ffn_norm"]):
+            if t.dtype != torch.bfloat16 or t.get_device() != self.index or not t.is_contiguous():
+                raise ValueError("norm gains and the embedding must be contiguous bf16 tensors on the matrices' device")
+        n = len(self.norms["attn_norm"])
+        self._arrays = {k: (c_void_p * n)(*[t.data_ptr() for t in rows]) for k, rows in self.norms.items()}
+        self._arrays |= {k: (spec_w4 * n)(*[m.struct for m in layers]) for k, layers in self.matrices.items()}
+        a = {k: ctypes.cast(v, POINTER(v._type_)) for k, v in self._arrays.items()}
+        self.struct = spec_weights_w4(self.tok_embed.data_ptr(), self.final_norm.data_ptr(), self.lm_head.struct,
+                                      a["attn_norm"], a["wqkv"], a["wo"], a["ffn_norm"], a["w_gate"], a["w_up"],
+                                      a["w_down"])
+
+
+def spec_workspace_bytes_w4(cfg, max_batch, max_tokens, max_pages=0, sampled=False) -> int:
+    c = make_config(cfg)
+    return int(lib().spec_workspace_bytes_w4(ctypes.byref(c), max_batch, max_tokens, max_pages, int(bool(sampled))))
+
+
+def spec_verify_w4(cfg, weights: W4Weights, pool, sample_ids, tree_offsets, tree_tokens, tree_parents,
+                   seq_lens, workspace, accepted_len, next_token, accepted_nodes, temperature=0.0, eos_token=-1,
+                   draft_probs=None, uniforms=None, debug=None, stream=None):
+    """spec_verify (or, with a temperature or an EOS token, spec_verify_sampled) with weights in 4
+    bits, over a KVPool or a KV4Pool."""
+    if weights.index != pool.index:
+        raise ValueError(f"the weights are on device {weights.index}, the pool on device {pool.index}")
+    if len(weights.norms["attn_norm"]) != cfg.n_layers or len(weights.final_norm) != cfg.hidden \
+            or tuple(weights.tok_embed.shape) != (cfg.vocab, cfg.hidden) \
+            or any(len(t) != cfg.hidden for rows in weights.norms.values() for t in rows):
+        raise ValueError("the weights are of another shape than the model's")
+    kv, kv4 = (None, pool.handle) if isinstance(pool, KV4Pool) else (pool.handle, None)
+    _verify_pool(lib().spec_verify_w4, (ctypes.byref(weights.struct), kv, kv4), cfg, pool, sample_ids, tree_offsets,
+                 tree_tokens, tree_parents, seq_lens, workspace, accepted_len, next_token, accepted_nodes,
+                 temperature, eos_token, draft_probs, uniforms, debug, stream)
 
 
 def _w4_workspace(m, n, workspace, stream):

@@ -15,6 +15,7 @@
 #include "kv4_host.h"
 #include "reorder.h"
 #include "specverify.h"
+#include "w4.h"
 
 using namespace spec;
 
@@ -89,7 +90,7 @@ size_t sample_bytes(const spec_model_config* c, int32_t cap) {
 // Workspace carving; every region 256-byte aligned.
 struct WsLayout {
   size_t blob, toks, anc, rope, x, h, q, o, act, part_o, part_ml, lm_val, lm_idx, argmax, splitk,
-      logits, resid, kv4_step, kv4_rows, total;
+      logits, resid, kv4_step, kv4_rows, qkv, total;
   size_t blob_bytes;
 };
 
@@ -99,8 +100,9 @@ int64_t max_row_tiles(const spec_model_config* c, int64_t max_batch, int64_t max
 }
 
 // kv4_pages > 0: over the 4-bit pool, the attention's plan and partials are the step's.
+// w4: with weights in 4 bits, whose products leave q, k, v and the logits in fp32.
 WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_tokens,
-                   bool sampling = false, int64_t kv4_pages = 0) {
+                   bool sampling = false, int64_t kv4_pages = 0, bool w4 = false) {
   WsLayout L{};
   const bool kv4 = kv4_pages > 0;
   const int64_t part_cap = kv4 ? 0 : kPartCap;
@@ -130,11 +132,11 @@ WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_to
   L.lm_val = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.lm_idx = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.argmax = take(max_tokens * 4);
-  L.splitk = take(gemm_partial_bytes());
-  if (sampling) {   // speculative sampling: fp32 logits, node decisions, fp64 residual rows
-    L.logits = take(max_tokens * (size_t)c->vocab * 4);
+  L.splitk = take(w4 ? kW4PartialCap : gemm_partial_bytes());
+  if (sampling || w4) L.logits = take(max_tokens * (size_t)c->vocab * 4);
+  if (sampling)     // speculative sampling: node decisions, fp64 residual rows
     L.resid = take(sample_accept_scratch((int)max_batch, (int)max_tokens, c->vocab));
-  }
+  if (w4) L.qkv = take(max_tokens * (nq_hd + 2 * (size_t)c->n_kv_heads * c->head_dim) * 4);
   if (kv4) {   // the step's plan, and one layer's rotated K/V on their way into the cache
     L.kv4_step = take(kv4_step_bytes(c, max_batch, max_tokens, kv4_pages));
     L.kv4_rows = take(max_tokens * 2 * (size_t)c->n_kv_heads * c->head_dim * 2);
@@ -401,25 +403,53 @@ void plan_split_kv(const spec_model_config* cfg, const std::vector<SampleInfo>& 
   deal_items(wide8);
 }
 
-// Over the bf16 pool `kv`, or over the 4-bit one `kv4`.
+int check_w4_matrix(const spec_w4& m, int rows, int cols, const char* what) {
+  if (!m.data) return fail(SPEC_ERR_INVALID, "null weight pointer: %s", what);
+  if ((uintptr_t)m.data % kAlign) return fail(SPEC_ERR_INVALID, "%s: matrix data not 256-byte aligned", what);
+  if (m.rows != rows || m.cols != cols)
+    return fail(SPEC_ERR_INVALID, "%s is %d x %d, the model's %d x %d", what, m.rows, m.cols, rows, cols);
+  return SPEC_OK;
+}
+
+int check_w4_weights(const spec_model_config* c, const spec_weights_w4* w) {
+  if (!w->tok_embed || !w->final_norm || !w->attn_norm || !w->wqkv || !w->wo || !w->ffn_norm || !w->w_gate ||
+      !w->w_up || !w->w_down)
+    return fail(SPEC_ERR_INVALID, "null weight pointer");
+  const int q = c->n_heads * c->head_dim, kv = c->n_kv_heads * c->head_dim;
+  if (int rc = check_w4_matrix(w->lm_head, c->vocab, c->hidden, "lm_head")) return rc;
+  for (int l = 0; l < c->n_layers; ++l) {
+    if (!w->attn_norm[l] || !w->ffn_norm[l]) return fail(SPEC_ERR_INVALID, "null weight pointer in layer %d", l);
+    if (int rc = check_w4_matrix(w->wqkv[l], q + 2 * kv, c->hidden, "wqkv")) return rc;
+    if (int rc = check_w4_matrix(w->wo[l], c->hidden, q, "wo")) return rc;
+    if (int rc = check_w4_matrix(w->w_gate[l], c->ffn, c->hidden, "w_gate")) return rc;
+    if (int rc = check_w4_matrix(w->w_up[l], c->ffn, c->hidden, "w_up")) return rc;
+    if (int rc = check_w4_matrix(w->w_down[l], c->hidden, c->ffn, "w_down")) return rc;
+  }
+  return SPEC_OK;
+}
+
+// Over the bf16 pool `kv`, or over the 4-bit one `kv4`; with weights w, or w4.
 int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv, spec_kv4* kv4,
                 int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets, const int32_t* tree_tokens,
                 const int32_t* tree_parents, const int32_t* seq_lens, void* workspace,
                 size_t ws_bytes, void* stream, const spec_sampling* samp, int32_t* accepted_len,
                 int32_t* next_token, int32_t* accepted_nodes, const spec_debug* dbg,
-                bool noalloc = false) {
+                bool noalloc = false, const spec_weights_w4* w4 = nullptr) {
   // ---- validation (no side effects) ----
-  if (!cfg || !w || (!kv && !kv4) || !sample_ids || !tree_offsets || !tree_tokens || !tree_parents ||
+  if (!cfg || (!w && !w4) || (!kv && !kv4) || !sample_ids || !tree_offsets || !tree_tokens || !tree_parents ||
       !seq_lens || (!workspace && !noalloc) || !accepted_len || !next_token || !accepted_nodes)
     return fail(SPEC_ERR_INVALID, "null argument");
   std::string why;
   if (!config_ok(cfg, &why)) return fail(SPEC_ERR_UNSUPPORTED, "%s", why.c_str());
   if (!same_config(cfg, kv4 ? &kv4->cfg : &kv->cfg)) return fail(SPEC_ERR_INVALID, "config differs from the KV pool's");
   if (batch < 1) return fail(SPEC_ERR_INVALID, "batch must be >= 1");
-  if (!w->tok_embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wq || !w->wk ||
-      !w->wv || !w->wo || !w->ffn_norm || !w->w_gate || !w->w_up || !w->w_down)
+  if (w4) {
+    if (int rc = check_w4_weights(cfg, w4)) return rc;
+  } else if (!w->tok_embed || !w->final_norm || !w->lm_head || !w->attn_norm || !w->wq || !w->wk ||
+             !w->wv || !w->wo || !w->ffn_norm || !w->w_gate || !w->w_up || !w->w_down) {
     return fail(SPEC_ERR_INVALID, "null weight pointer");
-  for (int l = 0; l < cfg->n_layers; ++l)
+  }
+  for (int l = 0; !w4 && l < cfg->n_layers; ++l)
     if (!w->attn_norm[l] || !w->wq[l] || !w->wk[l] || !w->wv[l] || !w->wo[l] || !w->ffn_norm[l] ||
         !w->w_gate[l] || !w->w_up[l] || !w->w_down[l])
       return fail(SPEC_ERR_INVALID, "null weight pointer in layer %d", l);
@@ -465,7 +495,9 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   }
   const int N = tree_offsets[batch];
   const int64_t pages = kv4 ? kv4_step_pages(kv4, batch, tree_offsets, seq_lens) : 0;
-  const size_t need = ws_layout(cfg, batch, N, sampled, pages).total;
+  if (w4 && N > 65535) return fail(SPEC_ERR_UNSUPPORTED, "%d tree nodes in one call, at most 65535", N);
+  const WsLayout ly = ws_layout(cfg, batch, N, sampled, pages, w4 != nullptr);
+  const size_t need = ly.total;
   if (noalloc && need > SPEC_NOALLOC_SCRATCH_BYTES)
     return fail(SPEC_ERR_WORKSPACE,
                 "%d samples with %d tree nodes need %zu bytes of workspace, more than the %zu "
@@ -476,7 +508,7 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
     ws_bytes = SPEC_NOALLOC_SCRATCH_BYTES;
   }
   if (ws_bytes < need) return fail(SPEC_ERR_WORKSPACE, "workspace %zu bytes, needs %zu", ws_bytes, need);
-  if (kv4) {
+  if (kv4 || w4) {
     if ((uintptr_t)workspace % kAlign) return fail(SPEC_ERR_INVALID, "workspace not 256-byte aligned");
     if (int rc = refuse_capture(stream)) return rc;
   }
@@ -484,7 +516,6 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   // ---- planning ----
   const int L = cfg->n_layers, H = cfg->hidden, nq = cfg->n_heads, nkv = cfg->n_kv_heads;
   const int hd = cfg->head_dim, F = cfg->ffn, V = cfg->vocab;
-  const WsLayout ly = ws_layout(cfg, batch, N, sampled, pages);
   char* ws = (char*)workspace;
   hipStream_t s = (hipStream_t)stream;
 
@@ -561,7 +592,11 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
                              D.anc, s),
             "tree meta");
   }
-  HIP_TRY(launch_row_front(d_toks, d_tok, (const bf16*)w->tok_embed, (const bf16*)w->attn_norm[0], d_x, d_h,
+  const void* const* attn_norm = w4 ? w4->attn_norm : w->attn_norm;
+  const void* const* ffn_norm = w4 ? w4->ffn_norm : w->ffn_norm;
+  const void* final_norm = w4 ? w4->final_norm : w->final_norm;
+  const void* tok_embed = w4 ? w4->tok_embed : w->tok_embed;
+  HIP_TRY(launch_row_front(d_toks, d_tok, (const bf16*)tok_embed, (const bf16*)attn_norm[0], d_x, d_h,
                            N, H, cfg->rms_eps, hd, cfg->rope_theta, d_rope, s),
           "row front");
 
@@ -608,59 +643,98 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
     if (!fused) HIP_TRY(launch_rmsnorm(d_x, (const bf16*)gain, d_h, N, H, cfg->rms_eps, s), "rmsnorm");
     return SPEC_OK;
   };
-  const GemmPlan p_qkv = product_plan(cfg, SPEC_K_GEMM_QKV, N), p_o = product_plan(cfg, SPEC_K_GEMM_O, N),
-                 p_gate_up = product_plan(cfg, SPEC_K_GEMM_GATE_UP, N),
-                 p_down = product_plan(cfg, SPEC_K_GEMM_DOWN, N), p_head = product_plan(cfg, SPEC_K_LM_HEAD, N);
-  for (int l = 0; l < L; ++l) {
-    GemmArgs g = ga;
-    g.plan = p_qkv;
-    g.A = d_h;
-    g.K = H;
-    g.B0 = (const bf16*)w->wq[l];
-    g.B1 = (const bf16*)w->wk[l];
-    g.B2 = (const bf16*)w->wv[l];
-    g.n0 = nq * hd;
-    g.n1 = g.n2 = nkv * hd;
-    g.N = g.n0 + g.n1 + g.n2;
-    g.q_out = d_q;
-    g.layer = kv4 ? 0 : l;
-    HIP_TRY(timed(SPEC_K_GEMM_QKV, s, [&] { return launch_gemm(EPI_QKV, g, s); }), "qkv gemm");
+  // One product with weights in 4 bits, of the plan that its kind of product has in all layers.
+  auto w4_product = [&](int kind, const W4Plan& plan, const spec_w4& m, const spec_w4* up, const bf16* x, void* out,
+                        int out_kind, const char* what) -> int {
+    const W4Args a{plan, (const char*)m.data, up ? (const char*)up->data : nullptr, m.rows, m.cols, x, m.cols, N,
+                   out, m.rows, out_kind, (float*)(ws + ly.splitk)};
+    HIP_TRY(timed(kind, s, [&] { return launch_w4(a, s); }), what);
+    return SPEC_OK;
+  };
+  auto attend = [&](int l) -> int {
     if (kv4) {
       if (int rc = kv4_append_blocks(&step, l, d_kv4, s)) return rc;
-      if (int rc = kv4_attend(&step, l, d_q, (int64_t)nq * hd, d_o, s)) return rc;
-    } else {
-      aa.layer = l;
-      HIP_TRY(timed(SPEC_K_ATTENTION, s, [&] { return launch_attention(aa, s); }), "attention");
+      return kv4_attend(&step, l, d_q, (int64_t)nq * hd, d_o, s);
     }
-    g = ga;
-    g.plan = p_o;
-    g.A = d_o;
-    g.K = nq * hd;
-    g.B0 = (const bf16*)w->wo[l];
-    g.n0 = g.N = H;
-    g.x = d_x;
-    if (int rc = resid_then_norm(SPEC_K_GEMM_O, g, w->ffn_norm[l], "o gemm")) return rc;
-    g = ga;
-    g.plan = p_gate_up;
-    g.A = d_h;
-    g.K = H;
-    g.B0 = (const bf16*)w->w_gate[l];
-    g.B1 = (const bf16*)w->w_up[l];
-    g.n0 = g.n1 = F;
-    g.N = 2 * F;
-    g.act_out = d_act;
-    HIP_TRY(timed(SPEC_K_GEMM_GATE_UP, s, [&] { return launch_gemm(EPI_GATE_UP, g, s); }), "gate/up gemm");
-    g = ga;
-    g.plan = p_down;
-    g.A = d_act;
-    g.K = F;
-    g.B0 = (const bf16*)w->w_down[l];
-    g.n0 = g.N = H;
-    g.x = d_x;
-    const void* next_norm = l + 1 < L ? w->attn_norm[l + 1] : w->final_norm;
-    if (int rc = resid_then_norm(SPEC_K_GEMM_DOWN, g, next_norm, "down gemm")) return rc;
-  }
-  {
+    aa.layer = l;
+    HIP_TRY(timed(SPEC_K_ATTENTION, s, [&] { return launch_attention(aa, s); }), "attention");
+    return SPEC_OK;
+  };
+  if (w4) {
+    float* d_qkv = (float*)(ws + ly.qkv);
+    float* logits = D.logits ? D.logits : (float*)(ws + ly.logits);
+    const int wide = (nq + 2 * nkv) * hd;
+    const W4Plan p_qkv = plan_w4(wide, H, N, false), p_o = plan_w4(H, nq * hd, N, false),
+                 p_gate_up = plan_w4(F, H, N, true), p_down = plan_w4(H, F, N, false),
+                 p_head = plan_w4(V, H, N, false);
+    for (int l = 0; l < L; ++l) {
+      const void* next_norm = l + 1 < L ? attn_norm[l + 1] : final_norm;
+      if (int rc = w4_product(SPEC_K_GEMM_QKV, p_qkv, w4->wqkv[l], nullptr, d_h, d_qkv, SPEC_W4_F32, "qkv product"))
+        return rc;
+      HIP_TRY(launch_place_qkv(d_qkv, N, d_si, d_toks, d_rope, d_q, kv4 ? d_kv4 : kv->pool, kv4 ? 0 : l, nq, nkv, hd,
+                               s),
+              "place q, k, v");
+      if (int rc = attend(l)) return rc;
+      if (int rc = w4_product(SPEC_K_GEMM_O, p_o, w4->wo[l], nullptr, d_o, d_x, SPEC_W4_ADD, "o product")) return rc;
+      HIP_TRY(launch_rmsnorm(d_x, (const bf16*)ffn_norm[l], d_h, N, H, cfg->rms_eps, s), "rmsnorm");
+      if (int rc = w4_product(SPEC_K_GEMM_GATE_UP, p_gate_up, w4->w_gate[l], &w4->w_up[l], d_h, d_act, SPEC_W4_BF16,
+                              "gate/up product"))
+        return rc;
+      if (int rc = w4_product(SPEC_K_GEMM_DOWN, p_down, w4->w_down[l], nullptr, d_act, d_x, SPEC_W4_ADD,
+                              "down product"))
+        return rc;
+      HIP_TRY(launch_rmsnorm(d_x, (const bf16*)next_norm, d_h, N, H, cfg->rms_eps, s), "rmsnorm");
+    }
+    if (int rc = w4_product(SPEC_K_LM_HEAD, p_head, w4->lm_head, nullptr, d_h, logits, SPEC_W4_F32, "lm head"))
+      return rc;
+    HIP_TRY(launch_logit_max(logits, N, V, d_lmv, d_lmi, s), "logits' maxima");
+  } else {
+    const GemmPlan p_qkv = product_plan(cfg, SPEC_K_GEMM_QKV, N), p_o = product_plan(cfg, SPEC_K_GEMM_O, N),
+                   p_gate_up = product_plan(cfg, SPEC_K_GEMM_GATE_UP, N),
+                   p_down = product_plan(cfg, SPEC_K_GEMM_DOWN, N), p_head = product_plan(cfg, SPEC_K_LM_HEAD, N);
+    for (int l = 0; l < L; ++l) {
+      GemmArgs g = ga;
+      g.plan = p_qkv;
+      g.A = d_h;
+      g.K = H;
+      g.B0 = (const bf16*)w->wq[l];
+      g.B1 = (const bf16*)w->wk[l];
+      g.B2 = (const bf16*)w->wv[l];
+      g.n0 = nq * hd;
+      g.n1 = g.n2 = nkv * hd;
+      g.N = g.n0 + g.n1 + g.n2;
+      g.q_out = d_q;
+      g.layer = kv4 ? 0 : l;
+      HIP_TRY(timed(SPEC_K_GEMM_QKV, s, [&] { return launch_gemm(EPI_QKV, g, s); }), "qkv gemm");
+      if (int rc = attend(l)) return rc;
+      g = ga;
+      g.plan = p_o;
+      g.A = d_o;
+      g.K = nq * hd;
+      g.B0 = (const bf16*)w->wo[l];
+      g.n0 = g.N = H;
+      g.x = d_x;
+      if (int rc = resid_then_norm(SPEC_K_GEMM_O, g, ffn_norm[l], "o gemm")) return rc;
+      g = ga;
+      g.plan = p_gate_up;
+      g.A = d_h;
+      g.K = H;
+      g.B0 = (const bf16*)w->w_gate[l];
+      g.B1 = (const bf16*)w->w_up[l];
+      g.n0 = g.n1 = F;
+      g.N = 2 * F;
+      g.act_out = d_act;
+      HIP_TRY(timed(SPEC_K_GEMM_GATE_UP, s, [&] { return launch_gemm(EPI_GATE_UP, g, s); }), "gate/up gemm");
+      g = ga;
+      g.plan = p_down;
+      g.A = d_act;
+      g.K = F;
+      g.B0 = (const bf16*)w->w_down[l];
+      g.n0 = g.N = H;
+      g.x = d_x;
+      const void* next_norm = l + 1 < L ? attn_norm[l + 1] : final_norm;
+      if (int rc = resid_then_norm(SPEC_K_GEMM_DOWN, g, next_norm, "down gemm")) return rc;
+    }
     GemmArgs g = ga;
     g.plan = p_head;
     g.A = d_h;
@@ -672,7 +746,7 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
     g.logits = D.logits ? D.logits : sampled ? (float*)(ws + ly.logits) : nullptr;
     HIP_TRY(timed(SPEC_K_LM_HEAD, s, [&] { return launch_gemm(EPI_ARGMAX, g, s); }), "lm head");
   }
-  HIP_TRY(launch_argmax_reduce(d_lmv, d_lmi, N, V / 64, d_arg, D.argmax, s), "argmax");
+  HIP_TRY(launch_argmax_reduce(d_lmv, d_lmi, N, w4 ? logit_parts(V) : V / 64, d_arg, D.argmax, s), "argmax");
   if (sampled) {
     const float* logits = D.logits ? D.logits : (const float*)(ws + ly.logits);
     HIP_TRY(timed(SPEC_K_ACCEPT, s, [&] {
@@ -758,6 +832,27 @@ SPEC_API int spec_verify_kv4(const spec_model_config* cfg, const spec_weights* w
     if (!kv) return fail(SPEC_ERR_INVALID, "null argument");
     return verify_impl(cfg, w, nullptr, kv, batch, sample_ids, tree_offsets, tree_tokens, tree_parents, seq_lens,
                        workspace, ws_bytes, stream, samp, accepted_len, next_token, accepted_nodes, dbg);
+  });
+}
+
+SPEC_API size_t spec_workspace_bytes_w4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
+                                        int32_t max_pages, int32_t sampled) {
+  std::string why;
+  if (!cfg || max_batch < 1 || max_tokens < max_batch || max_pages < 0 || !config_ok(cfg, &why)) return 0;
+  return ws_layout(cfg, max_batch, max_tokens, sampled != 0, max_pages, true).total;
+}
+
+SPEC_API int spec_verify_w4(const spec_model_config* cfg, const spec_weights_w4* w, spec_kv* kv, spec_kv4* kv4,
+                            int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets,
+                            const int32_t* tree_tokens, const int32_t* tree_parents, const int32_t* seq_lens,
+                            void* workspace, size_t ws_bytes, void* stream, const spec_sampling* samp,
+                            int32_t* accepted_len, int32_t* next_token, int32_t* accepted_nodes,
+                            const spec_debug* dbg) {
+  return guarded([&]() -> int {
+    if (!w) return fail(SPEC_ERR_INVALID, "null argument");
+    if (!kv == !kv4) return fail(SPEC_ERR_INVALID, "one pool: kv or kv4");
+    return verify_impl(cfg, nullptr, kv, kv4, batch, sample_ids, tree_offsets, tree_tokens, tree_parents, seq_lens,
+                       workspace, ws_bytes, stream, samp, accepted_len, next_token, accepted_nodes, dbg, false, w);
   });
 }
 

@@ -176,6 +176,15 @@ hipError_t launch_rmsnorm(const float* x, const bf16* gain, bf16* out, int n, in
                           float eps, hipStream_t s);
 hipError_t launch_argmax_reduce(const float* part_val, const int32_t* part_idx, int n, int parts,
                                 int32_t* argmax, int32_t* dbg_argmax, hipStream_t s);
+// q, k and v of a product of their own, fp32 [n][(n_heads + 2 n_kv_heads) head_dim]: q and k rotated,
+// q to its rows, k and v to their slots of layer `layer`.
+hipError_t launch_place_qkv(const float* qkv, int n, const SampleInfo* samples, const TokInfo* toks,
+                            const float2* rope_cs, bf16* q, bf16* kv_pool, int layer, int n_heads,
+                            int n_kv_heads, int head_dim, hipStream_t s);
+// Row maxima of fp32 logits [n][vocab], lowest index of equal ones, per logit_parts() part.
+int logit_parts(int vocab);
+hipError_t launch_logit_max(const float* logits, int n, int vocab, float* part_val, int32_t* part_idx,
+                            hipStream_t s);
 // Greedy acceptance; eos: the end-of-sequence token, -1 for none.
 hipError_t launch_accept(const SampleInfo* samples, int batch, const int32_t* tokens,
                          const int32_t* parents, const TokInfo* toks, const uint64_t* anc,

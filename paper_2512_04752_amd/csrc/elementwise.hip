@@ -174,6 +174,89 @@ __global__ __launch_bounds__(256) void row_front_kernel(const TokInfo* toks, con
   }
 }
 
+// The rotation and the places of q, k and v behind a product that leaves them in fp32 rows
+// (the 4-bit products; the bf16 one has this in its epilogue).  A thread has four dims and
+// their partners half a head on.  Bound by its launch below some hundred rows.
+__global__ __launch_bounds__(256) void place_qkv_kernel(const float* qkv, int n, const SampleInfo* samples,
+                                                        const TokInfo* toks, const float2* rope_cs, bf16* q,
+                                                        bf16* kv_pool, int layer, int n_heads, int n_kv_heads,
+                                                        int hd) {
+  const int half = hd / 2, quads = half / 4, heads = n_heads + 2 * n_kv_heads, per_row = heads * quads;
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (idx >= (int64_t)n * per_row) return;
+  const int row = (int)(idx / per_row), rem = (int)(idx % per_row);
+  int head = rem / quads;
+  const int fi = rem % quads * 4;
+  const float* src = qkv + ((int64_t)row * heads + head) * hd + fi;
+  f32x4 x1 = *(const f32x4*)src, x2 = *(const f32x4*)(src + half);
+  bf16* dst;
+  if (head < n_heads) {
+    dst = q + ((int64_t)row * n_heads + head) * hd + fi;
+  } else {
+    head -= n_heads;
+    const int value = head >= n_kv_heads;
+    const SampleInfo sv = samples[toks[row].sample];
+    dst = kv_pool + sv.kv_base +
+          ((((int64_t)layer * 2 + value) * n_kv_heads + head - value * n_kv_heads) * sv.cap + sv.seq_len +
+           toks[row].node) * hd + fi;
+    head = value ? -1 : 0;
+  }
+  if (head >= 0) {                       // a query or a key
+    const float* cs = (const float*)(rope_cs + (int64_t)row * half + fi);
+    const f32x4 t0 = *(const f32x4*)cs, t1 = *(const f32x4*)(cs + 4);      // (cos, sin) x 4
+    const float co[4] = {t0[0], t0[2], t1[0], t1[2]}, si[4] = {t0[1], t0[3], t1[1], t1[3]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y1 = x1[e] * co[e] - x2[e] * si[e];
+      const float y2 = x2[e] * co[e] + x1[e] * si[e];
+      x1[e] = y1;
+      x2[e] = y2;
+    }
+  }
+  bf16x4 v1, v2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v1[e] = (bf16)x1[e];
+    v2[e] = (bf16)x2[e];
+  }
+  *(bf16x4*)dst = v1;
+  *(bf16x4*)(dst + half) = v2;
+}
+
+// Maximum, and its lowest index, of kLogitPart logits of a row (argmax_reduce_kernel joins the
+// parts): eight loads of a thread in flight, which streams the logits at the rate of HBM.
+constexpr int kLogitPart = 2048;
+__global__ __launch_bounds__(256) void logit_max_kernel(const float* logits, int vocab, float* part_val,
+                                                        int32_t* part_idx) {
+  constexpr int U = kLogitPart / 256;
+  __shared__ float sv[4];
+  __shared__ int si[4];
+  const int part = blockIdx.x, row = blockIdx.y, first = part * kLogitPart + threadIdx.x;
+  const float* z = logits + (int64_t)row * vocab;
+  float x[U], v = -INFINITY;
+  int idx = 0x7fffffff;
+#pragma unroll
+  for (int u = 0; u < U; ++u) x[u] = first + 256 * u < vocab ? z[first + 256 * u] : __builtin_nanf("");
+#pragma unroll
+  for (int u = 0; u < U; ++u)            // a NaN is no maximum
+    if (x[u] > v || (x[u] == v && first + 256 * u < idx)) { v = x[u]; idx = first + 256 * u; }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    const float ov = __shfl_xor(v, m);
+    const int oi = __shfl_xor(idx, m);
+    if (ov > v || (ov == v && oi < idx)) { v = ov; idx = oi; }
+  }
+  if ((threadIdx.x & 63) == 0) { sv[threadIdx.x >> 6] = v; si[threadIdx.x >> 6] = idx; }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 4; ++w)
+      if (sv[w] > v || (sv[w] == v && si[w] < idx)) { v = sv[w]; idx = si[w]; }
+    part_val[(int64_t)row * gridDim.x + part] = v;
+    part_idx[(int64_t)row * gridDim.x + part] = idx;
+  }
+}
+
 // Row maximum over the LM-head partials; ties go to the lowest token id.
 __global__ __launch_bounds__(256) void argmax_reduce_kernel(const float* part_val,
                                                             const int32_t* part_idx, int parts,
@@ -372,6 +455,25 @@ hipError_t launch_rmsnorm(const float* x, const bf16* gain, bf16* out, int n, in
   with_chunks(hidden, [&](auto c) {
     rmsnorm_kernel<decltype(c)::value><<<n, 256, 0, s>>>(x, gain, out, hidden, eps);
   });
+  return hipGetLastError();
+}
+
+hipError_t launch_place_qkv(const float* qkv, int n, const SampleInfo* samples, const TokInfo* toks,
+                            const float2* rope_cs, bf16* q, bf16* kv_pool, int layer, int n_heads,
+                            int n_kv_heads, int head_dim, hipStream_t s) {
+  const int64_t threads = (int64_t)n * (n_heads + 2 * n_kv_heads) * (head_dim / 8);
+  if (threads > 0xffffff00ll) return hipErrorInvalidValue;
+  place_qkv_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(qkv, n, samples, toks, rope_cs, q, kv_pool,
+                                                                     layer, n_heads, n_kv_heads, head_dim);
+  return hipGetLastError();
+}
+
+int logit_parts(int vocab) { return (vocab + kLogitPart - 1) / kLogitPart; }
+
+hipError_t launch_logit_max(const float* logits, int n, int vocab, float* part_val, int32_t* part_idx,
+                            hipStream_t s) {
+  if (n > 65535) return hipErrorInvalidValue;
+  logit_max_kernel<<<dim3(logit_parts(vocab), n), 256, 0, s>>>(logits, vocab, part_val, part_idx);
   return hipGetLastError();
 }
 

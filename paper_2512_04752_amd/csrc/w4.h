@@ -41,6 +41,7 @@ struct W4Args {
   float* partial;           // [splits][matrices][n][16 * row tiles]
 };
 
+constexpr size_t kW4PartialCap = 64ull << 20;      // most bytes of a product's partial sums
 constexpr int kMostSplitRows = 4096;     // rows of x from which on columns are not split
 W4Plan plan_w4(int rows, int cols, int n, bool gate_up);
 size_t w4_partial_bytes(int rows, int cols, int n, bool gate_up);

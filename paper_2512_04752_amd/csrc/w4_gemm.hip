@@ -402,7 +402,6 @@ __global__ __launch_bounds__(256) void w4_reduce_kernel(W4Args a) {
 }
 
 constexpr int kLds = 160 * 1024;         // of a CU
-constexpr size_t kPartialCap = 64ull << 20;
 
 // Let a kernel have that much LDS, once per device (a call takes a microsecond).
 hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>* ready) {
@@ -491,7 +490,7 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
     W4Plan p{W4_STREAM, kStreamWaves, 1};
     while (p.splits <= 16 && stream_lds(cols, n, mats, p) > kLds) ++p.splits;
     while (p.wide > 1 && (int64_t)tiles * p.wide * p.splits > 256 * kStreamWaves) p.wide /= 2;
-    if (p.splits <= 16 && (p.splits == 1 || partials(p.splits) <= kPartialCap)) return p;
+    if (p.splits <= 16 && (p.splits == 1 || partials(p.splits) <= kW4PartialCap)) return p;
   }
   struct Tile {
     W4Shape shape;
@@ -511,7 +510,7 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
     const int64_t count = ((int64_t)n + s.bm - 1) / s.bm * (((int64_t)tiles * mats + s.bt - 1) / s.bt);
     for (int splits = 1; splits <= (n <= kMostSplitRows ? 16 : 1); ++splits) {
       const double part = partials(splits);
-      if (splits > 1 && (T / splits < 4 || part > kPartialCap)) break;
+      if (splits > 1 && (T / splits < 4 || part > kW4PartialCap)) break;
       const int64_t wgs = count * splits;
       const double steps = (T + splits * s.kg - 1) / (splits * s.kg), at_once = 256.0 * s.slots;
       auto step = [&](int k) { return k == 0 ? 0.0 : std::max(s.alone, k * s.each); };

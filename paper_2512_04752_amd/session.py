@@ -22,14 +22,20 @@ def flatten_trees(trees):
 
 class Verifier:
     def __init__(self, cfg, W, capacity, max_batch, max_tokens, device="cuda", sampling=False,
-                 cache="bf16"):
-        """sampling=True sizes the workspace for verify_sampled at temperature > 0.  cache="kv4"
+                 cache="bf16", weights="bf16"):
+        """weights="w4" quantises the matrices of W to 4 bits (W may be a W4Weights already).
+        sampling=True sizes the workspace for verify_sampled at temperature > 0.  cache="kv4"
         holds K and V in the 4-bit paged pool, every sample with pages of its own for its
         capacity (remap them with self.kv.map; the workspace holds steps whose samples' positions
         take no more pages than the max_batch largest capacities do)."""
         self.cfg = cfg
         self.cache = cache
-        self.weights = B.Weights(W)
+        if weights not in ("bf16", "w4"):
+            raise ValueError(f"weights must be 'bf16' or 'w4', not {weights!r}")
+        if isinstance(W, B.W4Weights) and weights != "w4":
+            raise ValueError("weights in 4 bits need weights='w4'")
+        self.w4 = weights == "w4"
+        self.weights = W if isinstance(W, B.W4Weights) else B.W4Weights(W) if self.w4 else B.Weights(W)
         if cache == "kv4":
             need = [-(-int(c) // B.SPEC_KV4_PAGE) for c in capacity]
             self.kv = B.KV4Pool(cfg, len(need), sum(need), device=device)
@@ -39,10 +45,12 @@ class Verifier:
                 first += n
             # pages of the longest samples that a step can hold at once
             most = sum(sorted(need)[-max_batch:])
-            nbytes = B.spec_workspace_bytes_kv4(cfg, max_batch, max_tokens, most, sampling)
+            nbytes = (B.spec_workspace_bytes_w4 if self.w4 else B.spec_workspace_bytes_kv4)(
+                cfg, max_batch, max_tokens, most, sampling)
         elif cache == "bf16":
             self.kv = B.KVPool(cfg, capacity, device=device)
-            nbytes = (B.spec_workspace_bytes_sampled if sampling else B.spec_workspace_bytes)(
+            nbytes = B.spec_workspace_bytes_w4(cfg, max_batch, max_tokens, 0, sampling) if self.w4 else \
+                (B.spec_workspace_bytes_sampled if sampling else B.spec_workspace_bytes)(
                 cfg, max_batch, max_tokens)
         else:
             raise ValueError(f"cache must be 'bf16' or 'kv4', not {cache!r}")
@@ -70,10 +78,10 @@ class Verifier:
         """Enqueue one verify step; returns views of the device outputs."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
-        if self.cache == "kv4":
-            B.spec_verify_kv4(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
-                              seq_lens, self.workspace, self.accepted_len, self.next_token,
-                              self.accepted_nodes, debug=debug, stream=stream)
+        if self.w4 or self.cache == "kv4":
+            (B.spec_verify_w4 if self.w4 else B.spec_verify_kv4)(
+                self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents, seq_lens, self.workspace,
+                self.accepted_len, self.next_token, self.accepted_nodes, debug=debug, stream=stream)
             return self.accepted_len[:b], self.next_token[:b], self.accepted_nodes[:b]
         B.spec_verify(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
                       seq_lens, self.workspace, self.accepted_len, self.next_token,
@@ -85,8 +93,8 @@ class Verifier:
         session's workspace (spec_verify_noalloc)."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
-        if self.cache != "bf16":
-            raise ValueError("verify_noalloc runs over the bf16 cache")
+        if self.cache != "bf16" or self.w4:
+            raise ValueError("verify_noalloc runs over the bf16 cache, with bf16 weights")
         B.spec_verify_noalloc(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens,
                               parents, seq_lens, self.accepted_len, self.next_token,
                               self.accepted_nodes, debug=debug, stream=stream)
@@ -97,11 +105,11 @@ class Verifier:
         """Enqueue one verify step with speculative-sampling acceptance."""
         offsets, tokens, parents = flat if flat is not None else flatten_trees(trees)
         b = len(sample_ids)
-        if self.cache == "kv4":
-            B.spec_verify_kv4(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
-                              seq_lens, self.workspace, self.accepted_len, self.next_token,
-                              self.accepted_nodes, temperature, eos_token, draft_probs, uniforms,
-                              debug=debug, stream=stream)
+        if self.w4 or self.cache == "kv4":
+            (B.spec_verify_w4 if self.w4 else B.spec_verify_kv4)(
+                self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents, seq_lens, self.workspace,
+                self.accepted_len, self.next_token, self.accepted_nodes, temperature, eos_token, draft_probs,
+                uniforms, debug=debug, stream=stream)
             return self.accepted_len[:b], self.next_token[:b], self.accepted_nodes[:b]
         B.spec_verify_sampled(self.cfg, self.weights, self.kv, sample_ids, offsets, tokens, parents,
                               seq_lens, self.workspace, self.accepted_len, self.next_token,

@@ -210,3 +210,88 @@ def test_oracle_select_by_hand():
     assert p.tolist() == [[0, 0, 0, 1]] and t.tolist() == [[0, 1, 2, 1]] and s[0, 3] == -5.0
     p, t, s = O.select(z, [[-np.inf, np.nan]], 2)
     assert p.tolist() == [[-1, -1]] and np.isneginf(s).all()
+
+
+# ---- the verify step with weights in 4 bits ------------------------------------
+
+class FakeStep:
+    """spec_verify_w4 with pointers that stand in for device memory."""
+
+    def __init__(self, cfg=wl.TINY, n=3):
+        self.cfg, self.c, self.L = cfg, B.make_config(cfg), B.lib()
+        self.kv, self.kv4 = ctypes.c_void_p(), ctypes.c_void_p()
+        assert self.L.spec_kv_alloc(ctypes.byref(self.c), n, (ctypes.c_int32 * n)(*[100] * n), P, 1 << 40,
+                                    ctypes.byref(self.kv)) == 0
+        assert self.L.spec_kv4_alloc(ctypes.byref(self.c), n, 2 * n, P, 1 << 40, ctypes.byref(self.kv4)) == 0
+        for s in range(n):
+            assert self.L.spec_kv4_map(self.kv4, s, 2, (ctypes.c_int32 * 2)(2 * s, 2 * s + 1)) == 0
+        q, kv, layers = cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim, cfg.n_layers
+        shapes = dict(wqkv=(q + 2 * kv, cfg.hidden), wo=(cfg.hidden, q), w_gate=(cfg.ffn, cfg.hidden),
+                      w_up=(cfg.ffn, cfg.hidden), w_down=(cfg.hidden, cfg.ffn))
+        self.m = {k: (B.spec_w4 * layers)(*[B.spec_w4(P, *shape)] * layers) for k, shape in shapes.items()}
+        self.norms = (ctypes.c_void_p * layers)(*[P] * layers)
+        self.w = B.spec_weights_w4(P, P, B.spec_w4(P, cfg.vocab, cfg.hidden), self.norms, self.m["wqkv"],
+                                   self.m["wo"], self.norms, self.m["w_gate"], self.m["w_up"], self.m["w_down"])
+
+    def call(self, kv=True, kv4=False, w=True, tokens=(5, 6, 7), parents=(-1, 0, 0), length=10, ws=P, ws_bytes=None,
+             outs=P, sample=1):
+        if ws_bytes is None:
+            ws_bytes = sv.spec_workspace_bytes_w4(self.cfg, 1, len(tokens), 2 if kv4 else 0)
+        kept, (ids, offs, toks, pars, lens) = zip(*map(B._i32, ([sample], [0, len(tokens)], tokens, parents, [length])))
+        return self.L.spec_verify_w4(ctypes.byref(self.c), ctypes.byref(self.w) if w else None,
+                                     self.kv if kv else None, self.kv4 if kv4 else None, 1, ids, offs, toks, pars,
+                                     lens, ws, ws_bytes, None, None, outs, P, P, None)
+
+    def close(self):
+        self.L.spec_kv_free(self.kv)
+        self.L.spec_kv4_free(self.kv4)
+
+
+@pytest.fixture
+def step():
+    f = FakeStep()
+    yield f
+    f.close()
+
+
+@pytest.mark.parametrize("changed,code", [
+    (dict(w=False), INVALID), (dict(kv=False), INVALID), (dict(kv4=True), INVALID), (dict(outs=None), INVALID),
+    (dict(ws=None), INVALID), (dict(ws=P + 16), INVALID), (dict(ws_bytes=1 << 20), WORKSPACE),
+    (dict(sample=3), INVALID), (dict(length=98), CAPACITY), (dict(length=-1), INVALID),
+    (dict(tokens=(5, 6, wl.TINY.vocab)), -2), (dict(parents=(-1, 1, 0)), -2), (dict(parents=(0, 0, 0)), -2),
+    (dict(kv=False, kv4=True, length=126), CAPACITY), (dict(kv=False, kv4=True, ws=P + 16), INVALID),
+    (dict(kv=False, kv4=True, tokens=(-1, 6, 7)), -2)])
+def test_w4_step_refusals(step, changed, code):
+    assert step.call(**changed) == code
+    assert B.lib().spec_last_error()
+
+
+@pytest.mark.parametrize("name", ["lm_head", "wqkv", "wo", "w_gate", "w_up", "w_down"])
+@pytest.mark.parametrize("field,value", [("data", None), ("data", P + 16), ("rows", 16), ("cols", 32)])
+def test_w4_step_refuses_matrices(step, name, field, value):
+    setattr(step.w.lm_head if name == "lm_head" else step.m[name][step.cfg.n_layers - 1], field, value)
+    assert step.call() == INVALID
+    assert name.encode() in B.lib().spec_last_error()
+
+
+def test_w4_step_refuses_missing_arrays(step):
+    for name in ("tok_embed", "final_norm", "attn_norm", "wqkv", "wo", "ffn_norm", "w_gate", "w_up", "w_down"):
+        kept = bytes(step.w)
+        setattr(step.w, name, None)
+        assert step.call() == INVALID and b"null" in B.lib().spec_last_error()
+        ctypes.memmove(ctypes.byref(step.w), kept, len(kept))
+    step.norms[1] = None
+    assert step.call() == INVALID and b"layer 1" in B.lib().spec_last_error()
+
+
+def test_w4_step_workspace():
+    size = sv.spec_workspace_bytes_w4
+    for pages in (0, 40):
+        got = [size(wl.TINY, b, n, pages) for b, n in ((1, 1), (1, 2), (4, 16), (4, 300), (64, 5000))]
+        assert got == sorted(got) and got[0] > 0
+        assert size(wl.TINY, 4, 16, pages, True) > size(wl.TINY, 4, 16, pages)
+    for bad in ((0, 1, 0), (2, 1, 0), (1, 1, -1)):
+        assert size(wl.TINY, *bad) == 0
+    # what a step sets aside for partial sums is enough for any product
+    for rows, cols in ((16, 32), (6144, 4096), (4096, 14336), (14336, 4096), (128256, 4096), (1 << 20, 1 << 16)):
+        assert sv.spec_w4_workspace_bytes(rows, cols, 5000) <= 64 << 20

@@ -1,0 +1,157 @@
+"""The verify step with weights in 4 bits (spec_verify_w4), over both pools, against the
+float64 oracle on the weights that the codes stand for, under the comparison rules of the
+bf16 step: those weights are exact in bf16, and every rounding is one that it has too."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_04752_amd as sv
+import workload as wl
+from oracle import sampling as SA
+from tests.gpu_util import check_tree_kv, full_check, run_gpu, split_rows
+from tests.test_gpu_kv4_verify import check_verify, fill
+
+pytestmark = pytest.mark.gpu
+
+CONFIGS = {
+    "tiny": wl.TINY,
+    "d128": wl.ModelConfig(2, 1024, 8, 2, 128, 2048, 1024, rope_theta=5e5),
+    "g1": wl.ModelConfig(2, 256, 4, 4, 64, 1024, 1024),
+    "g8": wl.ModelConfig(1, 1024, 16, 2, 64, 1152, 896),      # widths off 256, part of a chunk of logits
+    "wide": wl.ModelConfig(1, 1152, 8, 2, 128, 3200, 4224),
+}
+MATRICES = ("wo", "w_gate", "w_up", "w_down")
+
+
+def setup(cfg, caps, seed, max_tokens, cache="bf16", sampling=False):
+    """Weights that the 4-bit matrices stand for, on the CPU, and a session."""
+    W = wl.make_weights(cfg, seed, device="cuda")
+    w4 = sv.W4Weights(W)
+    q, kv = cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+    held = {"tok_embed": W["tok_embed"].cpu(), "final_norm": W["final_norm"].cpu(),
+            "lm_head": w4.lm_head.unpack().cpu(), "layers": []}
+    for l, lw in enumerate(W["layers"]):
+        m = {k: w4.matrices[k][l].unpack().cpu() for k in MATRICES}
+        m["wq"], m["wk"], m["wv"] = w4.matrices["wqkv"][l].unpack().cpu().split([q, kv, kv])
+        m |= {k: lw[k].cpu() for k in ("attn_norm", "ffn_norm")}
+        held["layers"].append(m)
+    return held, sv.Verifier(cfg, w4, caps, len(caps), max_tokens, cache=cache, weights="w4", sampling=sampling)
+
+
+def trees_of(rng, cfg, rows):
+    return [(wl.random_tokens(rng, n, cfg.vocab), wl.recursive_tree(rng, n, min(n, 8), 4)) for n in rows]
+
+
+def fill_bf16(ver, lens, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    for b, s in enumerate(lens):
+        wl.fill_prefix_kv(*ver.kv.sample_view(b), int(s), wl.prefix_kv_std(ver.cfg), gen)
+
+
+@pytest.mark.parametrize("rows", [[1], [1, 1, 2, 1], [5, 17, 8, 64], [200, 33, 1, 150]], ids=str)
+@pytest.mark.parametrize("name", sorted(CONFIGS))
+def test_over_the_bf16_pool(name, rows):
+    cfg = CONFIGS[name]
+    rng = np.random.default_rng(len(rows) + rows[-1])
+    lens = [130, 0, 63, 300][:len(rows)]
+    caps = [s + 256 for s in lens]
+    W, ver = setup(cfg, caps, 3, 400)
+    fill_bf16(ver, lens, 1)
+    before = [tuple(x.clone() for x in ver.kv.sample_view(b)) for b in range(len(rows))]
+    ids = list(range(len(rows)))[::-1]
+    trees = trees_of(rng, cfg, rows)
+    at = [lens[i] for i in ids]
+    out, r, _ = full_check(cfg, W, ver, ids, trees, at)
+    check_tree_kv(cfg, ver, ids, trees, at, r, range(len(ids)))
+    for b, i in enumerate(ids):              # no other position is touched
+        for got, want in zip(ver.kv.sample_view(i), before[i]):
+            keep = torch.ones(caps[i], dtype=torch.bool)
+            keep[at[b]:at[b] + rows[b]] = False
+            assert torch.equal(got[:, :, keep].view(torch.int16), want[:, :, keep].view(torch.int16))
+
+
+@pytest.mark.parametrize("name", ["tiny", "d128", "g1"])
+def test_over_the_4bit_pool_with_commits(monkeypatch, name):
+    cfg = CONFIGS[name]
+    rng = np.random.default_rng(6)
+    lens = [0, 130, 63, 400]
+    W, ver = setup(cfg, [s + 200 for s in lens], 5, 140, cache="kv4")
+    fill(ver, lens, 1)
+    ids = [2, 0, 3, 1]
+    lens = [lens[i] for i in ids]
+    for rows in ([9, 33, 1, 40], [1, 1, 2, 1]):
+        out, _ = check_verify(monkeypatch, cfg, W, ver, ids, trees_of(rng, cfg, rows), lens)
+        lens = ver.commit(ids, lens).tolist()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "kv4"])
+def test_sampled_and_eos(cache):
+    cfg = wl.TINY
+    rng = np.random.default_rng(9)
+    lens = [40, 129]
+    W, ver = setup(cfg, [400, 400], 4, 64, cache=cache, sampling=True)
+    (fill_bf16 if cache == "bf16" else fill)(ver, lens, 2)
+    trees = trees_of(rng, cfg, [12, 20])
+    q = torch.softmax(torch.randn(32, cfg.vocab, generator=torch.Generator("cuda").manual_seed(1), device="cuda"), -1)
+    u = torch.rand(32, 2, generator=torch.Generator("cuda").manual_seed(2), device="cuda")
+    dbg = ver.debug_buffers(32)
+    acc, nxt, nodes = ver.verify_sampled([0, 1], trees, lens, 1.0, draft_probs=q, uniforms=u, debug=dbg)
+    with_dump = acc.tolist(), nxt.tolist(), [n[:a + 1].tolist() for n, a in zip(nodes, acc.tolist())]
+    offs = split_rows(trees)
+    for b, (tok, par) in enumerate(trees):
+        sl = slice(offs[b], offs[b + 1])
+        a, n, path, margin = SA.sample_accept(tok, par, dbg["logits"][sl].double().cpu().numpy(), 1.0,
+                                              q[sl].double().cpu().numpy(), u[sl].double().cpu().numpy())
+        assert margin < 1e-11 or (int(acc[b]), int(nxt[b]), nodes[b, :a + 1].tolist()) == (a, n, path)
+    acc, nxt, nodes = ver.verify_sampled([0, 1], trees, lens, 1.0, draft_probs=q, uniforms=u)
+    assert with_dump == (acc.tolist(), nxt.tolist(), [n[:a + 1].tolist() for n, a in zip(nodes, acc.tolist())])
+    eos = int(trees[0][0][0])
+    acc, nxt, _ = ver.verify_sampled([0, 1], trees, lens, 0.0, eos_token=eos)
+    assert (int(acc[0]), int(nxt[0])) == (0, -1)
+
+
+def test_sessions_share_weights_and_repeat_bitwise():
+    cfg = CONFIGS["d128"]
+    rng = np.random.default_rng(1)
+    lens = [500, 7]
+    W, ver = setup(cfg, [600, 300], 6, 64)
+    other = sv.Verifier(cfg, ver.weights, [600, 300], 2, 64, weights="w4")
+    for v in (ver, other):
+        fill_bf16(v, lens, 3)
+    trees = trees_of(rng, cfg, [30, 10])
+    a, b, c = (run_gpu(v, [0, 1], trees, lens) for v in (ver, ver, other))
+    assert torch.equal(a["logits"], b["logits"]) and torch.equal(a["logits"], c["logits"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    dbg = ver.debug_buffers(40)
+    ver.verify([0, 1], trees, lens, debug=dbg, stream=side)
+    side.synchronize()
+    assert torch.equal(dbg["logits"].cpu(), a["logits"])
+
+
+def test_refusals():
+    cfg = wl.TINY
+    W, ver = setup(cfg, [64], 2, 16)
+    tree = ([1, 2, 3], [-1, 0, 0])
+    with pytest.raises(sv.SpecError, match="CAPACITY"):
+        ver.verify([0], [tree], [62])
+    with pytest.raises(ValueError, match="noalloc"):
+        ver.verify_noalloc([0], [tree], [0])
+    with pytest.raises(ValueError, match="w4"):
+        sv.Verifier(cfg, ver.weights, [64], 1, 16)
+    with pytest.raises(ValueError, match="weights"):
+        sv.Verifier(cfg, ver.weights, [64], 1, 16, weights="int8")
+    ver.weights.norms["ffn_norm"].append(ver.weights.final_norm[:64])
+    with pytest.raises(ValueError, match="shape"):
+        ver.verify([0], [tree], [0])
+    ver.weights.norms["ffn_norm"].pop()
+    graph = torch.cuda.CUDAGraph()
+    out = torch.zeros(1, device="cuda")
+    with torch.cuda.graph(graph):
+        out += 1
+        with pytest.raises(sv.SpecError, match="captur"):
+            ver.verify([0], [tree], [0])
+    torch.cuda.synchronize()
+    acc, _, _ = ver.verify([0], [tree], [0])
+    assert 0 <= int(acc[0]) <= 1
