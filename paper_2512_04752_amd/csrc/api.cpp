@@ -90,7 +90,7 @@ size_t sample_bytes(const spec_model_config* c, int32_t cap) {
 // Workspace carving; every region 256-byte aligned.
 struct WsLayout {
   size_t blob, toks, anc, rope, x, h, q, o, act, part_o, part_ml, lm_val, lm_idx, argmax, splitk,
-      logits, resid, kv4_step, kv4_rows, qkv, total;
+      logits, resid, kv4_step, kv4_rows, total;
   size_t blob_bytes;
 };
 
@@ -132,11 +132,11 @@ WsLayout ws_layout(const spec_model_config* c, int64_t max_batch, int64_t max_to
   L.lm_val = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.lm_idx = take(max_tokens * (size_t)(c->vocab / 64) * 4);
   L.argmax = take(max_tokens * 4);
-  L.splitk = take(w4 ? kW4PartialCap : gemm_partial_bytes());
+  const size_t qkv = nq_hd + 2 * (size_t)c->n_kv_heads * c->head_dim;
+  L.splitk = take(w4 ? std::max(kW4PartialCap, max_tokens * std::max(qkv, (size_t)c->hidden) * 4) : gemm_partial_bytes());
   if (sampling || w4) L.logits = take(max_tokens * (size_t)c->vocab * 4);
   if (sampling)     // speculative sampling: node decisions, fp64 residual rows
     L.resid = take(sample_accept_scratch((int)max_batch, (int)max_tokens, c->vocab));
-  if (w4) L.qkv = take(max_tokens * (nq_hd + 2 * (size_t)c->n_kv_heads * c->head_dim) * 4);
   if (kv4) {   // the step's plan, and one layer's rotated K/V on their way into the cache
     L.kv4_step = take(kv4_step_bytes(c, max_batch, max_tokens, kv4_pages));
     L.kv4_rows = take(max_tokens * 2 * (size_t)c->n_kv_heads * c->head_dim * 2);
@@ -633,8 +633,9 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
   // Every RMSNorm after the first follows a residual product (O or down
   // projection); when that product is split over K the norm runs inside its
   // split-K reduction, otherwise on its own.
+  bool fused;
   auto resid_then_norm = [&](int kind, GemmArgs g, const void* gain, const char* what) -> int {
-    bool fused = false;
+    fused = false;
     g.norm_gain = (const bf16*)gain;
     g.norm_out = d_h;
     g.norm_eps = cfg->rms_eps;
@@ -661,29 +662,42 @@ int verify_impl(const spec_model_config* cfg, const spec_weights* w, spec_kv* kv
     return SPEC_OK;
   };
   if (w4) {
-    float* d_qkv = (float*)(ws + ly.qkv);
+    float* partial = (float*)(ws + ly.splitk);
     float* logits = D.logits ? D.logits : (float*)(ws + ly.logits);
     const int wide = (nq + 2 * nkv) * hd;
     const W4Plan p_qkv = plan_w4(wide, H, N, false), p_o = plan_w4(H, nq * hd, N, false),
                  p_gate_up = plan_w4(F, H, N, true), p_down = plan_w4(H, F, N, false),
                  p_head = plan_w4(V, H, N, false);
+    // x += a product, and the norm that follows in the kernel that joins its splits.
+    auto resid_norm = [&](int kind, const W4Plan& plan, const spec_w4& m, const bf16* x, const void* gain,
+                          const char* what) -> int {
+      if (int rc = w4_product(kind, plan, m, nullptr, x, nullptr, kW4Partial, what)) return rc;
+      GemmArgs g = ga;
+      g.plan.splits = plan.splits;
+      g.N = H;
+      g.x = d_x;
+      g.norm_gain = (const bf16*)gain;
+      g.norm_out = d_h;
+      g.norm_eps = cfg->rms_eps;
+      g.norm_done = &fused;
+      fused = false;
+      HIP_TRY(launch_resid_reduce(g, s), what);
+      if (!fused) HIP_TRY(launch_rmsnorm(d_x, (const bf16*)gain, d_h, N, H, cfg->rms_eps, s), "rmsnorm");
+      return SPEC_OK;
+    };
     for (int l = 0; l < L; ++l) {
       const void* next_norm = l + 1 < L ? attn_norm[l + 1] : final_norm;
-      if (int rc = w4_product(SPEC_K_GEMM_QKV, p_qkv, w4->wqkv[l], nullptr, d_h, d_qkv, SPEC_W4_F32, "qkv product"))
+      if (int rc = w4_product(SPEC_K_GEMM_QKV, p_qkv, w4->wqkv[l], nullptr, d_h, nullptr, kW4Partial, "qkv product"))
         return rc;
-      HIP_TRY(launch_place_qkv(d_qkv, N, d_si, d_toks, d_rope, d_q, kv4 ? d_kv4 : kv->pool, kv4 ? 0 : l, nq, nkv, hd,
+      HIP_TRY(launch_place_qkv(partial, p_qkv.splits, N, d_si, d_toks, d_rope, d_q, kv4 ? d_kv4 : kv->pool, kv4 ? 0 : l, nq, nkv, hd,
                                s),
               "place q, k, v");
       if (int rc = attend(l)) return rc;
-      if (int rc = w4_product(SPEC_K_GEMM_O, p_o, w4->wo[l], nullptr, d_o, d_x, SPEC_W4_ADD, "o product")) return rc;
-      HIP_TRY(launch_rmsnorm(d_x, (const bf16*)ffn_norm[l], d_h, N, H, cfg->rms_eps, s), "rmsnorm");
+      if (int rc = resid_norm(SPEC_K_GEMM_O, p_o, w4->wo[l], d_o, ffn_norm[l], "o product")) return rc;
       if (int rc = w4_product(SPEC_K_GEMM_GATE_UP, p_gate_up, w4->w_gate[l], &w4->w_up[l], d_h, d_act, SPEC_W4_BF16,
                               "gate/up product"))
         return rc;
-      if (int rc = w4_product(SPEC_K_GEMM_DOWN, p_down, w4->w_down[l], nullptr, d_act, d_x, SPEC_W4_ADD,
-                              "down product"))
-        return rc;
-      HIP_TRY(launch_rmsnorm(d_x, (const bf16*)next_norm, d_h, N, H, cfg->rms_eps, s), "rmsnorm");
+      if (int rc = resid_norm(SPEC_K_GEMM_DOWN, p_down, w4->w_down[l], d_act, next_norm, "down product")) return rc;
     }
     if (int rc = w4_product(SPEC_K_LM_HEAD, p_head, w4->lm_head, nullptr, d_h, logits, SPEC_W4_F32, "lm head"))
       return rc;

@@ -138,6 +138,9 @@ hipError_t launch_gemm(int epi, const GemmArgs& a, hipStream_t s);
 // The plan of an [M x N] product with inner dimension K and weight segments of
 // n0, n1, ... rows; norm: an RMSNorm follows.
 GemmPlan plan_gemm(int epi, int M, int N, int K, int n0, int n1, bool norm);
+// What follows a residual product whose splits lie in a.partial, [plan.splits][M][N] in column order:
+// x += their sum, and the norm as above.
+hipError_t launch_resid_reduce(const GemmArgs& a, hipStream_t s);
 // Bytes of split-K partial storage launch_gemm may use through GemmArgs::partial.
 size_t gemm_partial_bytes();
 // Device address of the current device's static scratch (noalloc.hip).
@@ -176,9 +179,9 @@ hipError_t launch_rmsnorm(const float* x, const bf16* gain, bf16* out, int n, in
                           float eps, hipStream_t s);
 hipError_t launch_argmax_reduce(const float* part_val, const int32_t* part_idx, int n, int parts,
                                 int32_t* argmax, int32_t* dbg_argmax, hipStream_t s);
-// q, k and v of a product of their own, fp32 [n][(n_heads + 2 n_kv_heads) head_dim]: q and k rotated,
-// q to its rows, k and v to their slots of layer `layer`.
-hipError_t launch_place_qkv(const float* qkv, int n, const SampleInfo* samples, const TokInfo* toks,
+// q, k and v of a product whose splits are added here, fp32 [splits][n][(n_heads + 2 n_kv_heads)
+// head_dim]: q and k rotated, q to its rows, k and v to their slots of layer `layer`.
+hipError_t launch_place_qkv(const float* qkv, int splits, int n, const SampleInfo* samples, const TokInfo* toks,
                             const float2* rope_cs, bf16* q, bf16* kv_pool, int layer, int n_heads,
                             int n_kv_heads, int head_dim, hipStream_t s);
 // Row maxima of fp32 logits [n][vocab], lowest index of equal ones, per logit_parts() part.

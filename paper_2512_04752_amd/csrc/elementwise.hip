@@ -174,10 +174,10 @@ __global__ __launch_bounds__(256) void row_front_kernel(const TokInfo* toks, con
   }
 }
 
-// The rotation and the places of q, k and v behind a product that leaves them in fp32 rows
-// (the 4-bit products; the bf16 one has this in its epilogue).  A thread has four dims and
+// The join, the rotation and the places of q, k and v behind a product that leaves its splits
+// in fp32 (the 4-bit one; the bf16 one has this in its epilogue and its reduction).  A thread has four dims and
 // their partners half a head on.  Bound by its launch below some hundred rows.
-__global__ __launch_bounds__(256) void place_qkv_kernel(const float* qkv, int n, const SampleInfo* samples,
+__global__ __launch_bounds__(256) void place_qkv_kernel(const float* qkv, int splits, int n, const SampleInfo* samples,
                                                         const TokInfo* toks, const float2* rope_cs, bf16* q,
                                                         bf16* kv_pool, int layer, int n_heads, int n_kv_heads,
                                                         int hd) {
@@ -188,7 +188,13 @@ __global__ __launch_bounds__(256) void place_qkv_kernel(const float* qkv, int n,
   int head = rem / quads;
   const int fi = rem % quads * 4;
   const float* src = qkv + ((int64_t)row * heads + head) * hd + fi;
+  const int64_t plane = (int64_t)n * heads * hd;
   f32x4 x1 = *(const f32x4*)src, x2 = *(const f32x4*)(src + half);
+#pragma unroll 4
+  for (int p = 1; p < splits; ++p) {
+    x1 += *(const f32x4*)(src + p * plane);
+    x2 += *(const f32x4*)(src + p * plane + half);
+  }
   bf16* dst;
   if (head < n_heads) {
     dst = q + ((int64_t)row * n_heads + head) * hd + fi;
@@ -458,13 +464,13 @@ hipError_t launch_rmsnorm(const float* x, const bf16* gain, bf16* out, int n, in
   return hipGetLastError();
 }
 
-hipError_t launch_place_qkv(const float* qkv, int n, const SampleInfo* samples, const TokInfo* toks,
+hipError_t launch_place_qkv(const float* qkv, int splits, int n, const SampleInfo* samples, const TokInfo* toks,
                             const float2* rope_cs, bf16* q, bf16* kv_pool, int layer, int n_heads,
                             int n_kv_heads, int head_dim, hipStream_t s) {
   const int64_t threads = (int64_t)n * (n_heads + 2 * n_kv_heads) * (head_dim / 8);
   if (threads > 0xffffff00ll) return hipErrorInvalidValue;
-  place_qkv_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(qkv, n, samples, toks, rope_cs, q, kv_pool,
-                                                                     layer, n_heads, n_kv_heads, head_dim);
+  place_qkv_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(qkv, splits, n, samples, toks, rope_cs, q,
+                                                                     kv_pool, layer, n_heads, n_kv_heads, head_dim);
   return hipGetLastError();
 }
 

@@ -1025,6 +1025,8 @@ GemmPlan plan_gemm(int epi, int M, int N, int K, int n0, int n1, bool norm) {
 
 size_t gemm_partial_bytes() { return kPartialCap; }
 
+hipError_t launch_resid_reduce(const GemmArgs& a, hipStream_t s) { return launch_reduce<EPI_RESID>(a, s); }
+
 hipError_t launch_gemm(int epi, const GemmArgs& a, hipStream_t s) {
   switch (epi) {
     case EPI_QKV: return launch_epi<EPI_QKV>(a, s);

@@ -27,6 +27,8 @@ struct W4Plan {
   int splits;      // of the columns, over work-groups
 };
 
+constexpr int kW4Partial = -1;    // the sums of every split stay in W4Args::partial, for who joins them
+
 struct W4Args {
   W4Plan plan;
   const char* w0;           // W, or gate
@@ -37,7 +39,7 @@ struct W4Args {
   int n;                    // rows of x
   void* out;
   int64_t out_stride;
-  int kind;                 // SPEC_W4_*
+  int kind;                 // SPEC_W4_*, or kW4Partial
   float* partial;           // [splits][matrices][n][16 * row tiles]
 };
 

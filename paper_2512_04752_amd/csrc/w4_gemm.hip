@@ -80,7 +80,7 @@ __device__ __forceinline__ f32x4 gated(f32x4 g, f32x4 u) {
 template <bool PAIR>
 __device__ __forceinline__ void finish(const W4Args& a, int split, int row, int col, const f32x4 (&v)[PAIR ? 2 : 1]) {
   constexpr int MATS = PAIR ? 2 : 1;
-  if (a.plan.splits > 1) {
+  if (a.plan.splits > 1 || a.kind == kW4Partial) {
     const int padded = (a.rows + 15) / 16 * 16;
 #pragma unroll
     for (int k = 0; k < MATS; ++k)
@@ -460,7 +460,7 @@ hipError_t launch_shape(const W4Args& a, hipStream_t s) {
 template <bool PAIR>
 hipError_t launch_pair(const W4Args& a, hipStream_t s) {
   const hipError_t e = launch_shape<PAIR>(a, s);
-  if (e != hipSuccess || a.plan.splits == 1) return e;
+  if (e != hipSuccess || a.plan.splits == 1 || a.kind == kW4Partial) return e;
   const int64_t threads = (int64_t)a.n * ((a.rows + 15) / 16 * 4);
   if ((threads + 255) / 256 > kMaxGrid) return hipErrorInvalidValue;
   w4_reduce_kernel<PAIR><<<(unsigned)((threads + 255) / 256), 256, 0, s>>>(a);

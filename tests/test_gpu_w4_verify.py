@@ -71,6 +71,16 @@ def test_over_the_bf16_pool(name, rows):
             assert torch.equal(got[:, :, keep].view(torch.int16), want[:, :, keep].view(torch.int16))
 
 
+def test_rows_too_long_for_one_block():
+    """Rows of more than 8192 values: the norm takes a launch of its own."""
+    cfg = wl.ModelConfig(1, 8320, 2, 2, 64, 256, 384)
+    rng = np.random.default_rng(2)
+    W, ver = setup(cfg, [80, 80], 4, 40)
+    fill_bf16(ver, [20, 3], 1)
+    for rows in ([1, 1], [17, 9]):
+        full_check(cfg, W, ver, [0, 1], trees_of(rng, cfg, rows), [20, 3], envelope=True)
+
+
 @pytest.mark.parametrize("name", ["tiny", "d128", "g1"])
 def test_over_the_4bit_pool_with_commits(monkeypatch, name):
     cfg = CONFIGS[name]
