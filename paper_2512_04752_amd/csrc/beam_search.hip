@@ -20,36 +20,30 @@ namespace {
 
 constexpr int64_t kMaxGrid = 0xffffffffll / 1024;
 
-// e^d for -1000 <= d <= 690, relative error below 3e-10: 2^n times the series of exp(f ln 2),
-// d log2 e = n + f, |f| <= 1/2, cut where the next term, (ln 2 / 2)^9 / 9!, is 2e-10 (and of
-// a sum of many far less).  n comes out of an addition that leaves it in the low bits, and
-// goes into the exponent by an integer one: all of it at the rate of fp64 additions.  The
-// constants are held in scalar registers (of constants that the compiler knows, it copies
-// each into the result first and then accumulates, twice the instructions).
+// e^d for -1000 <= d <= 690, relative error below 5e-11: d log2 e = n + f, |f| <= 1/2, and 2^n
+// times the polynomial of degree 7 with the smallest largest relative error of 2^f (4.0e-11 by
+// Remez's exchange; the series needs degree 9 for that).  n comes out of an addition that leaves
+// it in the low bits, and goes into the exponent by an integer one: all of it at the rate of
+// fp64 additions.  The constants are held in scalar registers (of constants that the compiler
+// knows, it copies each into the result first and then accumulates, twice the instructions).
 struct Exp {
-  double log2e, big, c[9];
-  __device__ __forceinline__ Exp() {
-    constexpr double L = 0.69314718055994530942;
+  double log2e, big, c[8];
+  __device__ __forceinline__ Exp()
+      : c{0.9999999999616818, 0.6931471807284476, 0.24022651198157954, 0.05550410353446558, 0.009618027253642348,
+          0.0013333922564381022, 0.0001546929114641026, 1.5201921442377536e-05} {
     log2e = 1.44269504088896340736;
     // 1.5 * 2^52, and 2^12 that the shift drops: without it the low word is 0, and then this
     // compiler (ROCm 7.2) loads it by s_mov_b64 with a 64-bit literal, which there is none of.
     big = 6755399441055744.0 + 4096.0;
-    double t = L;
+    asm volatile("" : "+s"(log2e), "+s"(big), "+v"(c[7]));         // an instruction reads one scalar pair
 #pragma unroll
-    for (int i = 1; i < 9; ++i) {
-      c[i] = t;                              // ln 2^i / i!
-      t *= L / (i + 1);
-    }
-    asm volatile("" : "+s"(log2e), "+s"(big), "+v"(c[8]));         // an instruction reads one scalar pair
-#pragma unroll
-    for (int i = 1; i < 8; ++i) asm volatile("" : "+s"(c[i]));
+    for (int i = 0; i < 7; ++i) asm volatile("" : "+s"(c[i]));
   }
   __device__ __forceinline__ double operator()(double d) const {
     const double m = fma(d, log2e, big), f = fma(d, log2e, big - m);
-    double y = fma(f, c[8], c[7]);
+    double y = fma(f, c[7], c[6]);
 #pragma unroll
-    for (int i = 6; i >= 1; --i) y = fma(y, f, c[i]);
-    y = fma(y, f, 1.0);
+    for (int i = 5; i >= 0; --i) y = fma(y, f, c[i]);
     i32x2 b = __builtin_bit_cast(i32x2, y);
     b[1] += __builtin_bit_cast(i32x2, m)[0] << 20;
     return __builtin_bit_cast(double, b);
@@ -140,7 +134,7 @@ __device__ __forceinline__ void insert(uint64_t& l, uint64_t key, int lane) {
 
 // Put n <= 64 more into it, by counting for each what is better: about 5 instructions per new
 // entry and 3 per old one, where insert() takes 20 for each.
-constexpr int kFew = 5;
+constexpr int kFew = 5, kEnough = 32;
 __device__ __forceinline__ void merge(uint64_t& l, const uint64_t* found, uint64_t* merged, int n, int k, int lane) {
   const uint64_t x = lane < n ? found[lane] : 0;
   int rank = 0, old = lane;
@@ -217,9 +211,9 @@ struct Vectors {
 
 // A wave goes through its segment in batches of kVecs vectors per lane, the next batch on
 // its way while one is worked on.  Per number: 18 instructions of fp64 rate for its term,
-// one comparison with the k-th best so far, and the few that pass go into the list one by
-// one (k ln(n / k) of n in random order).  The first batch gives the list a lower bound to
-// start with.
+// one comparison with the k-th best so far, and the few that pass (k ln(n / k) of n in random
+// order) go side by side and into the list when there are enough of them.  The first batch
+// gives a bound to start with.
 template <class T>
 __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int PER = Vectors<T>::PER, kVecs = 16 / PER;
@@ -235,6 +229,7 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
   double sum = 0.0;
   uint64_t best = 0;
   float least = -INFINITY;      // only what is above can be one of the k best: tokens come in ascending order
+  int n = 0;                    // found since
   bool first = true;
   constexpr int kStep = 64 * kVecs;
   const T* at_lane = vec.row + (int64_t)(v0 + lane) * PER;
@@ -260,9 +255,13 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
 #pragma unroll
       for (int i = 1; i < PER; ++i) m[j] = __builtin_elementwise_maximum(m[j], z[j][i]);   // a NaN when there is one
     }
-    float most = m[0];
+    float most = m[0], lowest = z[0][0];
 #pragma unroll
     for (int j = 1; j < kVecs; ++j) most = __builtin_elementwise_maximum(most, m[j]);
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) lowest = __builtin_elementwise_minimum(lowest, z[j][i]);
     // Terms relative to `top`: doubles hold e^600, and what is below e^-690 of it counts as
     // that.  A NaN makes the sum one, an infinity `top`.
     if (__ballot(!(most <= top + 600.f))) {
@@ -271,12 +270,23 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
         top = most;
       }
     }
+    // (Vectors past the segment add nothing, and most rows have nothing to clamp.)
+    const int vecs = min(kVecs, (v1 - v + 63) / 64);
+    const double base = (double)top;
+    auto add = [&](auto clamp) {
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
+      for (int j = 0; j < kVecs; ++j) {
+        if (j >= vecs) break;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) sum += exp(fmax((double)z[j][i] - (double)top, -690.0));
-      __builtin_amdgcn_sched_barrier(0);       // else all terms at once, in more registers than there are
-    }
+        for (int i = 0; i < PER; ++i) {
+          const double d = (double)z[j][i] - base;
+          sum += exp(clamp ? fmax(d, -690.0) : d);
+        }
+        __builtin_amdgcn_sched_barrier(0);     // else all terms at once, in more registers than there are
+      }
+    };
+    if (__ballot(!(lowest >= top - 680.f))) add(std::true_type{});
+    else add(std::false_type{});
     if (first) {
       first = false;
       // k of the maxima of halves of the lanes' numbers are not below it.  What equals it has to pass.
@@ -287,12 +297,17 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
         for (int i = 0; i < PER; ++i) half[i & 1] = fmaxf(half[i & 1], z[j][i]);
       least = float_below(kth_bound(half, a.k));
     }
-    if (__ballot(most > least) == 0) continue;
-    // What can be among the k best, side by side, and into the list.  Within a batch the
-    // order is another: once the bound has risen in it, what equals the bound passes too.
-    int n = 0;
+    const bool none = __ballot(most > least) == 0;
+    if (none && (n == 0 || v + kStep < v1)) continue;
+    // What can be among the k best, side by side.  Within a batch the order is another: once
+    // the bound has risen in it, what equals the bound passes too.
     float kth = least;
     auto flush = [&]() {
+      wave_sync();
+      if (lane < n) {
+        const uint64_t x = found[wave][lane];
+        found[wave][lane] = key_of(__uint_as_float((uint32_t)(x >> 32)), (int)(uint32_t)x);
+      }
       wave_sync();
       if (n > kFew) {
         merge(best, found[wave], merged[wave], n, a.k, lane);
@@ -315,11 +330,12 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
           pass = __ballot(z[j][i] > least);
         }
         const int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(pass >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)pass, n));
-        if (pass >> lane & 1) found[wave][at] = key_of(z[j][i], (v + 64 * j + lane) * PER + i);
+        if (pass >> lane & 1)
+          found[wave][at] = (uint64_t)__float_as_uint(z[j][i]) << 32 | (uint32_t)((v + 64 * j + lane) * PER + i);
         n += __popcll(pass);
       }
     }
-    flush();
+    if (n >= kEnough || v + kStep >= v1) flush();
     least = kth;
   }
   // over the wave
