@@ -370,7 +370,7 @@ constexpr int kPick = 512;         // threads
 constexpr int kHeads = kPick / 2;  // candidates that bound the k-th best
 constexpr int kListed = 1024;      // candidates that can be ranked side by side
 static_assert(kHeads == 4 * 64, "four per lane");
-constexpr int kMaxLists = 4096;    // lists of a group: plan_beam()
+constexpr int kMaxLists = 1024;    // lists of a group: plan_beam()
 static_assert(kPick / 64 * kMaxBeams <= kListed && kMaxBeams <= kHeads, "the waves' lists, and the bound's rank");
 
 // -infinity by way of vector registers: as a scalar one this compiler (ROCm 7.2) makes it
@@ -553,14 +553,19 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
 
 }  // namespace
 
-// Segments: about 4096 waves' worth of rows' pieces fill the chip, none below 64 vectors
-// (one load of each lane), at most 256 of a row.
+// Segments: about 4096 waves' worth of rows' pieces fill the chip (4 to a SIMD), none below 64
+// vectors (one load of each lane), and at most kMaxLists in a group, each a list that one
+// work-group picks from.  us, with 2048 / 4096 / 6144 / 8192 waves: 17 x 12 x 50001 bf16, k 24,
+// 30.0 / 29.2 / 28.9 / 30.3; 3 x 64 x 32000, k 64, 38.9 / 37.7 / 38.0 / 44.4; 128 x 8 x 128256
+// 114 / 112 / 112 / 113.  With 512 / 1024 / 2048 / 4096 lists: 1 x 32 x 128256 bf16, k 64, 46.5 /
+// 38.0 / 36.4 / 43.9; 1 x 16 x 128256, k 16, 23.2 / 20.9 / 22.8 / 31.0; 1 x 64 x 128000, k 64, 64.0 /
+// 49.6 / 45.3 / 52.2; 1 x 16 x 128256 bf16, k 4, 18.0 / 16.2 / 18.3 / 25.7.
 void plan_beam(BeamArgs* a) {
   const int per = a->is_bf16 ? 8 : 4;
   const int64_t rows = (int64_t)a->groups * a->width;
   const int64_t vectors = (a->vocab + per - 1) / per;
   const int64_t want = std::max<int64_t>(1, 4096 / rows), most = (vectors + 63) / 64;
-  const int64_t segs = std::min<int64_t>({want, most, 256});
+  const int64_t segs = std::min<int64_t>({want, most, kMaxLists / a->width});
   a->seg = (int)((vectors + 64 * segs - 1) / (64 * segs) * 64);
   a->segs = (int)((vectors + a->seg - 1) / a->seg);
 }
