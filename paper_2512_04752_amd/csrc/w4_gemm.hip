@@ -101,11 +101,15 @@ __device__ __forceinline__ f32x4 zeros() {
 // Few rows (up to 16): bound by the weights' bytes, and so by how many of them are on their
 // way at a time (some 10 MB over the chip).  The rows of x, or their columns of this split,
 // lie in LDS as a whole; after that a wave only loads weights, up to 2 D column tiles of a row
-// tile (of both matrices) ahead, and meets no barrier.  The sixteen waves of a work-group take KG ranges of
-// the columns for 16 / KG groups of row tiles (KG > 1: their sums meet in LDS, in order) and go
-// on with the next such set until there is none.  (Per wave and column tile 4 KB of x come
+// tile (of both matrices) ahead, and meets no barrier.  The sixteen waves of a work-group take
+// KG ranges of the columns for 16 / KG groups of row tiles (KG > 1: their sums meet in LDS, in
+// order) and go on with the next such set until there is none.  (Per wave and column tile 4 KB of x come
 // out of LDS for 1 KB of weights out of HBM; read from L2 instead, x takes more of the
 // load path than the weights, and its loads, waited for in order, hold theirs up.)
+// Calls, three copies of the weights in turn (the last-level cache may hold them): gate/up
+// 14336 x 4096, 4 rows, 12.7 us (62.5 MB, 4.9 TB/s); 4096 x 14336, 16 rows, 11.3 (31.8 MB; four
+// splits, whose reduction is 3 of it); 2048 x 2048, 1 row, 5.6: the launch and one trip through
+// the loads.
 constexpr int kStreamWaves = 16;
 template <bool PAIR>
 __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args a) {
@@ -224,7 +228,9 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
       phase_barrier();
       if (kg > 0) continue;
     }
-    if (tile < row_tiles && r < a.n) finish<PAIR>(a, split, r, tile * 16 + 4 * g, acc);
+    int row = r;
+    if constexpr (PAIR) asm volatile("" : "+v"(row));      // else places of outputs are kept over the loads, in scratch
+    if (tile < row_tiles && row < a.n) finish<PAIR>(a, split, row, tile * 16 + 4 * g, acc);
   }
 }
 
@@ -234,7 +240,9 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
 // column tile (256 bytes of every row) at a time, the 16-byte chunk of a row XOR-ed with the row,
 // so that the operand reads (16 rows, one chunk) hit all 64 banks once.  The weights go
 // straight to registers.  Both are loaded for the next column tile while one is multiplied:
-// one barrier per tile, at which the loads issued a whole tile ago have arrived.
+// one barrier per tile, at which the loads issued a whole tile ago have arrived.  Gate/up
+// 14336 x 4096, 1024 rows: 184 us, 1.30 PFLOP/s (a large bf16 product reaches 1.41), matrix cores
+// 67 % busy, vector instructions 45 %; head 128256 x 4096, 24 rows: 58 us, 5.0 TB/s.
 template <int MB, int NB, int WM, int WN, int KG, bool PAIR>
 __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_kernel(W4Args a) {
   constexpr int BM = 16 * MB * WM, BT = NB * WN / (PAIR ? 2 : 1), STAGE = BM * 256, LOADS = BM / 4 / (WM * WN);
@@ -382,7 +390,8 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_k
     }
 }
 
-// Sum the splits, in their order, and store.
+// Sum the splits, in their order, and store.  A launch, 3 us at 16 x 4096, beside which the bytes
+// (out of L2 and the last-level cache) count from about 10 MB on.
 template <bool PAIR>
 __global__ __launch_bounds__(256) void w4_reduce_kernel(W4Args a) {
   constexpr int MATS = PAIR ? 2 : 1;
@@ -470,8 +479,8 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 }  // namespace
 
 // Up to 16 rows: the stream kernel, x in LDS over as few column splits as its place there
-// allows (unless these are many), and as many waves to a row tile as still leave one round of work-groups.  (us, the
-// splits cold: 1 row 4096 x 14336, 16 / 8 / 4 / 2 waves 9.3 / 9.9 / 12.6 / 19.5; gate/up of 4 rows,
+// allows (unless these are many), and as many waves to a row tile as still leave one round of
+// work-groups.  (us, the weights out of HBM: 1 row 4096 x 14336, 16 / 8 / 4 / 2 waves 9.3 / 9.9 / 12.6 / 19.5; gate/up of 4 rows,
 // 14336 x 4096, 17.9 / 14.8 / 14.0 / 15.3; head of 1 row, 128256 x 4096, 73 / 54 / 52 / 50 and
 // alone 49; 16 rows 4096 x 14336 in 4 splits 16.2 / 14.3 / 13.8 / 14.4, in 8 no better.)
 //

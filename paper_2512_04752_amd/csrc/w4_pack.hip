@@ -5,7 +5,9 @@
 // bf16, all its loads in flight at once).  Lane l has row 4 i + l / 16 and the 8 numbers
 // from column 8 (l % 16) of each tile, so that bf16 moves as 256 contiguous bytes of four
 // rows; a group is four lanes, whose maximum goes by two DPP moves, and their 8 codes each
-// are a word of the layout.
+// are a word of the layout.  14336 x 4096: 37 us to pack and 23 to unpack, of 149 MB each (4.0
+// and 6.4 TB/s; what the first writes was last read, what the second reads was just written);
+// 61 as two calls, where a copy of as many bytes takes 58.  2048 x 2048: 5.4 and 5.0.
 #include "e2m1.h"
 #include "w4.h"
 
