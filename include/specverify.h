@@ -662,7 +662,7 @@ enum {
   SPEC_K_TRANSFER = 7,   /* spec_kv_pack / spec_kv_unpack */
   SPEC_K_ACCEPT = 8,     /* tree acceptance: greedy, greedy with EOS, or sampled */
   SPEC_K_KV4_APPEND = 9, /* spec_kv4_append (SPEC_K_ATTENTION: spec_kv4_attend too) */
-  SPEC_K_W4 = 10,        /* spec_w4_linear / spec_w4_gate_up */
+  SPEC_K_W4 = 10,        /* spec_w4_linear / spec_w4_gate_up (spec_verify_w4's: 0, 2 .. 5) */
   SPEC_K_BEAM = 11,      /* spec_beam_select */
   SPEC_K_REORDER = 12,   /* spec_kv_reorder / spec_kv4_reorder */
   SPEC_K_COUNT = 13

@@ -845,10 +845,14 @@ class W4Weights:
                 for k, layers in self.matrices.items():
                     w = torch.cat([lw["wq"], lw["wk"], lw["wv"]]) if k == "wqkv" else lw[k]
                     layers.append(W4Matrix(w, stream))
-        for t in (self.tok_embed, self.final_norm, *self.norms["attn_norm"], *self.norms["ffn_norm"]):
+        n, gains = len(self.norms["attn_norm"]), [self.final_norm, *self.norms["attn_norm"], *self.norms["ffn_norm"]]
+        vocab, hidden = self.tok_embed.shape
+        for t in (self.tok_embed, *gains):
             if t.dtype != torch.bfloat16 or t.get_device() != self.index or not t.is_contiguous():
                 raise ValueError("norm gains and the embedding must be contiguous bf16 tensors on the matrices' device")
-        n = len(self.norms["attn_norm"])
+        if any(t.shape != (hidden,) for t in gains):
+            raise ValueError(f"norm gains must have the embedding's {hidden} values")
+        self.shape = (n, hidden, vocab)
         self._arrays = {k: (c_void_p * n)(*[t.data_ptr() for t in rows]) for k, rows in self.norms.items()}
         self._arrays |= {k: (spec_w4 * n)(*[m.struct for m in layers]) for k, layers in self.matrices.items()}
         a = {k: ctypes.cast(v, POINTER(v._type_)) for k, v in self._arrays.items()}
@@ -869,9 +873,7 @@ def spec_verify_w4(cfg, weights: W4Weights, pool, sample_ids, tree_offsets, tree
     bits, over a KVPool or a KV4Pool."""
     if weights.index != pool.index:
         raise ValueError(f"the weights are on device {weights.index}, the pool on device {pool.index}")
-    if len(weights.norms["attn_norm"]) != cfg.n_layers or len(weights.final_norm) != cfg.hidden \
-            or tuple(weights.tok_embed.shape) != (cfg.vocab, cfg.hidden) \
-            or any(len(t) != cfg.hidden for rows in weights.norms.values() for t in rows):
+    if weights.shape != (cfg.n_layers, cfg.hidden, cfg.vocab):
         raise ValueError("the weights are of another shape than the model's")
     kv, kv4 = (None, pool.handle) if isinstance(pool, KV4Pool) else (pool.handle, None)
     _verify_pool(lib().spec_verify_w4, (ctypes.byref(weights.struct), kv, kv4), cfg, pool, sample_ids, tree_offsets,

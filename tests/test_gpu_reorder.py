@@ -124,6 +124,39 @@ def test_kv4_pool(kv_heads, d, layers, groups, width, begin, end, kind):
     assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("n_pages,pages", [(65536, [65535, 0]), (65600, [65599, 65536])], ids=str)
+def test_high_page_ids(n_pages, pages):
+    """Page ids take 16 bits where they go along as kernel arguments: not in a pool of more."""
+    cfg = config(2, 64, 1)
+    pool = sv.KV4Pool(cfg, 2, n_pages)
+    held = pool.buf[:sv.spec_kv4_page_bytes(cfg) * n_pages].view(n_pages, -1)
+    held.zero_()
+    for s, p in enumerate(pages):
+        pool.map(s, [p])
+        held[p] = s + 1
+    sv.spec_kv4_reorder(pool, [[0, 1]], [0], [PAGE], torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"))
+    assert (held[pages[0]] == 2).all() and (held[pages[1]] == 1).all()
+    assert int(held.long().sum()) == 3 * held.shape[1]
+
+
+def test_far_block_of_the_bf16_pool():
+    """A sample whose block begins past 4 GB."""
+    cfg = config(8, 128, 16)
+    cap = 1 + (1 << 32) // (cfg.n_layers * 2 * cfg.n_kv_heads * cfg.head_dim * 2)
+    pool = sv.KVPool(cfg, [cap, 8, 8])
+    want = []
+    for s in (1, 2):
+        k, v = pool.sample_view(s)
+        k.normal_()
+        v.normal_()
+        want.append((k.clone(), v.clone()))
+    sv.spec_kv_reorder(pool, [[1, 2]], [2], [7], torch.tensor([[1, 0]], dtype=torch.int32, device="cuda"))
+    for s in (1, 2):
+        for got, own, other in zip(pool.sample_view(s), want[s - 1], want[2 - s]):
+            assert torch.equal(got[:, :, 2:7], other[:, :, 2:7])
+            assert torch.equal(got[:, :, :2], own[:, :, :2]) and torch.equal(got[:, :, 7:], own[:, :, 7:])
+
+
 def test_refusals():
     cfg = config(2, 64, 1)
     kv, kv4 = sv.KVPool(cfg, [100] * 4), sv.KV4Pool(cfg, 4, 8)

@@ -2,6 +2,8 @@
 float64 oracle on the weights that the codes stand for, under the comparison rules of the
 bf16 step: those weights are exact in bf16, and every rounding is one that it has too."""
 
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -152,10 +154,13 @@ def test_refusals():
         sv.Verifier(cfg, ver.weights, [64], 1, 16)
     with pytest.raises(ValueError, match="weights"):
         sv.Verifier(cfg, ver.weights, [64], 1, 16, weights="int8")
-    ver.weights.norms["ffn_norm"].append(ver.weights.final_norm[:64])
+    bad = wl.make_weights(cfg, 1, device="cuda")
+    bad["layers"][1]["ffn_norm"] = bad["layers"][1]["ffn_norm"][:64]
+    with pytest.raises(ValueError, match="gains"):
+        sv.W4Weights(bad)
+    deeper = sv.Verifier(dataclasses.replace(cfg, n_layers=3), ver.weights, [64], 1, 16, weights="w4")
     with pytest.raises(ValueError, match="shape"):
-        ver.verify([0], [tree], [0])
-    ver.weights.norms["ffn_norm"].pop()
+        deeper.verify([0], [tree], [0])
     graph = torch.cuda.CUDAGraph()
     out = torch.zeros(1, device="cuda")
     with torch.cuda.graph(graph):
