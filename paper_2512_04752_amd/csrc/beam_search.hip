@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "beam.h"
+#include "gemm_tile.h"
 
 namespace spec {
 
@@ -216,14 +217,34 @@ struct Vectors {
 // gives a bound to start with.  128 x 8 x 128256 fp32: 102 us for 525 MB (5.1 TB/s), vector
 // instructions 80 % busy; 17 x 12 x 50001 bf16, k 24: 20 us for 20 MB, 60 % busy, of whose 1480
 // instructions per wave the list takes a third; 4 x 32000 fp32: 5.4, launch and one trip.
-template <class T>
-__global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
+//
+// TEAM: the four waves of a work-group have four segments of one row, of which the k best
+// matter.  Each tells the others its k / 4-th best so far: k numbers are not below the
+// smallest of these four, and what is stays out of every list (which need not fill up).  They
+// are read as they are, however old: a bound only rises.
+constexpr int kTeam = 4;
+template <class T, bool TEAM>
+__global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int PER = Vectors<T>::PER, kVecs = 16 / PER;
-  __shared__ uint64_t found[4][64], merged[4][64];
+  __shared__ uint64_t found[kTeam][64], merged[kTeam][64];
+  __shared__ __attribute__((aligned(16))) float told[kTeam];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int row = (int)(id / a.segs), seg = (int)(id % a.segs);
+  const int teams = (a.segs + kTeam - 1) / kTeam;
+  const int64_t id = (int64_t)blockIdx.x * kTeam + wave;
+  const int row = TEAM ? (int)(blockIdx.x / teams) : (int)(id / a.segs);
+  const int seg = TEAM ? (int)(blockIdx.x % teams) * kTeam + wave : (int)(id % a.segs);
   if (row >= a.groups * a.width || !beam_live(a, row)) return;
+  const int members = TEAM ? min(kTeam, a.segs - (seg - wave)) : 1, share = (a.k + members - 1) / members;
+  if (TEAM && wave >= members) {
+    if (lane == 0) told[wave] = INFINITY;
+    wait_lds();
+    phase_barrier();
+    return;
+  }
+  auto told_by_all = [&]() {
+    const f32x4 t = *(const volatile f32x4*)told;
+    return float_below(fminf(fminf(t[0], t[1]), fminf(t[2], t[3])));
+  };
   const Vectors<T> vec{(const T*)a.logits + row * a.row_stride, a.vocab};
   const int v0 = seg * a.seg, v1 = min((a.vocab + PER - 1) / PER, v0 + a.seg);
   float top = kLowest;          // the lane's reference: its largest logit so far, less 600 at most
@@ -297,8 +318,15 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
       for (int j = 0; j < kVecs; ++j)
 #pragma unroll
         for (int i = 0; i < PER; ++i) half[i & 1] = fmaxf(half[i & 1], z[j][i]);
-      least = float_below(kth_bound(half, a.k));
+      const float bound = kth_bound(half, share);
+      if constexpr (TEAM) {
+        if (lane == 0) told[wave] = bound;
+        wait_lds();
+        phase_barrier();
+      }
+      least = TEAM ? told_by_all() : float_below(bound);
     }
+    if constexpr (TEAM) least = fmaxf(least, told_by_all());
     const bool none = __ballot(most > least) == 0;
     if (none && (n == 0 || v + kStep < v1)) continue;
     // What can be among the k best, side by side.  Within a batch the order is another: once
@@ -318,6 +346,7 @@ __global__ __launch_bounds__(256, 4) void beam_scan_kernel(BeamArgs a) {
       }
       n = 0;
       kth = fmaxf(least, logit_of(lane_value64(best, a.k - 1)));
+      if (TEAM && lane == 0) told[wave] = fmaxf(told[wave], logit_of(lane_value64(best, share - 1)));
     };
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
@@ -590,12 +619,20 @@ size_t beam_scratch(BeamArgs* a, char* base) {
 }
 
 hipError_t launch_beam(const BeamArgs& a, hipStream_t s) {
-  const int64_t waves = (int64_t)a.groups * a.width * a.segs;
-  if ((waves + 3) / 4 > kMaxGrid) return hipErrorInvalidValue;
-  const unsigned grid = (unsigned)((waves + 3) / 4);
-  if (a.is_bf16) beam_scan_kernel<bf16><<<grid, 256, 0, s>>>(a);
-  else beam_scan_kernel<float><<<grid, 256, 0, s>>>(a);
-  if (const hipError_t e = hipGetLastError()) return e;
+  const int64_t rows = (int64_t)a.groups * a.width;
+  auto scan = [&](auto kernel, int64_t blocks) {
+    if (blocks > kMaxGrid) return hipErrorInvalidValue;
+    kernel<<<(unsigned)blocks, 64 * kTeam, 0, s>>>(a);
+    return hipGetLastError();
+  };
+  const int64_t teams = rows * ((a.segs + kTeam - 1) / kTeam), pieces = (rows * a.segs + kTeam - 1) / kTeam;
+  // Up to 8 best the team's words cost more than they save (us: 4 x 32000, k 4, 13.2 alone and 13.5
+  // as teams; 8 x 128256, k 8, 15.6 and 15.9; 16 x 128256, k 16, 20.9 and 20.6; 17 x 12 x 50001, k 24,
+  // 29.2 and 27.6; 3 x 64 x 32000, k 64, 36.7 and 30.8; 4 x 64 x 128256 bf16, k 64, 69.5 and 57.6).
+  const hipError_t e = a.segs >= kTeam && a.k > 8
+                           ? a.is_bf16 ? scan(beam_scan_kernel<bf16, true>, teams) : scan(beam_scan_kernel<float, true>, teams)
+                           : a.is_bf16 ? scan(beam_scan_kernel<bf16, false>, pieces) : scan(beam_scan_kernel<float, false>, pieces);
+  if (e != hipSuccess) return e;
   beam_pick_kernel<<<a.groups, kPick, 0, s>>>(a);
   return hipGetLastError();
 }
