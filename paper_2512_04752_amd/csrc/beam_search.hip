@@ -215,8 +215,8 @@ struct Vectors {
 // one comparison with the k-th best so far, and the few that pass (k ln(n / k) of n in random
 // order) go side by side and into the list when there are enough of them.  The first batch
 // gives a bound to start with.  128 x 8 x 128256 fp32: 102 us for 525 MB (5.1 TB/s), vector
-// instructions 80 % busy; 17 x 12 x 50001 bf16, k 24: 20 us for 20 MB, 60 % busy, of whose 1480
-// instructions per wave the list takes a third; 4 x 32000 fp32: 5.4, launch and one trip.
+// instructions 80 % busy; 17 x 12 x 50001 bf16, k 24: 18 us for 20 MB, 61 % busy, half of whose
+// 1270 instructions per wave are the terms; 4 x 32000 fp32: 5.4, launch and one trip.
 //
 // TEAM: the four waves of a work-group have four segments of one row, of which the k best
 // matter.  Each tells the others its k / 4-th best so far: k numbers are not below the
@@ -593,11 +593,14 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
 // 114 / 112 / 112 / 113.  With 512 / 1024 / 2048 / 4096 lists: 1 x 32 x 128256 bf16, k 64, 46.5 /
 // 38.0 / 36.4 / 43.9; 1 x 16 x 128256, k 16, 23.2 / 20.9 / 22.8 / 31.0; 1 x 64 x 128000, k 64, 64.0 /
 // 49.6 / 45.3 / 52.2; 1 x 16 x 128256 bf16, k 4, 18.0 / 16.2 / 18.3 / 25.7.
+// Many rows have few segments: four, for a team, where 16 or more are chosen from 1000 vectors or
+// more (with less than four / four: 90 x 24 x 32000, k 24, 91.6 / 75.6; 128 x 64 x 8000 bf16, k 64,
+// 107 / 99; but 150 x 10 x 50001, k 10, 70.2 / 73.0; 128 x 64 x 2000, k 32, 39.7 / 52.5).
 void plan_beam(BeamArgs* a) {
   const int per = a->is_bf16 ? 8 : 4;
   const int64_t rows = (int64_t)a->groups * a->width;
   const int64_t vectors = (a->vocab + per - 1) / per;
-  const int64_t want = std::max<int64_t>(1, 4096 / rows), most = (vectors + 63) / 64;
+  const int64_t want = std::max<int64_t>(a->k >= 16 && vectors >= 1000 ? kTeam : 1, 4096 / rows), most = (vectors + 63) / 64;
   const int64_t segs = std::min<int64_t>({want, most, kMaxLists / a->width});
   a->seg = (int)((vectors + 64 * segs - 1) / (64 * segs) * 64);
   a->segs = (int)((vectors + a->seg - 1) / a->seg);

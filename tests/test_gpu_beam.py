@@ -50,7 +50,7 @@ def scores(seed, groups, width):
 @pytest.mark.parametrize("groups,width,vocab,k", [
     (1, 1, 1, 1), (1, 1, 5, 3), (3, 2, 63, 7), (2, 5, 64, 64), (1, 4, 257, 4), (4, 8, 1000, 8), (1, 64, 300, 64),
     (2, 64, 1025, 1), (1, 1, 32001, 17), (5, 3, 4099, 33), (2, 12, 50001, 24), (1, 1, 128256, 64), (9, 7, 8192, 10),
-    (70, 9, 515, 9)])
+    (70, 9, 515, 9), (40, 30, 8001, 20)])
 def test_select(groups, width, vocab, k, dtype):
     """bf16 logits bring many equal ones within a beam: the lower token first."""
     z = logits(vocab + k, groups, width, vocab, dtype)
