@@ -91,16 +91,67 @@ __device__ __forceinline__ X from_below64(X x) {
   return __builtin_bit_cast(X, (uint64_t)hi << 32 | lo);
 }
 
+// Both halves of 2 S lanes, whose S lanes each have the same of their own: x and its partner's,
+// the same pair in all.  Moves inside and between rows of 16 lanes; through LDS (a shuffle)
+// each takes some 100 cycles, which at a wave's end nothing hides.
+template <int S>
+__device__ __forceinline__ void halves_of(uint32_t x, uint32_t* a, uint32_t* b) {
+  if constexpr (S < 16) {
+    constexpr int MOVE = S == 1 ? 0xb1 : S == 2 ? 0x4e : S == 4 ? 0x141 : 0x140;    // quads' lanes, mirrors of 8 and 16
+    *a = x;
+    *b = (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, MOVE, 0xf, 0xf, false);
+  } else {
+    const auto r = S == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false)
+                           : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    *a = r[0];
+    *b = r[1];
+  }
+}
+template <int S>
+__device__ __forceinline__ float max_of_halves(float x) {
+  uint32_t a, b;
+  halves_of<S>(__float_as_uint(x), &a, &b);
+  return __builtin_elementwise_maximum(__uint_as_float(a), __uint_as_float(b));
+}
+template <int S>
+__device__ __forceinline__ double sum_of_halves(double x) {
+  const i32x2 v = __builtin_bit_cast(i32x2, x);
+  uint32_t a[2], b[2];
+  halves_of<S>((uint32_t)v[0], &a[0], &b[0]);
+  halves_of<S>((uint32_t)v[1], &a[1], &b[1]);
+  return __builtin_bit_cast(double, i32x2{(int)a[0], (int)a[1]}) + __builtin_bit_cast(double, i32x2{(int)b[0], (int)b[1]});
+}
+// Over groups of `lanes` neighbours (a power of two), every lane of a group the same.
+__device__ __forceinline__ float max_over(float x, int lanes) {
+  if (lanes > 1) x = max_of_halves<1>(x);
+  if (lanes > 2) x = max_of_halves<2>(x);
+  if (lanes > 4) x = max_of_halves<4>(x);
+  if (lanes > 8) x = max_of_halves<8>(x);
+  if (lanes > 16) x = max_of_halves<16>(x);
+  if (lanes > 32) x = max_of_halves<32>(x);
+  return x;
+}
+__device__ __forceinline__ double sum_over(double x, int lanes) {
+  if (lanes > 1) x = sum_of_halves<1>(x);
+  if (lanes > 2) x = sum_of_halves<2>(x);
+  if (lanes > 4) x = sum_of_halves<4>(x);
+  if (lanes > 8) x = sum_of_halves<8>(x);
+  if (lanes > 16) x = sum_of_halves<16>(x);
+  if (lanes > 32) x = sum_of_halves<32>(x);
+  return x;
+}
+
 // The largest float below x; -infinity and NaN stay.
 __device__ __forceinline__ float float_below(float x) {
   const int b = __float_as_int(x);
   return !(x > -INFINITY) ? x : b == 0 ? -1e-45f : __int_as_float(b > 0 ? b - 1 : b + 1);
 }
 
-// A bound that at least k of the wave's N x 64 numbers are not below, within 2^-11 of the
-// k-th largest (k <= 64 N): the leading 20 bits of its place in the order of floats, found
-// from the top by counting.  -infinity where it is that.
-template <int N>
+// A bound that at least k of the wave's N x 64 numbers are not below, within 2^-7 of the
+// k-th largest (k <= 64 N): the leading 16 bits of its place in the order of floats, found
+// from the top by counting, BITS at a time (a step waits for its counts, some 100 cycles).
+// -infinity where it is that.
+template <int BITS, int N>
 __device__ __forceinline__ float kth_bound(const float (&x)[N], int k) {
   uint32_t u[N], t = 0;
 #pragma unroll
@@ -109,12 +160,16 @@ __device__ __forceinline__ float kth_bound(const float (&x)[N], int k) {
     u[i] = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
   }
 #pragma unroll
-  for (int bit = 31; bit >= 12; --bit) {
-    const uint32_t with = t | 1u << bit;
-    int n = 0;
+  for (int bit = 32 - BITS; bit >= 16; bit -= BITS) {
+    uint32_t up = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += __popcll(__ballot(u[i] >= with));
-    if (n >= k) t = with;
+    for (uint32_t c = 1; c < 1u << BITS; ++c) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) n += __popcll(__ballot(u[i] >= (t | c << bit)));
+      up += n >= k;
+    }
+    t |= up << bit;
   }
   return t <= 0x007fffffu ? -INFINITY : __uint_as_float(t & 0x80000000u ? t ^ 0x80000000u : ~t);
 }
@@ -318,7 +373,7 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
       for (int j = 0; j < kVecs; ++j)
 #pragma unroll
         for (int i = 0; i < PER; ++i) half[i & 1] = fmaxf(half[i & 1], z[j][i]);
-      const float bound = kth_bound(half, share);
+      const float bound = kth_bound<1>(half, share);
       if constexpr (TEAM) {
         if (lane == 0) told[wave] = bound;
         wait_lds();
@@ -370,12 +425,8 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
     least = kth;
   }
   // over the wave
-  float all = top;
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) all = __builtin_elementwise_maximum(all, __shfl_xor(all, x));
-  sum = exp.scaled(sum, (double)top - (double)all);
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+  const float all = max_over(top, 64);
+  sum = sum_over(exp.scaled(sum, (double)top - (double)all), 64);
   const int64_t at = (int64_t)row * a.segs + seg;
   if (lane == 0) {
     a.tops[at] = all;
@@ -470,11 +521,11 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     float top = t0;
     for (int i = sub + lanes; i < a.segs; i += lanes)
       top = __builtin_elementwise_maximum(top, a.tops[(int64_t)row * a.segs + i]);
-    for (int x = lanes / 2; x >= 1; x >>= 1) top = __builtin_elementwise_maximum(top, __shfl_xor(top, x));
+    top = max_over(top, lanes);
     double sum = sub < a.segs ? exp.scaled(x0, (double)t0 - (double)top) : 0.0;
     for (int i = sub + lanes; i < a.segs; i += lanes)
       sum += exp.scaled(a.sums[(int64_t)row * a.segs + i], (double)a.tops[(int64_t)row * a.segs + i] - (double)top);
-    for (int x = lanes / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+    sum = sum_over(sum, lanes);
     if (sub == 0 && w < a.width) {
       lse[w] = live && top < INFINITY ? (double)top + log(sum) : NAN;
       score[w] = s;
@@ -490,13 +541,13 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   auto kth_of = [&](double x) {
     float h = (float)x;                          // not above the double
     if ((double)h > x) h = float_below(h);
-    h = fmaxf(h, __shfl_xor(h, 1));
+    h = max_of_halves<1>(h);
     __syncthreads();
     if ((lane & 1) == 0) heads[threadIdx.x / 2] = h;
     __syncthreads();
     const f32x4 o = *(const f32x4*)(heads + 4 * lane);
     const float all[4] = {o[0], o[1], o[2], o[3]};
-    return (double)kth_bound(all, k);
+    return (double)kth_bound<2>(all, k);
   };
   double least_score = kth_of(head);
   for (int l = threadIdx.x; l < lists; l += kPick) {
