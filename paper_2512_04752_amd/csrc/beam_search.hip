@@ -449,11 +449,9 @@ __device__ __forceinline__ bool better(const Cand& p, const Cand& q) {
 }
 __device__ __forceinline__ uint64_t id_of(int w, int y) { return (uint64_t)(uint32_t)w << 32 | (uint32_t)y; }
 constexpr int kPick = 512;         // threads
-constexpr int kHeads = kPick / 2;  // candidates that bound the k-th best
 constexpr int kListed = 1024;      // candidates that can be ranked side by side
-static_assert(kHeads == 4 * 64, "four per lane");
 constexpr int kMaxLists = 1024;    // lists of a group: plan_beam()
-static_assert(kPick / 64 * kMaxBeams <= kListed && kMaxBeams <= kHeads, "the waves' lists, and the bound's rank");
+static_assert(kPick / 64 * kMaxBeams <= kListed && kMaxBeams <= 128, "the waves' lists, and the bound's rank");
 
 // -infinity by way of vector registers: as a scalar one this compiler (ROCm 7.2) makes it
 // s_mov_b64 with a 64-bit literal, which the instruction does not have, and it arrives as 0.
@@ -477,7 +475,7 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   __shared__ double lse[kMaxBeams];              // NaN: the beam offers nothing
   __shared__ float score[kMaxBeams];
   __shared__ Cand listed[kListed];
-  __shared__ __attribute__((aligned(16))) float heads[kHeads];
+  __shared__ float heads[kPick];
   __shared__ uint16_t open[kMaxLists];
   __shared__ int count, opened;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -500,31 +498,43 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     }
     return c;
   };
-  // Threads' own entries, in the order of all lists' first entries, then all second ones ..
-  const int mine = min((int)threadIdx.x, total - 1), l0 = mine % lists, e0 = mine / lists;
-  const float z0 = a.cand_z[entry(l0, e0)];
-  const int y0 = a.cand_y[entry(l0, e0)];
-  if (threadIdx.x == 0) count = opened = 0;
-  // normalisers: as many lanes per row as there are for all rows at once
+  // Normalisers: as many lanes (a power of two) per row as there are for all rows at once.
   const Exp exp;
-  int lanes = 64;
-  while (lanes > 1 && (lanes / 2 >= a.segs || lanes * a.width > kPick)) lanes /= 2;
-  const int rows_at_once = 64 / lanes, sub = lane & (lanes - 1);
-  for (int w0 = wave * rows_at_once; w0 < a.width; w0 += kWaves * rows_at_once) {
-    const int w = w0 + lane / lanes, row = g * a.width + min(w, a.width - 1);
-    // The first segment of every lane before anything waits, then the others.  (What is read
+  int lg = 6;
+  while (lg > 0 && ((1 << (lg - 1)) >= a.segs || a.width << lg > kPick)) --lg;
+  const int lanes = 1 << lg, rows_at_once = 64 >> lg, sub = lane & (lanes - 1);
+  // Threads' own entries, in the order of all lists' first entries, then all second ones ..
+  const int mine = min((int)threadIdx.x, total - 1);
+  int l0 = mine, e0 = 0;
+  float z0;
+  int y0;
+  if (threadIdx.x == 0) count = opened = 0;
+  for (int w0 = wave * rows_at_once, trip = 0; trip == 0 || w0 < a.width; w0 += kWaves * rows_at_once, ++trip) {
+    const int w = w0 + (lane >> lg), row = g * a.width + min(w, a.width - 1);
+    // Every lane's first two segments before anything waits, then the others.  (What is read
     // of a beam that is not live is not used.)
-    const int i0 = min(sub, a.segs - 1);
-    const float s = a.scores[row], t0 = a.tops[(int64_t)row * a.segs + i0];
-    const double x0 = a.sums[(int64_t)row * a.segs + i0];
+    const float* tops = a.tops + (int64_t)row * a.segs;
+    const double* sums = a.sums + (int64_t)row * a.segs;
+    const int i0 = min(sub, a.segs - 1), i1 = min(sub + lanes, a.segs - 1);
+    const float s = a.scores[row], t0 = tops[i0], t1 = tops[i1];
+    const double x0 = sums[i0], x1 = sums[i1];
     const bool live = beam_live(a, row);
-    float top = t0;
-    for (int i = sub + lanes; i < a.segs; i += lanes)
-      top = __builtin_elementwise_maximum(top, a.tops[(int64_t)row * a.segs + i]);
+    if (trip == 0) {
+      if (lists < kPick) {
+        e0 = mine / lists;
+        l0 = mine - e0 * lists;
+      }
+      z0 = a.cand_z[entry(l0, e0)];
+      y0 = a.cand_y[entry(l0, e0)];
+    }
+    float top = __builtin_elementwise_maximum(t0, t1);
+#pragma unroll 4
+    for (int i = sub + 2 * lanes; i < a.segs; i += lanes) top = __builtin_elementwise_maximum(top, tops[i]);
     top = max_over(top, lanes);
     double sum = sub < a.segs ? exp.scaled(x0, (double)t0 - (double)top) : 0.0;
-    for (int i = sub + lanes; i < a.segs; i += lanes)
-      sum += exp.scaled(a.sums[(int64_t)row * a.segs + i], (double)a.tops[(int64_t)row * a.segs + i] - (double)top);
+    if (sub + lanes < a.segs) sum += exp.scaled(x1, (double)t1 - (double)top);
+#pragma unroll 4
+    for (int i = sub + 2 * lanes; i < a.segs; i += lanes) sum += exp.scaled(sums[i], (double)tops[i] - (double)top);
     sum = sum_over(sum, lanes);
     if (sub == 0 && w < a.width) {
       lse[w] = live && top < INFINITY ? (double)top + log(sum) : NAN;
@@ -537,17 +547,21 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   const double own = head;
   for (int l = threadIdx.x + kPick; l < lists; l += kPick)
     head = fmax(head, candidate(l / a.segs, a.cand_z[entry(l, 0)], a.cand_y[entry(l, 0)]).s);
-  // A bound that k of the threads' candidates are not below, from the maxima of pairs.
+  // A bound that k of the threads' candidates are not below, from the maxima of 64 groups (of
+  // threads 64 apart: neighbours often have the same beam) while k is far below that, of 128
+  // otherwise.  A step of the search takes three counts of 64, or six.
   auto kth_of = [&](double x) {
     float h = (float)x;                          // not above the double
     if ((double)h > x) h = float_below(h);
-    h = max_of_halves<1>(h);
     __syncthreads();
-    if ((lane & 1) == 0) heads[threadIdx.x / 2] = h;
+    heads[threadIdx.x] = h;
     __syncthreads();
-    const f32x4 o = *(const f32x4*)(heads + 4 * lane);
-    const float all[4] = {o[0], o[1], o[2], o[3]};
-    return (double)kth_bound<2>(all, k);
+    float most[2] = {heads[lane], heads[64 + lane]};
+#pragma unroll
+    for (int i = 2; i < kWaves; ++i) most[i & 1] = fmaxf(most[i & 1], heads[64 * i + lane]);
+    if (k > 24) return (double)kth_bound<2>(most, k);
+    const float one[1] = {fmaxf(most[0], most[1])};
+    return (double)kth_bound<2>(one, k);
   };
   double least_score = kth_of(head);
   for (int l = threadIdx.x; l < lists; l += kPick) {
@@ -566,15 +580,17 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     if (e >= k) return Cand{no_score(), 0};
     return candidate(l / a.segs, a.cand_z[entry(l, e)], a.cand_y[entry(l, e)]);
   };
+  Cand first_one{no_score(), 0};                 // of the first block
+  if ((int)threadIdx.x < block) first_one = opened_entry(threadIdx.x, 0);
   if (lists_open * k > 2 * kMaxBeams) {          // a closer bound
-    head = no_score();
-    for (int i = threadIdx.x; i < block; i += kPick) head = fmax(head, opened_entry(i, 0).s);
+    head = first_one.s;
+    for (int i = threadIdx.x + kPick; i < block; i += kPick) head = fmax(head, opened_entry(i, 0).s);
     least_score = fmax(least_score, kth_of(head));
   }
   for (int at = 0; at < k && lists_open > 0; at += deep) {
     bool more = false;                           // a list's last entry here passes
     for (int i = threadIdx.x; i < block; i += kPick) {
-      const Cand c = opened_entry(i, at);
+      const Cand c = at == 0 && i < kPick ? first_one : opened_entry(i, at);
       if (c.s >= least_score && c.s > -INFINITY) {
         more |= i >= block - lists_open;
         const int to = atomicAdd(&count, 1);
@@ -616,12 +632,20 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     __syncthreads();
     n = count;
   }
-  for (int i = threadIdx.x; i < n; i += kPick) {
-    const Cand c = listed[i];
-    int rank = 0;
+  // Eight threads to a candidate count what is better.
+  for (int i0 = 0; i0 < n; i0 += kPick / 8) {
+    const int i = i0 + (threadIdx.x >> 3);
+    const Cand c = listed[min(i, n - 1)];
+    uint32_t rank = 0, other;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += better(listed[j], c);
-    if (rank < k) {
+    for (int j = threadIdx.x & 7; j < n; j += 8) rank += better(listed[j], c);
+    halves_of<1>(rank, &rank, &other);
+    rank += other;
+    halves_of<2>(rank, &rank, &other);
+    rank += other;
+    halves_of<4>(rank, &rank, &other);
+    rank += other;
+    if (i < n && (threadIdx.x & 7) == 0 && (int)rank < k) {
       const int64_t at = (int64_t)g * k + rank;
       a.parents[at] = (int32_t)(c.id >> 32);
       a.tokens[at] = (int32_t)c.id;
