@@ -662,12 +662,13 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
 }  // namespace
 
 // Segments: about 4096 waves' worth of rows' pieces fill the chip (4 to a SIMD), none below 64
-// vectors (one load of each lane), and at most kMaxLists in a group, each a list that one
-// work-group picks from.  us, with 2048 / 4096 / 6144 / 8192 waves: 17 x 12 x 50001 bf16, k 24,
-// 30.0 / 29.2 / 28.9 / 30.3; 3 x 64 x 32000, k 64, 38.9 / 37.7 / 38.0 / 44.4; 128 x 8 x 128256
-// 114 / 112 / 112 / 113.  With 512 / 1024 / 2048 / 4096 lists: 1 x 32 x 128256 bf16, k 64, 46.5 /
-// 38.0 / 36.4 / 43.9; 1 x 16 x 128256, k 16, 23.2 / 20.9 / 22.8 / 31.0; 1 x 64 x 128000, k 64, 64.0 /
-// 49.6 / 45.3 / 52.2; 1 x 16 x 128256 bf16, k 4, 18.0 / 16.2 / 18.3 / 25.7.
+// vectors (one load of each lane), at most kMaxLists in a group, each a list that one
+// work-group picks from, and 128 in a row, whose normaliser takes two loads of 64 lanes.  us,
+// with 2048 / 4096 / 6144 / 8192 waves: 17 x 12 x 50001 bf16, k 24, 28.3 / 24.6 / 25.1 / 25.4; 3 x 64 x
+// 32000, k 64, 32.5 / 27.2 / 27.1 / 27.2; 128 x 8 x 128256 112 / 109 / 111 / 113.  With 512 / 1024 /
+// 2048 lists: 1 x 32 x 128256 bf16, k 64, 34.0 / 27.6 / 28.0; 1 x 64 x 128000, k 64, 46.8 / 36.9 / 35.6;
+// 1 x 16 x 128256, k 16, 19.6 / 17.4 / 20.0.  With 64 / 128 / 256 segments: 8 x 128256, k 8, 14.1 /
+// 13.4 / 17.2; 4 x 128256, k 4, - / 11.6 / 13.5.
 // Many rows have few segments: four, for a team, where 16 or more are chosen from 1000 vectors or
 // more (with less than four / four: 90 x 24 x 32000, k 24, 91.6 / 75.6; 128 x 64 x 8000 bf16, k 64,
 // 107 / 99; but 150 x 10 x 50001, k 10, 70.2 / 73.0; 128 x 64 x 2000, k 32, 39.7 / 52.5).
@@ -676,7 +677,7 @@ void plan_beam(BeamArgs* a) {
   const int64_t rows = (int64_t)a->groups * a->width;
   const int64_t vectors = (a->vocab + per - 1) / per;
   const int64_t want = std::max<int64_t>(a->k >= 16 && vectors >= 1000 ? kTeam : 1, 4096 / rows), most = (vectors + 63) / 64;
-  const int64_t segs = std::min<int64_t>({want, most, kMaxLists / a->width});
+  const int64_t segs = std::min<int64_t>({want, most, 128, kMaxLists / a->width});
   a->seg = (int)((vectors + 64 * segs - 1) / (64 * segs) * 64);
   a->segs = (int)((vectors + a->seg - 1) / a->seg);
 }
