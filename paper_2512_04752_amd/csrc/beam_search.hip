@@ -271,7 +271,7 @@ struct Vectors {
 // order) go side by side and into the list when there are enough of them.  The first batch
 // gives a bound to start with.  128 x 8 x 128256 fp32: 102 us for 525 MB (5.1 TB/s), vector
 // instructions 80 % busy; 17 x 12 x 50001 bf16, k 24: 18 us for 20 MB, 61 % busy, half of whose
-// 1270 instructions per wave are the terms; 4 x 32000 fp32: 5.4, launch and one trip.
+// 1270 instructions per wave are the terms; 4 x 32000 fp32: 5.2, launch and one trip.
 //
 // TEAM: the four waves of a work-group have four segments of one row, of which the k best
 // matter.  Each tells the others its k / 4-th best so far: k numbers are not below the
@@ -468,8 +468,8 @@ __device__ __forceinline__ double no_score() {
 // hold bounds it again (one beam far ahead of the others has k better ones than the second
 // beam's best), and what is not below (about k, unless many are equal) is ranked by counting.
 // Where that is more than fits, each wave keeps a sorted list instead, and these are ranked.
-// 7.1 us for 128 groups of 8 x 4 lists of 8, 10.4 for 17 of 12 x 20 of 24, of which launch and
-// end are 3.4.
+// 6.7 us for 128 groups of 8 x 4 lists of 8, 7.8 for 17 of 12 x 20 of 24, 5.6 for one of 4 x 125 of
+// 4; launch and end are 3.4 of each.
 __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   constexpr int kWaves = kPick / 64;
   __shared__ double lse[kMaxBeams];              // NaN: the beam offers nothing
