@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
@@ -731,6 +732,7 @@ def spec_kv4_commit(pool: KV4Pool, sample_ids, seq_lens, accepted_len, accepted_
 
 # ---- products with weights in 4 bits ----
 
+@functools.lru_cache(maxsize=4096)
 def spec_w4_bytes(rows, cols) -> int:
     return int(lib().spec_w4_bytes(rows, cols))
 
@@ -782,8 +784,10 @@ def spec_w4_pack(w, data, stream=None):
     index = w.get_device()
     stride = _device_rows(w, torch.bfloat16, rows, cols, "w", index)
     p, n = _device_workspace(data, index)
-    with _on(index):
-        rc = lib().spec_w4_pack(w.data_ptr(), stride, rows, cols, p, n, _device_stream(index, stream))
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return spec_w4_pack(w, data, stream)
+    rc = lib().spec_w4_pack(w.data_ptr(), stride, rows, cols, p, n, _device_stream(index, stream))
     if rc:
         _check(rc)
 
@@ -794,10 +798,12 @@ def spec_w4_unpack(data, w, stream=None):
     index = w.get_device()
     stride = _device_rows(w, torch.bfloat16, rows, cols, "w", index)
     p, n = _device_workspace(data, index)
-    if n < lib().spec_w4_bytes(rows, cols):
+    if n < spec_w4_bytes(rows, cols):
         raise ValueError(f"data holds {n} bytes, a matrix of {rows} x {cols} {spec_w4_bytes(rows, cols)}")
-    with _on(index):
-        rc = lib().spec_w4_unpack(spec_w4(p, rows, cols), w.data_ptr(), stride, _device_stream(index, stream))
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return spec_w4_unpack(data, w, stream)
+    rc = lib().spec_w4_unpack(spec_w4(p, rows, cols), w.data_ptr(), stride, _device_stream(index, stream))
     if rc:
         _check(rc)
 
