@@ -239,10 +239,12 @@ __global__ __launch_bounds__(64 * kStreamWaves, 4) void w4_stream_kernel(W4Args 
 // pair, half of them each one's); a wave 16 MB x 16 NB.  x moves into LDS by direct loads, a
 // column tile (256 bytes of every row) at a time, the 16-byte chunk of a row XOR-ed with the row,
 // so that the operand reads (16 rows, one chunk) hit all 64 banks once.  The weights go
-// straight to registers.  Both are loaded for the next column tile while one is multiplied:
-// one barrier per tile, at which the loads issued a whole tile ago have arrived.  Gate/up
-// 14336 x 4096, 1024 rows: 184 us, 1.30 PFLOP/s (a large bf16 product reaches 1.41), matrix cores
-// 67 % busy, vector instructions 45 %; head 128256 x 4096, 24 rows: 58 us, 5.0 TB/s.
+// straight to registers.  While a column tile is multiplied, x of the next and the weights of
+// the one after it are on their way; one barrier per tile.  (Weights one tile ahead: head
+// 128256 x 4096, 24 rows, 58.5 us instead of 55.0; 6144 x 4096, 128 rows, 14.1 instead of 13.5; gate/up
+// 14336 x 4096, 64 rows, 20.1 instead of 20.4.)  Gate/up 14336 x 4096, 1024 rows: 185 us, 1.30 PFLOP/s
+// (a large bf16 product reaches 1.41), matrix cores 67 % busy, vector instructions 45 %; the
+// head of 24 rows 5.3 TB/s.
 template <int MB, int NB, int WM, int WN, int KG, bool PAIR>
 __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_kernel(W4Args a) {
   constexpr int BM = 16 * MB * WM, BT = NB * WN / (PAIR ? 2 : 1), STAGE = BM * 256, LOADS = BM / 4 / (WM * WN);
@@ -328,12 +330,14 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_k
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[j], f[i], acc[i][j], 0, 0, 0);
     }
   };
-  // Every group runs the same number of steps; one past its last tile multiplies nothing.
+  // Every group runs the same number of steps, one at least; past its last tile it multiplies nothing.
   const int steps = (t1 - t0 + KG - 1) / KG;
-  Weights wa, wb;
-  auto step = [&](int i, int buf, Weights& now, Weights& next) {
-    const int t = t0 + i * KG + kg;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // x a step ahead, the weights two.  Loads past the last step repeat the last tile, so that
+  // waits can count them.
+  Weights w0, w1, w2;
+  auto step = [&](int i, Weights& now, Weights& after_next) {
+    const int t = t0 + i * KG + kg, buf = i & 1;
+    wait_vm<2 * NB>();                           // all but the next step's weights
     // Here and not where they are first used, behind the next loads; nor does anything of
     // theirs (the shift of the scales) move up to those.
 #pragma unroll
@@ -343,20 +347,23 @@ __global__ __launch_bounds__(64 * WM * WN * KG, WM * WN * KG / 4) void w4_tile_k
       wait_lds();
     }
     phase_barrier();
-    if (i + 1 < steps) {
-      load_x(min(t + KG, t1 - 1), buf ^ 1);
-      load_w(next, min(t + KG, t1 - 1));
-    }
+    load_x(min(t + KG, t1 - 1), buf ^ 1);
+    load_w(after_next, min(t + 2 * KG, t1 - 1));
     if (t < t1) multiply(now, buf);
   };
-  if (steps > 0) {
-    load_x(min(t0 + kg, t1 - 1), 0);
-    load_w(wa, min(t0 + kg, t1 - 1));
+  load_x(min(t0 + kg, t1 - 1), 0);
+  load_w(w0, min(t0 + kg, t1 - 1));
+  __builtin_amdgcn_sched_barrier(0);
+  load_w(w1, min(t0 + KG + kg, t1 - 1));
+  for (int i = 0;; i += 3) {       // left by breaks: where paths met, registers would be copied, and waited for
+    step(i, w0, w2);
+    if (i + 1 >= steps) break;
+    step(i + 1, w1, w0);
+    if (i + 2 >= steps) break;
+    step(i + 2, w2, w1);
+    if (i + 3 >= steps) break;
   }
-  for (int i = 0; i < steps; i += 2) {
-    step(i, 0, wa, wb);
-    if (i + 1 < steps) step(i + 1, 1, wb, wa);
-  }
+  wait_vm<0>();
   if constexpr (KG > 1) {                // the groups' sums meet in LDS, in their order
     constexpr int BLOCKS = MB * NB;
     static_assert((KG - 1) * WM * WN * BLOCKS * 1024 <= KG * 2 * STAGE, "sums fit");
