@@ -492,13 +492,12 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 // alone 49; 16 rows 4096 x 14336 in 4 splits 16.2 / 14.3 / 13.8 / 14.4, in 8 no better.)
 //
 // More rows: the cost model below, in us.  Work-groups run `slots` to a CU; k of them on one
-// take max(alone, k * each) per step of a column tile (the kernel's KG at a time), `fixed`
-// more per round; weights stream at `tbs` TB/s; the larger of both, an eighth of the smaller
-// (they overlap imperfectly), 5.7 for a launch in a graph and, where columns are split, 2.1 and
-// the partials written and read at 5 TB/s for the reduction.  Fitted to 2550 launches (8
-// matrices of the 1B and 8B shapes, 17 to 2048 rows, all tiles, 1 to 16 splits, weights from
-// HBM): 9 % rms, and the choice is on average 1.7 % slower than the best of them, at worst
-// 19 % (4096 x 4096, 768 rows).
+// take k * each per step of a column tile (the kernel's KG at a time), `fixed` more per round;
+// weights stream at `tbs` TB/s; the larger of both, an eighth of the smaller (they overlap
+// imperfectly), 5.9 for a launch in a graph and, where columns are split, 2.3 and the partials
+// written and read at 5.8 TB/s for the reduction.  Fitted to 2550 launches (8 matrices of the 1B
+// and 8B shapes, 17 to 2048 rows, all tiles, 1 to 16 splits, weights from HBM): 7.5 % rms, and the
+// choice is on average 1.0 % slower than the best of them, at worst 8 % (128256 x 4096, 17 rows).
 W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   const int tiles = (rows + 15) / 16, mats = gate_up ? 2 : 1, T = w4_col_tiles(cols);
   auto partials = [&](int splits) { return 4.0 * splits * mats * n * tiles * 16; };      // bytes
@@ -511,14 +510,14 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   struct Tile {
     W4Shape shape;
     int bm, bt, kg, slots;
-    double alone, each, fixed, tbs;
+    double each, fixed, tbs;
   };
-  static constexpr Tile shapes[] = {{W4_TILE32, 32, 8, 2, 3, 0.548, 0.512, 0.0, 4.74},
-                                    {W4_TILE32W, 32, 32, 1, 1, 0.988, 0, 0.16, 5.13},
-                                    {W4_TILE64, 64, 8, 2, 2, 0.907, 0.845, 0.03, 3.84},
-                                    {W4_TILE64W, 64, 16, 1, 2, 0.843, 0.317, 0.38, 4.03},
-                                    {W4_TILE128, 128, 16, 1, 1, 1.507, 0, 0.41, 2.80},
-                                    {W4_TILE256, 256, 16, 1, 1, 2.732, 0, 1.29, 1e9}};
+  static constexpr Tile shapes[] = {{W4_TILE32, 32, 8, 2, 3, 0.538, 0.0, 4.56},
+                                    {W4_TILE32W, 32, 32, 1, 1, 0.880, 0.32, 5.18},
+                                    {W4_TILE64, 64, 8, 2, 2, 0.854, 0.33, 4.03},
+                                    {W4_TILE64W, 64, 16, 1, 2, 0.771, 0.55, 5.40},
+                                    {W4_TILE128, 128, 16, 1, 1, 1.614, 1.17, 2.62},
+                                    {W4_TILE256, 256, 16, 1, 1, 2.675, 2.28, 6.71}};
   W4Plan best{W4_TILE64, 1, 1};
   double best_us = 1e30;
   for (const Tile& s : shapes) {
@@ -529,7 +528,7 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
       if (splits > 1 && (T / splits < 4 || part > kW4PartialCap)) break;
       const int64_t wgs = count * splits;
       const double steps = (T + splits * s.kg - 1) / (splits * s.kg), at_once = 256.0 * s.slots;
-      auto step = [&](int k) { return k == 0 ? 0.0 : std::max(s.alone, k * s.each); };
+      auto step = [&](int k) { return k * s.each; };
       double work;
       if (wgs > 3 * at_once) {
         work = wgs / at_once * (steps * step(s.slots) + s.fixed);
@@ -539,7 +538,7 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
       }
       const double stream = mats * (double)rows * cols * 17 / 32 / s.tbs / 1e6;
       double us = std::max(work, stream) + 0.13 * std::min(work, stream);
-      if (splits > 1) us += 2.1 + 2 * part / 5e6;
+      if (splits > 1) us += 2.3 + 2 * part / 5.8e6;
       if (us < best_us) {
         best_us = us;
         best = W4Plan{s.shape, 1, splits};
