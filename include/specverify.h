@@ -561,13 +561,15 @@ typedef struct {
 } spec_weights_w4;
 
 /* Workspace bytes spec_verify_w4 needs: max_pages 0 for a bf16 pool, otherwise as in
- * spec_workspace_bytes_kv4; 0 if an argument is invalid. */
+ * spec_workspace_bytes_kv4; 0 if an argument is invalid.  (It holds all nodes' logits in
+ * fp32.) */
 size_t spec_workspace_bytes_w4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
                                int32_t max_pages, int32_t sampled);
 
 /* spec_verify (samp NULL) or spec_verify_sampled with w, over the bf16 pool kv (kv4
  * NULL) or the 4-bit one kv4 (kv NULL): otherwise the same arguments, outputs and
- * commit as theirs or spec_verify_kv4's.  Refuses a capturing stream. */
+ * commit as theirs or spec_verify_kv4's, at most 65535 nodes in all.  Refuses a
+ * capturing stream. */
 int spec_verify_w4(const spec_model_config* cfg, const spec_weights_w4* w, spec_kv* kv, spec_kv4* kv4,
                    int32_t batch, const int32_t* sample_ids, const int32_t* tree_offsets,
                    const int32_t* tree_tokens, const int32_t* tree_parents, const int32_t* seq_lens,
