@@ -163,6 +163,48 @@ def test_in_place_outputs_graph_and_streams():
     check(z, s, 7, got=got)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("k", [9, 24, 64])
+def test_segments_that_share_their_bounds(k, dtype):
+    """More than 8 of a long row: its waves leave out what the others' bounds rule out, so rows
+    whose candidates lie in one segment, or nowhere, or all at one value."""
+    groups, width, vocab, eos = 8, 3, 9001, 17
+    z, s = logits(k, groups, width, vocab, dtype), scores(k, groups, width)
+    lowest = torch.finfo(dtype).min
+    z[0, :, 500:] = -INF                 # all in the first segment
+    z[1, :, :8900] = -INF                # all in the last
+    z[2, :, 5:] = -INF                   # fewer than k
+    z[3, :, 3000:] = lowest
+    z[3, 1] = lowest
+    z[4, 0] = 2.5                        # ties over all segments
+    z[4, 1, ::2] = 7.0
+    z[5, 0, 4000], z[5, 1, 8999] = float("nan"), INF
+    z[6] = -INF
+    z[6, 1, ::1000] = 1.0
+    z[7, 0] += torch.arange(vocab, device="cuda").to(dtype) * 0.25
+    last = torch.zeros(groups, width, dtype=torch.int32, device="cuda")
+    last[0, 1] = last[5, 2] = eos
+    check(z, s, k, last, eos)
+    check(z, s, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_graph_with_shared_bounds(dtype):
+    groups, width, vocab = 3, 12, 7000
+    z, s = logits(9, groups, width, vocab, dtype), scores(9, groups, width)
+    last = torch.zeros(groups, width, dtype=torch.int32, device="cuda")
+    parents = torch.empty_like(last)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sv.spec_beam_select(z, s, parents, last, s)
+    for step in range(4):
+        z.copy_(logits(30 + step, groups, width, vocab, dtype))
+        before = s.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(z, before, width, got=(parents, last, s))
+
+
 def test_refusals_of_tensors():
     z, s = logits(1, 2, 3, 100), scores(1, 2, 3)
     i32 = dict(dtype=torch.int32, device="cuda")
