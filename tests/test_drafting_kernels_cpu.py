@@ -38,12 +38,10 @@ def test_wait_state_between_m0_and_lds_loads(compiled):
                 assert body[n - 1].startswith("s_nop") and "m0" in body[n - 2]
 
 
+@pytest.mark.parametrize("compiled", ["w4_gemm.hip"], indirect=True)
 def test_lds_reads_are_complete_at_barriers(compiled):
     """A tile's place is refilled by direct loads behind the barrier."""
-    name, text = compiled
-    if name != "w4_gemm.hip":
-        pytest.skip("no direct loads")
-    found = kernels(text)
+    found = kernels(compiled[1])
     tiles = [body for k, body in found.items() if "w4_tile_kernel" in k]
     assert len(tiles) == 12
     for body in tiles:
