@@ -361,8 +361,8 @@ int spec_w4_gate_up(const spec_w4* gate, const spec_w4* up, const void* x, int64
  *   last_tokens  device int32 [groups][width], or NULL: the beams' last tokens, read
  *                when eos_token >= 0
  * Candidate (w, y) scores scores[w] + log softmax(logits of w)[y], in fp64, the logarithm
- * of the sum to 1e-9 (and the same for equal rows).  A beam whose last token is eos_token has ended: it offers (w, eos_token) alone, at
- * scores[w].  No candidates: tokens whose logit is -infinity; beams whose score is not
+ * of the sum to 1e-9 (and the same for equal rows).  A beam whose last token is eos_token
+ * has ended: it offers (w, eos_token) alone, at scores[w].  No candidates: tokens whose logit is -infinity; beams whose score is not
  * finite; live beams with a logit that is NaN or +infinity.
  * Outputs, per group the k best, best first, the lower (w, y) of equal scores first:
  *   parents      device int32 [groups][k]  w

@@ -676,7 +676,8 @@ void plan_beam(BeamArgs* a) {
   const int per = a->is_bf16 ? 8 : 4;
   const int64_t rows = (int64_t)a->groups * a->width;
   const int64_t vectors = (a->vocab + per - 1) / per;
-  const int64_t want = std::max<int64_t>(a->k >= 16 && vectors >= 1000 ? kTeam : 1, 4096 / rows), most = (vectors + 63) / 64;
+  const int64_t want = std::max<int64_t>(a->k >= 16 && vectors >= 1000 ? kTeam : 1, 4096 / rows);
+  const int64_t most = (vectors + 63) / 64;
   const int64_t segs = std::min<int64_t>({want, most, 128, kMaxLists / a->width});
   a->seg = (int)((vectors + 64 * segs - 1) / (64 * segs) * 64);
   a->segs = (int)((vectors + a->seg - 1) / a->seg);
@@ -708,9 +709,11 @@ hipError_t launch_beam(const BeamArgs& a, hipStream_t s) {
   // Up to 8 best the team's words cost more than they save (us: 4 x 32000, k 4, 13.2 alone and 13.5
   // as teams; 8 x 128256, k 8, 15.6 and 15.9; 16 x 128256, k 16, 20.9 and 20.6; 17 x 12 x 50001, k 24,
   // 29.2 and 27.6; 3 x 64 x 32000, k 64, 36.7 and 30.8; 4 x 64 x 128256 bf16, k 64, 69.5 and 57.6).
-  const hipError_t e = a.segs >= kTeam && a.k > 8
-                           ? a.is_bf16 ? scan(beam_scan_kernel<bf16, true>, teams) : scan(beam_scan_kernel<float, true>, teams)
-                           : a.is_bf16 ? scan(beam_scan_kernel<bf16, false>, pieces) : scan(beam_scan_kernel<float, false>, pieces);
+  const bool team = a.segs >= kTeam && a.k > 8;
+  const hipError_t e = a.is_bf16 ? team ? scan(beam_scan_kernel<bf16, true>, teams)
+                                        : scan(beam_scan_kernel<bf16, false>, pieces)
+                                 : team ? scan(beam_scan_kernel<float, true>, teams)
+                                        : scan(beam_scan_kernel<float, false>, pieces);
   if (e != hipSuccess) return e;
   beam_pick_kernel<<<a.groups, kPick, 0, s>>>(a);
   return hipGetLastError();
