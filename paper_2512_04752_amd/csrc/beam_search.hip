@@ -49,9 +49,9 @@ struct Exp {
     b[1] += __builtin_bit_cast(i32x2, m)[0] << 20;
     return __builtin_bit_cast(double, b);
   }
-  // x e^d, d <= 690; a NaN for a NaN; 0 where that is below e^-690 of x.
+  // x e^d, d <= 690; a NaN for a NaN in either; 0 where that is below e^-690 of x.
   __device__ __forceinline__ double scaled(double x, double d) const {
-    return d != d ? d : d < -690.0 ? 0.0 : x * (*this)(d);
+    return d != d ? d : x * (d < -690.0 ? 0.0 : (*this)(d));
   }
 };
 

@@ -1,0 +1,81 @@
+"""The choice of beams where a row's pieces carry their statistics over several steps of a
+wave: numbers that are not finite, wherever they stand.
+
+The reference takes log softmax(z)[y] as (z_y - max z) - log sum exp(z - max z) in float64,
+which is exact to 1e-13 for logits of any size (the difference of two fp32 numbers is
+exact while they are within 2^29 of each other, and counts for nothing beyond).  Parents and
+tokens are equal, scores within 1e-9 and half a step of fp32."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_04752_amd as sv
+from tests.test_gpu_beam import logits, scores
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def reference(z, s, k):
+    z, s = z.double(), s.double()
+    groups = z.shape[0]
+    top = z.amax(-1, keepdim=True)                         # a NaN when there is one
+    key = s[..., None] + ((z - top) - torch.log(torch.exp(z - top).sum(-1, keepdim=True)))
+    key = torch.where((top.abs() < INF) & (s.abs() < INF)[..., None], key, -INF).view(groups, -1)
+    got, at = torch.sort(key, dim=1, descending=True, stable=True)
+    got, at = got[:, :k], at[:, :k]
+    none = got == -INF
+    return (torch.where(none, -1, at // z.shape[2]), torch.where(none, -1, at % z.shape[2]), got)
+
+
+def check(z, s, k):
+    groups = z.shape[0]
+    parents, tokens = (torch.full((groups, k), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    new = torch.full((groups, k), 7.0, device="cuda")
+    sv.spec_beam_select(z, s, parents, tokens, new)
+    want = reference(z, s, k)
+    assert parents.tolist() == want[0].tolist()
+    assert tokens.tolist() == want[1].tolist()
+    some = want[2] > -INF
+    assert torch.equal(new > -INF, some)
+    assert ((new.double() - want[2]).abs()[some] <= 1e-9 + 2.0 ** -24 * want[2].abs()[some]).all()
+
+
+# many rows, so that a wave goes through its segment in several batches, the last of them partial
+GROUPS, WIDTH, VOCAB = 17, 12, 50001
+
+
+@pytest.fixture(params=[torch.float32, torch.bfloat16], ids=str)
+def rows(request):
+    return logits(1, GROUPS, WIDTH, VOCAB, request.param), scores(1, GROUPS, WIDTH)
+
+
+@pytest.mark.parametrize("seed", range(4))
+@pytest.mark.parametrize("k", [4, 24])
+def test_nan_in_every_piece_of_a_row(rows, k, seed):
+    """A NaN takes its beam out, at tokens spread over the segments' batches and lanes; the last
+    batch of the last segment has no numbers for some lanes."""
+    z, s = rows
+    rng = np.random.default_rng(seed)
+    n = GROUPS * WIDTH
+    at = np.concatenate((VOCAB - 1 - rng.integers(0, 2600, size=n // 2), rng.integers(0, VOCAB, size=n - n // 2)))
+    at = rng.permutation(at).reshape(GROUPS, WIDTH)
+    for g in range(GROUPS):
+        for w in range(WIDTH):
+            if w != g % WIDTH:
+                z[g, w, int(at[g, w])] = float("nan")
+    check(z, s, k)
+
+
+@pytest.mark.parametrize("what", [float("nan"), INF], ids=str)
+@pytest.mark.parametrize("k", [4, 24])
+def test_not_finite_before_masked_tokens(rows, k, what):
+    """All that follows is masked, or all but what another batch, lane or segment has."""
+    z, s = rows
+    for g in range(GROUPS):
+        for w in range(WIDTH - 1):
+            at = (g * WIDTH + w) * 233 % (VOCAB - 8)
+            z[g, w, at] = what
+            z[g, w, at + 1:(VOCAB, at + 3000, VOCAB - 2)[w % 3]] = -INF
+    check(z, s, k)
