@@ -21,7 +21,7 @@ namespace {
 
 constexpr int64_t kMaxGrid = 0xffffffffll / 1024;
 
-// e^d for -1000 <= d <= 690, relative error below 5e-11: d log2 e = n + f, |f| <= 1/2, and 2^n
+// e^d for -708 <= d <= 690 (the result's exponent is a normal one), relative error below 5e-11: d log2 e = n + f, |f| <= 1/2, and 2^n
 // times the polynomial of degree 7 with the smallest largest relative error of 2^f (4.0e-11 by
 // Remez's exchange; the series needs degree 9 for that).  n comes out of an addition that leaves
 // it in the low bits, and goes into the exponent by an integer one: all of it at the rate of
@@ -341,8 +341,9 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) lowest = __builtin_elementwise_minimum(lowest, z[j][i]);
     // Terms relative to `top`: doubles hold e^600, and what is below e^-690 of it counts as
-    // that.  A NaN makes the sum one, an infinity `top`.
-    if (__ballot(!(most <= top + 600.f))) {
+    // that.  A NaN makes the sum one, an infinity `top`.  (Differences are compared: of numbers
+    // so large that neighbours are further apart, top + 600 would be another float than it is.)
+    if (__ballot(!(most - top <= 600.f))) {
       if (!(most <= top)) {
         sum = exp.scaled(sum, (double)top - (double)most);
         top = most;
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
         __builtin_amdgcn_sched_barrier(0);     // else all terms at once, in more registers than there are
       }
     };
-    if (__ballot(!(lowest >= top - 680.f))) add(std::true_type{});
+    if (__ballot(!(lowest - top >= -680.f))) add(std::true_type{});
     else add(std::false_type{});
     if (first) {
       first = false;

@@ -1,5 +1,5 @@
 """The choice of beams where a row's pieces carry their statistics over several steps of a
-wave: numbers that are not finite, wherever they stand.
+wave: numbers that are not finite, wherever they stand, and logits of any size.
 
 The reference takes log softmax(z)[y] as (z_y - max z) - log sum exp(z - max z) in float64,
 which is exact to 1e-13 for logits of any size (the difference of two fp32 numbers is
@@ -29,7 +29,7 @@ def reference(z, s, k):
     return (torch.where(none, -1, at // z.shape[2]), torch.where(none, -1, at % z.shape[2]), got)
 
 
-def check(z, s, k):
+def check(z, s, k, off=1e-9):
     groups = z.shape[0]
     parents, tokens = (torch.full((groups, k), 77, dtype=torch.int32, device="cuda") for _ in range(2))
     new = torch.full((groups, k), 7.0, device="cuda")
@@ -39,7 +39,7 @@ def check(z, s, k):
     assert tokens.tolist() == want[1].tolist()
     some = want[2] > -INF
     assert torch.equal(new > -INF, some)
-    assert ((new.double() - want[2]).abs()[some] <= 1e-9 + 2.0 ** -24 * want[2].abs()[some]).all()
+    assert ((new.double() - want[2]).abs() <= off + 2.0 ** -24 * want[2].abs())[some].all()
 
 
 # many rows, so that a wave goes through its segment in several batches, the last of them partial
@@ -79,3 +79,33 @@ def test_not_finite_before_masked_tokens(rows, k, what):
             z[g, w, at] = what
             z[g, w, at + 1:(VOCAB, at + 3000, VOCAB - 2)[w % 3]] = -INF
     check(z, s, k)
+
+
+def patterns(n):
+    """Rows of small whole numbers: up and down once, with every batch of a wave, every token."""
+    at = torch.arange(n, device="cuda")
+    batch, half = at // 1024, (at >= n // 2).long()
+    return torch.stack((half, -half, batch % 2, -(batch % 2), batch % 3 - 1, at % 2, batch // 2 % 2 + at % 2, at % 7 - 3))
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("k", [4, 24])
+def test_steps_at_large_magnitudes(sign, k):
+    """Near 2^e neighbouring floats are 2^(e - 23) apart: below, around and beyond what an
+    exponential holds.  A normaliser of 2^e rounded to fp64 is off by 2^(e - 53), and its
+    difference by as much."""
+    steps = patterns(100003)
+    sizes = torch.tensor([2.0 ** e for e in range(22, 42)], dtype=torch.float64, device="cuda")[:, None, None]
+    exact = sign * sizes * 1.5 + steps * sizes * 2.0 ** -23
+    z = exact.float()
+    assert torch.equal(z.double(), exact)
+    check(z, scores(3, *z.shape[:2]), k, off=1e-9 + 2 * sizes[..., 0] * 2.0 ** -53)
+
+
+@pytest.mark.parametrize("k", [4, 24])
+def test_steps_around_what_an_exponential_holds(k):
+    """Rises and falls by 590 .. 720, where terms begin and cease to count."""
+    sizes = [590.0, 599.5, 600.0, 600.5, 610.0, 679.5, 680.0, 680.5, 689.0, 690.0, 691.0, 700.0, 709.0, 720.0]
+    z = patterns(100003) * torch.tensor(sizes, device="cuda")[:, None, None]
+    z += torch.linspace(0, 1, z.shape[2], device="cuda")
+    check(z, scores(3, *z.shape[:2]), k)
