@@ -888,15 +888,16 @@ def spec_verify_w4(cfg, weights: W4Weights, pool, sample_ids, tree_offsets, tree
 
 
 def _w4_workspace(m, n, workspace, stream):
+    """(tensor, pointer, bytes); the tensor is the caller's to hold until the product is launched."""
     if workspace is not None:
-        return _device_workspace(workspace, m.index)
+        return workspace, *_device_workspace(workspace, m.index)
     nbytes = m.needs.get(n)
     if nbytes is None:                       # asked once: the library searches
         nbytes = m.needs[n] = lib().spec_w4_workspace_bytes(m.rows, m.cols, n)
     if nbytes == 0:
-        return None, 0
+        return None, None, 0
     workspace = _made_workspace(nbytes, m.index, stream)
-    return workspace.data_ptr(), nbytes
+    return workspace, workspace.data_ptr(), nbytes
 
 
 def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
@@ -912,7 +913,7 @@ def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
     os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", index)
     if n == 0:
         return
-    p, nbytes = _w4_workspace(m, n, workspace, stream)
+    workspace, p, nbytes = _w4_workspace(m, n, workspace, stream)
     rc = lib().spec_w4_linear(m.struct, x.data_ptr(), xs, n, out.data_ptr(), os, kind, p, nbytes,
                               _device_stream(index, stream))
     if rc:
@@ -932,7 +933,7 @@ def spec_w4_gate_up(gate: W4Matrix, up: W4Matrix, x, out, workspace=None, stream
     os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", index)
     if n == 0:
         return
-    p, nbytes = _w4_workspace(gate, n, workspace, stream)
+    workspace, p, nbytes = _w4_workspace(gate, n, workspace, stream)
     rc = lib().spec_w4_gate_up(gate.struct, up.struct, x.data_ptr(), xs, n, out.data_ptr(), os, p, nbytes,
                                _device_stream(index, stream))
     if rc:

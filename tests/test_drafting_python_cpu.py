@@ -1,0 +1,50 @@
+"""What the Python calls of the drafting operators hand to the library, without a GPU: the
+library, the device and its tensors are stand-ins."""
+
+import weakref
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import paper_2512_04752_amd as sv
+from paper_2512_04752_amd import binding as B
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """Workspaces that calls make, as weak references, and whether each lived when the library
+    was called."""
+    got = SimpleNamespace(refs=[], alive=[])
+
+    def make(nbytes, index, stream):
+        t = torch.empty(nbytes, dtype=torch.uint8)
+        got.refs.append(weakref.ref(t))
+        return t
+
+    def launch(*args):
+        got.alive.append(got.refs[-1]() is not None)
+        return 0
+
+    fake = SimpleNamespace(spec_w4_workspace_bytes=lambda *a: 4096, spec_w4_linear=launch, spec_w4_gate_up=launch,
+                           spec_beam_workspace_bytes=lambda *a: 4096, spec_beam_select=launch,
+                           spec_kv4_reorder_bytes=lambda *a: 4096, spec_kv4_reorder=launch)
+    monkeypatch.setattr(B, "lib", lambda: fake)
+    monkeypatch.setattr(B, "_made_workspace", make)
+    monkeypatch.setattr(B, "_device_rows", lambda t, *a: t.shape[1])
+    monkeypatch.setattr(B, "_device_workspace", lambda t, index: (t.data_ptr(), t.numel()))
+    monkeypatch.setattr(B, "_device_stream", lambda index, stream: None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    return got
+
+
+def matrix(rows, cols):
+    return SimpleNamespace(index=0, rows=rows, cols=cols, needs={}, struct=B.spec_w4(0, rows, cols))
+
+
+def test_products_hold_their_workspace_until_they_are_launched(made):
+    m, x = matrix(48, 64), torch.zeros(3, 64, dtype=torch.bfloat16)
+    sv.spec_w4_linear(m, x, torch.zeros(3, 48))
+    sv.spec_w4_gate_up(m, m, x, torch.zeros(3, 48, dtype=torch.bfloat16))
+    assert made.alive == [True, True]
+    assert all(ref() is None for ref in made.refs)         # and no longer
