@@ -469,6 +469,8 @@ __device__ __forceinline__ double no_score() {
 // hold bounds it again (one beam far ahead of the others has k better ones than the second
 // beam's best), and what is not below (about k, unless many are equal) is ranked by counting.
 // Where that is more than fits, each wave keeps a sorted list instead, and these are ranked.
+// Lists go by logits, and scores may be equal where logits are not (of 1e30, or of logits near
+// 1e-20): then the beams that have the k-th best score are gone through once more for it.
 // 6.7 us for 128 groups of 8 x 4 lists of 8, 7.8 for 17 of 12 x 20 of 24, 5.6 for one of 4 x 125 of
 // 4; launch and end are 3.4 of each.
 __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
@@ -478,7 +480,9 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   __shared__ Cand listed[kListed];
   __shared__ float heads[kPick];
   __shared__ uint16_t open[kMaxLists];
-  __shared__ int count, opened;
+  __shared__ int count, opened, merges, above, passing[kPick / 64];
+  __shared__ uint32_t over[2], tied[2];          // beams, a bit each
+  __shared__ double kth;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = blockIdx.x, k = a.k;
   const int per_row = a.segs * k, lists = a.width * a.segs, total = a.width * per_row;
@@ -509,7 +513,7 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   int l0 = mine, e0 = 0;
   float z0;
   int y0;
-  if (threadIdx.x == 0) count = opened = 0;
+  if (threadIdx.x == 0) count = opened = merges = above = tied[0] = tied[1] = 0;
   for (int w0 = wave * rows_at_once, trip = 0; trip == 0 || w0 < a.width; w0 += kWaves * rows_at_once, ++trip) {
     const int w = w0 + (lane >> lg), row = g * a.width + min(w, a.width - 1);
     // Every lane's first two segments before anything waits, then the others.  (What is read
@@ -572,28 +576,34 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
   if (wave == 0 && a.eos >= 0) {
     const Cand c = ended(lane);
     if (fabs(c.s) < INFINITY) listed[atomicAdd(&count, 1)] = c;
+    const uint64_t all = __ballot(fabs(c.s) < INFINITY);
+    if (lane < 2) over[lane] = (uint32_t)(all >> 32 * lane);
   }
   __syncthreads();
   // The open lists in blocks of `deep` entries of each, as many as there are threads for.
   const int lists_open = opened, deep = max(1, kPick / max(1, lists_open)), block = lists_open * deep;
-  auto opened_entry = [&](int i, int at) {
+  auto opened_entry = [&](int i, int at, float* z) {
     const int l = open[i % lists_open], e = at + i / lists_open;
     if (e >= k) return Cand{no_score(), 0};
-    return candidate(l / a.segs, a.cand_z[entry(l, e)], a.cand_y[entry(l, e)]);
+    *z = a.cand_z[entry(l, e)];
+    return candidate(l / a.segs, *z, a.cand_y[entry(l, e)]);
   };
   Cand first_one{no_score(), 0};                 // of the first block
-  if ((int)threadIdx.x < block) first_one = opened_entry(threadIdx.x, 0);
+  float first_z = 0.f, z;
+  if ((int)threadIdx.x < block) first_one = opened_entry(threadIdx.x, 0, &first_z);
   if (lists_open * k > 2 * kMaxBeams) {          // a closer bound
     head = first_one.s;
-    for (int i = threadIdx.x + kPick; i < block; i += kPick) head = fmax(head, opened_entry(i, 0).s);
+    for (int i = threadIdx.x + kPick; i < block; i += kPick) head = fmax(head, opened_entry(i, 0, &z).s);
     least_score = fmax(least_score, kth_of(head));
   }
   for (int at = 0; at < k && lists_open > 0; at += deep) {
     bool more = false;                           // a list's last entry here passes
     for (int i = threadIdx.x; i < block; i += kPick) {
-      const Cand c = at == 0 && i < kPick ? first_one : opened_entry(i, at);
+      z = first_z;
+      const Cand c = at == 0 && i < kPick ? first_one : opened_entry(i, at, &z);
       if (c.s >= least_score && c.s > -INFINITY) {
         more |= i >= block - lists_open;
+        if (candidate((int)(c.id >> 32), float_below(z), 0).s == c.s) merges = 1;
         const int to = atomicAdd(&count, 1);
         if (to < kListed) listed[to] = c;
       }
@@ -651,6 +661,52 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
       a.parents[at] = (int32_t)(c.id >> 32);
       a.tokens[at] = (int32_t)c.id;
       a.new_scores[at] = (float)c.s;
+      if ((int)rank == k - 1) kth = c.s;
+    }
+  }
+  // What is better than the k-th best score is listed, and where that score is (a beam that has
+  // it has it listed too): of the tokens that have it the lowest, beam after beam.
+  if (merges && n >= k) {
+    __syncthreads();
+    const double score_k = kth;
+    for (int i = threadIdx.x; i < n; i += kPick) {
+      const Cand c = listed[i];
+      if (c.s > score_k) atomicAdd(&above, 1);
+      if (c.s == score_k) atomicOr(&tied[c.id >> 37], 1u << (c.id >> 32 & 31));
+    }
+    __syncthreads();
+    int at = above;
+    auto put = [&](int w, int y, int to) {
+      a.parents[(int64_t)g * k + to] = w;
+      a.tokens[(int64_t)g * k + to] = y;
+      a.new_scores[(int64_t)g * k + to] = (float)score_k;
+    };
+    for (int w = 0; w < a.width && at < k; ++w) {
+      if (!(tied[w >> 5] >> (w & 31) & 1)) continue;
+      if (a.eos >= 0 && (over[w >> 5] >> (w & 31) & 1)) {
+        if (threadIdx.x == 0) put(w, a.eos, at);
+        ++at;
+        continue;
+      }
+      const int64_t row = (int64_t)(g * a.width + w) * a.row_stride;
+      for (int y0 = 0; y0 < a.vocab && at < k; y0 += kPick) {
+        const int y = y0 + (int)threadIdx.x;
+        bool has = false;
+        if (y < a.vocab) {
+          const float x = a.is_bf16 ? (float)((const bf16*)a.logits)[row + y] : ((const float*)a.logits)[row + y];
+          has = x > -INFINITY && candidate(w, x, y).s == score_k;
+        }
+        const uint64_t all = __ballot(has);
+        if (lane == 0) passing[wave] = __popcll(all);
+        __syncthreads();
+        int to = at + __popcll(all & ((1ull << lane) - 1));
+        for (int i = 0; i < kWaves; ++i) {
+          if (i < wave) to += passing[i];
+          at += passing[i];
+        }
+        if (has && to < k) put(w, y, to);
+        __syncthreads();
+      }
     }
   }
   for (int i = n + threadIdx.x; i < k; i += kPick) {

@@ -1,0 +1,89 @@
+"""Choices between continuations whose scores fp64 cannot tell apart, although their logits
+differ: behind scores so large that logits are lost in them, or between logits so small that
+they are lost in the normaliser.  The lower (beam, token) of equal scores comes first, as in
+the float64 oracle."""
+
+import pytest
+import torch
+
+import paper_2512_04752_amd as sv
+from tests.test_gpu_beam import INF, check, logits, run
+
+pytestmark = pytest.mark.gpu
+LOWEST = torch.finfo(torch.float32).min
+TYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+SIZES = pytest.mark.parametrize("groups,width,vocab,k", [
+    (1, 1, 300, 1), (2, 3, 257, 5), (3, 4, 9001, 4), (2, 12, 20001, 24), (1, 64, 700, 64), (4, 2, 5000, 64), (40, 20, 1500, 7)])
+
+
+def masked(z):
+    """Tokens that are no candidates, the first ones among them."""
+    z[:, :, :3] = -INF
+    z[:, :, 10:200:2] = -INF
+    return z
+
+
+@TYPES
+@SIZES
+@pytest.mark.parametrize("score", [1e30, -1e30, LOWEST])
+def test_scores_that_swallow_the_logits(groups, width, vocab, k, dtype, score):
+    z = masked(logits(vocab, groups, width, vocab, dtype))
+    check(z, torch.full((groups, width), score, device="cuda"), k)
+
+
+@TYPES
+@SIZES
+def test_scores_that_swallow_parts_of_the_logits(groups, width, vocab, k, dtype):
+    """Steps of 2^-13 between scores, some thousandths between logits."""
+    z = masked(logits(vocab, groups, width, vocab, dtype, std=0.001))
+    check(z, torch.full((groups, width), 1e12, device="cuda"), k)
+
+
+@TYPES
+@SIZES
+def test_logits_that_vanish_beside_the_normaliser(groups, width, vocab, k, dtype):
+    z = masked(logits(vocab, groups, width, vocab, dtype, std=1e-25))
+    z[:, -1:, 5:9] = 2.0                     # and some that do not
+    check(z, torch.zeros(groups, width, device="cuda"), k)
+
+
+@TYPES
+def test_dead_beams_at_the_lowest_score(dtype):
+    """Few tokens are left to the one live beam: the rest comes from the next beams, which have
+    the lowest score there is, one of them ended."""
+    groups, width, vocab, eos = 5, 6, 4003, 77
+    z = logits(3, groups, width, vocab, dtype)
+    z[:, 0, 3:] = -INF
+    z[1, 1, 6:] = z[2, 1] = -INF
+    z[3, 1:] = torch.finfo(dtype).min
+    s = torch.full((groups, width), LOWEST, device="cuda")
+    s[:, 0] = -3.0
+    s[4] = LOWEST
+    last = torch.zeros(groups, width, dtype=torch.int32, device="cuda")
+    last[:, 2] = eos
+    for k in (2, 3, 6, 16, 64):
+        check(z, s, k, last, eos)
+
+
+@TYPES
+def test_equal_logits_of_zero(dtype):
+    """Nothing to tell apart at all."""
+    z = torch.zeros(3, 5, 30001, device="cuda", dtype=dtype)
+    z[1, :, ::2] = -INF
+    for k in (1, 9, 64):
+        check(z, torch.zeros(3, 5, device="cuda"), k)
+
+
+def test_in_place_with_ties():
+    """Scores and last tokens are replaced while ties are settled."""
+    groups, width, vocab, eos = 4, 8, 5003, 9
+    z = logits(4, groups, width, vocab)
+    s = torch.full((groups, width), 1e30, device="cuda")
+    last = torch.zeros(groups, width, dtype=torch.int32, device="cuda")
+    last[:, 0] = last[1, 1] = last[2, :7] = eos
+    last[3] = eos
+    before = s.clone(), last.clone()
+    parents = torch.empty_like(last)
+    sv.spec_beam_select(z, s, parents, last, s, last_tokens=last, eos_token=eos)
+    check(z, before[0], width, before[1], eos, got=(parents, last, s))
+    assert [t.tolist() for t in run(z, *before[:1], width, before[1], eos)] == [t.tolist() for t in (parents, last, s)]
