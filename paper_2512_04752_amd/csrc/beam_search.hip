@@ -19,7 +19,6 @@ namespace spec {
 
 namespace {
 
-constexpr int64_t kMaxGrid = 0xffffffffll / 1024;
 
 // e^d for -708 <= d <= 690 (the result's exponent is a normal one), relative error below 5e-11: d log2 e = n + f, |f| <= 1/2, and 2^n
 // times the polynomial of degree 7 with the smallest largest relative error of 2^f (4.0e-11 by
@@ -278,6 +277,7 @@ struct Vectors {
 // smallest of these four, and what is stays out of every list (which need not fill up).  They
 // are read as they are, however old: a bound only rises.
 constexpr int kTeam = 4;
+constexpr int64_t kMaxGrid = 0xffffffffll / (64 * kTeam);      // a grid has less than 2^32 threads
 template <class T, bool TEAM>
 __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
   constexpr int PER = Vectors<T>::PER, kVecs = 16 / PER;

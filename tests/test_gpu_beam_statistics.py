@@ -109,3 +109,21 @@ def test_steps_around_what_an_exponential_holds(k):
     z = patterns(100003) * torch.tensor(sizes, device="cuda")[:, None, None]
     z += torch.linspace(0, 1, z.shape[2], device="cuda")
     check(z, scores(3, *z.shape[:2]), k)
+
+
+def test_the_most_rows_there_can_be():
+    """2^22 rows in segments for teams of waves; few of them have a token that is not masked."""
+    groups, width, vocab, k = 65536, 64, 8000, 16
+    z = torch.full((groups, width, vocab), -INF, dtype=torch.bfloat16, device="cuda")
+    picked = [0, 1, 40000, groups - 1]
+    z[picked] = logits(5, len(picked), width, vocab, torch.bfloat16)
+    s = scores(5, groups, width)
+    parents, tokens = (torch.full((groups, k), 77, dtype=torch.int32, device="cuda") for _ in range(2))
+    new = torch.full((groups, k), 7.0, device="cuda")
+    sv.spec_beam_select(z, s, parents, tokens, new)
+    want = reference(z[picked], s[picked], k)
+    assert torch.equal(parents[picked].long(), want[0]) and torch.equal(tokens[picked].long(), want[1])
+    parents[picked] = -1
+    assert (parents == -1).all()
+    del z
+    torch.cuda.empty_cache()
