@@ -829,6 +829,8 @@ class W4Matrix:
         if out is None:
             with torch.cuda.stream(stream):
                 out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16, device=self.data.device)
+        elif out.shape != (self.rows, self.cols):
+            raise ValueError(f"out must have the matrix's shape, {self.rows} x {self.cols}")
         spec_w4_unpack(self.data, out, stream)
         return out
 

@@ -48,3 +48,16 @@ def test_products_hold_their_workspace_until_they_are_launched(made):
     sv.spec_w4_gate_up(m, m, x, torch.zeros(3, 48, dtype=torch.bfloat16))
     assert made.alive == [True, True]
     assert all(ref() is None for ref in made.refs)         # and no longer
+
+
+def test_a_matrix_reads_back_into_its_own_shape(monkeypatch):
+    """Another shape of as many bytes would be read as another layout."""
+    calls = []
+    monkeypatch.setattr(B, "spec_w4_unpack", lambda data, out, stream=None: calls.append(tuple(out.shape)))
+    m = sv.W4Matrix.__new__(sv.W4Matrix)
+    m.rows, m.cols, m.data = 32, 256, None
+    for shape in ((64, 128), (32, 128), (16, 256), (256, 32), (8192,)):
+        with pytest.raises(ValueError, match="32"):
+            m.unpack(torch.empty(shape, dtype=torch.bfloat16))
+    m.unpack(torch.empty(32, 256, dtype=torch.bfloat16))
+    assert calls == [(32, 256)]
