@@ -853,6 +853,8 @@ class W4Weights:
                 for k, layers in self.matrices.items():
                     w = torch.cat([lw["wq"], lw["wk"], lw["wv"]]) if k == "wqkv" else lw[k]
                     layers.append(W4Matrix(w, stream))
+                    if layers[-1].index != self.index:
+                        raise ValueError(f"{k} of layer {len(layers) - 1} is on another device than the head")
         n, gains = len(self.norms["attn_norm"]), [self.final_norm, *self.norms["attn_norm"], *self.norms["ffn_norm"]]
         vocab, hidden = self.tok_embed.shape
         for t in (self.tok_embed, *gains):

@@ -61,3 +61,32 @@ def test_a_matrix_reads_back_into_its_own_shape(monkeypatch):
             m.unpack(torch.empty(shape, dtype=torch.bfloat16))
     m.unpack(torch.empty(32, 256, dtype=torch.bfloat16))
     assert calls == [(32, 256)]
+
+
+class Matrix:
+    """Stands in for a matrix of W4Weights; a tensor's device is what it is said to be."""
+
+    devices = {}
+
+    def __init__(self, w, stream=None):
+        self.index = self.devices.get(w.data_ptr(), -1)
+        self.struct = B.spec_w4(0, *w.shape)
+
+
+@pytest.mark.parametrize("field", [None, "wo", "w_gate", "w_up", "w_down"])
+@pytest.mark.parametrize("layer", [0, 1])
+def test_weights_lie_on_one_device(monkeypatch, layer, field):
+    """A step's kernels run on one device, and read every matrix."""
+    def bf16(*shape):
+        return torch.zeros(shape, dtype=torch.bfloat16)
+
+    W = dict(tok_embed=bf16(128, 64), final_norm=bf16(64), lm_head=bf16(128, 64), layers=[
+        dict(attn_norm=bf16(64), ffn_norm=bf16(64), wq=bf16(64, 64), wk=bf16(64, 64), wv=bf16(64, 64), wo=bf16(64, 64),
+             w_gate=bf16(96, 64), w_up=bf16(96, 64), w_down=bf16(64, 96)) for _ in range(2)])
+    monkeypatch.setattr(B, "W4Matrix", Matrix)
+    monkeypatch.setattr(Matrix, "devices", {} if field is None else {W["layers"][layer][field].data_ptr(): 1})
+    if field is None:
+        assert sv.W4Weights(W).shape == (2, 64, 128)
+    else:
+        with pytest.raises(ValueError, match="device"):
+            sv.W4Weights(W)
