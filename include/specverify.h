@@ -329,8 +329,12 @@ enum {
 
 /* Workspace bytes that a product of up to max_n rows of x with one such matrix (or, in
  * spec_w4_gate_up, with two) may need.  May be 0, also if an argument is invalid.  (A search
- * over n, up to a millisecond: for setting up, not for every call.) */
+ * over n, about a microsecond for each, up to 4096 of them: for setting up, not for every call.) */
 size_t spec_w4_workspace_bytes(int32_t rows, int32_t cols, int32_t max_n);
+
+/* What a product of n rows needs, with one matrix or (pair 1) two: at most the above for
+ * max_n = n, without the search.  May be 0, also if an argument is invalid. */
+size_t spec_w4_product_bytes(int32_t rows, int32_t cols, int32_t n, int32_t pair);
 
 /* Products of 0 <= n <= 2^20 rows (n * rows <= 2^34).  The weights enter as the numbers they stand for, sums are
  * fp32, in an order that depends on the shapes and n alone.

@@ -39,7 +39,7 @@ EXPORTS = ("spec_kv_bytes", "spec_kv_alloc", "spec_kv_free", "spec_kv_sample_lay
            "spec_kv4_read", "spec_kv4_attend", "spec_kv4_commit",
            "spec_workspace_bytes_kv4", "spec_verify_kv4", "spec_workspace_bytes_w4",
            "spec_verify_w4", "spec_w4_bytes", "spec_w4_pack", "spec_w4_unpack",
-           "spec_w4_workspace_bytes", "spec_w4_linear", "spec_w4_gate_up",
+           "spec_w4_workspace_bytes", "spec_w4_product_bytes", "spec_w4_linear", "spec_w4_gate_up",
            "spec_beam_workspace_bytes", "spec_beam_select", "spec_kv_reorder",
            "spec_kv4_reorder_bytes", "spec_kv4_reorder")
 SPEC_KV4_PAGE = 64                # positions per page of the 4-bit pool
@@ -175,6 +175,7 @@ def lib():
     w4 = POINTER(spec_w4)
     L.spec_w4_bytes.argtypes = [c_int32, c_int32]
     L.spec_w4_workspace_bytes.argtypes = [c_int32, c_int32, c_int32]
+    L.spec_w4_product_bytes.argtypes = [c_int32] * 4
     L.spec_w4_pack.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_size_t, c_void_p]
     L.spec_w4_unpack.argtypes = [w4, c_void_p, c_int64, c_void_p]
     L.spec_w4_linear.argtypes = [w4, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int32, c_void_p,
@@ -189,7 +190,8 @@ def lib():
     L.spec_kv4_reorder_bytes.argtypes = [c_void_p, c_int32, c_int32, c_int32]
     L.spec_kv4_reorder.argtypes = [c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_size_t, c_void_p]
-    for name in ("spec_w4_bytes", "spec_w4_workspace_bytes", "spec_beam_workspace_bytes", "spec_kv4_reorder_bytes"):
+    for name in ("spec_w4_bytes", "spec_w4_workspace_bytes", "spec_w4_product_bytes", "spec_beam_workspace_bytes",
+                 "spec_kv4_reorder_bytes"):
         getattr(L, name).restype = c_size_t
     for name in ("spec_w4_pack", "spec_w4_unpack", "spec_w4_linear", "spec_w4_gate_up", "spec_beam_select",
                  "spec_kv_reorder", "spec_kv4_reorder", "spec_verify_kv4", "spec_verify_w4",
@@ -741,6 +743,10 @@ def spec_w4_workspace_bytes(rows, cols, max_n) -> int:
     return int(lib().spec_w4_workspace_bytes(rows, cols, max_n))
 
 
+def spec_w4_product_bytes(rows, cols, n, pair=False) -> int:
+    return int(lib().spec_w4_product_bytes(rows, cols, n, int(bool(pair))))
+
+
 def _device_rows(t, dtype, rows, cols, what, index=None):
     """Row stride of a device tensor [rows, cols] whose rows are contiguous."""
     shape = t.shape
@@ -822,7 +828,7 @@ class W4Matrix:
         self.data = _made_workspace(nbytes, self.index, stream)
         spec_w4_pack(w, self.data, stream)
         self.struct = spec_w4(self.data.data_ptr(), self.rows, self.cols)
-        self.needs = {}                      # workspace bytes by rows of x
+        self.needs = {}                      # workspace bytes by rows of x, alone and of a pair
 
     def unpack(self, out=None, stream=None):
         """What the matrix stands for, as bf16."""
@@ -891,13 +897,13 @@ def spec_verify_w4(cfg, weights: W4Weights, pool, sample_ids, tree_offsets, tree
                  temperature, eos_token, draft_probs, uniforms, debug, stream)
 
 
-def _w4_workspace(m, n, workspace, stream):
+def _w4_workspace(m, n, pair, workspace, stream):
     """(tensor, pointer, bytes); the tensor is the caller's to hold until the product is launched."""
     if workspace is not None:
         return workspace, *_device_workspace(workspace, m.index)
-    nbytes = m.needs.get(n)
-    if nbytes is None:                       # asked once: the library searches
-        nbytes = m.needs[n] = lib().spec_w4_workspace_bytes(m.rows, m.cols, n)
+    nbytes = m.needs.get((n, pair))
+    if nbytes is None:
+        nbytes = m.needs[n, pair] = lib().spec_w4_product_bytes(m.rows, m.cols, n, pair)
     if nbytes == 0:
         return None, None, 0
     workspace = _made_workspace(nbytes, m.index, stream)
@@ -917,7 +923,7 @@ def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
     os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", index)
     if n == 0:
         return
-    workspace, p, nbytes = _w4_workspace(m, n, workspace, stream)
+    workspace, p, nbytes = _w4_workspace(m, n, 0, workspace, stream)
     rc = lib().spec_w4_linear(m.struct, x.data_ptr(), xs, n, out.data_ptr(), os, kind, p, nbytes,
                               _device_stream(index, stream))
     if rc:
@@ -937,7 +943,7 @@ def spec_w4_gate_up(gate: W4Matrix, up: W4Matrix, x, out, workspace=None, stream
     os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", index)
     if n == 0:
         return
-    workspace, p, nbytes = _w4_workspace(gate, n, workspace, stream)
+    workspace, p, nbytes = _w4_workspace(gate, n, 1, workspace, stream)
     rc = lib().spec_w4_gate_up(gate.struct, up.struct, x.data_ptr(), xs, n, out.data_ptr(), os, p, nbytes,
                                _device_stream(index, stream))
     if rc:

@@ -122,6 +122,11 @@ SPEC_API size_t spec_w4_workspace_bytes(int32_t rows, int32_t cols, int32_t max_
   return align_up(most);
 }
 
+SPEC_API size_t spec_w4_product_bytes(int32_t rows, int32_t cols, int32_t n, int32_t pair) {
+  if (!dims_ok(rows, cols) || n < 1 || n > kMaxN || (pair != 0 && pair != 1)) return 0;
+  return align_up(w4_partial_bytes(rows, cols, n, pair == 1));
+}
+
 SPEC_API int spec_w4_linear(const spec_w4* m, const void* x, int64_t x_stride, int32_t n, void* out,
                             int64_t out_stride, int32_t kind, void* workspace, size_t ws_bytes, void* stream) {
   clear_error();

@@ -15,7 +15,7 @@ from paper_2512_04752_amd import binding as B
 def made(monkeypatch):
     """Workspaces that calls make, as weak references, and whether each lived when the library
     was called."""
-    got = SimpleNamespace(refs=[], alive=[])
+    got = SimpleNamespace(refs=[], alive=[], asked=[])
 
     def make(nbytes, index, stream):
         t = torch.empty(nbytes, dtype=torch.uint8)
@@ -26,7 +26,7 @@ def made(monkeypatch):
         got.alive.append(got.refs[-1]() is not None)
         return 0
 
-    fake = SimpleNamespace(spec_w4_workspace_bytes=lambda *a: 4096, spec_w4_linear=launch, spec_w4_gate_up=launch,
+    fake = SimpleNamespace(spec_w4_product_bytes=lambda *a: got.asked.append(a) or 4096, spec_w4_linear=launch, spec_w4_gate_up=launch,
                            spec_beam_workspace_bytes=lambda *a: 4096, spec_beam_select=launch,
                            spec_kv4_reorder_bytes=lambda *a: 4096, spec_kv4_reorder=launch)
     monkeypatch.setattr(B, "lib", lambda: fake)
@@ -48,6 +48,31 @@ def test_products_hold_their_workspace_until_they_are_launched(made):
     sv.spec_w4_gate_up(m, m, x, torch.zeros(3, 48, dtype=torch.bfloat16))
     assert made.alive == [True, True]
     assert all(ref() is None for ref in made.refs)         # and no longer
+
+
+def test_products_ask_for_their_own_rows_alone(made):
+    """One plan, not a search over all numbers of rows up to theirs, and once."""
+    m = matrix(48, 64)
+    for n in (3, 700, 3):
+        x = torch.zeros(n, 64, dtype=torch.bfloat16)
+        sv.spec_w4_linear(m, x, torch.zeros(n, 48))
+        sv.spec_w4_gate_up(m, m, x, torch.zeros(n, 48, dtype=torch.bfloat16))
+    assert made.asked == [(48, 64, 3, 0), (48, 64, 3, 1), (48, 64, 700, 0), (48, 64, 700, 1)]
+
+
+@pytest.mark.parametrize("rows,cols", [(16, 32), (293, 1088), (4096, 14336), (2048, 2048), (40, 70016)])
+def test_a_product_needs_what_the_search_finds(rows, cols):
+    most = 0
+    for n in range(1, 150):
+        most = max(most, *(sv.spec_w4_product_bytes(rows, cols, n, pair) for pair in (False, True)))
+        if n in (1, 2, 16, 17, 64, 149):
+            assert sv.spec_w4_workspace_bytes(rows, cols, n) == most
+    assert sv.spec_w4_product_bytes(rows, cols, 5000) == 0                # so many rows are not split
+
+
+def test_a_product_s_bytes_of_invalid_arguments():
+    for bad in ((0, 32, 1, 0), (1, 40, 1, 0), (48, 64, 0, 0), (48, 64, -1, 0), (48, 64, (1 << 20) + 1, 0), (48, 64, 1, 2)):
+        assert B.lib().spec_w4_product_bytes(*bad) == 0
 
 
 def test_a_matrix_reads_back_into_its_own_shape(monkeypatch):
