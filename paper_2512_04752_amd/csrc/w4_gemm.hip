@@ -492,12 +492,16 @@ hipError_t launch_pair(const W4Args& a, hipStream_t s) {
 // alone 49; 16 rows 4096 x 14336 in 4 splits 16.2 / 14.3 / 13.8 / 14.4, in 8 no better.)
 //
 // More rows: the cost model below, in us.  Work-groups run `slots` to a CU; k of them on one
-// take k * each per step of a column tile (the kernel's KG at a time), `fixed` more per round;
+// take k * each per step of a column tile (the kernel's KG at a time; the 64 x 256 tiles of one
+// matrix, alone on their CU, `alone`), `fixed` more per round;
 // weights stream at `tbs` TB/s; the larger of both, an eighth of the smaller (they overlap
 // imperfectly), 5.9 for a launch in a graph and, where columns are split, 2.3 and the partials
 // written and read at 5.8 TB/s for the reduction.  Fitted to 2550 launches (8 matrices of the 1B
-// and 8B shapes, 17 to 2048 rows, all tiles, 1 to 16 splits, weights from HBM): 7.5 % rms, and the
-// choice is on average 1.0 % slower than the best of them, at worst 8 % (128256 x 4096, 17 rows).
+// and 8B shapes, 17 to 2048 rows, all tiles, 1 to 16 splits, weights from HBM): 8 % rms, and the
+// choice is on average 0.9 % slower than the best of them, at worst 8 % (128256 x 4096, 17 rows); of 1775
+// others (the 8B shape's, 19 numbers of rows) 1.2 % and 8 %.  Without `alone` these are 1.0 and
+// 1.9 %, at worst 12 (4096 x 14336: 900 rows 111 us instead of 99, 1024 rows 109 instead of 103).  A pair's
+// tiles measure as much, but so do the others that they compete with there.
 W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   const int tiles = (rows + 15) / 16, mats = gate_up ? 2 : 1, T = w4_col_tiles(cols);
   auto partials = [&](int splits) { return 4.0 * splits * mats * n * tiles * 16; };      // bytes
@@ -510,14 +514,14 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
   struct Tile {
     W4Shape shape;
     int bm, bt, kg, slots;
-    double each, fixed, tbs;
+    double alone, each, fixed, tbs;
   };
-  static constexpr Tile shapes[] = {{W4_TILE32, 32, 8, 2, 3, 0.538, 0.0, 4.56},
-                                    {W4_TILE32W, 32, 32, 1, 1, 0.880, 0.32, 5.18},
-                                    {W4_TILE64, 64, 8, 2, 2, 0.854, 0.33, 4.03},
-                                    {W4_TILE64W, 64, 16, 1, 2, 0.771, 0.55, 5.40},
-                                    {W4_TILE128, 128, 16, 1, 1, 1.614, 1.17, 2.62},
-                                    {W4_TILE256, 256, 16, 1, 1, 2.675, 2.28, 6.71}};
+  static constexpr Tile shapes[] = {{W4_TILE32, 32, 8, 2, 3, 0, 0.538, 0.0, 4.56},
+                                    {W4_TILE32W, 32, 32, 1, 1, 0, 0.880, 0.32, 5.18},
+                                    {W4_TILE64, 64, 8, 2, 2, 0, 0.854, 0.33, 4.03},
+                                    {W4_TILE64W, 64, 16, 1, 2, 0.88, 0.771, 0.55, 5.40},
+                                    {W4_TILE128, 128, 16, 1, 1, 0, 1.614, 1.17, 2.62},
+                                    {W4_TILE256, 256, 16, 1, 1, 0, 2.675, 2.28, 6.71}};
   W4Plan best{W4_TILE64, 1, 1};
   double best_us = 1e30;
   for (const Tile& s : shapes) {
@@ -528,7 +532,7 @@ W4Plan plan_w4(int rows, int cols, int n, bool gate_up) {
       if (splits > 1 && (T / splits < 4 || part > kW4PartialCap)) break;
       const int64_t wgs = count * splits;
       const double steps = (T + splits * s.kg - 1) / (splits * s.kg), at_once = 256.0 * s.slots;
-      auto step = [&](int k) { return k * s.each; };
+      auto step = [&](int k) { return k == 1 && !gate_up ? std::max(s.alone, s.each) : k * s.each; };
       double work;
       if (wgs > 3 * at_once) {
         work = wgs / at_once * (steps * step(s.slots) + s.fixed);
