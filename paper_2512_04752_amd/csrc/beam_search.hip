@@ -343,8 +343,12 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
     // Terms relative to `top`: doubles hold e^600, and what is below e^-690 of it counts as
     // that.  A NaN makes the sum one, an infinity `top`.  (Differences are compared: of numbers
     // so large that neighbours are further apart, top + 600 would be another float than it is.)
-    if (__ballot(!(most - top <= 600.f))) {
-      if (!(most <= top)) {
+    // Lanes rescale their sums by themselves, by e^-600 or less: a second time leaves nothing of
+    // what met a first one, so a term meets four exponentials at most (its own, this one, those at
+    // the wave's and at the row's end), and errors do not add up along a row.
+    const bool far = !(most - top <= 600.f);
+    if (__ballot(far)) {
+      if (far) {
         sum = exp.scaled(sum, (double)top - (double)most);
         top = most;
       }

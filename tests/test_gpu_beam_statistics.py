@@ -127,3 +127,46 @@ def test_the_most_rows_there_can_be():
     assert (parents == -1).all()
     del z
     torch.cuda.empty_cache()
+
+
+BOUND = 4 * 4.1e-11 + 1e-12
+
+
+def check_normaliser(z, rows):
+    """Scores that are nearly nothing, an fp32 number less the best candidate's logarithm: fp32
+    rounds 1e-6 by 2^-24 of it, and what is left is the normaliser's error.  A term is the
+    product of at most four exponentials (its own to its lane's reference, once from there to a
+    later one, to its wave's and to its row's; a second later reference would be 600 above it),
+    each off by at most 4.1e-11 of itself, and so are a sum and its logarithm by four times that;
+    the doubles' roundings are below 1e-12."""
+    groups = len(z)
+    near = torch.log_softmax(z[rows].double(), -1).amax(-1)
+    s = torch.zeros(groups, 1, device="cuda")
+    s[rows] = (-near).float()
+    parents, tokens = (torch.empty(groups, 4, dtype=torch.int32, device="cuda") for _ in range(2))
+    new = torch.empty(groups, 4, device="cuda")
+    sv.spec_beam_select(z, s, parents, tokens, new)
+    best = (s[rows].double() + near)[:, 0]
+    assert (best.abs() < 1e-6).all()
+    assert ((new[rows, 0].double() - best).abs() <= BOUND + 2.0 ** -24 * best.abs()).all()
+
+
+def test_slow_rises_beside_steep_ones():
+    """One lane's logits rise by 700 at every step of a wave, far below the others', which rise a
+    little each time."""
+    groups, vocab = 4096, 128000             # one segment a row, 125 steps of 1024
+    at = torch.arange(vocab, device="cuda")
+    z = (at // 1024 * 0.001)[None, None].repeat(groups, 1, 1)
+    z[:, :, at % 256 < 4] = -100000.0        # 16 of a step's 1024 are a lane's
+    z[:, :, at % 1024 == 0] += at[at % 1024 == 0] // 1024 * 700.0
+    rows = [0, 1, 2000, groups - 1]
+    z[rows] += (at % 256 >= 4) * 1e-4 * torch.rand(len(rows), 1, vocab, device="cuda",
+                                                    generator=torch.Generator("cuda").manual_seed(1))
+    check_normaliser(z, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("groups,vocab", [(6, 1), (6, 64), (6, 1000), (6, 50001), (6, 128256), (300, 50001), (4096, 9001)])
+@pytest.mark.parametrize("std", [0.01, 0.5, 5.0])
+def test_normalisers_to_their_bound(groups, vocab, dtype, std):
+    check_normaliser(logits(vocab, groups, 1, vocab, dtype, std=std), [0, 1, groups // 2, groups - 1])
