@@ -20,24 +20,27 @@ namespace spec {
 namespace {
 
 
-// e^d for -708 <= d <= 690 (the result's exponent is a normal one), relative error below 5e-11: d log2 e = n + f, |f| <= 1/2, and 2^n
-// times the polynomial of degree 7 with the smallest largest relative error of 2^f (4.0e-11 by
-// Remez's exchange; the series needs degree 9 for that).  n comes out of an addition that leaves
-// it in the low bits, and goes into the exponent by an integer one: all of it at the rate of
-// fp64 additions.  The constants are held in scalar registers (of constants that the compiler
-// knows, it copies each into the result first and then accumulates, twice the instructions).
+// e^d for -708 <= d <= 690 (the result's exponent is a normal one), relative error below 5e-11:
+// d log2 e = n + f, |f| <= 1/2, and 2^n times the polynomial of degree 7 that is 1 at 0 with the
+// smallest largest relative error of 2^f (4.67e-11 by Remez's exchange; the series needs degree 9
+// for that).  e^0 is 1 exactly (without that 4.0e-11), so that beams that are sure of a token, and
+// beams with equally many equally likely ones, have equal normalisers.  n comes out of an
+// addition that leaves it in the low bits, and goes into the exponent by an integer one: all of
+// it at the rate of fp64 additions.  The constants are held in scalar registers (of constants
+// that the compiler knows, it copies each into the result first and then accumulates, twice the
+// instructions), but the 1, which an instruction has itself.
 struct Exp {
   double log2e, big, c[8];
   __device__ __forceinline__ Exp()
-      : c{0.9999999999616818, 0.6931471807284476, 0.24022651198157954, 0.05550410353446558, 0.009618027253642348,
-          0.0013333922564381022, 0.0001546929114641026, 1.5201921442377536e-05} {
+      : c{1.0, 0.693147180704532, 0.24022651066560827, 0.055504103659919514, 0.009618038132083197,
+          0.0013333935054941355, 0.00015466756313134368, 1.5196156729123239e-05} {
     log2e = 1.44269504088896340736;
     // 1.5 * 2^52, and 2^12 that the shift drops: without it the low word is 0, and then this
     // compiler (ROCm 7.2) loads it by s_mov_b64 with a 64-bit literal, which there is none of.
     big = 6755399441055744.0 + 4096.0;
     asm volatile("" : "+s"(log2e), "+s"(big), "+v"(c[7]));         // an instruction reads one scalar pair
 #pragma unroll
-    for (int i = 0; i < 7; ++i) asm volatile("" : "+s"(c[i]));
+    for (int i = 1; i < 7; ++i) asm volatile("" : "+s"(c[i]));
   }
   __device__ __forceinline__ double operator()(double d) const {
     const double m = fma(d, log2e, big), f = fma(d, log2e, big - m);

@@ -87,3 +87,34 @@ def test_in_place_with_ties():
     sv.spec_beam_select(z, s, parents, last, s, last_tokens=last, eos_token=eos)
     check(z, before[0], width, before[1], eos, got=(parents, last, s))
     assert [t.tolist() for t in run(z, *before[:1], width, before[1], eos)] == [t.tolist() for t in (parents, last, s)]
+
+
+@TYPES
+@pytest.mark.parametrize("groups,width,vocab,k", [(6, 24, 31, 5), (3, 64, 2000, 28), (4, 42, 15001, 40), (40, 6, 1300, 6)])
+def test_beams_that_are_sure(groups, width, vocab, k, dtype):
+    """One token has all the probability, in beams of equal scores, some of which have ended: the
+    logarithm of such a sum is zero."""
+    z = logits(vocab, groups, width, vocab, dtype, std=300.0)
+    best = z.float().amax(-1, keepdim=True)
+    z = torch.where(z.float() < best - 40.0, z, z.float().amin().to(dtype))      # no second one near the best
+    z.scatter_(2, torch.randint(vocab, (groups, width, 1), device="cuda", generator=torch.Generator("cuda").manual_seed(1)),
+               best.to(dtype))
+    s = torch.full((groups, width), -1.5, device="cuda")
+    s[:, ::3] = 0.0
+    last = torch.zeros(groups, width, dtype=torch.int32, device="cuda")
+    last[:, 4::5] = vocab - 1
+    check(z, s, k, last, vocab - 1)
+    check(z, s, k)
+
+
+@TYPES
+@pytest.mark.parametrize("groups,width,vocab,k", [(6, 24, 64, 5), (3, 64, 2000, 28), (4, 42, 15001, 40), (40, 6, 1300, 6)])
+def test_beams_of_equally_many_tokens(groups, width, vocab, k, dtype):
+    """A row's tokens are equally likely, the same number of them in several beams, others masked:
+    sums of ones."""
+    gen = torch.Generator("cuda").manual_seed(vocab)
+    order = torch.rand(groups, width, vocab, device="cuda", generator=gen).argsort(-1)
+    some = torch.randint(1, 4, (groups, width, 1), device="cuda", generator=gen) * (vocab // 4)
+    level = torch.randint(-3, 4, (groups, width, 1), device="cuda", generator=gen).float()
+    z = torch.where(order < some, level, -INF).to(dtype)
+    check(z, torch.zeros(groups, width, device="cuda"), k)
