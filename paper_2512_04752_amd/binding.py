@@ -897,17 +897,12 @@ def spec_verify_w4(cfg, weights: W4Weights, pool, sample_ids, tree_offsets, tree
                  temperature, eos_token, draft_probs, uniforms, debug, stream)
 
 
-def _w4_workspace(m, n, pair, workspace, stream):
-    """(tensor, pointer, bytes); the tensor is the caller's to hold until the product is launched."""
-    if workspace is not None:
-        return workspace, *_device_workspace(workspace, m.index)
+def _w4_workspace(m, n, pair, stream):
+    """A workspace that a product needs, the caller's to hold until it is launched, or None."""
     nbytes = m.needs.get((n, pair))
     if nbytes is None:
         nbytes = m.needs[n, pair] = lib().spec_w4_product_bytes(m.rows, m.cols, n, pair)
-    if nbytes == 0:
-        return None, None, 0
-    workspace = _made_workspace(nbytes, m.index, stream)
-    return workspace, workspace.data_ptr(), nbytes
+    return _made_workspace(nbytes, m.index, stream) if nbytes else None
 
 
 def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
@@ -923,7 +918,9 @@ def spec_w4_linear(m: W4Matrix, x, out, add=False, workspace=None, stream=None):
     os = _device_rows(out, torch.float32 if kind else torch.bfloat16, n, m.rows, "out", index)
     if n == 0:
         return
-    workspace, p, nbytes = _w4_workspace(m, n, 0, workspace, stream)
+    if workspace is None:
+        workspace = _w4_workspace(m, n, 0, stream)
+    p, nbytes = (None, 0) if workspace is None else _device_workspace(workspace, index)
     rc = lib().spec_w4_linear(m.struct, x.data_ptr(), xs, n, out.data_ptr(), os, kind, p, nbytes,
                               _device_stream(index, stream))
     if rc:
@@ -943,7 +940,9 @@ def spec_w4_gate_up(gate: W4Matrix, up: W4Matrix, x, out, workspace=None, stream
     os = _device_rows(out, torch.bfloat16, n, gate.rows, "out", index)
     if n == 0:
         return
-    workspace, p, nbytes = _w4_workspace(gate, n, 1, workspace, stream)
+    if workspace is None:
+        workspace = _w4_workspace(gate, n, 1, stream)
+    p, nbytes = (None, 0) if workspace is None else _device_workspace(workspace, index)
     rc = lib().spec_w4_gate_up(gate.struct, up.struct, x.data_ptr(), xs, n, out.data_ptr(), os, p, nbytes,
                                _device_stream(index, stream))
     if rc:
