@@ -364,10 +364,12 @@ int spec_w4_gate_up(const spec_w4* gate, const spec_w4* up, const void* x, int64
  *   scores       device fp32 [groups][width], e.g. log probabilities so far
  *   last_tokens  device int32 [groups][width], or NULL: the beams' last tokens, read
  *                when eos_token >= 0
- * Candidate (w, y) scores scores[w] + log softmax(logits of w)[y], in fp64, the logarithm
- * of the sum to 1e-9 (and the same for equal rows).  A beam whose last token is eos_token
- * has ended: it offers (w, eos_token) alone, at scores[w].  No candidates: tokens whose logit is -infinity; beams whose score is not
- * finite; live beams with a logit that is NaN or +infinity.
+ * Candidate (w, y) scores scores[w] + (logits of w)[y] - lse_w in fp64.  The beam's lse_w =
+ * log sum exp(logits of w) is one fp64 number, right to 1e-9 (and to its own rounding, which
+ * counts more beside logits above 2^22), and the same for equal rows.  A beam whose last
+ * token is eos_token has ended: it offers (w, eos_token) alone, at scores[w].  No candidates:
+ * tokens whose logit is -infinity; beams whose score is not finite; live beams with a logit
+ * that is NaN or +infinity.
  * Outputs, per group the k best, best first, the lower (w, y) of equal scores first:
  *   parents      device int32 [groups][k]  w
  *   tokens       device int32 [groups][k]  y
@@ -396,8 +398,8 @@ int spec_beam_select(const void* logits, int64_t row_stride, int32_t bf16, int32
  *   sample_ids  host [groups][width]   distinct
  *   begin, end  host [groups]          0 <= begin <= end <= every beam's capacity
  *   parents     device int32 [groups][width]
- * 1 <= width <= SPEC_MAX_BEAMS.  A large call uploads descriptors: a capturing stream is
- * refused. */
+ * 1 <= width <= SPEC_MAX_BEAMS.  A capturing stream is refused: samples and ranges are the
+ * call's host values, which a replay would not see change, and large calls upload them. */
 int spec_kv_reorder(spec_kv* kv, int32_t groups, int32_t width, const int32_t* sample_ids,
                     const int32_t* begin, const int32_t* end, const int32_t* parents, void* stream);
 
@@ -566,7 +568,7 @@ typedef struct {
 
 /* Workspace bytes spec_verify_w4 needs: max_pages 0 for a bf16 pool, otherwise as in
  * spec_workspace_bytes_kv4; 0 if an argument is invalid.  (It holds all nodes' logits in
- * fp32.) */
+ * fp32, 525 MB of 1024 nodes and 128256 tokens, for greedy steps too.) */
 size_t spec_workspace_bytes_w4(const spec_model_config* cfg, int32_t max_batch, int32_t max_tokens,
                                int32_t max_pages, int32_t sampled);
 
@@ -668,7 +670,10 @@ enum {
   SPEC_K_TRANSFER = 7,   /* spec_kv_pack / spec_kv_unpack */
   SPEC_K_ACCEPT = 8,     /* tree acceptance: greedy, greedy with EOS, or sampled */
   SPEC_K_KV4_APPEND = 9, /* spec_kv4_append (SPEC_K_ATTENTION: spec_kv4_attend too) */
-  SPEC_K_W4 = 10,        /* spec_w4_linear / spec_w4_gate_up (spec_verify_w4's: 0, 2 .. 5) */
+  SPEC_K_W4 = 10,        /* spec_w4_linear / spec_w4_gate_up.  spec_verify_w4's products are in 0
+                            and 2 .. 5, by themselves: what joins their splits, rotates, adds,
+                            normalises or takes maxima, which these classes hold in the other
+                            steps, is in none */
   SPEC_K_BEAM = 11,      /* spec_beam_select */
   SPEC_K_REORDER = 12,   /* spec_kv_reorder / spec_kv4_reorder */
   SPEC_K_COUNT = 13

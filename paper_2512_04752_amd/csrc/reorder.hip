@@ -8,8 +8,9 @@
 // parent is read once (a second beam's read of it hits the caches) and every moving beam
 // written once; beams that stay cost nothing.
 // 16 groups of 8 beams, 5 of them moving 500 tokens of the 4-bit pool (8 layers of 8 heads of
-// 128): 108 us for 549 MB, the 5.1 TB/s that a copy of 1 GiB reaches.  8 beams, 5 of them
-// moving 100 tokens of the bf16 pool (16 such layers): 9.6 us for 52 MB (caches take part).
+// 128): 119 us (the median; 107 at best) for 549 MB, 4.6 TB/s where a copy of 1 GiB reaches 5.15.
+// 8 beams, 5 of them moving 100 tokens of the bf16 pool (16 such layers): 10.8 us for 52 MB
+// (caches take part).
 #include <algorithm>
 #include <type_traits>
 
