@@ -447,7 +447,8 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
 }
 
 // A candidate of the last stage: a higher score is better, then a lower id, which is the
-// beam above the token; score -infinity: none.
+// beam above the token above a bit; score -infinity: none.  The bit: the next lower float as a
+// logit would have the same score.
 struct Cand {
   double s;
   uint64_t id;
@@ -455,7 +456,7 @@ struct Cand {
 __device__ __forceinline__ bool better(const Cand& p, const Cand& q) {
   return (p.s > q.s) | ((p.s == q.s) & (p.id < q.id));
 }
-__device__ __forceinline__ uint64_t id_of(int w, int y) { return (uint64_t)(uint32_t)w << 32 | (uint32_t)y; }
+__device__ __forceinline__ uint64_t id_of(int w, int y) { return (uint64_t)(uint32_t)w << 32 | (uint32_t)y << 1; }
 constexpr int kPick = 512;         // threads
 constexpr int kListed = 1024;      // candidates that can be ranked side by side
 constexpr int kMaxLists = 1024;    // lists of a group: plan_beam()
@@ -500,6 +501,11 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     Cand c{no_score(), id_of(w, y)};
     const double norm = lse[w];
     if (norm == norm && y >= 0) c.s = (double)score[w] + ((double)z - norm);
+    return c;
+  };
+  auto with_bit = [&](Cand c, float z) {
+    const int w = (int)(c.id >> 32);
+    c.id |= candidate(w, float_below(z), 0).s == c.s;
     return c;
   };
   auto ended = [&](int w) {                      // a beam that has ended, as a candidate
@@ -607,10 +613,11 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     bool more = false;                           // a list's last entry here passes
     for (int i = threadIdx.x; i < block; i += kPick) {
       z = first_z;
-      const Cand c = at == 0 && i < kPick ? first_one : opened_entry(i, at, &z);
+      Cand c = at == 0 && i < kPick ? first_one : opened_entry(i, at, &z);
       if (c.s >= least_score && c.s > -INFINITY) {
         more |= i >= block - lists_open;
-        if (candidate((int)(c.id >> 32), float_below(z), 0).s == c.s) merges = 1;
+        c = with_bit(c, z);
+        if (c.id & 1) merges = 1;
         const int to = atomicAdd(&count, 1);
         if (to < kListed) listed[to] = c;
       }
@@ -638,7 +645,8 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     };
     for (int i = wave * 64; i < total; i += kPick) {
       const int at = min(i + lane, total - 1);
-      const Cand c = candidate(at / per_row, a.cand_z[first + at], a.cand_y[first + at]);
+      const float z = a.cand_z[first + at];
+      const Cand c = with_bit(candidate(at / per_row, z, a.cand_y[first + at]), z);
       offer(c, i + lane < total && c.s > -INFINITY);
     }
     if (a.eos >= 0 && wave == 0) {
@@ -666,23 +674,27 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
     if (i < n && (threadIdx.x & 7) == 0 && (int)rank < k) {
       const int64_t at = (int64_t)g * k + rank;
       a.parents[at] = (int32_t)(c.id >> 32);
-      a.tokens[at] = (int32_t)c.id;
+      a.tokens[at] = (int32_t)((uint32_t)c.id >> 1);
       a.new_scores[at] = (float)c.s;
       if ((int)rank == k - 1) kth = c.s;
     }
   }
   // What is better than the k-th best score is listed, and where that score is (a beam that has
-  // it has it listed too): of the tokens that have it the lowest, beam after beam.
+  // it has it listed too): of the tokens that have it the lowest, beam after beam.  A row of
+  // 128256 takes 60 us if its last token is the one; most often there are some among the first.
   if (merges && n >= k) {
+    __syncthreads();
+    if (threadIdx.x == 0) merges = 0;
     __syncthreads();
     const double score_k = kth;
     for (int i = threadIdx.x; i < n; i += kPick) {
       const Cand c = listed[i];
       if (c.s > score_k) atomicAdd(&above, 1);
       if (c.s == score_k) atomicOr(&tied[c.id >> 37], 1u << (c.id >> 32 & 31));
+      if (c.s == score_k && (c.id & 1)) merges = 1;
     }
     __syncthreads();
-    int at = above;
+    int at = merges ? above : k;                 // not where only better ones' neighbours merge
     auto put = [&](int w, int y, int to) {
       a.parents[(int64_t)g * k + to] = w;
       a.tokens[(int64_t)g * k + to] = y;
@@ -696,23 +708,33 @@ __global__ __launch_bounds__(kPick) void beam_pick_kernel(BeamArgs a) {
         continue;
       }
       const int64_t row = (int64_t)(g * a.width + w) * a.row_stride;
-      for (int y0 = 0; y0 < a.vocab && at < k; y0 += kPick) {
-        const int y = y0 + (int)threadIdx.x;
-        bool has = false;
-        if (y < a.vocab) {
-          const float x = a.is_bf16 ? (float)((const bf16*)a.logits)[row + y] : ((const float*)a.logits)[row + y];
-          has = x > -INFINITY && candidate(w, x, y).s == score_k;
+      constexpr int kAhead = 8;
+      for (int y0 = threadIdx.x; y0 - (int)threadIdx.x < a.vocab && at < k; y0 += kAhead * kPick) {
+        float x[kAhead];
+        uint32_t has = 0;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int64_t from = row + min(y0 + j * kPick, a.vocab - 1);
+          x[j] = a.is_bf16 ? (float)((const bf16*)a.logits)[from] : ((const float*)a.logits)[from];
         }
-        const uint64_t all = __ballot(has);
-        if (lane == 0) passing[wave] = __popcll(all);
-        __syncthreads();
-        int to = at + __popcll(all & ((1ull << lane) - 1));
-        for (int i = 0; i < kWaves; ++i) {
-          if (i < wave) to += passing[i];
-          at += passing[i];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int y = y0 + j * kPick;
+          has |= (uint32_t)(y < a.vocab && x[j] > -INFINITY && candidate(w, x[j], y).s == score_k) << j;
         }
-        if (has && to < k) put(w, y, to);
-        __syncthreads();
+        if (!__syncthreads_or(has)) continue;
+        for (int j = 0; j < kAhead && at < k; ++j) {
+          const uint64_t all = __ballot(has >> j & 1);
+          if (lane == 0) passing[wave] = __popcll(all);
+          __syncthreads();
+          int to = at + __popcll(all & ((1ull << lane) - 1));
+          for (int i = 0; i < kWaves; ++i) {
+            if (i < wave) to += passing[i];
+            at += passing[i];
+          }
+          if ((has >> j & 1) && to < k) put(w, y0 + j * kPick, to);
+          __syncthreads();
+        }
       }
     }
   }

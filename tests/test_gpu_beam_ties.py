@@ -118,3 +118,27 @@ def test_beams_of_equally_many_tokens(groups, width, vocab, k, dtype):
     level = torch.randint(-3, 4, (groups, width, 1), device="cuda", generator=gen).float()
     z = torch.where(order < some, level, -INF).to(dtype)
     check(z, torch.zeros(groups, width, device="cuda"), k)
+
+
+@TYPES
+def test_logits_that_are_logarithms_of_probabilities(dtype):
+    """The best of them are zeros, below which there are floats that fp64 scores do not tell from
+    zero; the k-th best is another."""
+    z = torch.log_softmax(logits(5, 20, 6, 5003, std=8.0), -1)
+    z[::2, :, 7] = 0.0
+    z[1::3, ::2] = torch.where(z[1::3, ::2] < z[1::3, ::2].amax(-1, keepdim=True), -80.0, 0.0)
+    for k in (1, 6, 20):
+        check(z.to(dtype), torch.zeros(20, 6, device="cuda"), k)
+
+
+@TYPES
+@pytest.mark.parametrize("k", [1, 8, 30, 64])
+def test_few_tokens_far_into_the_rows(dtype, k):
+    """Beams that offer some tokens each, anywhere in long rows, at one score."""
+    groups, width, vocab = 6, 9, 30011
+    z = logits(8, groups, width, vocab, dtype)
+    keep = torch.rand(z.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(2)) < 5 / vocab
+    keep[:, ::4, -1] = keep[1, :, 4095:4098] = keep[2, 1, 511:514] = True
+    keep[3, 2:] = False
+    z = torch.where(keep, z, torch.full_like(z, -INF))
+    check(z, torch.full((groups, width), -1e30, device="cuda"), k)
