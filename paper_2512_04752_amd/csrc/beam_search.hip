@@ -305,7 +305,7 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
   };
   const Vectors<T> vec{(const T*)a.logits + row * a.row_stride, a.vocab};
   const int v0 = seg * a.seg, v1 = min((a.vocab + PER - 1) / PER, v0 + a.seg);
-  float top = kLowest;          // the lane's reference: its largest logit so far, less 600 at most
+  float top = kLowest;          // the lane's reference: its largest logit so far, less 32 at most
   const Exp exp;
   double sum = 0.0;
   uint64_t best = 0;
@@ -343,13 +343,14 @@ __global__ __launch_bounds__(64 * kTeam, 4) void beam_scan_kernel(BeamArgs a) {
     for (int j = 0; j < kVecs; ++j)
 #pragma unroll
       for (int i = 0; i < PER; ++i) lowest = __builtin_elementwise_minimum(lowest, z[j][i]);
-    // Terms relative to `top`: doubles hold e^600, and what is below e^-690 of it counts as
-    // that.  A NaN makes the sum one, an infinity `top`.  (Differences are compared: of numbers
-    // so large that neighbours are further apart, top + 600 would be another float than it is.)
-    // Lanes rescale their sums by themselves, by e^-600 or less: a second time leaves nothing of
-    // what met a first one, so a term meets four exponentials at most (its own, this one, those at
-    // the wave's and at the row's end), and errors do not add up along a row.
-    const bool far = !(most - top <= 600.f);
+    // Terms relative to `top`; what is below e^-690 of it counts as that.  A NaN makes the sum
+    // one, an infinity `top`.  Lanes rescale their sums by themselves, by e^-32 or less: a second
+    // time leaves nothing of what met a first one, so a term meets four exponentials at most (its
+    // own, this one, those at the wave's and at the row's end), and errors do not add up along a
+    // row.  A logit that has all the probability is its lane's reference, and its term 1.
+    // (Differences are compared: of numbers so large that neighbours are further apart, top + 32
+    // would be another float than it is.)
+    const bool far = !(most - top <= 32.f);
     if (__ballot(far)) {
       if (far) {
         sum = exp.scaled(sum, (double)top - (double)most);

@@ -90,7 +90,8 @@ def test_in_place_with_ties():
 
 
 @TYPES
-@pytest.mark.parametrize("groups,width,vocab,k", [(6, 24, 31, 5), (3, 64, 2000, 28), (4, 42, 15001, 40), (40, 6, 1300, 6)])
+@pytest.mark.parametrize("groups,width,vocab,k", [(6, 24, 31, 5), (3, 64, 2000, 28), (4, 42, 15001, 40), (40, 6, 1300, 6),
+                                                  (17, 12, 50001, 9)])
 def test_beams_that_are_sure(groups, width, vocab, k, dtype):
     """One token has all the probability, in beams of equal scores, some of which have ended: the
     logarithm of such a sum is zero."""
