@@ -19,7 +19,6 @@ namespace spec {
 
 namespace {
 
-
 // e^d for -708 <= d <= 690 (the result's exponent is a normal one), relative error below 5e-11:
 // d log2 e = n + f, |f| <= 1/2, and 2^n times the polynomial of degree 7 that is 1 at 0 with the
 // smallest largest relative error of 2^f (4.67e-11 by Remez's exchange; the series needs degree 9
