@@ -105,7 +105,8 @@ def test_steps_at_large_magnitudes(sign, k):
 @pytest.mark.parametrize("k", [4, 24])
 def test_steps_around_what_an_exponential_holds(k):
     """Rises and falls around 32, and by 590 .. 720, where terms begin and cease to count."""
-    sizes = [1.0, 20.0, 31.0, 31.999, 32.0, 33.0, 36.0, 64.0, 590.0, 599.5, 600.0, 600.5, 610.0, 679.5, 680.0, 680.5, 689.0, 690.0, 691.0, 700.0, 709.0, 720.0]
+    sizes = [1.0, 20.0, 31.0, 31.999, 32.0, 33.0, 36.0, 64.0, 590.0, 599.5, 600.0, 600.5, 610.0, 679.5, 680.0, 680.5,
+             689.0, 690.0, 691.0, 700.0, 709.0, 720.0]
     z = patterns(100003) * torch.tensor(sizes, device="cuda")[:, None, None]
     z += torch.linspace(0, 1, z.shape[2], device="cuda")
     check(z, scores(3, *z.shape[:2]), k)
